@@ -1,4 +1,5 @@
-"""Builds the HIP library in-tree: paper_2012_15198_amd/libcxmix.so (gfx950 only)."""
+"""Builds the HIP libraries in-tree (gfx950 only): paper_2012_15198_amd/libcxmix.so, the mixing library, and libcxlm.so, the
+language-model operators."""
 from __future__ import annotations
 
 import os
@@ -16,6 +17,11 @@ SOURCES = [os.path.join(CSRC, f) for f in ("cx_host.cpp", "cx_hbm.cpp", "cx_api_
                                            "cx_api_noalloc.hip", "cx_api_fused16.hip", "cx_api_pushsum16.hip")]
 HEADERS = [os.path.join(ROOT, "include", "cx_mix.h")] + [os.path.join(CSRC, h) for h in (
     "cx_columns.hpp", "cx_schedule.hpp", "cx_tile.hpp", "cx_ops.hpp", "cx_ops16.hpp", "cx_kernels.hpp", "cx_launch.hpp")]
+LM_LIB = os.path.join(HERE, "libcxlm.so")
+LM_CSRC = os.path.join(CSRC, "lm")
+LM_SOURCES = [os.path.join(LM_CSRC, f) for f in ("cx_lm_embed.hip", "cx_lm_scan.hip", "cx_lm_scores.hip", "cx_lm_distill.hip")]
+LM_HEADERS = [os.path.join(ROOT, "include", h) for h in ("cx_lm.h", "cx_mix.h")] + [os.path.join(LM_CSRC, h) for h in (
+    "lm_common.hpp", "lm_vocab.hpp")]
 OBJDIR = os.path.join(HERE, "_build")
 
 HIPCC_FLAGS = [
@@ -27,35 +33,37 @@ HIPCC_FLAGS = [
 ]
 
 
-def stale() -> bool:
-    if not os.path.exists(LIB):
+def stale(lib: str = LIB, files=None) -> bool:
+    if not os.path.exists(lib):
         return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(p) > t for p in SOURCES + HEADERS)
+    t = os.path.getmtime(lib)
+    return any(os.path.getmtime(p) > t for p in files or SOURCES + HEADERS)
 
 
 def build_library(force: bool = True, verbose: bool = False) -> str:
-    """Compile every HIP/C++ source of the library for gfx950 (cross-compiles without a GPU)."""
-    if not force and not stale():
-        return LIB
+    """Compile every HIP/C++ source of the libraries for gfx950 (cross-compiles without a GPU).  The mixing library's path."""
+    wanted = [(lib, sources) for lib, sources, headers in ((LIB, SOURCES, HEADERS), (LM_LIB, LM_SOURCES, LM_HEADERS))
+              if force or stale(lib, sources + headers)]
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJDIR, exist_ok=True)
-    objs = [os.path.join(OBJDIR, os.path.basename(src) + ".o") for src in SOURCES]
+    obj_of = lambda src: os.path.join(OBJDIR, os.path.basename(src) + ".o")
 
-    def compile_one(pair):
-        src, obj = pair
-        cmd = [hipcc, *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-c", src, "-o", obj]
+    def compile_one(src):
+        cmd = [hipcc, *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-c", src, "-o", obj_of(src)]
         if verbose:
             print(" ".join(cmd), file=sys.stderr)
         subprocess.check_call(cmd)
 
     # one translation unit per entry point: compile them side by side, then link
-    with ThreadPoolExecutor(max_workers=min(len(SOURCES), int(os.environ.get("MAX_JOBS", "8")))) as pool:
-        list(pool.map(compile_one, zip(SOURCES, objs)))
-    link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
-    if verbose:
-        print(" ".join(link), file=sys.stderr)
-    subprocess.check_call(link)
+    todo = [src for _, sources in wanted for src in sources]
+    if todo:
+        with ThreadPoolExecutor(max_workers=min(len(todo), int(os.environ.get("MAX_JOBS", "8")))) as pool:
+            list(pool.map(compile_one, todo))
+    for lib, sources in wanted:
+        link = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *map(obj_of, sources), "-o", lib]
+        if verbose:
+            print(" ".join(link), file=sys.stderr)
+        subprocess.check_call(link)
     return LIB
 
 

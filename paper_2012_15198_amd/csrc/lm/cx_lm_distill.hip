@@ -1,0 +1,337 @@
+// C-ABI entry points cx_distill_loss*, cx_distill_grad*, cx_distill_step*, cx_distill_workspace: distillation from a teacher's
+// top logits with the label's cross entropy beside it (see include/cx_lm.h).
+//
+//   q = softmax(t / tau) over the teacher's valid ids      p = softmax(z / tau)      p1 = softmax(z)
+//   loss = w_kl tau^2 sum_k q_k (log q_k - log p[id_k])  -  w_ce log p1[label]
+//   dz   = gout (w_kl tau (p - q) + w_ce (p1 - onehot(label)))
+//
+// Bound by memory where the exponentials allow it: a row of logits is read once for its maximum and both sums, and once more, last part
+// first, when its gradient is written; the second reading finds the row in the caches.  q and the label touch K + 1 elements: every
+// element is written with its share of p and p1, and behind a barrier those few are written again with their targets.
+// Where rows are few, several workgroups share one: part_kernel leaves the parts' statistics in the workspace, and each
+// workgroup of the second launch joins them for itself.
+#include "lm_vocab.hpp"
+
+namespace {
+
+constexpr int kMaxTeacher = CX_MAX_TEACHER;
+static_assert(kMaxTeacher < kRowThreads, "a thread for every target");
+
+template <class E>
+struct DistillArgs {
+    const typename E::T *z;
+    typename E::T *dz;                                  // NULL: the loss alone
+    const int32_t *ids, *labels;
+    const float *t, *gout;
+    float *loss, *stats;                                // stats: [N][4]: maximum, sum at tau, sum at 1
+    int64_t ld, ld_dz, V;
+    int K, parts;
+    float tau, w_kl, w_ce;
+    Stats *part_stats;                                  // [N][parts]
+};
+
+// Both sums at their factors of log2(e) z: one sum where tau = 1 or only one of the two terms counts.
+template <class E>
+__device__ __forceinline__ float soft_factor(const DistillArgs<E> &a) { return a.w_kl != 0.0f ? kLog2e / a.tau : kLog2e; }
+
+template <class E, Extra X>
+__device__ __forceinline__ Stats slice_stats(const Slice<E> &slice, float c, Stats (&lds)[kRowWaves])
+{
+    Stats own{kLowest, 0.0f, 0.0f};
+    const int rounds = slice.rounds();
+    for (int round = 0; round < rounds; ++round) {
+        float v[kAhead * E::kPer16];
+        slice.load(round, v);
+        accumulate<X>(own, v, c, kLog2e);
+    }
+    if (slice.has_tail()) {
+        const float v[1] = {E::widen(slice.z[slice.tail_at()])};
+        accumulate<X>(own, v, c, kLog2e);
+    }
+    return join_workgroup<X>(own, lds, c, kLog2e);
+}
+
+// Grid (parts, N).
+template <class E, Extra X>
+__global__ __launch_bounds__(kRowThreads) void part_kernel(const DistillArgs<E> a)
+{
+    __shared__ Stats lds[kRowWaves];
+    const int64_t n = blockIdx.y;
+    const Slice<E> slice(a.z + n * a.ld, part_begin(a.V, a.parts, blockIdx.x, E::kPer16), part_begin(a.V, a.parts, blockIdx.x + 1, E::kPer16));
+    const Stats all = slice_stats<E, X>(slice, soft_factor(a), lds);
+    if (threadIdx.x == 0) a.part_stats[n * a.parts + blockIdx.x] = all;
+}
+
+struct Targets {
+    int id[kMaxTeacher + 1];                            // of the teacher's tokens, then the label; -1: none
+    float q[kMaxTeacher + 1];                           // gout-free weight of the gradient's target: w_kl tau q, w_ce
+    float soft, hard, loss;                             // w_kl tau, w_ce if these terms count in this row; the row's loss
+};
+
+// Wavefront 0: targets and, if it is wanted, loss of row n from its statistics.  The loss reads logits of the whole row.
+template <class E>
+__device__ __forceinline__ void row_targets(const DistillArgs<E> &a, int64_t n, const Stats &all, bool want_loss, Targets &to)
+{
+    constexpr int kEach = kMaxTeacher / kWave;
+    const int lane = threadIdx.x;
+    const typename E::T *z = a.z + n * a.ld;
+    const float inv_tau = 1.0f / a.tau, lowest = -__builtin_inff();
+    float t[kEach], high = lowest;
+    int id[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int k = i * kWave + lane;
+        id[i] = k < a.K ? a.ids[n * a.K + k] : -1;
+        if (id[i] < 0 || id[i] >= a.V) id[i] = -1;
+        t[i] = id[i] >= 0 ? a.t[n * a.K + k] * inv_tau : lowest;
+        high = fmaxf(high, t[i]);
+    }
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d /= 2) high = fmaxf(high, __shfl_xor(high, d));
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sum += t[i] == lowest ? 0.0f : expf(t[i] - high);
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d /= 2) sum += __shfl_xor(sum, d);
+    const bool row = all.s != 0.0f;                     // a row of -inf alone has no distribution: it counts for nothing
+    const bool soft = row && a.w_kl != 0.0f && sum != 0.0f;
+    const float log_sum = logf(sum), log_s = logf(all.s);
+    float loss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int k = i * kWave + lane;
+        float q = 0.0f;
+        if (soft && id[i] >= 0 && t[i] != lowest) {
+            const float log_q = t[i] - high - log_sum;
+            q = expf(log_q);
+            if (want_loss && q != 0.0f) loss += q * (log_q - ((E::widen(z[id[i]]) - all.m) * inv_tau - log_s));
+        }
+        if (k < a.K) { to.id[k] = id[i]; to.q[k] = a.w_kl * a.tau * q; }
+    }
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d /= 2) loss += __shfl_xor(loss, d);
+    loss *= soft ? a.w_kl * a.tau * a.tau : 0.0f;
+    if (lane == 0) {
+        int label = a.labels && a.w_ce != 0.0f && row ? a.labels[n] : -1;
+        if (label < 0 || label >= a.V) label = -1;
+        if (!soft) loss = 0.0f;
+        if (want_loss && label >= 0) loss -= a.w_ce * ((E::widen(z[label]) - all.m) - logf(all.u));
+        to.id[a.K] = label;
+        to.q[a.K] = label >= 0 ? a.w_ce : 0.0f;
+        to.soft = soft ? a.w_kl * a.tau : 0.0f;
+        to.hard = label >= 0 ? a.w_ce : 0.0f;
+        to.loss = loss;
+    }
+}
+
+enum Source { kHere, kParts, kSaved };                  // where a row's statistics come from
+
+// Grid (parts, N).  kHere: one part.
+template <class E, Extra X, Source FROM>
+__global__ __launch_bounds__(kRowThreads) void distill_kernel(const DistillArgs<E> a)
+{
+    __shared__ Stats lds[kRowWaves];
+    __shared__ Targets to;
+    const int part = FROM == kHere ? 0 : blockIdx.x, parts = FROM == kHere ? 1 : a.parts;
+    const int64_t n = blockIdx.y, lo = part_begin(a.V, parts, part, E::kPer16), hi = part_begin(a.V, parts, part + 1, E::kPer16);
+    const Slice<E> slice(a.z + n * a.ld, lo, hi);
+    const float c = soft_factor(a);
+    Stats all;
+    if constexpr (FROM == kHere) {
+        all = slice_stats<E, X>(slice, c, lds);
+    } else if constexpr (FROM == kParts) {
+        all = a.part_stats[n * parts];
+        for (int k = 1; k < parts; ++k) all = join<X>(all, a.part_stats[n * parts + k], c, kLog2e);
+    } else {
+        all = {a.stats[n * 4], a.stats[n * 4 + 1], a.stats[n * 4 + 2]};
+    }
+    if (FROM != kSaved && X != kDual) all.u = all.s;    // one sum serves both
+    if (threadIdx.x < kWave) {
+        const bool want_loss = FROM != kSaved && part == 0 && a.loss;
+        row_targets<E>(a, n, all, want_loss, to);
+        if (want_loss && threadIdx.x == 0) {
+            a.loss[n] = to.loss;
+            if (a.stats) {
+                a.stats[n * 4] = all.m; a.stats[n * 4 + 1] = all.s; a.stats[n * 4 + 2] = all.u; a.stats[n * 4 + 3] = 0.0f;
+            }
+        }
+    }
+    if (!a.dz) return;
+    __syncthreads();
+    // the few elements that have a target: their logits before anything is written (dz may be z)
+    const int k = threadIdx.x;
+    const int id = k <= a.K ? to.id[k] : -1;
+    const bool target = id >= lo && id < hi;
+    float z_target = 0.0f, q = 0.0f;
+    if (target) {
+        z_target = E::widen(a.z[n * a.ld + id]);
+        for (int i = 0; i <= a.K; ++i) q += to.id[i] == id ? to.q[i] : 0.0f;
+    }
+    __syncthreads();
+    const float gout = a.gout[n], soft = to.soft == 0.0f ? 0.0f : gout * to.soft / all.s, hard = to.hard == 0.0f ? 0.0f : gout * to.hard / all.u;
+    const auto share = [&](float z) {
+        const float d = z - all.m;
+        if (X == kDual) return __builtin_fmaf(soft, exp2_fast(d * c), hard * exp2_fast(d * kLog2e));
+        return (soft + hard) * exp2_fast(d * c);
+    };
+    typename E::T *dz = a.dz + n * a.ld_dz + lo;
+    if (to.soft == 0.0f && to.hard == 0.0f) {           // a row without targets has no gradient, whatever its logits are
+        if (slice.has_tail()) dz[slice.tail_at()] = E::narrow(0.0f);
+        for (int at = threadIdx.x; at < slice.vectors; at += kRowThreads) store16<E>(dz + static_cast<int64_t>(at) * E::kPer16, u4{});
+        return;
+    }
+    if (slice.has_tail()) dz[slice.tail_at()] = E::narrow(share(E::widen(slice.z[slice.tail_at()])));
+    for (int round = slice.rounds() - 1; round >= 0; --round) {
+        float v[kAhead * E::kPer16];
+        slice.load(round, v);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            float g[E::kPer16];
+#pragma unroll
+            for (int j = 0; j < E::kPer16; ++j) g[j] = share(v[i * E::kPer16 + j]);
+            const int at = slice.vector_of(round, i);
+            if (at < slice.vectors) store16<E>(dz + static_cast<int64_t>(at) * E::kPer16, E::pack(g));
+        }
+    }
+    __syncthreads();
+    if (target) dz[id - lo] = E::narrow(__builtin_fmaf(-gout, q, share(z_target)));
+}
+
+struct DistillSpace {
+    int parts;
+    int64_t bytes;
+};
+
+DistillSpace distill_space(int64_t N, int64_t V, int per16)
+{
+    const int parts = parts_of(N, V, per16);
+    return {parts, parts > 1 ? N * parts * static_cast<int64_t>(sizeof(Stats)) : 0};
+}
+
+int check_sizes(int64_t N, int32_t V, int32_t K)
+{
+    return N < 0 || N > CX_MAX_TOKENS || V < 1 || V > CX_MAX_VOCAB || K < 0 || K > kMaxTeacher ? CX_ERR_SHAPE : CX_OK;
+}
+
+// from_saved: the gradient alone, from the statistics that the loss left.
+template <class E>
+int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    const int rc = check_sizes(N, static_cast<int32_t>(a.V), a.K);
+    if (rc != CX_OK) return rc;
+    if (!(a.tau > 0.0f) || !(a.tau <= 3.0e38f) || !(a.w_kl >= 0.0f) || !(a.w_ce >= 0.0f) || !(a.w_kl <= 3.0e38f) || !(a.w_ce <= 3.0e38f)) return CX_ERR_SHAPE;
+    if (N == 0) return CX_OK;
+    if (!a.z || (a.K > 0 && (!a.ids || !a.t)) || (want_dz && (!a.dz || !a.gout)) || (!from_saved && !a.loss) || (from_saved && !a.stats)) return CX_ERR_NULL;
+    if (bad_matrix(N, a.ld, a.V) || (want_dz && bad_matrix(N, a.ld_dz, a.V))) return CX_ERR_SHAPE;
+    const DistillSpace space = distill_space(N, a.V, E::kPer16);
+    const int64_t need = from_saved ? 0 : space.bytes;
+    if (need > 0 && !workspace) return CX_ERR_NULL;
+    if (need > 0 && workspace_bytes < need) return CX_ERR_SHAPE;
+    constexpr int kElem = sizeof(typename E::T);
+    if (misaligned_to(a.z, kElem) || misaligned_to(a.dz, kElem) || misaligned_to(a.ids, 4) || misaligned_to(a.labels, 4) || misaligned_to(a.t, 4) ||
+        misaligned_to(a.gout, 4) || misaligned_to(a.loss, 4) || misaligned_to(a.stats, 4) || misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
+    const uint64_t z_bytes = span(N, a.ld, a.V, kElem), row_bytes = N * 4, top_bytes = N * a.K * 4;
+    const struct { const void *p; uint64_t bytes; } in[5] = {{a.z, z_bytes}, {a.ids, top_bytes}, {a.t, top_bytes}, {a.labels, row_bytes}, {a.gout, row_bytes}};
+    const struct { const void *p; uint64_t bytes; } out[4] = {{a.dz, want_dz ? span(N, a.ld_dz, a.V, kElem) : 0}, {a.loss, from_saved ? 0 : row_bytes},
+                                                              {a.stats, row_bytes * 4}, {workspace, static_cast<uint64_t>(need)}};
+    for (int i = 0; i < 4; ++i) {
+        for (int k = 0; k < 5; ++k) {
+            if (i == 0 && k == 0 && static_cast<const void *>(a.dz) == a.z && a.ld_dz == a.ld) continue;     // in place
+            if (overlap(out[i].p, out[i].bytes, in[k].p, in[k].bytes)) return CX_ERR_ALIAS;
+        }
+        for (int k = i + 1; k < 4; ++k)
+            if (overlap(out[i].p, out[i].bytes, out[k].p, out[k].bytes)) return CX_ERR_ALIAS;
+    }
+    if (!want_dz) a.dz = nullptr;
+    a.parts = space.parts;
+    a.part_stats = static_cast<Stats *>(workspace);
+    const bool dual = a.w_kl != 0.0f && a.w_ce != 0.0f && a.tau != 1.0f;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+#define CX_DISTILL(KERNEL, GRID) hipLaunchKernelGGL(KERNEL, GRID, dim3(kRowThreads), 0, st, b)
+    for (int64_t n0 = 0; n0 < N; n0 += 65535) {         // rows in slices of a grid's second dimension
+        const unsigned rows = static_cast<unsigned>(N - n0 < 65535 ? N - n0 : 65535);
+        DistillArgs<E> b = a;
+        b.z += n0 * a.ld;
+        if (b.dz) b.dz += n0 * a.ld_dz;
+        if (b.ids) b.ids += n0 * a.K;
+        if (b.t) b.t += n0 * a.K;
+        if (b.labels) b.labels += n0;
+        if (b.gout) b.gout += n0;
+        if (b.loss) b.loss += n0;
+        if (b.stats) b.stats += n0 * 4;
+        const dim3 grid(space.parts, rows);
+        if (from_saved) {
+            if (dual) CX_DISTILL((distill_kernel<E, kDual, kSaved>), grid); else CX_DISTILL((distill_kernel<E, kNone, kSaved>), grid);
+        } else if (space.parts == 1) {
+            if (dual) CX_DISTILL((distill_kernel<E, kDual, kHere>), grid); else CX_DISTILL((distill_kernel<E, kNone, kHere>), grid);
+        } else {                                        // few rows: one slice
+            if (dual) CX_DISTILL((part_kernel<E, kDual>), grid); else CX_DISTILL((part_kernel<E, kNone>), grid);
+            if (launched() != CX_OK) return CX_ERR_HIP;
+            // the loss reads logits of all parts: where gradients replace them, it comes first, in a launch of its own
+            const bool in_place = want_dz && static_cast<const void *>(a.dz) == a.z;
+            if (in_place) {
+                b.dz = nullptr;
+                const dim3 one(1, rows);
+                if (dual) CX_DISTILL((distill_kernel<E, kDual, kParts>), one); else CX_DISTILL((distill_kernel<E, kNone, kParts>), one);
+                if (launched() != CX_OK) return CX_ERR_HIP;
+                b.dz = a.dz;
+                b.loss = nullptr;
+            }
+            const dim3 second(want_dz ? space.parts : 1, rows);
+            if (dual) CX_DISTILL((distill_kernel<E, kDual, kParts>), second); else CX_DISTILL((distill_kernel<E, kNone, kParts>), second);
+        }
+        if (launched() != CX_OK) return CX_ERR_HIP;
+    }
+#undef CX_DISTILL
+    return CX_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+#define CX_LM_DISTILL(SUFFIX, E)                                                                                                      \
+    int cx_distill_loss##SUFFIX(const E::T *z, int64_t ld, int64_t N, int32_t V, int32_t K, const int32_t *ids, const float *t,       \
+                                const int32_t *labels, float tau, float w_kl, float w_ce, float *loss, float *stats,                  \
+                                void *workspace, int64_t workspace_bytes, void *stream)                                               \
+    {                                                                                                                                 \
+        DistillArgs<E> a{};                                                                                                           \
+        a.z = z; a.ids = ids; a.labels = labels; a.t = t; a.loss = loss; a.stats = stats; a.ld = ld; a.V = V; a.K = K;                \
+        a.tau = tau; a.w_kl = w_kl; a.w_ce = w_ce;                                                                                    \
+        return distill<E>(a, N, false, false, workspace, workspace_bytes, stream);                                                    \
+    }                                                                                                                                 \
+    int cx_distill_grad##SUFFIX(const E::T *z, int64_t ld, int64_t N, int32_t V, int32_t K, const int32_t *ids, const float *t,       \
+                                const int32_t *labels, float tau, float w_kl, float w_ce, const float *stats, const float *gout,      \
+                                E::T *dz, int64_t ld_dz, void *stream)                                                                \
+    {                                                                                                                                 \
+        DistillArgs<E> a{};                                                                                                           \
+        a.z = z; a.ids = ids; a.labels = labels; a.t = t; a.stats = const_cast<float *>(stats); a.gout = gout; a.dz = dz; a.ld = ld;  \
+        a.ld_dz = ld_dz; a.V = V; a.K = K; a.tau = tau; a.w_kl = w_kl; a.w_ce = w_ce;                                                 \
+        return distill<E>(a, N, true, true, nullptr, 0, stream);                                                                      \
+    }                                                                                                                                 \
+    int cx_distill_step##SUFFIX(const E::T *z, int64_t ld, int64_t N, int32_t V, int32_t K, const int32_t *ids, const float *t,       \
+                                const int32_t *labels, float tau, float w_kl, float w_ce, const float *gout, float *loss,             \
+                                E::T *dz, int64_t ld_dz, void *workspace, int64_t workspace_bytes, void *stream)                      \
+    {                                                                                                                                 \
+        DistillArgs<E> a{};                                                                                                           \
+        a.z = z; a.ids = ids; a.labels = labels; a.t = t; a.loss = loss; a.gout = gout; a.dz = dz; a.ld = ld; a.ld_dz = ld_dz;        \
+        a.V = V; a.K = K; a.tau = tau; a.w_kl = w_kl; a.w_ce = w_ce;                                                                  \
+        return distill<E>(a, N, false, true, workspace, workspace_bytes, stream);                                                     \
+    }
+CX_LM_DISTILL(, F32)
+CX_LM_DISTILL(_bf16, Bf16)
+CX_LM_DISTILL(_f16, F16)
+#undef CX_LM_DISTILL
+
+int cx_distill_workspace(int64_t N, int32_t V, int64_t *bytes)
+{
+    if (!bytes) return CX_ERR_NULL;
+    *bytes = 0;
+    const int rc = check_sizes(N, V, 0);
+    if (rc != CX_OK || N == 0) return rc;
+    const int64_t wide = distill_space(N, V, F32::kPer16).bytes, narrow = distill_space(N, V, Bf16::kPer16).bytes;
+    *bytes = wide > narrow ? wide : narrow;
+    return CX_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,145 @@
+// One pass over a row of logits (internal header): running maximum and sums of exponentials of what a workgroup reads, and the
+// joining of such statistics over lanes, wavefronts and the parts of a split row.
+//
+// Logits count as differences to the running maximum, so that rows of a type's lowest value are a uniform distribution
+// rather than an overflow.  The maximum starts at the lowest finite value: a row of -inf alone ends with s = 0, +inf and NaN
+// make s NaN.
+#ifndef CX_LM_VOCAB_HPP
+#define CX_LM_VOCAB_HPP
+#include "lm_common.hpp"
+
+namespace {
+
+constexpr int kRowThreads = 512, kRowWaves = kRowThreads / kWave;
+constexpr int kAhead = 4;                               // 16-byte loads a thread has in flight
+constexpr float kLowest = -3.40282346638528859812e38f;
+constexpr float kVanish = -200.0f;                      // exponents (base 2) from here on give 0; keeps 0 * inf out of the sums
+
+// u: WITH_ENTROPY: sum of e * log2(e), e = 2^((z - m) c);  DUAL: the sum of 2^((z - m) c2);  otherwise unused.
+enum Extra { kNone, kEntropy, kDual };
+
+struct Stats {
+    float m, s, u;
+};
+
+__device__ __forceinline__ float not_below(float v, float lowest) { return v < lowest ? lowest : v; }
+
+template <Extra X>
+__device__ __forceinline__ void rebase(Stats &a, float m, float c, float c2)
+{
+    const float d = not_below((a.m - m) * c, kVanish), f = exp2_fast(d);
+    if (X == kEntropy) a.u = f * __builtin_fmaf(a.s, d, a.u);
+    if (X == kDual) a.u *= exp2_fast(not_below((a.m - m) * c2, kVanish));
+    a.s *= f;
+    a.m = m;
+}
+
+template <Extra X>
+__device__ __forceinline__ Stats join(Stats a, Stats b, float c, float c2)
+{
+    const float m = fmaxf(a.m, b.m);
+    rebase<X>(a, m, c, c2);
+    rebase<X>(b, m, c, c2);
+    return {m, a.s + b.s, a.u + b.u};
+}
+
+template <Extra X, int N>
+__device__ __forceinline__ float accumulate(Stats &a, const float (&z)[N], float c, float c2)
+{
+    float top = z[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) top = fmaxf(top, z[j]);
+    rebase<X>(a, fmaxf(a.m, top), c, c2);
+    float s[2] = {}, u[2] = {};
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float d = z[j] - a.m, t = d * c, e = exp2_fast(t);
+        s[j & 1] += e;
+        if (X == kEntropy) u[j & 1] = __builtin_fmaf(e, fmaxf(t, kVanish), u[j & 1]);
+        if (X == kDual) u[j & 1] += exp2_fast(d * c2);
+    }
+    a.s += s[0] + s[1];
+    a.u += u[0] + u[1];
+    return top;
+}
+
+// The statistics of all threads of the workgroup, in every thread.
+template <Extra X>
+__device__ __forceinline__ Stats join_workgroup(Stats a, Stats (&lds)[kRowWaves], float c, float c2)
+{
+#pragma unroll
+    for (int d = kWave / 2; d > 0; d /= 2)
+        a = join<X>(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.u, d)}, c, c2);
+    if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = a;
+    __syncthreads();
+    a = lds[0];
+#pragma unroll
+    for (int k = 1; k < kRowWaves; ++k) a = join<X>(a, lds[k], c, c2);
+    return a;
+}
+
+// A slice of a row: `vectors` whole 16-byte vectors from its first element on (which need not be aligned to more than an
+// element), then `tail` elements.
+template <class E>
+struct Slice {
+    const typename E::T *z;
+    int vectors, tail;
+    __device__ __forceinline__ Slice(const typename E::T *row, int64_t lo, int64_t hi)
+        : z(row + lo), vectors(static_cast<int>((hi - lo) / E::kPer16)), tail(static_cast<int>((hi - lo) % E::kPer16)) {}
+    __device__ __forceinline__ int rounds() const { return (vectors + kRowThreads * kAhead - 1) / (kRowThreads * kAhead); }
+    static __device__ __forceinline__ int vector_of(int round, int k) { return (round * kAhead + k) * kRowThreads + static_cast<int>(threadIdx.x); }
+    // the thread's kAhead vectors of a round; what lies beyond the slice counts as -inf
+    __device__ __forceinline__ void load(int round, float (&v)[kAhead * E::kPer16]) const
+    {
+        u4 w[kAhead];
+        if ((round + 1) * kAhead * kRowThreads <= vectors) {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) w[k] = load16<E>(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) unpack(w[k], v, k);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (vector_of(round, k) < vectors) w[k] = load16<E>(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
+                else w[k] = u4{};
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                unpack(w[k], v, k);
+                if (vector_of(round, k) >= vectors)
+#pragma unroll
+                    for (int j = 0; j < E::kPer16; ++j) v[k * E::kPer16 + j] = -__builtin_inff();
+            }
+        }
+    }
+    static __device__ __forceinline__ void unpack(const u4 &w, float (&v)[kAhead * E::kPer16], int k)
+    {
+        float one[E::kPer16];
+        E::unpack(w, one);
+#pragma unroll
+        for (int j = 0; j < E::kPer16; ++j) v[k * E::kPer16 + j] = one[j];
+    }
+    __device__ __forceinline__ bool has_tail() const { return static_cast<int>(threadIdx.x) < tail; }
+    __device__ __forceinline__ int64_t tail_at() const { return static_cast<int64_t>(vectors) * E::kPer16 + threadIdx.x; }
+};
+
+// How many workgroups share a row: where rows alone leave CUs idle, as many as give each CU two, and no part shorter than
+// a workgroup's first loads.
+[[maybe_unused]] int parts_of(int64_t N, int64_t V, int per16)
+{
+    constexpr int64_t kWanted = 512, kMost = 32;
+    int64_t parts = N < kWanted ? ceil_div(kWanted, N) : 1;
+    const int64_t fit = ceil_div(V, static_cast<int64_t>(kRowThreads) * per16 * 2);
+    parts = parts < fit ? parts : fit;
+    return static_cast<int>(parts < kMost ? parts : kMost);
+}
+
+// Columns of part `part`: whole vectors but for the last part's end.
+__host__ __device__ __forceinline__ int64_t part_begin(int64_t V, int parts, int part, int per16)
+{
+    const int64_t each = (V / per16 + parts - 1) / parts * per16, at = each * part;
+    return part >= parts || at > V ? V : at;
+}
+
+}  // namespace
+
+#endif  // CX_LM_VOCAB_HPP

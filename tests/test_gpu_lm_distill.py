@@ -1,0 +1,158 @@
+"""cx_distill_loss, cx_distill_grad and cx_distill_step against their formulas in 64 bits."""
+import pytest
+import torch
+
+import lm_reference as R
+from paper_2012_15198_amd import cxlm as lm
+
+DEV = "cuda:0"
+pytestmark = pytest.mark.gpu
+
+
+def make(N, V, K, dtype, seed, sigma=2.5):
+    gen = torch.Generator().manual_seed(seed)
+    z = (torch.randn((N, V), generator=gen) * sigma).to(dtype)
+    ids = torch.stack([torch.randperm(V, generator=gen)[:K] if K <= V else torch.randint(0, V, (K,), generator=gen) for _ in range(N)]).int() \
+        if N and K else torch.empty((N, K), dtype=torch.int32)
+    t = torch.randn((N, K), generator=gen) * 2 + 5
+    labels = torch.randint(0, V, (N,), generator=gen).int()
+    gout = torch.rand(N, generator=gen) + 0.5
+    return z, ids, t, labels, gout
+
+
+def run(suffix, z, ids, t, labels, gout, tau, w_kl, w_ce, offset=0, in_place=False):
+    """Both ways: loss then gradient, and the step; their results, which are the same bits."""
+    N, V = z.shape
+    on = lambda v: None if v is None else v.to(DEV)
+
+    def placed(v):
+        m = torch.full((N, V + offset + (1 if offset else 0)), 3.0, dtype=z.dtype, device=DEV)
+        m[:, offset:offset + V] = v.to(DEV)
+        return m[:, offset:offset + V]
+
+    results = []
+    for step in (False, True):
+        zd = placed(z)
+        dz = zd if in_place else placed(torch.full_like(z, 7.0))
+        loss, stats = torch.full((N,), 7.0, device=DEV), torch.empty((N, 4), device=DEV)
+        head = (zd, on(ids), on(t), on(labels))
+        if step:
+            getattr(lm, "cx_distill_step" + suffix)(*head, on(gout), loss, dz, tau, w_kl, w_ce)
+        else:
+            getattr(lm, "cx_distill_loss" + suffix)(*head, loss, stats, tau, w_kl, w_ce)
+            getattr(lm, "cx_distill_grad" + suffix)(*head, stats, on(gout), dz, tau, w_kl, w_ce)
+        if offset:
+            assert (dz._base[:, :offset] == 3).all() and (dz._base[:, offset + V:] == 3).all()
+            assert in_place or (zd._base[:, :offset] == 3).all()
+        results.append((loss, dz))
+    for a, b in zip(*results):
+        assert torch.equal(a.nan_to_num(99.0), b.nan_to_num(99.0))
+    return results[0]
+
+
+def compare(suffix, z, ids, t, labels, gout, tau, w_kl, w_ce, **kw):
+    loss, dz = run(suffix, z, ids, t, labels, gout, tau, w_kl, w_ce, **kw)
+    ref, grad, slack, grad_slack = R.distill(z, ids, t, labels, gout, tau, w_kl, w_ce)
+    R.check(loss, ref, slack, "loss")
+    R.check(dz, grad, grad_slack, "dz")
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("N,V,K", [(1, 1, 1), (2, 3, 2), (3, 17, 5), (1, 4096, 32), (2, 4097, 256), (5, 1000, 0), (700, 70, 9), (515, 4_111, 64),
+                                   (1, 50_001, 64), (3, 20_000, 100)])
+def test_rows(suffix, in_place, N, V, K):
+    z, ids, t, labels, gout = make(N, V, K, R.TYPES[suffix], N + V + K)
+    if N > 2:
+        labels[0], labels[1] = -1, V
+        if K:
+            ids[2, ::2], ids[1, 0] = -1, V
+    compare(suffix, z, ids, t, labels, gout, 2.0, 0.7, 0.3, offset=N % 3, in_place=in_place)
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("tau,w_kl,w_ce", [(1.0, 0.7, 0.3), (0.5, 1.0, 1.0), (4.0, 1.0, 0.0), (2.0, 0.0, 1.0), (3.0, 0.0, 0.0)])
+@pytest.mark.parametrize("N", [3, 520])
+def test_weights_and_temperatures(suffix, N, tau, w_kl, w_ce):
+    z, ids, t, labels, gout = make(N, 1_501, 12, R.TYPES[suffix], 9)
+    compare(suffix, z, ids, t, labels, gout, tau, w_kl, w_ce)
+    compare(suffix, z, ids, t, None, gout, tau, w_kl, w_ce)
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("N,V", [(12, 6_000), (12, 30), (530, 700)])
+def test_masks_empty_rows_and_repeated_ids(suffix, N, V):
+    dtype = R.TYPES[suffix]
+    z, ids, t, labels, gout = make(N, V, 8, dtype, N + V)
+    ids[0] = -1                                        # no teacher
+    labels[0] = -1                                     # and no label: the row counts for nothing
+    z[0, ::3] = torch.nan
+    z[1] = -torch.inf                                  # no student
+    ids[2, 3:] = ids[2, 2]                             # an id six times
+    labels[2] = ids[2, 2]                              # which is the label too
+    t[3, 4:] = -torch.inf                              # teacher's logits that count for nothing
+    t[4] = -torch.inf
+    z[5, torch.rand(V, generator=torch.Generator().manual_seed(1)) < 0.5] = -torch.inf
+    z[5, ids[5].long()] = 1.0
+    z[5, labels[5]] = 0.5
+    ids[6, 1:] = -1                                    # a teacher that is certain
+    z[7] = 0.25                                        # uniform
+    z[8] = torch.finfo(dtype).min                      # uniform, of the lowest value
+    z[9, 1:] = torch.finfo(dtype).min                  # one logit above masks of the lowest value
+    z[9, ids[9].long()], z[9, labels[9]] = 1.0, 2.0
+    ids[10], labels[10] = -1, V // 2                   # a label alone
+    labels[11] = -5
+    loss, dz = run(suffix, z, ids, t, labels, gout, 2.0, 0.7, 0.3)
+    ref, grad, slack, grad_slack = R.distill(z, ids, t, labels, gout, 2.0, 0.7, 0.3)
+    assert float(loss[0]) == 0 and (dz[0] == 0).all() and float(loss[1]) == 0 and (dz[1] == 0).all()
+    extreme = torch.zeros(N, dtype=torch.bool)
+    extreme[[0, 8, 9]] = True
+    R.check(loss.cpu()[~extreme], ref[~extreme], slack[~extreme])
+    R.check(dz.cpu()[~extreme], grad[~extreme], grad_slack[~extreme])
+    # the lowest value: as a row of equal logits; as masks: as -inf
+    for row, like in ((8, 0.25), (9, -torch.inf)):
+        other = z[row:row + 1].clone()
+        other[other == torch.finfo(dtype).min] = like
+        one = slice(row, row + 1)
+        want, wgrad, wslack, wgslack = R.distill(other, ids[one], t[one], labels[one], gout[one], 2.0, 0.7, 0.3)
+        R.check(loss[one], want, wslack)
+        R.check(dz[one], wgrad, wgslack)
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+def test_nan_and_infinite_logits_stay_in_their_rows(suffix):
+    z, ids, t, labels, gout = make(530, 900, 4, R.TYPES[suffix], 3)
+    z[5, 7], z[6, 8] = torch.nan, torch.inf
+    for rows in (slice(0, 530), slice(4, 9)):          # a workgroup a row, and several
+        loss, dz = run(suffix, z[rows], ids[rows], t[rows], labels[rows], gout[rows], 2.0, 0.7, 0.3)
+        broken = torch.zeros(530, dtype=torch.bool)
+        broken[5:7] = True
+        assert torch.equal(loss.isnan().cpu(), broken[rows]) and torch.equal(dz.isnan().all(1).cpu(), broken[rows])
+        assert torch.equal(dz.isnan().any(1).cpu(), broken[rows])
+
+
+def test_gradient_against_differences():
+    """Central differences of the 64-bit loss at drawn logits, teacher's ids and the label."""
+    tau, w_kl, w_ce = 1.7, 0.8, 0.4
+    z, ids, t, labels, gout = make(2, 60, 5, torch.float32, 21)
+    _, dz = run("", z, ids, t, labels, gout, tau, w_kl, w_ce)
+    value = lambda z: R.distill(z, ids, t, labels, gout, tau, w_kl, w_ce)[0]
+    for row in range(2):
+        for v in [*ids[row].tolist(), int(labels[row]), 0, 17, 59]:
+            up, down = z.double().clone(), z.double().clone()
+            up[row, v] += 1e-5
+            down[row, v] -= 1e-5
+            slope = float((value(up) - value(down))[row]) / 2e-5 * float(gout[row])
+            assert abs(slope - float(dz[row, v])) < 1e-6, (row, v)
+
+
+def test_no_rows_and_top_scores_of_a_teacher():
+    e = lambda *s, d=torch.float32: torch.empty(s, dtype=d, device=DEV)
+    lm.cx_distill_step(e(0, 9), e(0, 2, d=torch.int32), e(0, 2), None, e(0), e(0), e(0, 9), 1.0, 1.0, 0.0)
+    # a student that is its own teacher, all alternatives given: loss and gradient vanish
+    z = torch.randn((6, 50), device=DEV)
+    ids, top = e(6, 50, d=torch.int32), e(6, 50)
+    lm.cx_token_scores(z, None, None, None, ids, top)
+    loss, dz = e(6), torch.empty_like(z)
+    lm.cx_distill_step(z, ids, top, None, torch.ones(6, device=DEV), loss, dz, 1.0, 1.0, 0.0)
+    assert loss.abs().max() < 200 * R.U * 10 and dz.abs().max() < 200 * R.U
