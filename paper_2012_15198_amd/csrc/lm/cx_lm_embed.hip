@@ -8,22 +8,22 @@
 //
 // The gradient writes each row of the table once and adds in a fixed order, which atomics would not.  Three launches:
 //   sort_kernel   a stable counting sort of each worker's tokens.  A workgroup owns 512 ids and reads all N tokens
-//                 itself, twice, instead of exchanging counts with the others: no passes, no atomics on memory, and where the
+//                 itself instead of exchanging counts with the others: no passes, no atomics on memory, and where the
 //                 table has 32,768 rows 64 workgroups a worker read 64 x 16 KB of tokens from the cache.
-//   grad_kernel   a group of lanes for every row of the table: sums the rows of dout that the sorted list names (none: zeros).
-//                 Lists longer than kLong would make one group work long after the others, so those are cut at every
-//                 kLong-th place of the sorted list into pieces that other workgroups of the same launch sum up;
-//   join_kernel   adds the pieces of such a list in order.
+//   grad_kernel   the sorted list in pieces of equal length, one to a group of lanes, so that a frequent token keeps no group longer than
+//                 a rare one: it adds up the rows of dout that its piece names, list by list, and writes what lists lie inside the
+//                 piece; what reaches beyond goes to the workspace.  Other workgroups of the same launch write the rows that no
+//                 token names.
+//   join_kernel   adds up the lists that reach over several pieces, in order.
 #include "lm_common.hpp"
 
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBins = 512;                  // ids of a workgroup of the sort
-constexpr int kSortWaves = 8;
-constexpr int kSortAhead = 4;               // tokens a lane loads before it looks at them
-constexpr int kLong = 64;                   // tokens of one id from which its list is cut; also the length of a piece
-constexpr int kRowsPerGroup = 4;            // rows of the table a group of lanes handles one after the other
+constexpr int kSortWaves = 16;
+constexpr int kHeld = 8;                    // tokens a lane of the sort keeps in registers between its two walks
+constexpr int kEmptyRows = 8;               // rows of the table a group of lanes looks at for being named by no token
 constexpr int64_t kMaxTokens = CX_MAX_TOKENS;
 constexpr int32_t kMaxVocab = CX_MAX_VOCAB, kMaxWidth = CX_MAX_WIDTH;
 
@@ -91,123 +91,110 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const typename E::T *t
         if (n0 + r < N) c.store(out + (w * N + n0 + r) * ld_out, v[r]);
 }
 
-// starts[w][v]: where the list of id v begins in order[w]; order[w]: places of the tokens, by id, then ascending.
-__global__ __launch_bounds__(kSortWaves *kWave) void sort_kernel(const int32_t *tokens, int64_t N, int32_t V, int32_t *starts, int32_t *order)
+struct Sorted {
+    int32_t id, n;                          // a token and its place
+};
+
+// sorted[w]: the tokens of worker w by id, then by place; named[w]: a bit for every id, set if a token is that id;
+// total[w]: the tokens that are an id at all.
+__global__ __launch_bounds__(kSortWaves *kWave) void sort_kernel(const int32_t *tokens, int64_t N, int32_t V, Sorted *sorted, uint64_t *named,
+                                                                 int32_t *total)
 {
     __shared__ unsigned count[kSortWaves][kBins];
-    __shared__ unsigned below_of[kSortWaves], total_of[kSortWaves];
+    __shared__ unsigned below_of[kSortWaves], sum_of[kBins / kWave];
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
     const int32_t lo = static_cast<int32_t>(blockIdx.x) * kBins;
     const unsigned ids = V - lo < kBins ? V - lo : kBins;
     tokens += blockIdx.y * N;
-    order += blockIdx.y * N;
-    starts += blockIdx.y * (static_cast<int64_t>(V) + 1) + lo;
-#pragma unroll
-    for (int k = 0; k < kSortWaves; ++k) count[k][threadIdx.x] = 0;
-    __syncthreads();
-    // every wavefront counts a contiguous part of the tokens
+    sorted += blockIdx.y * N;
+    // every wavefront has a contiguous part of the tokens
     const int64_t part = (N + kSortWaves * kWave - 1) / (kSortWaves * kWave) * kWave;
     const int64_t from = wave * part, to = from + part < N ? from + part : N;
+    int held[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) held[k] = from + k * kWave + lane < to ? tokens[from + k * kWave + lane] : -1;
+    for (int k = threadIdx.x; k < kSortWaves * kBins; k += kSortWaves * kWave) (&count[0][0])[k] = 0;
+    __syncthreads();
     int below = 0;
-    for (int64_t n = from; n < to; n += kSortAhead * kWave) {
-        int token[kSortAhead];
+    const auto tally = [&](int token) {
+        below += __popcll(__ballot(token >= 0 && token < lo));
+        const unsigned bin = static_cast<unsigned>(token) - static_cast<unsigned>(lo);
+        if (token >= 0 && bin < ids) atomicAdd(&count[wave][bin], 1u);                 // in LDS, integers
+    };
 #pragma unroll
-        for (int k = 0; k < kSortAhead; ++k) token[k] = n + k * kWave + lane < to ? tokens[n + k * kWave + lane] : -1;
-#pragma unroll
-        for (int k = 0; k < kSortAhead; ++k) {
-            below += __popcll(__ballot(token[k] >= 0 && token[k] < lo));
-            const unsigned bin = static_cast<unsigned>(token[k]) - static_cast<unsigned>(lo);
-            if (token[k] >= 0 && bin < ids) atomicAdd(&count[wave][bin], 1u);          // in LDS, integers
-        }
-    }
+    for (int k = 0; k < kHeld; ++k) tally(held[k]);
+    for (int64_t n = from + kHeld * kWave; n < to; n += kWave) tally(n + lane < to ? tokens[n + lane] : -1);
     if (lane == 0) below_of[wave] = below;
     __syncthreads();
-    // exclusive sums: over the wavefronts of a bin, then over the bins
-    unsigned mine = 0, first = 0;
+    // a thread for every id: exclusive sums over the wavefronts, then over the ids
+    unsigned mine = 0, sum = 0;
+    if (threadIdx.x < kBins) {
 #pragma unroll
-    for (int k = 0; k < kSortWaves; ++k) {
-        const unsigned c = count[k][threadIdx.x];
-        count[k][threadIdx.x] = mine;
-        mine += c;
-        first += below_of[k];
-    }
-    unsigned sum = mine;
+        for (int k = 0; k < kSortWaves; ++k) {
+            const unsigned c = count[k][threadIdx.x];
+            count[k][threadIdx.x] = mine;
+            mine += c;
+        }
+        sum = mine;
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const unsigned other = __shfl_up(sum, d);
-        if (lane >= d) sum += other;
+        for (int d = 1; d < kWave; d *= 2) {
+            const unsigned other = __shfl_up(sum, d);
+            if (lane >= d) sum += other;
+        }
+        if (lane == kWave - 1) sum_of[wave] = sum;
+        const uint64_t bits = __ballot(mine != 0);
+        if (lane == 0 && threadIdx.x < ids) named[blockIdx.y * ((static_cast<int64_t>(V) + 63) / 64) + lo / 64 + wave] = bits;
     }
-    if (lane == kWave - 1) total_of[wave] = sum;
     __syncthreads();
-    for (int k = 0; k < wave; ++k) first += total_of[k];
-    first += sum - mine;
-    if (threadIdx.x < ids) starts[threadIdx.x] = static_cast<int32_t>(first);
-    if (threadIdx.x + 1 == ids && lo + static_cast<int32_t>(ids) == V) starts[ids] = static_cast<int32_t>(first + mine);
+    if (threadIdx.x < kBins) {
+        unsigned first = sum - mine;
+        for (int k = 0; k < kSortWaves; ++k) first += below_of[k];
+        for (int k = 0; k < wave; ++k) first += sum_of[k];
+        if (threadIdx.x + 1 == ids && lo + static_cast<int32_t>(ids) == V) total[blockIdx.y] = static_cast<int32_t>(first + mine);
 #pragma unroll
-    for (int k = 0; k < kSortWaves; ++k) count[k][threadIdx.x] += first;
+        for (int k = 0; k < kSortWaves; ++k) count[k][threadIdx.x] += first;
+    }
     __syncthreads();
     // the same walk again: the lanes of a wavefront that hold one id take consecutive places
-    for (int64_t n = from; n < to; n += kSortAhead * kWave) {
-        int token[kSortAhead];
+    const auto put = [&](int token, int64_t n) {
+        const unsigned bin = static_cast<unsigned>(token) - static_cast<unsigned>(lo);
+        const bool here = token >= 0 && bin < ids;
+        unsigned long long same = __ballot(here);
+        if (same == 0) return;
 #pragma unroll
-        for (int k = 0; k < kSortAhead; ++k) token[k] = n + k * kWave + lane < to ? tokens[n + k * kWave + lane] : -1;
-#pragma unroll
-        for (int k = 0; k < kSortAhead; ++k) {
-            const unsigned bin = static_cast<unsigned>(token[k]) - static_cast<unsigned>(lo);
-            const bool here = token[k] >= 0 && bin < ids;
-            unsigned long long same = __ballot(here);
-            if (same == 0) continue;
-#pragma unroll
-            for (int bit = 1; bit < kBins; bit *= 2) {
-                const unsigned long long set = __ballot((bin & bit) != 0);
-                same &= (bin & bit) != 0 ? set : ~set;
-            }
-            const int leader = here ? __ffsll(same) - 1 : lane;
-            unsigned at = 0;
-            if (here && lane == leader) at = atomicAdd(&count[wave][bin], static_cast<unsigned>(__popcll(same)));
-            at = __shfl(at, leader);
-            if (here) order[at + __popcll(same & ((1ull << lane) - 1))] = static_cast<int32_t>(n + k * kWave + lane);
+        for (int bit = 1; bit < kBins; bit *= 2) {
+            const unsigned long long set = __ballot((bin & bit) != 0);
+            same &= (bin & bit) != 0 ? set : ~set;
         }
-    }
+        const int leader = here ? __ffsll(same) - 1 : lane;
+        unsigned at = 0;
+        if (here && lane == leader) at = atomicAdd(&count[wave][bin], static_cast<unsigned>(__popcll(same)));
+        at = __shfl(at, leader);
+        if (here) sorted[at + __popcll(same & ((1ull << lane) - 1))] = {token, static_cast<int32_t>(n + lane)};
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) put(held[k], from + k * kWave);
+    for (int64_t n = from + kHeld * kWave; n < to; n += kWave) put(n + lane < to ? tokens[n + lane] : -1, n);
 }
 
 template <class E>
 struct GradArgs {
     const typename E::T *dout;
     int64_t ld_dout;
-    const int32_t *tokens, *starts, *order;
-    float *pieces;                          // [W][chunks][2][D]
+    const Sorted *sorted;
+    const uint64_t *named;
+    const int32_t *total;
+    float *pieces;                          // [W][chunks][2][D]: a piece's sums of the list that begins before it, of the one that goes on behind it
     const typename E::T *g_in;              // first element of the table's columns, or NULL
     typename E::T *g_out;
     int64_t ld, N;
-    int32_t V, D, chunks;
+    int32_t V, D, chunks, chunk_blocks;
     float scale;
-    int shift;
+    int shift, piece;                       // lanes of a group (log2), tokens of a piece
 };
 
-// sum over i in [s, e) of rows[order[i]], in that order
 template <class E>
-__device__ __forceinline__ void add_rows(const Columns<E> &c, const typename E::T *rows, int64_t ld, const int32_t *order, int s, int e,
-                                         float (&sum)[E::kPer16])
-{
-    constexpr int kAhead = 4;
-    for (int i = s; i < e; i += kAhead) {
-        float v[kAhead][E::kPer16];
-        int at[kAhead];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) at[k] = order[i + k < e ? i + k : e - 1];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) c.load(rows + at[k] * ld, v[k]);
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (i + k < e)
-#pragma unroll
-                for (int j = 0; j < E::kPer16; ++j) sum[j] += v[k][j];
-    }
-}
-
-template <class E>
-__device__ __forceinline__ void finish(const GradArgs<E> &a, const Columns<E> &c, int64_t w, int32_t v, float (&sum)[E::kPer16])
+__device__ __forceinline__ void finish(const GradArgs<E> &a, const Columns<E> &c, int64_t w, int32_t v, const float (&sum)[E::kPer16])
 {
     const int64_t at = w * a.ld + static_cast<int64_t>(v) * a.D;
     float g[E::kPer16];
@@ -217,113 +204,138 @@ __device__ __forceinline__ void finish(const GradArgs<E> &a, const Columns<E> &c
     c.store(a.g_out + at, g);
 }
 
-// The groups' sums added in order of the groups; the first group holds the result.
+// One piece of the sorted list; `list` holds it and its neighbours (id -1: none).
 template <class E>
-__device__ __forceinline__ void add_groups(float (&sum)[E::kPer16], float *lds, int shift)
+__device__ __forceinline__ void sum_piece(const GradArgs<E> &a, const Columns<E> &c, int64_t w, int chunk, int tokens, const Sorted *list)
 {
-    const int lanes = 1 << shift;
-#pragma unroll
-    for (int j = 0; j < E::kPer16; ++j) lds[j * kThreads + threadIdx.x] = sum[j];
-    __syncthreads();
-    if (static_cast<int>(threadIdx.x) < lanes)
-        for (int at = threadIdx.x + lanes; at < kThreads; at += lanes)
-#pragma unroll
-            for (int j = 0; j < E::kPer16; ++j) sum[j] += lds[j * kThreads + at];
-    __syncthreads();
-}
-
-// A piece: places [kLong * chunk, kLong * (chunk + 1)) of the sorted list.  At most two lists longer than that reach into it: the
-// one that its first place belongs to (slot 0) and, if it is another, the one of its last place (slot 1).
-template <class E>
-__device__ void sum_piece(const GradArgs<E> &a, int chunk, float *lds)
-{
-    const int64_t w = blockIdx.z;
-    const int32_t *starts = a.starts + w * (static_cast<int64_t>(a.V) + 1), *order = a.order + w * a.N, *tokens = a.tokens + w * a.N;
-    const int all = starts[a.V], p0 = chunk * kLong;
-    if (p0 >= all) return;
-    const int p1 = p0 + kLong < all ? p0 + kLong : all;
-    const int lanes = 1 << a.shift, groups = kThreads >> a.shift, group = threadIdx.x >> a.shift;
-    const Columns<E> c = columns_of<E>(threadIdx.x & (lanes - 1), lanes, blockIdx.y, a.D);
-    const int first = tokens[order[p0]], last = tokens[order[p1 - 1]];
-    for (int slot = 0; slot < (first == last ? 1 : 2); ++slot) {
-        const int id = slot ? last : first;
-        const int s = starts[id], e = starts[id + 1];
-        if (e - s <= kLong) continue;                                  // the same for every thread of the workgroup
-        const int lo = s > p0 ? s : p0, hi = e < p1 ? e : p1, each = (hi - lo + groups - 1) / groups;
-        const int from = lo + group * each, to = from + each < hi ? from + each : hi;
-        float sum[E::kPer16] = {};
-        if (c.n) add_rows<E>(c, a.dout + w * a.N * a.ld_dout, a.ld_dout, order, from, to, sum);
-        add_groups<E>(sum, lds, a.shift);
-        if (group == 0 && c.n) {
-            float *to_row = a.pieces + ((w * a.chunks + chunk) * 2 + slot) * a.D + c.first;
+    constexpr int kRows = 4;                // rows of dout in flight
+    const typename E::T *rows = a.dout + w * a.N * a.ld_dout;
+    float sum[E::kPer16] = {};
+    int id = list[0].id;
+    bool began = list[-1].id != id;         // in this piece
+    const auto close = [&](bool ends) {
+        if (began && ends) {
+            finish<E>(a, c, w, id, sum);
+        } else {
+            float *to = a.pieces + ((w * a.chunks + chunk) * 2 + (began ? 1 : 0)) * a.D + c.first;
 #pragma unroll
             for (int j = 0; j < E::kPer16; ++j)
-                if (j < c.n) to_row[j] = sum[j];
+                if (j < c.n) to[j] = sum[j];
+        }
+    };
+    for (int i = 0; i < tokens; i += kRows) {
+        float v[kRows][E::kPer16];
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) c.load(rows + list[i + k < tokens ? i + k : tokens - 1].n * a.ld_dout, v[k]);
+#pragma unroll
+        for (int k = 0; k < kRows; ++k) {
+            if (i + k >= tokens) break;
+            const int next = list[i + k].id;
+            if (next != id) {
+                close(true);
+                id = next;
+                began = true;
+#pragma unroll
+                for (int j = 0; j < E::kPer16; ++j) sum[j] = 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < E::kPer16; ++j) sum[j] += v[k][j];
         }
     }
+    close(list[tokens].id != id);
 }
 
 // IN_PLACE: g_out is g_in, rows that no token names stay as they are.
 template <class E, bool IN_PLACE>
 __global__ __launch_bounds__(kThreads) void grad_kernel(const GradArgs<E> a)
 {
-    __shared__ float lds[kThreads * E::kPer16];
-    if (static_cast<int>(blockIdx.x) < a.chunks) { sum_piece<E>(a, blockIdx.x, lds); return; }
-    const int lanes = 1 << a.shift;
+    extern __shared__ Sorted list[];        // the pieces of this workgroup, one more on either side
+    const int lanes = 1 << a.shift, groups = kThreads >> a.shift, group = threadIdx.x >> a.shift;
     const Columns<E> c = columns_of<E>(threadIdx.x & (lanes - 1), lanes, blockIdx.y, a.D);
     const int64_t w = blockIdx.z;
-    const int64_t v0 = (static_cast<int64_t>(blockIdx.x - a.chunks) * (kThreads >> a.shift) + (threadIdx.x >> a.shift)) * kRowsPerGroup;
-    if (c.n == 0 || v0 >= a.V) return;
-    const int32_t *starts = a.starts + w * (static_cast<int64_t>(a.V) + 1) + v0;
-    const int rows = a.V - v0 < kRowsPerGroup ? static_cast<int>(a.V - v0) : kRowsPerGroup;
-    int edge[kRowsPerGroup + 1];
+    if (static_cast<int>(blockIdx.x) < a.chunk_blocks) {
+        const int all = a.total[w], p0 = static_cast<int>(blockIdx.x) * groups * a.piece;
+        if (p0 >= all) return;
+        const Sorted *sorted = a.sorted + w * a.N;
+        for (int k = threadIdx.x; k < groups * a.piece + 2; k += kThreads) {
+            const int p = p0 - 1 + k;
+            list[k] = p >= 0 && p < all ? sorted[p] : Sorted{-1, 0};
+        }
+        __syncthreads();
+        const int left = all - p0 - group * a.piece;
+        if (left > 0 && c.n) sum_piece<E>(a, c, w, blockIdx.x * groups + group, left < a.piece ? left : a.piece, list + 1 + group * a.piece);
+        return;
+    }
+    if constexpr (!IN_PLACE) {
+        const int64_t v0 = (static_cast<int64_t>(blockIdx.x - a.chunk_blocks) * groups + group) * kEmptyRows;
+        if (c.n == 0 || v0 >= a.V) return;
+        const uint64_t word = a.named[w * ((static_cast<int64_t>(a.V) + 63) / 64) + v0 / 64];
+        const unsigned bits = static_cast<unsigned>(word >> (v0 % 64));
+        const int64_t first = w * a.ld + v0 * a.D;
+        float g[kEmptyRows][E::kPer16];
 #pragma unroll
-    for (int r = 0; r <= kRowsPerGroup; ++r) edge[r] = starts[r < rows ? r : rows];
+        for (int r = 0; r < kEmptyRows; ++r) {
+            if (a.g_in && v0 + r < a.V && !((bits >> r) & 1u)) c.load(a.g_in + first + static_cast<int64_t>(r) * a.D, g[r]);
+            else
 #pragma unroll
-    for (int r = 0; r < kRowsPerGroup; ++r) {
-        const int s = edge[r], e = edge[r + 1];
-        if (r >= rows || (IN_PLACE && s == e) || e - s > kLong) continue;
-        float sum[E::kPer16] = {};
-        add_rows<E>(c, a.dout + w * a.N * a.ld_dout, a.ld_dout, a.order + w * a.N, s, e, sum);
-        finish<E>(a, c, w, static_cast<int32_t>(v0) + r, sum);
+                for (int j = 0; j < E::kPer16; ++j) g[r][j] = 0.0f;
+        }
+#pragma unroll
+        for (int r = 0; r < kEmptyRows; ++r)
+            if (v0 + r < a.V && !((bits >> r) & 1u)) c.store(a.g_out + first + static_cast<int64_t>(r) * a.D, g[r]);
     }
 }
 
-// The long list that begins in this chunk, if one does: its pieces, in order.
+// The list that begins in this piece and goes on behind it, if one does: its sums, in order.
 template <class E>
 __global__ __launch_bounds__(kThreads) void join_kernel(const GradArgs<E> a)
 {
-    __shared__ float lds[kThreads * E::kPer16];
+    __shared__ float lds[E::kPer16][kThreads];
     const int64_t w = blockIdx.z;
-    const int32_t *starts = a.starts + w * (static_cast<int64_t>(a.V) + 1), *order = a.order + w * a.N, *tokens = a.tokens + w * a.N;
-    const int chunk = blockIdx.x, all = starts[a.V], p0 = chunk * kLong;
-    if (p0 >= all) return;
-    const int p1 = p0 + kLong < all ? p0 + kLong : all;
-    const int first = tokens[order[p0]], id = tokens[order[p1 - 1]];
-    const int s = starts[id], e = starts[id + 1];
-    if (e - s <= kLong || s < p0) return;
+    const Sorted *sorted = a.sorted + w * a.N;
+    const int chunk = blockIdx.x, all = a.total[w], p0 = chunk * a.piece, p1 = p0 + a.piece;
+    if (p1 >= all) return;
+    const int id = sorted[p1 - 1].id;
+    if (sorted[p1].id != id || (sorted[p0].id == id && p0 > 0 && sorted[p0 - 1].id == id)) return;
+    int pieces = 1;                         // and those whose first token is of the list
+    for (;; pieces += kThreads) {
+        const int64_t p = static_cast<int64_t>(chunk + pieces + static_cast<int>(threadIdx.x)) * a.piece;
+        const int more = __syncthreads_count(p < all && sorted[p].id == id);
+        if (more < kThreads) { pieces += more; break; }
+    }
     const int lanes = 1 << a.shift, groups = kThreads >> a.shift, group = threadIdx.x >> a.shift;
     const Columns<E> c = columns_of<E>(threadIdx.x & (lanes - 1), lanes, blockIdx.y, a.D);
-    const int pieces = (e - 1) / kLong - chunk + 1, each = (pieces + groups - 1) / groups;
+    const int each = (pieces + groups - 1) / groups;
     const int from = group * each, to = from + each < pieces ? from + each : pieces;
     const float *row = a.pieces + (w * a.chunks + chunk) * 2 * a.D + c.first;
     float sum[E::kPer16] = {};
     for (int k = from; k < to; ++k) {
-        const float *piece = row + (static_cast<int64_t>(k) * 2 + (k == 0 && id != first)) * a.D;
+        const float *piece = row + (static_cast<int64_t>(k) * 2 + (k == 0)) * a.D;
 #pragma unroll
         for (int j = 0; j < E::kPer16; ++j)
             if (j < c.n) sum[j] += piece[j];
     }
-    add_groups<E>(sum, lds, a.shift);
-    if (group == 0 && c.n) finish<E>(a, c, w, id, sum);
+#pragma unroll
+    for (int j = 0; j < E::kPer16; ++j) lds[j][threadIdx.x] = sum[j];
+    __syncthreads();
+    if (group == 0 && c.n) {
+        for (int at = threadIdx.x + lanes; at < kThreads; at += lanes)
+#pragma unroll
+            for (int j = 0; j < E::kPer16; ++j) sum[j] += lds[j][at];
+        finish<E>(a, c, w, id, sum);
+    }
 }
 
-// log2 of the lanes that handle one row
+// log2 of the lanes of a group: enough for a row, or 64, 32 or 16 of them several times, whichever leaves fewest idle.
 template <class E>
 int lanes_shift(int32_t D)
 {
-    int shift = 0;
-    while (shift < 6 && (1 << shift) * E::kPer16 < D) ++shift;
+    const int64_t vectors = ceil_div(D, E::kPer16);
+    int shift = 2;
+    while (shift < 6 && (1 << shift) < vectors) ++shift;
+    if (shift < 6 || vectors <= 64) return shift;
+    for (int smaller = 5; smaller >= 4; --smaller)
+        if (round_up(vectors, 1 << smaller) < round_up(vectors, 1 << shift)) shift = smaller;
     return shift;
 }
 
@@ -360,16 +372,20 @@ int lookup(const typename E::T *x, int64_t ld, int32_t W, int64_t offset, int32_
 }
 
 struct GradSpace {
-    int64_t starts, order, pieces, bytes, chunks;
+    int64_t named, total, sorted, pieces, bytes, chunks;
+    int piece;
 };
 
 GradSpace grad_space(int32_t W, int64_t N, int32_t V, int32_t D)
 {
     GradSpace s{};
-    s.chunks = N > kLong ? ceil_div(N, kLong) : 0;         // shorter: no list is long
-    s.starts = 0;
-    s.order = round_up(W * (static_cast<int64_t>(V) + 1) * 4, 256);
-    s.pieces = s.order + round_up(W * N * 4, 256);
+    // tokens of a piece: few, so that there are many; more of them where a list of all tokens would leave thousands of sums to join
+    s.piece = N <= 16384 ? 16 : 64;
+    s.chunks = ceil_div(N, s.piece);
+    s.named = 0;
+    s.total = round_up(W * ceil_div(V, 64) * 8, 256);
+    s.sorted = s.total + round_up(W * 4, 256);
+    s.pieces = s.sorted + round_up(W * N * static_cast<int64_t>(sizeof(Sorted)), 256);
     s.bytes = s.pieces + W * s.chunks * 2 * D * 4;
     return s;
 }
@@ -394,22 +410,28 @@ int grad(const typename E::T *dout, int64_t ld_dout, const int32_t *tokens, int3
     if (overlap(workspace, space.bytes, g_out, g_bytes) || overlap(workspace, space.bytes, dout, dout_bytes) ||
         overlap(workspace, space.bytes, g_in, g_bytes) || overlap(workspace, space.bytes, tokens, token_bytes)) return CX_ERR_ALIAS;
     char *base = static_cast<char *>(workspace);
-    GradArgs<E> a{dout, ld_dout, tokens, reinterpret_cast<int32_t *>(base + space.starts), reinterpret_cast<int32_t *>(base + space.order),
-                  reinterpret_cast<float *>(base + space.pieces), g_in ? g_in + offset : nullptr, g_out + offset, ld, N, V, D,
-                  static_cast<int32_t>(space.chunks), scale, lanes_shift<E>(D)};
+    Sorted *sorted = reinterpret_cast<Sorted *>(base + space.sorted);
+    uint64_t *named = reinterpret_cast<uint64_t *>(base + space.named);
+    int32_t *total = reinterpret_cast<int32_t *>(base + space.total);
+    GradArgs<E> a{dout, ld_dout, sorted, named, total, reinterpret_cast<float *>(base + space.pieces), g_in ? g_in + offset : nullptr, g_out + offset,
+                  ld, N, V, D, static_cast<int32_t>(space.chunks), 0, scale, lanes_shift<E>(D), space.piece};
     const int groups = kThreads >> a.shift;
     const unsigned slabs = static_cast<unsigned>(ceil_div(ceil_div(D, E::kPer16), 1 << a.shift));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(sort_kernel, dim3(static_cast<unsigned>(ceil_div(V, kBins)), W), dim3(kSortWaves * kWave), 0, st, tokens, N, V,
-                       const_cast<int32_t *>(a.starts), const_cast<int32_t *>(a.order));
+    hipLaunchKernelGGL(sort_kernel, dim3(static_cast<unsigned>(ceil_div(V, kBins)), W), dim3(kSortWaves * kWave), 0, st, tokens, N, V, sorted, named,
+                       total);
     if (launched() != CX_OK) return CX_ERR_HIP;
-    const int64_t row_blocks = ceil_div(V, static_cast<int64_t>(groups) * kRowsPerGroup);
-    const dim3 grid(static_cast<unsigned>(space.chunks + row_blocks), slabs, W);
-    if (g_in == g_out) hipLaunchKernelGGL((grad_kernel<E, true>), grid, dim3(kThreads), 0, st, a);
-    else hipLaunchKernelGGL((grad_kernel<E, false>), grid, dim3(kThreads), 0, st, a);
-    if (launched() != CX_OK) return CX_ERR_HIP;
-    if (space.chunks == 0) return CX_OK;
-    hipLaunchKernelGGL(join_kernel<E>, dim3(static_cast<unsigned>(space.chunks), slabs, W), dim3(kThreads), 0, st, a);
+    a.chunk_blocks = static_cast<int32_t>(ceil_div(space.chunks, groups));
+    const int64_t empty_blocks = g_in == g_out ? 0 : ceil_div(V, static_cast<int64_t>(groups) * kEmptyRows);
+    const dim3 grid(static_cast<unsigned>(a.chunk_blocks + empty_blocks), slabs, W);
+    const unsigned list_bytes = (groups * a.piece + 2) * sizeof(Sorted);
+    if (grid.x > 0) {
+        if (g_in == g_out) hipLaunchKernelGGL((grad_kernel<E, true>), grid, dim3(kThreads), list_bytes, st, a);
+        else hipLaunchKernelGGL((grad_kernel<E, false>), grid, dim3(kThreads), list_bytes, st, a);
+        if (launched() != CX_OK) return CX_ERR_HIP;
+    }
+    if (space.chunks <= 1) return CX_OK;
+    hipLaunchKernelGGL(join_kernel<E>, dim3(static_cast<unsigned>(space.chunks - 1), slabs, W), dim3(kThreads), 0, st, a);
     return launched();
 }
 
