@@ -3,14 +3,14 @@
 //   a = sigmoid(f)    h_t = a_t * (reset_t ? 0 : h_{t-1}) + (1 - a_t) * x_t    y = round(h)
 //   r_t = dL/dh_t = dy_t + keep_{t+1} a_{t+1} r_{t+1}    dx = (1 - a) r    df = r (keep h_{t-1} - x) a (1 - a)
 //
-// One column's steps are a composition of affine maps h -> A h + S, and compositions associate: the steps are cut into pieces
-// of kSteps, a lane composes the maps of its piece in registers, the pieces' maps are joined through LDS, and the lane then
-// walks its piece once more with the state that enters it.  So the data are read once, whatever the length.
+// One column's steps are a composition of affine maps h -> A h + S, and compositions associate: the steps are cut into pieces,
+// a lane composes the maps of its piece in registers, the pieces' maps are joined through LDS, and the lane then walks its
+// piece once more with the state that enters it.  So the data are read once, whatever the length.
 //
-//   lane       kCols neighbouring columns (4 bytes of every row) and kSteps consecutive steps: 64 lanes read whole lines of
-//              a row, the walk needs no exchange between lanes, and a wavefront keeps 2 (gradient: 3) x 16 loads in flight
-//   wavefront  one piece of a tile;  workgroup: up to 8 wavefronts = a tile of 128 steps, tile after tile, the loads of the
-//              next one issued before the present one is computed
+//   lane       kCols neighbouring columns (4 bytes of every row) and 8 (gradient: 16) consecutive steps: 64 lanes read whole lines
+//              of a row, and a walk needs no exchange between lanes
+//   workgroup  16 (gradient: 8) wavefronts, one piece each = a tile of 128 steps, tile after tile; the loads of the next tile are
+//              issued before the present one is computed, into a second set of registers
 //   split      where columns are few (workgroups < kSplitBelow) the steps are also split over workgroups: a first launch composes
 //              the map of each span (it reads what the second reads again, from the last-level cache where the call fits there)
 //
@@ -21,17 +21,11 @@
 
 namespace {
 
-constexpr int kSteps = CX_SCAN_CHUNK;                   // steps of a lane's piece
-constexpr int kMaxWaves = 8;
-constexpr int kTile = kSteps * kMaxWaves;
+constexpr int kTile = 128;                              // steps of a full tile
+constexpr int kForward = 8, kGrad = CX_SCAN_CHUNK;      // steps of a piece
+static_assert(CX_SCAN_CHUNK % kForward == 0, "pieces begin where states are kept");
 constexpr int kMaxSpans = 64;                           // workgroups that the steps of one column are split over
 constexpr int64_t kMaxColumns = CX_MAX_WIDTH, kMaxSeq = CX_MAX_TOKENS;
-
-template <class E>
-struct Cols {                                           // what a lane loads of a row: 4 bytes
-    static constexpr int kCols = 4 / sizeof(typename E::T);
-    static constexpr int kSlab = kCols * kWave;
-};
 
 struct Map {
     float A, S;
@@ -57,51 +51,59 @@ __device__ __forceinline__ Gate gate(float f)
     return {a, e * a};
 }
 
-// A lane's columns.  16-bit rows: two, loaded as one pair.  The pair of the last lane of an odd row begins one column earlier, at its neighbour's,
-// whose results it does not store.
-template <class E>
+// A lane's columns: one, or of 16-bit rows two, loaded as one pair.  The pair of the last lane of an odd row begins one column
+// earlier, at its neighbour's, whose results it does not store.  32-bit offsets: rows have uniform addresses, lanes a place in them.
+template <class T>
+__device__ __forceinline__ const T &at_byte(const void *row, uint32_t byte) { return *reinterpret_cast<const T *>(static_cast<const char *>(row) + byte); }
+template <class T>
+__device__ __forceinline__ T &at_byte(void *row, uint32_t byte) { return *reinterpret_cast<T *>(static_cast<char *>(row) + byte); }
+
+template <class E, int N>
 struct LaneColumns;
-template <>
-struct LaneColumns<F32> {
-    static constexpr int N = 1;
-    int64_t first;
+template <class E>
+struct LaneColumns<E, 1> {
+    using T = typename E::T;
+    uint32_t byte, wide;                                // of the first column in rows of T and of float
     bool any;
-    __device__ __forceinline__ LaneColumns(int64_t column, int D) : first(column < D ? column : D - 1), any(column < D) {}
-    __device__ __forceinline__ unsigned load(const float *row) const { return __float_as_uint(row[first]); }
-    static __device__ __forceinline__ float value(unsigned w, int) { return __uint_as_float(w); }
-    __device__ __forceinline__ void store(float *row, const float (&v)[1]) const { if (any) row[first] = v[0]; }
-    __device__ __forceinline__ void load_wide(const float *row, float (&v)[1]) const { v[0] = row[first]; }
-    __device__ __forceinline__ void store_wide(float *row, const float (&v)[1]) const { if (any) row[first] = v[0]; }
+    __device__ __forceinline__ LaneColumns(int column, int D)
+        : byte((column < D ? column : D - 1) * sizeof(T)), wide((column < D ? column : D - 1) * 4), any(column < D) {}
+    __device__ __forceinline__ bool whole() const { return any; }
+    __device__ __forceinline__ T load(const T *row) const { return at_byte<T>(row, byte); }
+    static __device__ __forceinline__ float value(T w, int) { return E::widen(w); }
+    __device__ __forceinline__ void store_whole(T *row, const float (&v)[1]) const { at_byte<T>(row, byte) = E::narrow(v[0]); }
+    __device__ __forceinline__ void store(T *row, const float (&v)[1]) const { if (any) store_whole(row, v); }
+    __device__ __forceinline__ void load_wide(const float *row, float (&v)[1]) const { v[0] = at_byte<float>(row, wide); }
+    __device__ __forceinline__ void store_wide(float *row, const float (&v)[1]) const { if (any) at_byte<float>(row, wide) = v[0]; }
 };
 template <class E>
-struct LaneColumns {
-    static constexpr int N = 2;
-    int64_t first;
-    bool any, both, single;                             // single: rows of one column
-    __device__ __forceinline__ LaneColumns(int64_t column, int D)
-        : first(column + 2 <= D ? column : D >= 2 ? D - 2 : 0), any(column < D), both(column + 2 <= D), single(D < 2) {}
-    __device__ __forceinline__ unsigned load(const uint16_t *row) const
-    {
-        return single ? static_cast<unsigned>(row[0]) << 16 : *reinterpret_cast<const u1_at2 *>(row + first);
-    }
+struct LaneColumns<E, 2> {                              // at least two columns
+    using T = typename E::T;
+    uint32_t byte, wide;
+    bool any, both;
+    __device__ __forceinline__ LaneColumns(int column, int D)
+        : byte((column + 2 <= D ? column : D - 2) * 2), wide((column + 2 <= D ? column : D - 2) * 4), any(column < D), both(column + 2 <= D) {}
+    __device__ __forceinline__ bool whole() const { return both; }
+    __device__ __forceinline__ unsigned load(const T *row) const { return at_byte<u1_at2>(row, byte); }
     static __device__ __forceinline__ float value(unsigned w, int j) { return j ? E::high(w) : E::low(w); }
-    __device__ __forceinline__ void store(uint16_t *row, const float (&v)[2]) const
+    __device__ __forceinline__ void store_whole(T *row, const float (&v)[2]) const { at_byte<u1_at2>(row, byte) = E::two(v[0], v[1]); }
+    __device__ __forceinline__ void store(T *row, const float (&v)[2]) const
     {
-        if (both) *reinterpret_cast<u1_at2 *>(row + first) = E::two(v[0], v[1]);
-        else if (any) row[single ? 0 : first + 1] = E::narrow(v[1]);
+        if (both) store_whole(row, v);
+        else if (any) at_byte<T>(row, byte + 2) = E::narrow(v[1]);
     }
     __device__ __forceinline__ void load_wide(const float *row, float (&v)[2]) const
     {
-        const int64_t own = single ? 0 : first + 1;     // another workgroup may own the one before it
-        v[0] = row[both ? first : own];
-        v[1] = row[own];
+        v[0] = at_byte<float>(row, both ? wide : wide + 4);             // another workgroup may own the column before the last
+        v[1] = at_byte<float>(row, wide + 4);
     }
     __device__ __forceinline__ void store_wide(float *row, const float (&v)[2]) const
     {
-        if (both) row[first] = v[0];
-        if (any) row[single ? 0 : first + 1] = v[1];
+        if (both) at_byte<float>(row, wide) = v[0];
+        if (any) at_byte<float>(row, wide + 4) = v[1];
     }
 };
+template <class E, int N>
+using Word = std::conditional_t<N == 2, unsigned, typename E::T>;      // what a lane loads of a row
 
 template <class E>
 struct ScanArgs {
@@ -119,52 +121,81 @@ struct ScanArgs {
     int64_t span_steps;                                 // a multiple of kTile; the steps of one workgroup
 };
 
-// The gate's factor of each step's map and whether it forgets, for steps of one piece; steps beyond the end change nothing.
+// Bit i: step i of the piece forgets; the same for the wavefront.
+template <bool RESETS>
 __device__ __forceinline__ unsigned reset_bits(const uint8_t *reset, int64_t row, int steps)
 {
-    if (!reset) return 0;
+    if (!RESETS) return 0;
     const int lane = threadIdx.x & (kWave - 1);
     const bool here = lane < steps && reset[row + lane] != 0;
-    return static_cast<unsigned>(__ballot(here));       // bit i: step i of the piece; the same for the wavefront
+    return static_cast<unsigned>(__ballot(here));
 }
 
 template <int N>
-struct Exchange {                                       // the maps of the pieces of a tile, two tiles in turn
-    float2 map[2][kMaxWaves][N][kWave];
+struct alignas(8 * N) Maps {                            // of a lane's columns
+    Map of[N];
 };
 
-// The map that leads to this wavefront's piece and that of the whole tile, in the order of the walk.
-template <int N>
-__device__ __forceinline__ void join_pieces(Exchange<N> &lds, int turn, int wave, int waves, bool backwards, const Map (&mine)[N],
-                                            const float (&carry)[N], float (&enters)[N], float (&leaves)[N])
+template <int N, int STEPS>
+struct Exchange {                                       // the maps of the pieces of a tile, two tiles in turn
+    Maps<N> map[2][kTile / STEPS][kWave];
+};
+
+// What enters this wavefront's piece, and what leaves the tile, in the order of the walk.  One barrier.
+template <bool RESETS, int N, int STEPS>
+__device__ __forceinline__ void join_pieces(Exchange<N, STEPS> &lds, int turn, int place, int pieces, const Map (&mine)[N], float (&carry)[N],
+                                            float (&enters)[N])
 {
     const int lane = threadIdx.x & (kWave - 1);
-    if (waves == 1) {
+    const auto pass = [&](int k) {
+        const Maps<N> m = lds.map[turn][k][lane];
 #pragma unroll
-        for (int j = 0; j < N; ++j) { enters[j] = carry[j]; leaves[j] = apply(mine[j], carry[j]); }
-        return;
+        for (int j = 0; j < N; ++j) carry[j] = RESETS ? apply(m.of[j], carry[j]) : __builtin_fmaf(m.of[j].A, carry[j], m.of[j].S);
+    };
+    if (pieces > 1) {
+        Maps<N> m;
+#pragma unroll
+        for (int j = 0; j < N; ++j) m.of[j] = mine[j];
+        lds.map[turn][place][lane] = m;
+        __syncthreads();
+        for (int k = 0; k < place; ++k) pass(k);
     }
-    const int place = backwards ? waves - 1 - wave : wave;
 #pragma unroll
-    for (int j = 0; j < N; ++j) lds.map[turn][place][j][lane] = float2{mine[j].A, mine[j].S};
-    __syncthreads();
+    for (int j = 0; j < N; ++j) enters[j] = carry[j];
+    if (pieces > 1)
+        for (int k = place; k < pieces; ++k) pass(k);
+    else
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-        float h = carry[j];
-        enters[j] = h;
-        for (int k = 0; k < waves; ++k) {
-            const float2 m = lds.map[turn][k][j][lane];
-            h = apply({m.x, m.y}, h);
-            enters[j] = k + 1 == place ? h : enters[j];
+        for (int j = 0; j < N; ++j) carry[j] = apply(mine[j], carry[j]);
+}
+
+// The map of a tile behind those of the tiles before it (in the order of the walk).  One barrier.
+template <int N, int STEPS>
+__device__ __forceinline__ void compose_pieces(Exchange<N, STEPS> &lds, int turn, int place, int pieces, const Map (&mine)[N], Map (&whole)[N])
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    if (pieces > 1) {
+        Maps<N> m;
+#pragma unroll
+        for (int j = 0; j < N; ++j) m.of[j] = mine[j];
+        lds.map[turn][place][lane] = m;
+        __syncthreads();
+        for (int k = 0; k < pieces; ++k) {
+            m = lds.map[turn][k][lane];
+#pragma unroll
+            for (int j = 0; j < N; ++j) whole[j] = then(whole[j], m.of[j]);
         }
-        leaves[j] = h;
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) whole[j] = then(whole[j], mine[j]);
     }
 }
 
-// What enters this workgroup's span: the maps of the spans on the way to it, applied to what enters the first.
-template <class E, int N>
-__device__ __forceinline__ void entering(const ScanArgs<E> &a, const LaneColumns<E> &c, int64_t b, int span, bool backwards, const float *first,
-                                         float (&h)[N])
+// What enters this workgroup's span: the maps of the spans on the way to it, applied to what enters the first.  The wavefronts
+// compose a part of them each.  Nothing is left in LDS that a later tile's first exchange could meet: a barrier ends it.
+template <class E, int N, int STEPS>
+__device__ __forceinline__ void entering(const ScanArgs<E> &a, Exchange<N, STEPS> &lds, const LaneColumns<E, N> &c, int64_t b, int span, bool backwards,
+                                         const float *first, float (&h)[N])
 {
     if (a.spans == 1) {
         if (first) c.load_wide(first + b * a.D, h);
@@ -173,273 +204,292 @@ __device__ __forceinline__ void entering(const ScanArgs<E> &a, const LaneColumns
             for (int j = 0; j < N; ++j) h[j] = 0.0f;
         return;
     }
+    constexpr int kEach = kMaxSpans * STEPS / kTile;    // a split call has all its wavefronts
+    const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1);
     const float *maps = a.maps + b * a.spans * 2 * a.D;
     c.load_wide(a.maps + (static_cast<int64_t>(gridDim.x) * a.spans * 2 + b) * a.D, h);
     const int before = backwards ? a.spans - 1 - span : span;
-    for (int k = 0; k < before; k += 4) {
-        float A[4][N], S[4][N];
+    float A[kEach][N], S[kEach][N];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = k + i < before ? k + i : before - 1;
+    for (int i = 0; i < kEach; ++i) {
+        const int at = wave * kEach + i;
+        if (at < before) {
             const float *m = maps + static_cast<int64_t>(backwards ? a.spans - 1 - at : at) * 2 * a.D;
             c.load_wide(m, A[i]);
             c.load_wide(m + a.D, S[i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) { A[i][j] = 1.0f; S[i][j] = 0.0f; }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (k + i < before)
-#pragma unroll
-                for (int j = 0; j < N; ++j) h[j] = apply({A[i][j], S[i][j]}, h[j]);
     }
+    Maps<N> part;
+#pragma unroll
+    for (int j = 0; j < N; ++j) part.of[j] = {A[0][j], S[0][j]};
+#pragma unroll
+    for (int i = 1; i < kEach; ++i)
+#pragma unroll
+        for (int j = 0; j < N; ++j) part.of[j] = then(part.of[j], Map{A[i][j], S[i][j]});
+    lds.map[0][wave][lane] = part;
+    __syncthreads();
+    for (int k = 0; k * kEach < before; ++k) {
+        const Maps<N> m = lds.map[0][k][lane];
+#pragma unroll
+        for (int j = 0; j < N; ++j) h[j] = apply(m.of[j], h[j]);
+    }
+    __syncthreads();
 }
 
-// Loads of a piece: rows [t, t + kSteps) of the sequence, those beyond `end` as zeros.
-template <class E>
-__device__ __forceinline__ void load_piece(const LaneColumns<E> &c, const typename E::T *m, int64_t ld, int64_t row, int steps, unsigned (&v)[kSteps])
-{
-    const typename E::T *p = m + row * ld;
-    if (steps >= kSteps) {
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) v[i] = c.load(p + i * ld);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) v[i] = i < steps ? c.load(p + i * ld) : 0u;
-    }
-}
-
+template <int STEPS>
 __device__ __forceinline__ int steps_at(int64_t t, int64_t end)
 {
     const int64_t left = end - t;
-    return left >= kSteps ? kSteps : left > 0 ? static_cast<int>(left) : 0;
+    return left >= STEPS ? STEPS : left > 0 ? static_cast<int>(left) : 0;
 }
 
-// Grid (sequences, spans, slabs of columns).  ONLY_MAP: the first launch of a split call.
-template <class E, bool ONLY_MAP>
-__global__ __launch_bounds__(kMaxWaves *kWave) void scan_kernel(const ScanArgs<E> a)
+// The first `steps` rows of a piece, at row `row` of the matrix.
+template <class E, int N, int STEPS>
+__device__ __forceinline__ void load_piece(const LaneColumns<E, N> &c, const typename E::T *m, int64_t ld, int64_t row, int steps, Word<E, N> (&v)[STEPS])
 {
-    constexpr int N = LaneColumns<E>::N;
-    __shared__ Exchange<N> lds;
+    const typename E::T *p = m + row * ld;
+    if (steps >= STEPS) {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) v[i] = c.load(p + i * ld);
+    } else {
+#pragma unroll
+        for (int i = 0; i < STEPS; ++i) v[i] = i < steps ? c.load(p + i * ld) : 0;
+    }
+}
+
+template <class E, int N>
+__device__ __forceinline__ void store_map(const ScanArgs<E> &a, const LaneColumns<E, N> &c, int64_t b, int span, const Map (&whole)[N])
+{
+    float A[N], S[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) { A[j] = whole[j].A; S[j] = whole[j].S; }
+    float *m = a.maps + (b * a.spans + span) * 2 * a.D;
+    c.store_wide(m, A);
+    c.store_wide(m + a.D, S);
+}
+
+// What enters the first span of a split call goes to the workspace: the second launch may replace it (h_last may be h0).
+template <class E, int N>
+__device__ __forceinline__ void keep_first(const ScanArgs<E> &a, const LaneColumns<E, N> &c, int64_t b, const float *first)
+{
+    float h[N] = {};
+    if (first) c.load_wide(first + b * a.D, h);
+    c.store_wide(a.maps + (static_cast<int64_t>(gridDim.x) * a.spans * 2 + b) * a.D, h);
+}
+
+template <bool V>
+using Flag = std::integral_constant<bool, V>;
+
+// Grid (sequences, spans, slabs of columns).  ONLY_MAP: the first launch of a split call.
+template <class E, int N, bool RESETS, bool ONLY_MAP>
+__global__ __launch_bounds__(kTile / kForward *kWave) void scan_kernel(const ScanArgs<E> a)
+{
+    constexpr int STEPS = kForward;
+    __shared__ Exchange<N, STEPS> lds;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
     const int64_t b = blockIdx.x;
     const int span = blockIdx.y;
-    const LaneColumns<E> c(static_cast<int64_t>(blockIdx.z) * Cols<E>::kSlab + lane * N, a.D);
+    const LaneColumns<E, N> c((static_cast<int>(blockIdx.z) * kWave + lane) * N, a.D);
+    const bool whole_lanes = __ballot(c.whole()) == ~0ull;
     const int64_t row0 = b * a.T_, begin = span * a.span_steps, end = begin + a.span_steps < a.T_ ? begin + a.span_steps : a.T_;
-    const int tile = waves * kSteps;
+    const int tile = waves * STEPS;
+    Word<E, N> fw[2][STEPS], xw[2][STEPS];
+    int64_t t = begin + wave * STEPS;                   // of the piece whose rows were loaded last
+    int steps = steps_at<STEPS>(t, end);
+    load_piece(c, a.f, a.ldf, row0 + t, steps, fw[0]);
+    load_piece(c, a.x, a.ldx, row0 + t, steps, xw[0]);
     float carry[N];
     Map whole[N];
     if constexpr (ONLY_MAP) {
-        if (span == 0 && wave == 0) {                   // what enters the first span: the second launch may be given h_last = h0
-            float h[N] = {};
-            if (a.h0) c.load_wide(a.h0 + b * a.D, h);
-            c.store_wide(a.maps + (static_cast<int64_t>(gridDim.x) * a.spans * 2 + b) * a.D, h);
-        }
+        if (span == 0 && wave == 0) keep_first<E, N>(a, c, b, a.h0);
 #pragma unroll
         for (int j = 0; j < N; ++j) whole[j] = {1.0f, 0.0f};
     } else {
-        entering<E, N>(a, c, b, span, false, a.h0, carry);
+        entering<E>(a, lds, c, b, span, false, a.h0, carry);
     }
-    unsigned fw[kSteps], xw[kSteps];
-    int64_t t = begin + wave * kSteps;
-    int steps = steps_at(t, end);
-    load_piece<E>(c, a.f, a.ldf, row0 + t, steps, fw);
-    load_piece<E>(c, a.x, a.ldx, row0 + t, steps, xw);
-    int turn = 0;
-    for (int64_t tile0 = begin; tile0 < end; tile0 += tile, turn ^= 1) {
-        const unsigned resets = reset_bits(a.reset, row0 + t, steps);
-        float keep[kSteps][N], in[kSteps][N];
+    const auto one_tile = [&](auto turn_flag) {
+        constexpr int turn = decltype(turn_flag)::value;
+        const int64_t t_now = t;
+        const int steps_now = steps;
+        const unsigned resets = reset_bits<RESETS>(a.reset, row0 + t_now, steps_now);
+        t += tile;
+        steps = steps_at<STEPS>(t, end);
+        load_piece(c, a.f, a.ldf, row0 + t, steps, fw[!turn]);
+        load_piece(c, a.x, a.ldx, row0 + t, steps, xw[!turn]);
+        float keep[STEPS][N], in[STEPS][N];
         Map mine[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) mine[j] = {1.0f, 0.0f};
+        const auto maps = [&](auto full) {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const bool there = i < steps, cut = (resets >> i) & 1u;
+            for (int i = 0; i < STEPS; ++i) {
+                if (!decltype(full)::value && i >= steps_now) break;
+                const bool cut = RESETS && ((resets >> i) & 1u);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const Gate g = gate(c.value(fw[i], j));
-                keep[i][j] = there ? g.a : 1.0f;
-                in[i][j] = there ? g.b * c.value(xw[i], j) : 0.0f;
-                mine[j].S = cut ? in[i][j] : __builtin_fmaf(keep[i][j], mine[j].S, in[i][j]);
-                mine[j].A = cut ? -1.0f : keep[i][j] * mine[j].A;
+                for (int j = 0; j < N; ++j) {
+                    const Gate g = gate(c.value(fw[turn][i], j));
+                    keep[i][j] = g.a;
+                    in[i][j] = g.b * c.value(xw[turn][i], j);
+                    mine[j].S = cut ? in[i][j] : __builtin_fmaf(g.a, mine[j].S, in[i][j]);
+                    mine[j].A = cut ? -1.0f : g.a * mine[j].A;
+                }
             }
-        }
-        const int64_t t_now = t;
-        const int steps_now = steps;
-        t += tile;
-        steps = steps_at(t, end);
-        load_piece<E>(c, a.f, a.ldf, row0 + t, steps, fw);
-        load_piece<E>(c, a.x, a.ldx, row0 + t, steps, xw);
+        };
+        if (steps_now == STEPS) maps(Flag<true>{}); else maps(Flag<false>{});
         if constexpr (ONLY_MAP) {
-            // the composition of maps, one wavefront's piece after the other
-            Map piece[N];
-            if (waves > 1) {
-#pragma unroll
-                for (int j = 0; j < N; ++j) lds.map[turn][wave][j][lane] = float2{mine[j].A, mine[j].S};
-                __syncthreads();
-                for (int k = 0; k < waves; ++k)
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float2 m = lds.map[turn][k][j][lane];
-                        piece[j] = {m.x, m.y};
-                        whole[j] = then(whole[j], piece[j]);
-                    }
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j) whole[j] = then(whole[j], mine[j]);
-            }
+            compose_pieces(lds, turn, wave, waves, mine, whole);
         } else {
-            float h[N], leaves[N];
-            join_pieces<N>(lds, turn, wave, waves, false, mine, carry, h, leaves);
-            if (a.states && steps_now > 0) c.store_wide(a.states + (b * ceil_div(a.T_, kSteps) + t_now / kSteps) * a.D, h);
+            float h[N];
+            join_pieces<RESETS>(lds, turn, wave, waves, mine, carry, h);
+            if (a.states && steps_now > 0 && t_now % CX_SCAN_CHUNK == 0)
+                c.store_wide(a.states + (b * ceil_div(a.T_, CX_SCAN_CHUNK) + t_now / CX_SCAN_CHUNK) * a.D, h);
             typename E::T *out = a.y + (row0 + t_now) * a.ldy;
+            const auto walk = [&](auto full) {
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                if (i >= steps_now) break;
-                const bool cut = (resets >> i) & 1u;
+                for (int i = 0; i < STEPS; ++i) {
+                    if (!decltype(full)::value && i >= steps_now) break;
+                    const bool cut = RESETS && ((resets >> i) & 1u);
 #pragma unroll
-                for (int j = 0; j < N; ++j) h[j] = cut ? in[i][j] : __builtin_fmaf(keep[i][j], h[j], in[i][j]);
-                c.store(out + i * a.ldy, h);
-            }
-#pragma unroll
-            for (int j = 0; j < N; ++j) carry[j] = leaves[j];
+                    for (int j = 0; j < N; ++j) h[j] = cut ? in[i][j] : __builtin_fmaf(keep[i][j], h[j], in[i][j]);
+                    if (decltype(full)::value) c.store_whole(out + i * a.ldy, h); else c.store(out + i * a.ldy, h);
+                }
+            };
+            if (steps_now == STEPS && whole_lanes) walk(Flag<true>{}); else walk(Flag<false>{});
         }
+    };
+    for (int64_t tile0 = begin; tile0 < end; tile0 += 2 * tile) {
+        one_tile(Flag<false>{});
+        if (tile0 + tile < end) one_tile(Flag<true>{});
     }
     if constexpr (ONLY_MAP) {
-        if (wave == 0) {
-            float A[N], S[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) { A[j] = whole[j].A; S[j] = whole[j].S; }
-            float *m = a.maps + (b * a.spans + span) * 2 * a.D;
-            c.store_wide(m, A);
-            c.store_wide(m + a.D, S);
-        }
+        if (wave == 0) store_map<E>(a, c, b, span, whole);
     } else if (a.h_last && end == a.T_ && wave == waves - 1) {
         c.store_wide(a.h_last + b * a.D, carry);
     }
 }
 
 // The gradient, from the last step to the first.  What a piece hands to the one before it is keep a r of its first step.
-template <class E, bool ONLY_MAP>
-__global__ __launch_bounds__(kMaxWaves *kWave) void scan_grad_kernel(const ScanArgs<E> a)
+template <class E, int N, bool RESETS, bool ONLY_MAP>
+__global__ __launch_bounds__(kTile / kGrad *kWave) void scan_grad_kernel(const ScanArgs<E> a)
 {
-    constexpr int N = LaneColumns<E>::N;
-    __shared__ Exchange<N> lds;
+    constexpr int STEPS = kGrad;
+    __shared__ Exchange<N, STEPS> lds;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
     const int64_t b = blockIdx.x;
     const int span = blockIdx.y;
-    const LaneColumns<E> c(static_cast<int64_t>(blockIdx.z) * Cols<E>::kSlab + lane * N, a.D);
+    const LaneColumns<E, N> c((static_cast<int>(blockIdx.z) * kWave + lane) * N, a.D);
+    const bool whole_lanes = __ballot(c.whole()) == ~0ull;
     const int64_t row0 = b * a.T_, begin = span * a.span_steps, end = begin + a.span_steps < a.T_ ? begin + a.span_steps : a.T_;
-    const int tile = waves * kSteps;
+    const int tile = waves * STEPS;
+    Word<E, N> fw[2][STEPS], xw[2][STEPS], gw[2][STEPS];
+    int64_t tile0 = begin + (end - 1 - begin) / tile * tile;
+    int64_t t = tile0 + wave * STEPS;
+    int steps = steps_at<STEPS>(t, end);
+    float entered[2][N];                                // the state before the piece
+    const auto load = [&](auto turn_flag) {
+        constexpr int turn = decltype(turn_flag)::value;
+        load_piece(c, a.f, a.ldf, row0 + t, steps, fw[turn]);
+        load_piece(c, a.dy, a.lddy, row0 + t, steps, gw[turn]);
+        if constexpr (!ONLY_MAP) {
+            load_piece(c, a.x, a.ldx, row0 + t, steps, xw[turn]);
+            if (steps > 0) c.load_wide(a.states_in + (b * ceil_div(a.T_, CX_SCAN_CHUNK) + t / CX_SCAN_CHUNK) * a.D, entered[turn]);
+        }
+    };
+    load(Flag<false>{});
     float carry[N];
     Map whole[N];
     if constexpr (ONLY_MAP) {
-        if (span == 0 && wave == 0) {
-            float r[N] = {};
-            if (a.dh_last) c.load_wide(a.dh_last + b * a.D, r);
-            c.store_wide(a.maps + (static_cast<int64_t>(gridDim.x) * a.spans * 2 + b) * a.D, r);
-        }
+        if (span == 0 && wave == 0) keep_first<E, N>(a, c, b, a.dh_last);
 #pragma unroll
         for (int j = 0; j < N; ++j) whole[j] = {1.0f, 0.0f};
     } else {
-        entering<E, N>(a, c, b, span, true, a.dh_last, carry);
+        entering<E>(a, lds, c, b, span, true, a.dh_last, carry);
     }
-    int64_t tile0 = begin + (end - 1 - begin) / tile * tile;
-    int64_t t = tile0 + wave * kSteps;
-    int steps = steps_at(t, end);
-    unsigned fw[kSteps], xw[kSteps], gw[kSteps];
-    load_piece<E>(c, a.f, a.ldf, row0 + t, steps, fw);
-    if constexpr (!ONLY_MAP) load_piece<E>(c, a.x, a.ldx, row0 + t, steps, xw);
-    load_piece<E>(c, a.dy, a.lddy, row0 + t, steps, gw);
-    int turn = 0;
-    for (; tile0 >= begin; tile0 -= tile, turn ^= 1) {
-        const unsigned resets = reset_bits(a.reset, row0 + t, steps);
-        float keep[kSteps][N], open[kSteps][N], before[kSteps][N];
-        unsigned x_now[kSteps], dy_now[kSteps];
-        Map mine[N];
-        float h[N] = {};
-        if constexpr (!ONLY_MAP)
-            if (steps > 0) c.load_wide(a.states_in + (b * ceil_div(a.T_, kSteps) + t / kSteps) * a.D, h);
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const bool there = i < steps, cut = (resets >> i) & 1u;
-            dy_now[i] = gw[i];
-            if constexpr (!ONLY_MAP) x_now[i] = xw[i];
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const Gate g = gate(c.value(fw[i], j));
-                keep[i][j] = there ? g.a : 1.0f;
-                if constexpr (!ONLY_MAP) {
-                    open[i][j] = g.b;
-                    before[i][j] = cut ? 0.0f : h[j];
-                    const float in = g.b * c.value(xw[i], j);
-                    h[j] = cut ? in : __builtin_fmaf(g.a, h[j], in);
-                }
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < N; ++j) mine[j] = {1.0f, 0.0f};
-#pragma unroll
-        for (int i = kSteps - 1; i >= 0; --i) {
-            const bool cut = (resets >> i) & 1u;
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                mine[j].S = cut ? 0.0f : keep[i][j] * (c.value(dy_now[i], j) + mine[j].S);
-                mine[j].A = cut ? -1.0f : keep[i][j] * mine[j].A;
-            }
-        }
+    const auto one_tile = [&](auto turn_flag) {
+        constexpr int turn = decltype(turn_flag)::value;
         const int64_t t_now = t;
         const int steps_now = steps;
+        const unsigned resets = reset_bits<RESETS>(a.reset, row0 + t_now, steps_now);
         t -= tile;
-        steps = tile0 > begin ? kSteps : 0;
-        load_piece<E>(c, a.f, a.ldf, row0 + t, steps, fw);
-        if constexpr (!ONLY_MAP) load_piece<E>(c, a.x, a.ldx, row0 + t, steps, xw);
-        load_piece<E>(c, a.dy, a.lddy, row0 + t, steps, gw);
-        if constexpr (ONLY_MAP) {
-            if (waves > 1) {
+        steps = tile0 > begin ? STEPS : 0;
+        load(Flag<!turn>{});
+        float keep[STEPS][N], open[STEPS][N], pull[STEPS][N];     // pull: a (keep h - x)
+        Map mine[N];
 #pragma unroll
-                for (int j = 0; j < N; ++j) lds.map[turn][wave][j][lane] = float2{mine[j].A, mine[j].S};
-                __syncthreads();
-                for (int k = waves - 1; k >= 0; --k)
+        for (int j = 0; j < N; ++j) mine[j] = {1.0f, 0.0f};
+        const auto maps = [&](auto full) {
+            float h[N];
 #pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float2 m = lds.map[turn][k][j][lane];
-                        whole[j] = then(whole[j], {m.x, m.y});
-                    }
-            } else {
+            for (int j = 0; j < N; ++j) h[j] = ONLY_MAP ? 0.0f : entered[turn][j];
 #pragma unroll
-                for (int j = 0; j < N; ++j) whole[j] = then(whole[j], mine[j]);
-            }
-        } else {
-            float r[N], leaves[N];
-            join_pieces<N>(lds, turn, wave, waves, true, mine, carry, r, leaves);
-            typename E::T *df = a.df + (row0 + t_now) * a.lddf, *dx = a.dx + (row0 + t_now) * a.lddx;
-#pragma unroll
-            for (int i = kSteps - 1; i >= 0; --i) {
-                if (i >= steps_now) continue;
-                const bool cut = (resets >> i) & 1u;
-                float f_out[N], x_out[N];
+            for (int i = 0; i < STEPS; ++i) {
+                if (!decltype(full)::value && i >= steps_now) break;
+                const bool cut = RESETS && ((resets >> i) & 1u);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    const float g = c.value(dy_now[i], j) + r[j];
-                    x_out[j] = open[i][j] * g;
-                    f_out[j] = (before[i][j] - c.value(x_now[i], j)) * keep[i][j] * x_out[j];
-                    r[j] = cut ? 0.0f : keep[i][j] * g;
+                    const Gate g = gate(c.value(fw[turn][i], j));
+                    keep[i][j] = g.a;
+                    if constexpr (!ONLY_MAP) {
+                        const float x = c.value(xw[turn][i], j), in = g.b * x;
+                        open[i][j] = g.b;
+                        pull[i][j] = ((cut ? 0.0f : h[j]) - x) * g.a;
+                        h[j] = cut ? in : __builtin_fmaf(g.a, h[j], in);
+                    }
                 }
-                c.store(df + i * a.lddf, f_out);
-                c.store(dx + i * a.lddx, x_out);
             }
 #pragma unroll
-            for (int j = 0; j < N; ++j) carry[j] = leaves[j];
+            for (int i = STEPS - 1; i >= 0; --i) {
+                if (!decltype(full)::value && i >= steps_now) continue;
+                const bool cut = RESETS && ((resets >> i) & 1u);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    mine[j].S = cut ? 0.0f : keep[i][j] * (c.value(gw[turn][i], j) + mine[j].S);
+                    mine[j].A = cut ? -1.0f : keep[i][j] * mine[j].A;
+                }
+            }
+        };
+        if (steps_now == STEPS) maps(Flag<true>{}); else maps(Flag<false>{});
+        if constexpr (ONLY_MAP) {
+            compose_pieces(lds, turn, waves - 1 - wave, waves, mine, whole);
+        } else {
+            float r[N];
+            join_pieces<RESETS>(lds, turn, waves - 1 - wave, waves, mine, carry, r);
+            typename E::T *df = a.df + (row0 + t_now) * a.lddf, *dx = a.dx + (row0 + t_now) * a.lddx;
+            const auto walk = [&](auto full) {
+#pragma unroll
+                for (int i = STEPS - 1; i >= 0; --i) {
+                    if (!decltype(full)::value && i >= steps_now) continue;
+                    const bool cut = RESETS && ((resets >> i) & 1u);
+                    float f_out[N], x_out[N];
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const float g = c.value(gw[turn][i], j) + r[j];
+                        x_out[j] = open[i][j] * g;
+                        f_out[j] = pull[i][j] * x_out[j];
+                        r[j] = cut ? 0.0f : keep[i][j] * g;
+                    }
+                    if (decltype(full)::value) {
+                        c.store_whole(df + i * a.lddf, f_out);
+                        c.store_whole(dx + i * a.lddx, x_out);
+                    } else {
+                        c.store(df + i * a.lddf, f_out);
+                        c.store(dx + i * a.lddx, x_out);
+                    }
+                }
+            };
+            if (steps_now == STEPS && whole_lanes) walk(Flag<true>{}); else walk(Flag<false>{});
         }
+        tile0 -= tile;
+    };
+    while (tile0 >= begin) {
+        one_tile(Flag<false>{});
+        if (tile0 >= begin) one_tile(Flag<true>{});
     }
     if constexpr (ONLY_MAP) {
-        if (wave == 0) {
-            float A[N], S[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) { A[j] = whole[j].A; S[j] = whole[j].S; }
-            float *m = a.maps + (b * a.spans + span) * 2 * a.D;
-            c.store_wide(m, A);
-            c.store_wide(m + a.D, S);
-        }
+        if (wave == 0) store_map<E>(a, c, b, span, whole);
     } else if (a.dh0 && begin == 0 && wave == 0) {
         c.store_wide(a.dh0 + b * a.D, carry);
     }
@@ -452,6 +502,10 @@ __global__ __launch_bounds__(256) void pass_kernel(const float *from, float *to,
     if (i < n) to[i] = from ? from[i] : 0.0f;
 }
 
+// Columns of a lane.
+template <class E>
+int columns_of_lane(int32_t D) { return sizeof(typename E::T) == 2 && D > 1 ? 2 : 1; }
+
 struct Split {
     int spans;
     int64_t span_steps, bytes;
@@ -460,9 +514,9 @@ struct Split {
 // Fewer workgroups than this leave CUs idle for longer than a second reading takes.
 constexpr int64_t kSplitBelow = 128, kSplitTo = 512;
 
-Split split_of(int64_t B, int64_t T, int32_t D, int slab)
+Split split_of(int64_t B, int64_t T, int32_t D, int lane_columns)
 {
-    const int64_t groups = B * ceil_div(D, slab), tiles = ceil_div(T, kTile);
+    const int64_t groups = B * ceil_div(D, kWave * lane_columns), tiles = ceil_div(T, kTile);
     int64_t spans = groups < kSplitBelow ? ceil_div(kSplitTo, groups) : 1;
     spans = spans < tiles ? spans : tiles;
     spans = spans < kMaxSpans ? spans : kMaxSpans;
@@ -508,12 +562,12 @@ int scan(const typename E::T *f, int64_t ldf, const typename E::T *x, int64_t ld
     }
     if (!f || !x || !y) return CX_ERR_NULL;
     if (bad_matrix(B * T, ldf, D) || bad_matrix(B * T, ldx, D) || bad_matrix(B * T, ldy, D)) return CX_ERR_SHAPE;
-    const Split split = split_of(B, T, D, Cols<E>::kSlab);
+    const Split split = split_of(B, T, D, columns_of_lane<E>(D));
     if (split.bytes > 0 && !workspace) return CX_ERR_NULL;
     if (split.bytes > 0 && workspace_bytes < split.bytes) return CX_ERR_SHAPE;
     if (misaligned_to(f, kElem) || misaligned_to(x, kElem) || misaligned_to(y, kElem) || misaligned_to(states, 4) ||
         misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const uint64_t y_bytes = span(B * T, ldy, D, kElem), states_bytes = B * ceil_div(T, kSteps) * D * 4;
+    const uint64_t y_bytes = span(B * T, ldy, D, kElem), states_bytes = B * ceil_div(T, CX_SCAN_CHUNK) * D * 4;
     if (share<E>(y, ldy, f, ldf, B * T, D) || share<E>(y, ldy, x, ldx, B * T, D) || overlap(y, y_bytes, reset, B * T) ||
         overlap(y, y_bytes, h0, state_bytes) || overlap(y, y_bytes, h_last, state_bytes) || overlap(y, y_bytes, states, states_bytes) ||
         overlap(states, states_bytes, h0, state_bytes) || overlap(states, states_bytes, h_last, state_bytes)) return CX_ERR_ALIAS;
@@ -522,15 +576,23 @@ int scan(const typename E::T *f, int64_t ldf, const typename E::T *x, int64_t ld
     a.reset = reset; a.h0 = h0; a.h_last = h_last; a.states = states;
     a.maps = static_cast<float *>(workspace);
     a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
-    const int64_t pieces = ceil_div(T, kSteps);
-    const dim3 grid(static_cast<unsigned>(B), split.spans, static_cast<unsigned>(ceil_div(D, Cols<E>::kSlab)));
-    const dim3 block(static_cast<unsigned>(pieces < kMaxWaves ? pieces : kMaxWaves) * kWave);
-    if (split.spans > 1) {
-        hipLaunchKernelGGL((scan_kernel<E, true>), grid, block, 0, st, a);
-        if (launched() != CX_OK) return CX_ERR_HIP;
-    }
-    hipLaunchKernelGGL((scan_kernel<E, false>), grid, block, 0, st, a);
-    return launched();
+    const int64_t pieces = ceil_div(T, kForward);
+    const dim3 grid(static_cast<unsigned>(B), split.spans, static_cast<unsigned>(ceil_div(D, kWave * columns_of_lane<E>(D))));
+    const dim3 block(static_cast<unsigned>(pieces < kTile / kForward ? pieces : kTile / kForward) * kWave);
+    const auto launch = [&](auto lane_columns) -> int {
+        constexpr int N = decltype(lane_columns)::value;
+        if (split.spans > 1) {
+            if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, true>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((scan_kernel<E, N, false, true>), grid, block, 0, st, a);
+            if (launched() != CX_OK) return CX_ERR_HIP;
+        }
+        if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, false>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((scan_kernel<E, N, false, false>), grid, block, 0, st, a);
+        return launched();
+    };
+    if constexpr (sizeof(typename E::T) == 2)
+        if (D > 1) return launch(std::integral_constant<int, 2>{});
+    return launch(std::integral_constant<int, 1>{});
 }
 
 template <class E>
@@ -554,12 +616,12 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
     if (!f || !x || !dy || !df || !dx || !states) return CX_ERR_NULL;
     if (bad_matrix(B * T, ldf, D) || bad_matrix(B * T, ldx, D) || bad_matrix(B * T, lddy, D) || bad_matrix(B * T, lddf, D) ||
         bad_matrix(B * T, lddx, D)) return CX_ERR_SHAPE;
-    const Split split = split_of(B, T, D, Cols<E>::kSlab);
+    const Split split = split_of(B, T, D, columns_of_lane<E>(D));
     if (split.bytes > 0 && !workspace) return CX_ERR_NULL;
     if (split.bytes > 0 && workspace_bytes < split.bytes) return CX_ERR_SHAPE;
     if (misaligned_to(f, kElem) || misaligned_to(x, kElem) || misaligned_to(dy, kElem) || misaligned_to(df, kElem) ||
         misaligned_to(dx, kElem) || misaligned_to(states, 4) || misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const uint64_t states_bytes = B * ceil_div(T, kSteps) * D * 4;
+    const uint64_t states_bytes = B * ceil_div(T, CX_SCAN_CHUNK) * D * 4;
     const typename E::T *outs[2] = {df, dx};
     const int64_t lds[2] = {lddf, lddx};
     for (int k = 0; k < 2; ++k) {
@@ -574,15 +636,23 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
     a.reset = reset; a.states_in = states; a.dh_last = dh_last; a.dh0 = dh0;
     a.maps = static_cast<float *>(workspace);
     a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
-    const int64_t pieces = ceil_div(T, kSteps);
-    const dim3 grid(static_cast<unsigned>(B), split.spans, static_cast<unsigned>(ceil_div(D, Cols<E>::kSlab)));
-    const dim3 block(static_cast<unsigned>(pieces < kMaxWaves ? pieces : kMaxWaves) * kWave);
-    if (split.spans > 1) {
-        hipLaunchKernelGGL((scan_grad_kernel<E, true>), grid, block, 0, st, a);
-        if (launched() != CX_OK) return CX_ERR_HIP;
-    }
-    hipLaunchKernelGGL((scan_grad_kernel<E, false>), grid, block, 0, st, a);
-    return launched();
+    const int64_t pieces = ceil_div(T, kGrad);
+    const dim3 grid(static_cast<unsigned>(B), split.spans, static_cast<unsigned>(ceil_div(D, kWave * columns_of_lane<E>(D))));
+    const dim3 block(static_cast<unsigned>(pieces < kTile / kGrad ? pieces : kTile / kGrad) * kWave);
+    const auto launch = [&](auto lane_columns) -> int {
+        constexpr int N = decltype(lane_columns)::value;
+        if (split.spans > 1) {
+            if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, true>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((scan_grad_kernel<E, N, false, true>), grid, block, 0, st, a);
+            if (launched() != CX_OK) return CX_ERR_HIP;
+        }
+        if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, false>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((scan_grad_kernel<E, N, false, false>), grid, block, 0, st, a);
+        return launched();
+    };
+    if constexpr (sizeof(typename E::T) == 2)
+        if (D > 1) return launch(std::integral_constant<int, 2>{});
+    return launch(std::integral_constant<int, 1>{});
 }
 
 }  // namespace
@@ -615,7 +685,7 @@ int cx_scan_workspace(int64_t B, int64_t T, int32_t D, int64_t *bytes)
     *bytes = 0;
     const int rc = check_sizes(B, T, D);
     if (rc != CX_OK || B == 0 || T == 0) return rc;
-    const int64_t wide = split_of(B, T, D, Cols<F32>::kSlab).bytes, narrow = split_of(B, T, D, Cols<Bf16>::kSlab).bytes;
+    const int64_t wide = split_of(B, T, D, columns_of_lane<F32>(D)).bytes, narrow = split_of(B, T, D, columns_of_lane<Bf16>(D)).bytes;
     *bytes = wide > narrow ? wide : narrow;
     return CX_OK;
 }
