@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kRowThreads) void distill_kernel(const DistillArgs<
     } else {
         all = {a.stats[n * 4], a.stats[n * 4 + 1], a.stats[n * 4 + 2]};
     }
-    if (FROM != kSaved && X != kDual) all.u = all.s;    // one sum serves both
+    if (FROM != kSaved && !two_sums(X)) all.u = all.s;    // one sum serves both
     if (threadIdx.x < kWave) {
         const bool want_loss = FROM != kSaved && part == 0 && a.loss;
         row_targets<E>(a, n, all, want_loss, to);
@@ -170,9 +170,11 @@ __global__ __launch_bounds__(kRowThreads) void distill_kernel(const DistillArgs<
     __syncthreads();
     const float gout = a.gout[n], soft = to.soft == 0.0f ? 0.0f : gout * to.soft / all.s, hard = to.hard == 0.0f ? 0.0f : gout * to.hard / all.u;
     const auto share = [&](float z) {
-        const float d = z - all.m;
-        if (X == kDual) return __builtin_fmaf(soft, exp2_fast(d * c), hard * exp2_fast(d * kLog2e));
-        return (soft + hard) * exp2_fast(d * c);
+        const float d = z - all.m, e = exp2_fast(d * c);
+        if (X == kDual) return __builtin_fmaf(soft, e, hard * second<X>(d, e, kLog2e));
+        if (X == kSquare) return e * __builtin_fmaf(hard, e, soft);
+        if (X == kFourth) return e * __builtin_fmaf(hard * e, e * e, soft);
+        return (soft + hard) * e;
     };
     typename E::T *dz = a.dz + n * a.ld_dz + lo;
     if (to.soft == 0.0f && to.hard == 0.0f) {           // a row without targets has no gradient, whatever its logits are
@@ -246,8 +248,8 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
     a.parts = space.parts;
     a.part_stats = static_cast<Stats *>(workspace);
     const bool dual = a.w_kl != 0.0f && a.w_ce != 0.0f && a.tau != 1.0f;
+    const Extra sums = !dual ? kNone : a.tau == 2.0f ? kSquare : a.tau == 4.0f ? kFourth : kDual;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-#define CX_DISTILL(KERNEL, GRID) hipLaunchKernelGGL(KERNEL, GRID, dim3(kRowThreads), 0, st, b)
     for (int64_t n0 = 0; n0 < N; n0 += 65535) {         // rows in slices of a grid's second dimension
         const unsigned rows = static_cast<unsigned>(N - n0 < 65535 ? N - n0 : 65535);
         DistillArgs<E> b = a;
@@ -259,30 +261,33 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
         if (b.gout) b.gout += n0;
         if (b.loss) b.loss += n0;
         if (b.stats) b.stats += n0 * 4;
-        const dim3 grid(space.parts, rows);
-        if (from_saved) {
-            if (dual) CX_DISTILL((distill_kernel<E, kDual, kSaved>), grid); else CX_DISTILL((distill_kernel<E, kNone, kSaved>), grid);
-        } else if (space.parts == 1) {
-            if (dual) CX_DISTILL((distill_kernel<E, kDual, kHere>), grid); else CX_DISTILL((distill_kernel<E, kNone, kHere>), grid);
-        } else {                                        // few rows: one slice
-            if (dual) CX_DISTILL((part_kernel<E, kDual>), grid); else CX_DISTILL((part_kernel<E, kNone>), grid);
-            if (launched() != CX_OK) return CX_ERR_HIP;
-            // the loss reads logits of all parts: where gradients replace them, it comes first, in a launch of its own
-            const bool in_place = want_dz && static_cast<const void *>(a.dz) == a.z;
-            if (in_place) {
-                b.dz = nullptr;
-                const dim3 one(1, rows);
-                if (dual) CX_DISTILL((distill_kernel<E, kDual, kParts>), one); else CX_DISTILL((distill_kernel<E, kNone, kParts>), one);
-                if (launched() != CX_OK) return CX_ERR_HIP;
-                b.dz = a.dz;
-                b.loss = nullptr;
+        const dim3 whole(1, rows), parted(space.parts, rows), block(kRowThreads);
+        const auto launch = [&](auto kind) {
+            constexpr Extra X = decltype(kind)::value;
+            if (from_saved) {
+                hipLaunchKernelGGL((distill_kernel<E, X, kSaved>), parted, block, 0, st, b);
+            } else if (space.parts == 1) {
+                hipLaunchKernelGGL((distill_kernel<E, X, kHere>), whole, block, 0, st, b);
+            } else {                                    // few rows: one slice of them
+                hipLaunchKernelGGL((part_kernel<E, X>), parted, block, 0, st, b);
+                if (want_dz && static_cast<const void *>(a.dz) == a.z) {
+                    // the loss reads logits of all parts: where gradients replace them, it comes first, in a launch of its own
+                    DistillArgs<E> first = b;
+                    first.dz = nullptr;
+                    hipLaunchKernelGGL((distill_kernel<E, X, kParts>), whole, block, 0, st, first);
+                    b.loss = nullptr;
+                }
+                hipLaunchKernelGGL((distill_kernel<E, X, kParts>), want_dz ? parted : whole, block, 0, st, b);
             }
-            const dim3 second(want_dz ? space.parts : 1, rows);
-            if (dual) CX_DISTILL((distill_kernel<E, kDual, kParts>), second); else CX_DISTILL((distill_kernel<E, kNone, kParts>), second);
+        };
+        switch (sums) {
+        case kDual: launch(std::integral_constant<Extra, kDual>{}); break;
+        case kSquare: launch(std::integral_constant<Extra, kSquare>{}); break;
+        case kFourth: launch(std::integral_constant<Extra, kFourth>{}); break;
+        default: launch(std::integral_constant<Extra, kNone>{});
         }
         if (launched() != CX_OK) return CX_ERR_HIP;
     }
-#undef CX_DISTILL
     return CX_OK;
 }
 

@@ -7,9 +7,9 @@
 // vector column each of one row, so a short row does not leave a wavefront's lanes idle.
 //
 // The gradient writes each row of the table once and adds in a fixed order, which atomics would not.  Three launches:
-//   sort_kernel   a stable counting sort of each worker's tokens.  A workgroup owns 512 ids and reads all N tokens
+//   sort_kernel   a stable counting sort of each worker's tokens.  A workgroup owns 1,024 ids and reads all N tokens
 //                 itself instead of exchanging counts with the others: no passes, no atomics on memory, and where the
-//                 table has 32,768 rows 64 workgroups a worker read 64 x 16 KB of tokens from the cache.
+//                 table has 32,768 rows 32 workgroups a worker read 32 x 16 KB of tokens from the cache.
 //   grad_kernel   the sorted list in pieces of equal length, one to a group of lanes, so that a frequent token keeps no group longer than
 //                 a rare one: it adds up the rows of dout that its piece names, list by list, and writes what lists lie inside the
 //                 piece; what reaches beyond goes to the workspace.  Other workgroups of the same launch write the rows that no
@@ -20,10 +20,11 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBins = 512;                  // ids of a workgroup of the sort
-constexpr int kSortWaves = 16;
+constexpr int kBins = 1024;                 // ids of a workgroup of the sort
+constexpr int kSortWaves = 8, kSortThreads = kSortWaves * kWave;
+constexpr int kBinsEach = kBins / kSortThreads;
 constexpr int kHeld = 8;                    // tokens a lane of the sort keeps in registers between its two walks
-constexpr int kEmptyRows = 8;               // rows of the table a group of lanes looks at for being named by no token
+constexpr int kJoinThreads = kWave;         // few: most workgroups of the join find nothing to do
 constexpr int64_t kMaxTokens = CX_MAX_TOKENS;
 constexpr int32_t kMaxVocab = CX_MAX_VOCAB, kMaxWidth = CX_MAX_WIDTH;
 
@@ -97,23 +98,22 @@ struct Sorted {
 
 // sorted[w]: the tokens of worker w by id, then by place; named[w]: a bit for every id, set if a token is that id;
 // total[w]: the tokens that are an id at all.
-__global__ __launch_bounds__(kSortWaves *kWave) void sort_kernel(const int32_t *tokens, int64_t N, int32_t V, Sorted *sorted, uint64_t *named,
-                                                                 int32_t *total)
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(const int32_t *tokens, int64_t N, int32_t V, Sorted *sorted, uint64_t *named, int32_t *total)
 {
     __shared__ unsigned count[kSortWaves][kBins];
-    __shared__ unsigned below_of[kSortWaves], sum_of[kBins / kWave];
+    __shared__ unsigned below_of[kSortWaves], sum_of[kSortWaves];
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave);
     const int32_t lo = static_cast<int32_t>(blockIdx.x) * kBins;
     const unsigned ids = V - lo < kBins ? V - lo : kBins;
     tokens += blockIdx.y * N;
     sorted += blockIdx.y * N;
     // every wavefront has a contiguous part of the tokens
-    const int64_t part = (N + kSortWaves * kWave - 1) / (kSortWaves * kWave) * kWave;
+    const int64_t part = (N + kSortThreads - 1) / kSortThreads * kWave;
     const int64_t from = wave * part, to = from + part < N ? from + part : N;
     int held[kHeld];
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) held[k] = from + k * kWave + lane < to ? tokens[from + k * kWave + lane] : -1;
-    for (int k = threadIdx.x; k < kSortWaves * kBins; k += kSortWaves * kWave) (&count[0][0])[k] = 0;
+    for (int k = threadIdx.x; k < kSortWaves * kBins; k += kSortThreads) (&count[0][0])[k] = 0;
     __syncthreads();
     int below = 0;
     const auto tally = [&](int token) {
@@ -126,33 +126,46 @@ __global__ __launch_bounds__(kSortWaves *kWave) void sort_kernel(const int32_t *
     for (int64_t n = from + kHeld * kWave; n < to; n += kWave) tally(n + lane < to ? tokens[n + lane] : -1);
     if (lane == 0) below_of[wave] = below;
     __syncthreads();
-    // a thread for every id: exclusive sums over the wavefronts, then over the ids
-    unsigned mine = 0, sum = 0;
-    if (threadIdx.x < kBins) {
+    // a thread for every kBinsEach ids: exclusive sums over the wavefronts, then over the ids
+    unsigned mine[kBinsEach], own = 0;
+#pragma unroll
+    for (int i = 0; i < kBinsEach; ++i) {
+        const int bin = threadIdx.x * kBinsEach + i;
+        mine[i] = 0;
 #pragma unroll
         for (int k = 0; k < kSortWaves; ++k) {
-            const unsigned c = count[k][threadIdx.x];
-            count[k][threadIdx.x] = mine;
-            mine += c;
+            const unsigned c = count[k][bin];
+            count[k][bin] = mine[i];
+            mine[i] += c;
         }
-        sum = mine;
-#pragma unroll
-        for (int d = 1; d < kWave; d *= 2) {
-            const unsigned other = __shfl_up(sum, d);
-            if (lane >= d) sum += other;
-        }
-        if (lane == kWave - 1) sum_of[wave] = sum;
-        const uint64_t bits = __ballot(mine != 0);
-        if (lane == 0 && threadIdx.x < ids) named[blockIdx.y * ((static_cast<int64_t>(V) + 63) / 64) + lo / 64 + wave] = bits;
+        own += mine[i];
     }
-    __syncthreads();
-    if (threadIdx.x < kBins) {
-        unsigned first = sum - mine;
-        for (int k = 0; k < kSortWaves; ++k) first += below_of[k];
-        for (int k = 0; k < wave; ++k) first += sum_of[k];
-        if (threadIdx.x + 1 == ids && lo + static_cast<int32_t>(ids) == V) total[blockIdx.y] = static_cast<int32_t>(first + mine);
+    unsigned sum = own;
 #pragma unroll
-        for (int k = 0; k < kSortWaves; ++k) count[k][threadIdx.x] += first;
+    for (int d = 1; d < kWave; d *= 2) {
+        const unsigned other = __shfl_up(sum, d);
+        if (lane >= d) sum += other;
+    }
+    if (lane == kWave - 1) sum_of[wave] = sum;
+    __syncthreads();
+    unsigned first = sum - own;
+#pragma unroll
+    for (int k = 0; k < kSortWaves; ++k) first += below_of[k];
+    for (int k = 0; k < wave; ++k) first += sum_of[k];
+    if (blockIdx.x + 1 == gridDim.x && threadIdx.x + 1 == kSortThreads) total[blockIdx.y] = static_cast<int32_t>(first + own);
+    static_assert(kBinsEach == 2, "a wavefront's bits make two words");
+    const uint64_t even = __ballot(mine[0] != 0), odd = __ballot(mine[1] != 0);
+    if (lane < kBinsEach) {
+        uint64_t word = 0;                                  // of ids 2 * (64 * wave + 32 * lane) and on
+        for (int k = 0; k < 32; ++k) word |= ((even >> (32 * lane + k)) & 1) << (2 * k) | ((odd >> (32 * lane + k)) & 1) << (2 * k + 1);
+        const unsigned at = (2 * wave + lane) * 64;
+        if (at < ids) named[blockIdx.y * ((static_cast<int64_t>(V) + 63) / 64) + (lo + at) / 64] = word;
+    }
+#pragma unroll
+    for (int i = 0; i < kBinsEach; ++i) {
+#pragma unroll
+        for (int k = 0; k < kSortWaves; ++k) count[k][threadIdx.x * kBinsEach + i] += first;
+        first += mine[i];
     }
     __syncthreads();
     // the same walk again: the lanes of a wavefront that hold one id take consecutive places
@@ -267,30 +280,42 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const GradArgs<E> a)
         return;
     }
     if constexpr (!IN_PLACE) {
-        const int64_t v0 = (static_cast<int64_t>(blockIdx.x - a.chunk_blocks) * groups + group) * kEmptyRows;
-        if (c.n == 0 || v0 >= a.V) return;
+        // 64 rows, one word of bits; the slabs of the grid share its vectors, whichever rows these lie in
+        const int64_t v0 = static_cast<int64_t>(blockIdx.x - a.chunk_blocks) * 64;
+        const int rows = a.V - v0 < 64 ? static_cast<int>(a.V - v0) : 64, elements = rows * a.D;
         const uint64_t word = a.named[w * ((static_cast<int64_t>(a.V) + 63) / 64) + v0 / 64];
-        const unsigned bits = static_cast<unsigned>(word >> (v0 % 64));
-        const int64_t first = w * a.ld + v0 * a.D;
-        float g[kEmptyRows][E::kPer16];
+        const typename E::T *from = a.g_in ? a.g_in + w * a.ld + v0 * a.D : nullptr;
+        typename E::T *to = a.g_out + w * a.ld + v0 * a.D;
+        constexpr int kPer = E::kPer16, kAhead = 4;
+        const int stride = gridDim.y * kThreads;
+        int q = blockIdx.y * kThreads + threadIdx.x;
+        if (word == 0) {
+            for (; (q + (kAhead - 1) * stride + 1) * kPer <= elements; q += kAhead * stride) {
+                u4 v[kAhead];
 #pragma unroll
-        for (int r = 0; r < kEmptyRows; ++r) {
-            if (a.g_in && v0 + r < a.V && !((bits >> r) & 1u)) c.load(a.g_in + first + static_cast<int64_t>(r) * a.D, g[r]);
-            else
+                for (int k = 0; k < kAhead; ++k) v[k] = from ? load16<E>(from + (q + k * stride) * kPer) : u4{};
 #pragma unroll
-                for (int j = 0; j < E::kPer16; ++j) g[r][j] = 0.0f;
+                for (int k = 0; k < kAhead; ++k) store16<E>(to + (q + k * stride) * kPer, v[k]);
+            }
         }
-#pragma unroll
-        for (int r = 0; r < kEmptyRows; ++r)
-            if (v0 + r < a.V && !((bits >> r) & 1u)) c.store(a.g_out + first + static_cast<int64_t>(r) * a.D, g[r]);
+        for (; q * kPer < elements; q += stride) {
+            const int first = q * kPer, last = (first + kPer < elements ? first + kPer : elements) - 1;
+            const int r0 = first / a.D, r1 = last / a.D;
+            if (first + kPer <= elements && ((word >> r0) & ((2ull << (r1 - r0)) - 1)) == 0) {
+                store16<E>(to + first, from ? load16<E>(from + first) : u4{});
+            } else {
+                for (int at = first; at <= last; ++at)
+                    if (!((word >> (at / a.D)) & 1)) to[at] = from ? from[at] : E::narrow(0.0f);
+            }
+        }
     }
 }
 
 // The list that begins in this piece and goes on behind it, if one does: its sums, in order.
 template <class E>
-__global__ __launch_bounds__(kThreads) void join_kernel(const GradArgs<E> a)
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const GradArgs<E> a)
 {
-    __shared__ float lds[E::kPer16][kThreads];
+    __shared__ float lds[E::kPer16][kJoinThreads];
     const int64_t w = blockIdx.z;
     const Sorted *sorted = a.sorted + w * a.N;
     const int chunk = blockIdx.x, all = a.total[w], p0 = chunk * a.piece, p1 = p0 + a.piece;
@@ -298,28 +323,38 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const GradArgs<E> a)
     const int id = sorted[p1 - 1].id;
     if (sorted[p1].id != id || (sorted[p0].id == id && p0 > 0 && sorted[p0 - 1].id == id)) return;
     int pieces = 1;                         // and those whose first token is of the list
-    for (;; pieces += kThreads) {
+    for (;; pieces += kJoinThreads) {
         const int64_t p = static_cast<int64_t>(chunk + pieces + static_cast<int>(threadIdx.x)) * a.piece;
-        const int more = __syncthreads_count(p < all && sorted[p].id == id);
-        if (more < kThreads) { pieces += more; break; }
+        const int more = __popcll(__ballot(p < all && sorted[p].id == id));
+        if (more < kJoinThreads) { pieces += more; break; }
     }
-    const int lanes = 1 << a.shift, groups = kThreads >> a.shift, group = threadIdx.x >> a.shift;
+    const int lanes = 1 << a.shift, groups = kJoinThreads >> a.shift, group = threadIdx.x >> a.shift;
     const Columns<E> c = columns_of<E>(threadIdx.x & (lanes - 1), lanes, blockIdx.y, a.D);
     const int each = (pieces + groups - 1) / groups;
     const int from = group * each, to = from + each < pieces ? from + each : pieces;
     const float *row = a.pieces + (w * a.chunks + chunk) * 2 * a.D + c.first;
     float sum[E::kPer16] = {};
-    for (int k = from; k < to; ++k) {
-        const float *piece = row + (static_cast<int64_t>(k) * 2 + (k == 0)) * a.D;
+    constexpr int kAhead = 4;
+    for (int k0 = from; k0 < to; k0 += kAhead) {
+        float v[kAhead][E::kPer16];
 #pragma unroll
-        for (int j = 0; j < E::kPer16; ++j)
-            if (j < c.n) sum[j] += piece[j];
+        for (int i = 0; i < kAhead; ++i) {
+            const int k = k0 + i < to ? k0 + i : to - 1;
+            const float *piece = row + (static_cast<int64_t>(k) * 2 + (k == 0)) * a.D;
+#pragma unroll
+            for (int j = 0; j < E::kPer16; ++j) v[i][j] = j < c.n ? piece[j] : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (k0 + i < to)
+#pragma unroll
+                for (int j = 0; j < E::kPer16; ++j) sum[j] += v[i][j];
     }
 #pragma unroll
     for (int j = 0; j < E::kPer16; ++j) lds[j][threadIdx.x] = sum[j];
     __syncthreads();
     if (group == 0 && c.n) {
-        for (int at = threadIdx.x + lanes; at < kThreads; at += lanes)
+        for (int at = threadIdx.x + lanes; at < kJoinThreads; at += lanes)
 #pragma unroll
             for (int j = 0; j < E::kPer16; ++j) sum[j] += lds[j][at];
         finish<E>(a, c, w, id, sum);
@@ -418,11 +453,11 @@ int grad(const typename E::T *dout, int64_t ld_dout, const int32_t *tokens, int3
     const int groups = kThreads >> a.shift;
     const unsigned slabs = static_cast<unsigned>(ceil_div(ceil_div(D, E::kPer16), 1 << a.shift));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(sort_kernel, dim3(static_cast<unsigned>(ceil_div(V, kBins)), W), dim3(kSortWaves * kWave), 0, st, tokens, N, V, sorted, named,
+    hipLaunchKernelGGL(sort_kernel, dim3(static_cast<unsigned>(ceil_div(V, kBins)), W), dim3(kSortThreads), 0, st, tokens, N, V, sorted, named,
                        total);
     if (launched() != CX_OK) return CX_ERR_HIP;
     a.chunk_blocks = static_cast<int32_t>(ceil_div(space.chunks, groups));
-    const int64_t empty_blocks = g_in == g_out ? 0 : ceil_div(V, static_cast<int64_t>(groups) * kEmptyRows);
+    const int64_t empty_blocks = g_in == g_out ? 0 : ceil_div(V, 64);
     const dim3 grid(static_cast<unsigned>(a.chunk_blocks + empty_blocks), slabs, W);
     const unsigned list_bytes = (groups * a.piece + 2) * sizeof(Sorted);
     if (grid.x > 0) {
@@ -431,7 +466,7 @@ int grad(const typename E::T *dout, int64_t ld_dout, const int32_t *tokens, int3
         if (launched() != CX_OK) return CX_ERR_HIP;
     }
     if (space.chunks <= 1) return CX_OK;
-    hipLaunchKernelGGL(join_kernel<E>, dim3(static_cast<unsigned>(space.chunks - 1), slabs, W), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL(join_kernel<E>, dim3(static_cast<unsigned>(space.chunks - 1), slabs, W), dim3(kJoinThreads), 0, st, a);
     return launched();
 }
 

@@ -240,11 +240,22 @@ __global__ __launch_bounds__(kRowThreads) void join_kernel(const ScoreArgs<E> a)
     Stats all = a.part_stats[n * a.parts];
     for (int k = 1; k < a.parts; ++k) all = join<kEntropy>(all, a.part_stats[n * a.parts + k], c, 0.0f);
     if (TOP) {
+        // each part's K-th key is reached by K keys: the largest of them leaves little more than K
+        const Key *keys = a.part_keys + n * a.parts * a.K;
         if (threadIdx.x == 0) top.count = 0;
+        if (threadIdx.x < kWave) {
+            Key least = static_cast<int>(threadIdx.x) < a.parts ? keys[(threadIdx.x + 1) * a.K - 1] : 0;
+#pragma unroll
+            for (int d = kWave / 2; d > 0; d /= 2) {
+                const Key other = __shfl_xor(least, d);
+                least = other > least ? other : least;
+            }
+            if (threadIdx.x == 0) top.least = least;
+        }
         __syncthreads();
         for (int i = threadIdx.x; i < a.parts * a.K; i += kRowThreads) {
-            const Key key = a.part_keys[n * a.parts * a.K + i];
-            if (key) top.list[atomicAdd(&top.count, 1u)] = key;
+            const Key key = keys[i];
+            if (key && key >= top.least) top.list[atomicAdd(&top.count, 1u)] = key;
         }
         rank_list(top, a.K);
     }

@@ -15,8 +15,20 @@ constexpr int kAhead = 4;                               // 16-byte loads a threa
 constexpr float kLowest = -3.40282346638528859812e38f;
 constexpr float kVanish = -200.0f;                      // exponents (base 2) from here on give 0; keeps 0 * inf out of the sums
 
-// u: WITH_ENTROPY: sum of e * log2(e), e = 2^((z - m) c);  DUAL: the sum of 2^((z - m) c2);  otherwise unused.
-enum Extra { kNone, kEntropy, kDual };
+// With e = 2^((z - m) c), s is the sum of e, and u
+//   kEntropy          the sum of e * log2(e)
+//   kDual             the sum of 2^((z - m) c2);  kSquare, kFourth: the same where c2 is 2 c or 4 c: a power of e by
+//                     multiplications.  A kernel whose loop has two exponentials an element is bound by them, not by memory.
+enum Extra { kNone, kEntropy, kDual, kSquare, kFourth };
+__host__ __device__ constexpr bool two_sums(Extra x) { return x == kDual || x == kSquare || x == kFourth; }
+
+// 2^((z - m) c2), d = z - m, e = 2^(d c)
+template <Extra X>
+__device__ __forceinline__ float second(float d, float e, float c2)
+{
+    if (X == kDual) return __builtin_amdgcn_exp2f(d * c2);
+    return X == kFourth ? (e * e) * (e * e) : e * e;
+}
 
 struct Stats {
     float m, s, u;
@@ -29,7 +41,7 @@ __device__ __forceinline__ void rebase(Stats &a, float m, float c, float c2)
 {
     const float d = not_below((a.m - m) * c, kVanish), f = exp2_fast(d);
     if (X == kEntropy) a.u = f * __builtin_fmaf(a.s, d, a.u);
-    if (X == kDual) a.u *= exp2_fast(not_below((a.m - m) * c2, kVanish));
+    if (two_sums(X)) a.u *= second<X>(not_below(a.m - m, kLowest), f, c2);
     a.s *= f;
     a.m = m;
 }
@@ -56,7 +68,7 @@ __device__ __forceinline__ float accumulate(Stats &a, const float (&z)[N], float
         const float d = z[j] - a.m, t = d * c, e = exp2_fast(t);
         s[j & 1] += e;
         if (X == kEntropy) u[j & 1] = __builtin_fmaf(e, fmaxf(t, kVanish), u[j & 1]);
-        if (X == kDual) u[j & 1] += exp2_fast(d * c2);
+        if (two_sums(X)) u[j & 1] += second<X>(d, e, c2);
     }
     a.s += s[0] + s[1];
     a.u += u[0] + u[1];
