@@ -14,17 +14,17 @@
 //                 a rare one: it adds up the rows of dout that its piece names, list by list, and writes what lists lie inside the
 //                 piece; what reaches beyond goes to the workspace.  Other workgroups of the same launch write the rows that no
 //                 token names.
-//   join_kernel   adds up the lists that reach over several pieces, in order.
+//   join_kernel   adds up the lists that reach over several pieces, in order; the sort has noted where these begin.
 #include "lm_common.hpp"
 
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBins = 1024;                 // ids of a workgroup of the sort
-constexpr int kSortWaves = 8, kSortThreads = kSortWaves * kWave;
-constexpr int kBinsEach = kBins / kSortThreads;
-constexpr int kHeld = 8;                    // tokens a lane of the sort keeps in registers between its two walks
-constexpr int kJoinThreads = kWave;         // few: most workgroups of the join find nothing to do
+constexpr int kSortWaves = 16, kSortThreads = kSortWaves * kWave;
+static_assert(kBins == kSortThreads, "a thread for every id");
+constexpr int kHeld = 4;                    // tokens a lane of the sort loads at once; the first ones stay for the second walk
+constexpr int kFewPieces = 8;               // a list of no more is joined by one group of lanes
 constexpr int64_t kMaxTokens = CX_MAX_TOKENS;
 constexpr int32_t kMaxVocab = CX_MAX_VOCAB, kMaxWidth = CX_MAX_WIDTH;
 
@@ -32,15 +32,19 @@ template <class E>
 struct Columns {                            // the columns of a row that a lane handles
     int64_t first;
     int n;                                  // of kPer16; 0 beyond the row
-    __device__ __forceinline__ void load(const typename E::T *row, float (&v)[E::kPer16]) const
+    __device__ __forceinline__ u4 raw(const typename E::T *row) const
     {
-        if (n == E::kPer16) {
-            E::unpack(load16<E>(row + first), v);
-        } else {
+        if (n == E::kPer16) return load16<E>(row + first);
+        u4 w{};
 #pragma unroll
-            for (int j = 0; j < E::kPer16; ++j) v[j] = j < n ? E::widen(row[first + j]) : 0.0f;
-        }
+        for (int j = 0; j < E::kPer16; ++j)
+            if (j < n) {
+                if constexpr (E::kPer16 == 4) w[j] = __float_as_uint(row[first + j]);
+                else w[j / 2] |= static_cast<unsigned>(row[first + j]) << (16 * (j & 1));
+            }
+        return w;
     }
+    __device__ __forceinline__ void load(const typename E::T *row, float (&v)[E::kPer16]) const { E::unpack(raw(row), v); }
     __device__ __forceinline__ void store(typename E::T *row, const float (&v)[E::kPer16]) const
     {
         if (n == E::kPer16) {
@@ -96,9 +100,14 @@ struct Sorted {
     int32_t id, n;                          // a token and its place
 };
 
+struct Crossing {
+    int32_t id, pieces;                     // the list that begins in a piece and goes on behind it, and how many it reaches over; 0: none does
+};
+
 // sorted[w]: the tokens of worker w by id, then by place; named[w]: a bit for every id, set if a token is that id;
-// total[w]: the tokens that are an id at all.
-__global__ __launch_bounds__(kSortThreads) void sort_kernel(const int32_t *tokens, int64_t N, int32_t V, Sorted *sorted, uint64_t *named, int32_t *total)
+// total[w]: the tokens that are an id at all;  crossing[w]: for every piece that is followed by another one.
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(const int32_t *tokens, int64_t N, int32_t V, Sorted *sorted, uint64_t *named, int32_t *total,
+                                                            Crossing *crossing, int piece, int chunks)
 {
     __shared__ unsigned count[kSortWaves][kBins];
     __shared__ unsigned below_of[kSortWaves], sum_of[kSortWaves];
@@ -123,22 +132,22 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(const int32_t *token
     };
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) tally(held[k]);
-    for (int64_t n = from + kHeld * kWave; n < to; n += kWave) tally(n + lane < to ? tokens[n + lane] : -1);
+    for (int64_t n = from + kHeld * kWave; n < to; n += kHeld * kWave) {
+        int token[kHeld];
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) token[k] = n + k * kWave + lane < to ? tokens[n + k * kWave + lane] : -1;
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) tally(token[k]);
+    }
     if (lane == 0) below_of[wave] = below;
     __syncthreads();
-    // a thread for every kBinsEach ids: exclusive sums over the wavefronts, then over the ids
-    unsigned mine[kBinsEach], own = 0;
+    // a thread for every id: exclusive sums over the wavefronts, then over the ids
+    unsigned own = 0;
 #pragma unroll
-    for (int i = 0; i < kBinsEach; ++i) {
-        const int bin = threadIdx.x * kBinsEach + i;
-        mine[i] = 0;
-#pragma unroll
-        for (int k = 0; k < kSortWaves; ++k) {
-            const unsigned c = count[k][bin];
-            count[k][bin] = mine[i];
-            mine[i] += c;
-        }
-        own += mine[i];
+    for (int k = 0; k < kSortWaves; ++k) {
+        const unsigned c = count[k][threadIdx.x];
+        count[k][threadIdx.x] = own;
+        own += c;
     }
     unsigned sum = own;
 #pragma unroll
@@ -153,19 +162,17 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(const int32_t *token
     for (int k = 0; k < kSortWaves; ++k) first += below_of[k];
     for (int k = 0; k < wave; ++k) first += sum_of[k];
     if (blockIdx.x + 1 == gridDim.x && threadIdx.x + 1 == kSortThreads) total[blockIdx.y] = static_cast<int32_t>(first + own);
-    static_assert(kBinsEach == 2, "a wavefront's bits make two words");
-    const uint64_t even = __ballot(mine[0] != 0), odd = __ballot(mine[1] != 0);
-    if (lane < kBinsEach) {
-        uint64_t word = 0;                                  // of ids 2 * (64 * wave + 32 * lane) and on
-        for (int k = 0; k < 32; ++k) word |= ((even >> (32 * lane + k)) & 1) << (2 * k) | ((odd >> (32 * lane + k)) & 1) << (2 * k + 1);
-        const unsigned at = (2 * wave + lane) * 64;
-        if (at < ids) named[blockIdx.y * ((static_cast<int64_t>(V) + 63) / 64) + (lo + at) / 64] = word;
-    }
+    const uint64_t word = __ballot(own != 0);
+    if (lane == 0 && static_cast<unsigned>(wave * kWave) < ids) named[blockIdx.y * ((static_cast<int64_t>(V) + 63) / 64) + lo / 64 + wave] = word;
 #pragma unroll
-    for (int i = 0; i < kBinsEach; ++i) {
-#pragma unroll
-        for (int k = 0; k < kSortWaves; ++k) count[k][threadIdx.x * kBinsEach + i] += first;
-        first += mine[i];
+    for (int k = 0; k < kSortWaves; ++k) count[k][threadIdx.x] += first;
+    // the list [first, end) says what crosses the end of each piece whose last token is in it
+    if (own) {
+        const int end = static_cast<int>(first + own), begins = static_cast<int>(first / static_cast<unsigned>(piece));
+        for (int chunk = begins; (chunk + 1) * piece <= end; ++chunk) {
+            const bool crosses = chunk == begins && (chunk + 1) * piece < end;
+            crossing[blockIdx.y * static_cast<int64_t>(chunks) + chunk] = {lo + static_cast<int>(threadIdx.x), crosses ? (end - 1) / piece - begins + 1 : 0};
+        }
     }
     __syncthreads();
     // the same walk again: the lanes of a wavefront that hold one id take consecutive places
@@ -187,7 +194,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(const int32_t *token
     };
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) put(held[k], from + k * kWave);
-    for (int64_t n = from + kHeld * kWave; n < to; n += kWave) put(n + lane < to ? tokens[n + lane] : -1, n);
+    for (int64_t n = from + kHeld * kWave; n < to; n += kHeld * kWave) {
+        int token[kHeld];
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) token[k] = n + k * kWave + lane < to ? tokens[n + k * kWave + lane] : -1;
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) put(token[k], n + k * kWave);
+    }
 }
 
 template <class E>
@@ -197,65 +210,88 @@ struct GradArgs {
     const Sorted *sorted;
     const uint64_t *named;
     const int32_t *total;
-    float *pieces;                          // [W][chunks][2][D]: a piece's sums of the list that begins before it, of the one that goes on behind it
+    const Crossing *crossing;               // [W][chunks]
+    float *pieces;                          // [W][chunks][2][piece_ld]: a piece's sums of the list that begins before it, of the one that goes on behind it
     const typename E::T *g_in;              // first element of the table's columns, or NULL
     typename E::T *g_out;
-    int64_t ld, N;
+    int64_t ld, N, piece_ld;                // piece_ld: D in whole vectors
     int32_t V, D, chunks, chunk_blocks;
     float scale;
-    int shift, piece;                       // lanes of a group (log2), tokens of a piece
+    int shift, piece, slabs, fills, turn;   // lanes of a group (log2), tokens of a piece, groups to a row, workgroups to 64 rows
 };
 
-template <class E>
-__device__ __forceinline__ void finish(const GradArgs<E> &a, const Columns<E> &c, int64_t w, int32_t v, const float (&sum)[E::kPer16])
+// A lane's sums, in fp32, 16 bytes at a time.
+template <int N>
+__device__ __forceinline__ void store_wide(float *to, const float (&v)[N])
 {
-    const int64_t at = w * a.ld + static_cast<int64_t>(v) * a.D;
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+        const float part[4] = {v[j], v[j + 1], v[j + 2], v[j + 3]};
+        store16<F32>(to + j, F32::pack(part));
+    }
+}
+template <int N>
+__device__ __forceinline__ void load_wide(const float *from, float (&v)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+        float part[4];
+        F32::unpack(load16<F32>(from + j), part);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j + i] = part[i];
+    }
+}
+
+template <class E>
+__device__ __forceinline__ int64_t place_of(const GradArgs<E> &a, int64_t w, int32_t v) { return w * a.ld + static_cast<int64_t>(v) * a.D; }
+
+// g: the row of g_in, where there is one
+template <class E>
+__device__ __forceinline__ void finish(const GradArgs<E> &a, const Columns<E> &c, int64_t w, int32_t v, const float (&sum)[E::kPer16], const u4 &g_row)
+{
     float g[E::kPer16];
-    if (a.g_in) c.load(a.g_in + at, g);
+    E::unpack(g_row, g);
 #pragma unroll
     for (int j = 0; j < E::kPer16; ++j) g[j] = a.g_in ? __builtin_fmaf(a.scale, sum[j], g[j]) : a.scale * sum[j];
-    c.store(a.g_out + at, g);
+    c.store(a.g_out + place_of(a, w, v), g);
 }
 
 // One piece of the sorted list; `list` holds it and its neighbours (id -1: none).
 template <class E>
 __device__ __forceinline__ void sum_piece(const GradArgs<E> &a, const Columns<E> &c, int64_t w, int chunk, int tokens, const Sorted *list)
 {
-    constexpr int kRows = 4;                // rows of dout in flight
+    constexpr int kRows = 8;                // rows of dout in flight, and of g_in where a list ends
     const typename E::T *rows = a.dout + w * a.N * a.ld_dout;
     float sum[E::kPer16] = {};
-    int id = list[0].id;
-    bool began = list[-1].id != id;         // in this piece
-    const auto close = [&](bool ends) {
-        if (began && ends) {
-            finish<E>(a, c, w, id, sum);
-        } else {
-            float *to = a.pieces + ((w * a.chunks + chunk) * 2 + (began ? 1 : 0)) * a.D + c.first;
-#pragma unroll
-            for (int j = 0; j < E::kPer16; ++j)
-                if (j < c.n) to[j] = sum[j];
-        }
-    };
+    bool began = list[-1].id != list[0].id; // in this piece
     for (int i = 0; i < tokens; i += kRows) {
-        float v[kRows][E::kPer16];
+        u4 v[kRows], g[kRows];
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) c.load(rows + list[i + k < tokens ? i + k : tokens - 1].n * a.ld_dout, v[k]);
+        for (int k = 0; k < kRows; ++k) {
+            v[k] = g[k] = u4{};
+            if (i + k >= tokens) continue;
+            v[k] = c.raw(rows + list[i + k].n * a.ld_dout);
+            if (a.g_in && list[i + k].id != list[i + k + 1].id) g[k] = c.raw(a.g_in + place_of(a, w, list[i + k].id));
+        }
 #pragma unroll
         for (int k = 0; k < kRows; ++k) {
             if (i + k >= tokens) break;
-            const int next = list[i + k].id;
-            if (next != id) {
-                close(true);
-                id = next;
-                began = true;
+            float one[E::kPer16];
+            E::unpack(v[k], one);
 #pragma unroll
-                for (int j = 0; j < E::kPer16; ++j) sum[j] = 0.0f;
+            for (int j = 0; j < E::kPer16; ++j) sum[j] += one[j];
+            const bool ends = list[i + k].id != list[i + k + 1].id;
+            if (!ends && i + k + 1 < tokens) continue;
+            if (began && ends) {
+                finish<E>(a, c, w, list[i + k].id, sum, g[k]);
+            } else {
+                store_wide(a.pieces + ((w * a.chunks + chunk) * 2 + (began ? 1 : 0)) * a.piece_ld + c.first, sum);
             }
+            began = true;
 #pragma unroll
-            for (int j = 0; j < E::kPer16; ++j) sum[j] += v[k][j];
+            for (int j = 0; j < E::kPer16; ++j) sum[j] = 0.0f;
         }
     }
-    close(list[tokens].id != id);
 }
 
 // IN_PLACE: g_out is g_in, rows that no token names stay as they are.
@@ -264,10 +300,13 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const GradArgs<E> a)
 {
     extern __shared__ Sorted list[];        // the pieces of this workgroup, one more on either side
     const int lanes = 1 << a.shift, groups = kThreads >> a.shift, group = threadIdx.x >> a.shift;
-    const Columns<E> c = columns_of<E>(threadIdx.x & (lanes - 1), lanes, blockIdx.y, a.D);
-    const int64_t w = blockIdx.z;
-    if (static_cast<int>(blockIdx.x) < a.chunk_blocks) {
-        const int all = a.total[w], p0 = static_cast<int>(blockIdx.x) * groups * a.piece;
+    const int64_t w = blockIdx.y;
+    // workgroups of both kinds in turn, one that adds up for every a.turn of all: adding up waits, filling streams
+    const int x = blockIdx.x, turns = a.chunk_blocks * a.slabs;
+    if (x % a.turn == 0 && x / a.turn < turns) {
+        const int block = x / a.turn / a.slabs, slab = x / a.turn % a.slabs;
+        const Columns<E> c = columns_of<E>(threadIdx.x & (lanes - 1), lanes, slab, a.D);
+        const int all = a.total[w], p0 = block * groups * a.piece;
         if (p0 >= all) return;
         const Sorted *sorted = a.sorted + w * a.N;
         for (int k = threadIdx.x; k < groups * a.piece + 2; k += kThreads) {
@@ -276,29 +315,33 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const GradArgs<E> a)
         }
         __syncthreads();
         const int left = all - p0 - group * a.piece;
-        if (left > 0 && c.n) sum_piece<E>(a, c, w, blockIdx.x * groups + group, left < a.piece ? left : a.piece, list + 1 + group * a.piece);
+        if (left > 0 && c.n) sum_piece<E>(a, c, w, block * groups + group, left < a.piece ? left : a.piece, list + 1 + group * a.piece);
         return;
     }
     if constexpr (!IN_PLACE) {
-        // 64 rows, one word of bits; the slabs of the grid share its vectors, whichever rows these lie in
-        const int64_t v0 = static_cast<int64_t>(blockIdx.x - a.chunk_blocks) * 64;
+        // 64 rows, one word of bits, in a.fills workgroups that have a contiguous part of their vectors each, whichever rows these lie in
+        const int before = (x + a.turn - 1) / a.turn, block = x - (before < turns ? before : turns);
+        const int64_t v0 = static_cast<int64_t>(block / a.fills) * 64;
         const int rows = a.V - v0 < 64 ? static_cast<int>(a.V - v0) : 64, elements = rows * a.D;
         const uint64_t word = a.named[w * ((static_cast<int64_t>(a.V) + 63) / 64) + v0 / 64];
         const typename E::T *from = a.g_in ? a.g_in + w * a.ld + v0 * a.D : nullptr;
         typename E::T *to = a.g_out + w * a.ld + v0 * a.D;
         constexpr int kPer = E::kPer16, kAhead = 4;
-        const int stride = gridDim.y * kThreads;
-        int q = blockIdx.y * kThreads + threadIdx.x;
+        const int vectors = (elements + kPer - 1) / kPer, each = (vectors + a.fills - 1) / a.fills;
+        int q = block % a.fills * each;
+        const int end = q + each < vectors ? q + each : vectors;
+        q += threadIdx.x;
         if (word == 0) {
-            for (; (q + (kAhead - 1) * stride + 1) * kPer <= elements; q += kAhead * stride) {
+            const int whole = elements / kPer < end ? elements / kPer : end;            // the last vector may hang over the rows' end
+            for (; q + (kAhead - 1) * kThreads < whole; q += kAhead * kThreads) {
                 u4 v[kAhead];
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) v[k] = from ? load16<E>(from + (q + k * stride) * kPer) : u4{};
+                for (int k = 0; k < kAhead; ++k) v[k] = from ? load16<E>(from + (q + k * kThreads) * kPer) : u4{};
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) store16<E>(to + (q + k * stride) * kPer, v[k]);
+                for (int k = 0; k < kAhead; ++k) store16<E>(to + (q + k * kThreads) * kPer, v[k]);
             }
         }
-        for (; q * kPer < elements; q += stride) {
+        for (; q < end; q += kThreads) {
             const int first = q * kPer, last = (first + kPer < elements ? first + kPer : elements) - 1;
             const int r0 = first / a.D, r1 = last / a.D;
             if (first + kPer <= elements && ((word >> r0) & ((2ull << (r1 - r0)) - 1)) == 0) {
@@ -311,53 +354,64 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const GradArgs<E> a)
     }
 }
 
-// The list that begins in this piece and goes on behind it, if one does: its sums, in order.
+// The lists that reach over several pieces: their sums, in order.  A group of lanes for every piece that one may begin in; those of many pieces
+// are left to all groups together.
 template <class E>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(const GradArgs<E> a)
+__global__ __launch_bounds__(kThreads) void join_kernel(const GradArgs<E> a)
 {
-    __shared__ float lds[E::kPer16][kJoinThreads];
+    __shared__ float lds[E::kPer16][kThreads];
+    __shared__ Crossing here[kThreads / 4];
     const int64_t w = blockIdx.z;
-    const Sorted *sorted = a.sorted + w * a.N;
-    const int chunk = blockIdx.x, all = a.total[w], p0 = chunk * a.piece, p1 = p0 + a.piece;
-    if (p1 >= all) return;
-    const int id = sorted[p1 - 1].id;
-    if (sorted[p1].id != id || (sorted[p0].id == id && p0 > 0 && sorted[p0 - 1].id == id)) return;
-    int pieces = 1;                         // and those whose first token is of the list
-    for (;; pieces += kJoinThreads) {
-        const int64_t p = static_cast<int64_t>(chunk + pieces + static_cast<int>(threadIdx.x)) * a.piece;
-        const int more = __popcll(__ballot(p < all && sorted[p].id == id));
-        if (more < kJoinThreads) { pieces += more; break; }
+    const int lanes = 1 << a.shift, groups = kThreads >> a.shift, group = threadIdx.x >> a.shift, chunk0 = blockIdx.x * groups;
+    if (static_cast<int>(threadIdx.x) < groups) {
+        const int chunk = chunk0 + threadIdx.x;
+        const bool full = (static_cast<int64_t>(chunk) + 1) * a.piece <= a.total[w];
+        here[threadIdx.x] = full ? a.crossing[w * a.chunks + chunk] : Crossing{-1, 0};
     }
-    const int lanes = 1 << a.shift, groups = kJoinThreads >> a.shift, group = threadIdx.x >> a.shift;
-    const Columns<E> c = columns_of<E>(threadIdx.x & (lanes - 1), lanes, blockIdx.y, a.D);
-    const int each = (pieces + groups - 1) / groups;
-    const int from = group * each, to = from + each < pieces ? from + each : pieces;
-    const float *row = a.pieces + (w * a.chunks + chunk) * 2 * a.D + c.first;
-    float sum[E::kPer16] = {};
-    constexpr int kAhead = 4;
-    for (int k0 = from; k0 < to; k0 += kAhead) {
-        float v[kAhead][E::kPer16];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int k = k0 + i < to ? k0 + i : to - 1;
-            const float *piece = row + (static_cast<int64_t>(k) * 2 + (k == 0)) * a.D;
-#pragma unroll
-            for (int j = 0; j < E::kPer16; ++j) v[i][j] = j < c.n ? piece[j] : 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            if (k0 + i < to)
-#pragma unroll
-                for (int j = 0; j < E::kPer16; ++j) sum[j] += v[i][j];
-    }
-#pragma unroll
-    for (int j = 0; j < E::kPer16; ++j) lds[j][threadIdx.x] = sum[j];
     __syncthreads();
-    if (group == 0 && c.n) {
-        for (int at = threadIdx.x + lanes; at < kJoinThreads; at += lanes)
+    const Columns<E> c = columns_of<E>(threadIdx.x & (lanes - 1), lanes, blockIdx.y, a.D);
+    // pieces [from, to) of a list, the first one's slot 1, slot 0 of the others
+    const auto add = [&](int chunk, int from, int to, float (&sum)[E::kPer16]) {
+        constexpr int kAhead = 4;
+        const float *row = a.pieces + (w * a.chunks + chunk) * 2 * a.piece_ld + c.first;
+        for (int k0 = from; k0 < to; k0 += kAhead) {
+            float v[kAhead][E::kPer16];
 #pragma unroll
-            for (int j = 0; j < E::kPer16; ++j) sum[j] += lds[j][at];
-        finish<E>(a, c, w, id, sum);
+            for (int i = 0; i < kAhead; ++i) {
+                const int k = k0 + i < to ? k0 + i : to - 1;
+                load_wide(row + (static_cast<int64_t>(k) * 2 + (k == 0)) * a.piece_ld, v[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (k0 + i < to)
+#pragma unroll
+                    for (int j = 0; j < E::kPer16; ++j) sum[j] += v[i][j];
+        }
+    };
+    const auto old = [&](int id) { return a.g_in ? c.raw(a.g_in + place_of(a, w, id)) : u4{}; };
+    const Crossing own = here[group];
+    if (own.pieces > 0 && own.pieces <= kFewPieces && c.n) {
+        float sum[E::kPer16] = {};
+        const u4 g = old(own.id);
+        add(chunk0 + group, 0, own.pieces, sum);
+        finish<E>(a, c, w, own.id, sum, g);
+    }
+    for (int f = 0; f < groups; ++f) {
+        const Crossing list = here[f];
+        if (list.pieces <= kFewPieces) continue;        // the same for the workgroup
+        const int each = (list.pieces + groups - 1) / groups, from = group * each, to = from + each < list.pieces ? from + each : list.pieces;
+        float sum[E::kPer16] = {};
+        if (c.n) add(chunk0 + f, from, to, sum);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < E::kPer16; ++j) lds[j][threadIdx.x] = sum[j];
+        __syncthreads();
+        if (group == 0 && c.n) {
+            for (int at = threadIdx.x + lanes; at < kThreads; at += lanes)
+#pragma unroll
+                for (int j = 0; j < E::kPer16; ++j) sum[j] += lds[j][at];
+            finish<E>(a, c, w, list.id, sum, old(list.id));
+        }
     }
 }
 
@@ -407,7 +461,7 @@ int lookup(const typename E::T *x, int64_t ld, int32_t W, int64_t offset, int32_
 }
 
 struct GradSpace {
-    int64_t named, total, sorted, pieces, bytes, chunks;
+    int64_t named, total, sorted, crossing, pieces, bytes, chunks;
     int piece;
 };
 
@@ -420,8 +474,9 @@ GradSpace grad_space(int32_t W, int64_t N, int32_t V, int32_t D)
     s.named = 0;
     s.total = round_up(W * ceil_div(V, 64) * 8, 256);
     s.sorted = s.total + round_up(W * 4, 256);
-    s.pieces = s.sorted + round_up(W * N * static_cast<int64_t>(sizeof(Sorted)), 256);
-    s.bytes = s.pieces + W * s.chunks * 2 * D * 4;
+    s.crossing = s.sorted + round_up(W * N * static_cast<int64_t>(sizeof(Sorted)), 256);
+    s.pieces = s.crossing + round_up(W * s.chunks * static_cast<int64_t>(sizeof(Crossing)), 256);
+    s.bytes = s.pieces + W * s.chunks * 2 * round_up(D, 8) * 4;
     return s;
 }
 
@@ -448,17 +503,26 @@ int grad(const typename E::T *dout, int64_t ld_dout, const int32_t *tokens, int3
     Sorted *sorted = reinterpret_cast<Sorted *>(base + space.sorted);
     uint64_t *named = reinterpret_cast<uint64_t *>(base + space.named);
     int32_t *total = reinterpret_cast<int32_t *>(base + space.total);
-    GradArgs<E> a{dout, ld_dout, sorted, named, total, reinterpret_cast<float *>(base + space.pieces), g_in ? g_in + offset : nullptr, g_out + offset,
-                  ld, N, V, D, static_cast<int32_t>(space.chunks), 0, scale, lanes_shift<E>(D), space.piece};
+    Crossing *crossing = reinterpret_cast<Crossing *>(base + space.crossing);
+    GradArgs<E> a{dout, ld_dout, sorted, named, total, crossing, reinterpret_cast<float *>(base + space.pieces), g_in ? g_in + offset : nullptr, g_out + offset,
+                  ld, N, round_up(D, 8), V, D, static_cast<int32_t>(space.chunks), 0, scale, lanes_shift<E>(D), space.piece, 0, 1, 1};
     const int groups = kThreads >> a.shift;
-    const unsigned slabs = static_cast<unsigned>(ceil_div(ceil_div(D, E::kPer16), 1 << a.shift));
+    a.slabs = static_cast<int>(ceil_div(ceil_div(D, E::kPer16), 1 << a.shift));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(sort_kernel, dim3(static_cast<unsigned>(ceil_div(V, kBins)), W), dim3(kSortThreads), 0, st, tokens, N, V, sorted, named,
-                       total);
+    hipLaunchKernelGGL(sort_kernel, dim3(static_cast<unsigned>(ceil_div(V, kBins)), W), dim3(kSortThreads), 0, st, tokens, N, V, sorted, named, total,
+                       crossing, space.piece, static_cast<int32_t>(space.chunks));
     if (launched() != CX_OK) return CX_ERR_HIP;
     a.chunk_blocks = static_cast<int32_t>(ceil_div(space.chunks, groups));
-    const int64_t empty_blocks = g_in == g_out ? 0 : ceil_div(V, 64);
-    const dim3 grid(static_cast<unsigned>(a.chunk_blocks + empty_blocks), slabs, W);
+    int64_t fill_blocks = 0;
+    if (g_in != g_out) {
+        // a workgroup to four vectors a thread: short ones keep what is written at a time close together in memory
+        const int64_t words = ceil_div(V, 64);
+        a.fills = static_cast<int>(ceil_div(64 * static_cast<int64_t>(D), E::kPer16 * kThreads * 4));
+        fill_blocks = words * a.fills;
+    }
+    const int64_t sums = static_cast<int64_t>(a.chunk_blocks) * a.slabs;
+    if (sums > 0) a.turn = static_cast<int>((sums + fill_blocks) / sums);
+    const dim3 grid(static_cast<unsigned>(sums + fill_blocks), W);
     const unsigned list_bytes = (groups * a.piece + 2) * sizeof(Sorted);
     if (grid.x > 0) {
         if (g_in == g_out) hipLaunchKernelGGL((grad_kernel<E, true>), grid, dim3(kThreads), list_bytes, st, a);
@@ -466,7 +530,7 @@ int grad(const typename E::T *dout, int64_t ld_dout, const int32_t *tokens, int3
         if (launched() != CX_OK) return CX_ERR_HIP;
     }
     if (space.chunks <= 1) return CX_OK;
-    hipLaunchKernelGGL(join_kernel<E>, dim3(static_cast<unsigned>(space.chunks - 1), slabs, W), dim3(kJoinThreads), 0, st, a);
+    hipLaunchKernelGGL(join_kernel<E>, dim3(static_cast<unsigned>(ceil_div(space.chunks - 1, groups)), a.slabs, W), dim3(kThreads), 0, st, a);
     return launched();
 }
 
