@@ -5,9 +5,9 @@
 //   loss = w_kl tau^2 sum_k q_k (log q_k - log p[id_k])  -  w_ce log p1[label]
 //   dz   = gout (w_kl tau (p - q) + w_ce (p1 - onehot(label)))
 //
-// Bound by memory where the exponentials allow it: a row of logits is read once for its maximum and both sums, and once more, last part
-// first, when its gradient is written; the second reading finds the row in the caches.  q and the label touch K + 1 elements: every
-// element is written with its share of p and p1, and behind a barrier those few are written again with their targets.
+// Bound by memory where the exponentials allow it: loss and gradient together read a row of logits once, into registers, as long as it
+// fits there.  q and the label touch K + 1 elements: every element is written with its share of p and p1, and behind a
+// barrier those few are written again with their targets.
 // Where rows are few, several workgroups share one: part_kernel leaves the parts' statistics in the workspace, and each
 // workgroup of the second launch joins them for itself.
 #include "lm_vocab.hpp"
@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kMaxTeacher = CX_MAX_TEACHER;
 static_assert(kMaxTeacher < kRowThreads, "a thread for every target");
+constexpr int kMostThreads = 1024;
 
 template <class E>
 struct DistillArgs {
@@ -62,71 +63,200 @@ __global__ __launch_bounds__(kRowThreads) void part_kernel(const DistillArgs<E> 
     if (threadIdx.x == 0) a.part_stats[n * a.parts + blockIdx.x] = all;
 }
 
-struct Targets {
-    int id[kMaxTeacher + 1];                            // of the teacher's tokens, then the label; -1: none
-    float q[kMaxTeacher + 1];                           // gout-free weight of the gradient's target: w_kl tau q, w_ce
+struct Targets {                                        // of a row: the teacher's tokens, then the label
+    int id[kMaxTeacher + 1];                            // -1: none
+    float t[kMaxTeacher + 1];                           // t / tau (-inf: none), later log q
+    float z[kMaxTeacher + 1];                           // their logits
+    float q[kMaxTeacher + 1];                           // weight of the gradient's target, without gout: w_kl tau q, w_ce
     float soft, hard, loss;                             // w_kl tau, w_ce if these terms count in this row; the row's loss
 };
 
-// Wavefront 0: targets and, if it is wanted, loss of row n from its statistics.  The loss reads logits of the whole row.
+struct Target {
+    int id;
+    float t;
+};
+
+// The k-th of a row's targets, k <= K, from memory.
 template <class E>
-__device__ __forceinline__ void row_targets(const DistillArgs<E> &a, int64_t n, const Stats &all, bool want_loss, Targets &to)
+__device__ __forceinline__ Target load_target(const DistillArgs<E> &a, int64_t n, int k)
 {
-    constexpr int kEach = kMaxTeacher / kWave;
-    const int lane = threadIdx.x;
-    const typename E::T *z = a.z + n * a.ld;
-    const float inv_tau = 1.0f / a.tau, lowest = -__builtin_inff();
-    float t[kEach], high = lowest;
-    int id[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int k = i * kWave + lane;
-        id[i] = k < a.K ? a.ids[n * a.K + k] : -1;
-        if (id[i] < 0 || id[i] >= a.V) id[i] = -1;
-        t[i] = id[i] >= 0 ? a.t[n * a.K + k] * inv_tau : lowest;
-        high = fmaxf(high, t[i]);
-    }
+    if (k < a.K) return {a.ids[n * a.K + k], a.t[n * a.K + k]};
+    return {k == a.K && a.labels && a.w_ce != 0.0f ? a.labels[n] : -1, 0.0f};
+}
+template <class E>
+__device__ __forceinline__ void keep_target(const DistillArgs<E> &a, int64_t n, int k, Target own, Targets &to)
+{
+    if (k > a.K) return;
+    const bool valid = own.id >= 0 && own.id < a.V;
+    to.id[k] = valid ? own.id : -1;
+    to.t[k] = valid && k < a.K ? own.t / a.tau : -__builtin_inff();
+    to.z[k] = valid ? E::widen(a.z[n * a.ld + own.id]) : 0.0f;
+}
+template <class E>
+__device__ __forceinline__ void keep_others(const DistillArgs<E> &a, int64_t n, Targets &to)
+{
+    for (int k = threadIdx.x + blockDim.x; k <= a.K; k += blockDim.x) keep_target(a, n, k, load_target(a, n, k), to);
+}
+
+// Wavefront 0, behind a barrier: the teacher's distribution, and the loss from the row's statistics.  The row's own logits at
+// the targets count for the loss alone.
+template <class E>
+__device__ __forceinline__ void settle(const DistillArgs<E> &a, const Stats &all, Targets &to)
+{
+    const float lowest = -__builtin_inff();
+    float high = lowest, sum = 0.0f, loss = 0.0f;
+    for (int k = threadIdx.x; k < a.K; k += kWave) high = fmaxf(high, to.t[k]);
 #pragma unroll
     for (int d = kWave / 2; d > 0; d /= 2) high = fmaxf(high, __shfl_xor(high, d));
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) sum += t[i] == lowest ? 0.0f : expf(t[i] - high);
+    for (int k = threadIdx.x; k < a.K; k += kWave) sum += to.t[k] == lowest ? 0.0f : expf(to.t[k] - high);
 #pragma unroll
     for (int d = kWave / 2; d > 0; d /= 2) sum += __shfl_xor(sum, d);
     const bool row = all.s != 0.0f;                     // a row of -inf alone has no distribution: it counts for nothing
     const bool soft = row && a.w_kl != 0.0f && sum != 0.0f;
     const float log_sum = logf(sum), log_s = logf(all.s);
-    float loss = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int k = i * kWave + lane;
-        float q = 0.0f;
-        if (soft && id[i] >= 0 && t[i] != lowest) {
-            const float log_q = t[i] - high - log_sum;
-            q = expf(log_q);
-            if (want_loss && q != 0.0f) loss += q * (log_q - ((E::widen(z[id[i]]) - all.m) * inv_tau - log_s));
-        }
-        if (k < a.K) { to.id[k] = id[i]; to.q[k] = a.w_kl * a.tau * q; }
+    for (int k = threadIdx.x; k < a.K; k += kWave) {
+        const float log_q = to.t[k] - high - log_sum;
+        const float q = soft && to.t[k] != lowest ? expf(log_q) : 0.0f;
+        if (q != 0.0f) loss += q * (log_q - ((to.z[k] - all.m) / a.tau - log_s));
+        to.q[k] = a.w_kl * a.tau * q;
     }
 #pragma unroll
     for (int d = kWave / 2; d > 0; d /= 2) loss += __shfl_xor(loss, d);
-    loss *= soft ? a.w_kl * a.tau * a.tau : 0.0f;
-    if (lane == 0) {
-        int label = a.labels && a.w_ce != 0.0f && row ? a.labels[n] : -1;
-        if (label < 0 || label >= a.V) label = -1;
-        if (!soft) loss = 0.0f;
-        if (want_loss && label >= 0) loss -= a.w_ce * ((E::widen(z[label]) - all.m) - logf(all.u));
-        to.id[a.K] = label;
-        to.q[a.K] = label >= 0 ? a.w_ce : 0.0f;
+    if (threadIdx.x == 0) {
+        const bool hard = row && to.id[a.K] >= 0;
+        loss = soft ? a.w_kl * a.tau * a.tau * loss : 0.0f;
+        if (hard) loss -= a.w_ce * ((to.z[a.K] - all.m) - logf(all.u));
+        to.q[a.K] = hard ? a.w_ce : 0.0f;
         to.soft = soft ? a.w_kl * a.tau : 0.0f;
-        to.hard = label >= 0 ? a.w_ce : 0.0f;
+        to.hard = hard ? a.w_ce : 0.0f;
         to.loss = loss;
     }
 }
 
+// What a row's gradient is made of once its targets are settled: every element's share of p and p1, and the targets'.
+template <class E, Extra X>
+struct RowGradient {
+    float m, c, soft, hard, gout;
+    bool idle;                                          // a row without targets has no gradient, whatever its logits are
+    __device__ __forceinline__ RowGradient(const DistillArgs<E> &a, int64_t n, const Stats &all, const Targets &to)
+        : m(all.m), c(soft_factor(a)), gout(a.gout[n]), idle(to.soft == 0.0f && to.hard == 0.0f)
+    {
+        soft = to.soft == 0.0f ? 0.0f : gout * to.soft / all.s;
+        hard = to.hard == 0.0f ? 0.0f : gout * to.hard / all.u;
+    }
+    __device__ __forceinline__ float share(float z) const
+    {
+        const float d = z - m, e = exp2_fast(d * c);
+        if (X == kDual) return __builtin_fmaf(soft, e, hard * second<X>(d, e, kLog2e));
+        if (X == kSquare) return e * __builtin_fmaf(hard, e, soft);
+        if (X == kFourth) return e * __builtin_fmaf(hard * e, e * e, soft);
+        return (soft + hard) * e;
+    }
+    __device__ __forceinline__ u4 share_of(const u4 &w) const
+    {
+        float v[E::kPer16];
+        E::unpack(w, v);
+#pragma unroll
+        for (int j = 0; j < E::kPer16; ++j) v[j] = share(v[j]);
+        return E::pack(v);
+    }
+    // the targets in [lo, hi), behind a barrier that orders their second writing
+    __device__ __forceinline__ void write_targets(const DistillArgs<E> &a, int64_t n, int64_t lo, int64_t hi, const Targets &to) const
+    {
+        for (int k = threadIdx.x; k <= a.K; k += blockDim.x) {
+            const int id = to.id[k];
+            if (id < lo || id >= hi) continue;
+            float q = 0.0f;
+            for (int i = 0; i <= a.K; ++i) q += to.id[i] == id ? to.q[i] : 0.0f;        // an id may be there twice, and be the label
+            a.dz[n * a.ld_dz + id] = E::narrow(__builtin_fmaf(-gout, q, share(to.z[k])));
+        }
+    }
+};
+
+template <class E>
+__device__ __forceinline__ void write_loss(const DistillArgs<E> &a, int64_t n, const Stats &all, const Targets &to)
+{
+    if (!a.loss) return;
+    a.loss[n] = to.loss;
+    if (a.stats) {
+        a.stats[n * 4] = all.m; a.stats[n * 4 + 1] = all.s; a.stats[n * 4 + 2] = all.u; a.stats[n * 4 + 3] = 0.0f;
+    }
+}
+
+// Keeps the compiler from holding a row's widened values between the passes over it: they would take twice the registers.
+__device__ __forceinline__ void forget_widened(u4 &w) { asm volatile("" : "+v"(w)); }
+
+// Loss and, if it is wanted, gradient of a row that fits the registers of one workgroup, KV vectors to a thread: it is read once.  The caches do
+// not hold the rows of all workgroups, so a second reading would cross the same path as the first and the writing.
+template <class E, Extra X, int KV>
+__global__ __launch_bounds__(kMostThreads, KV > 8 ? 4 : 8) void row_kernel(const DistillArgs<E> a)
+{
+    __shared__ Stats lds[kMostThreads / kWave];
+    __shared__ Targets to;
+    const int64_t n = blockIdx.x;
+    const typename E::T *z = a.z + n * a.ld;
+    const int vectors = static_cast<int>(a.V / E::kPer16), tail = static_cast<int>(a.V % E::kPer16), threads = blockDim.x;
+    const Target own = load_target(a, n, threadIdx.x);
+    // a thread's vector of those that begin at vector `first`: a uniform address and a 32-bit offset
+    const uint32_t mine = threadIdx.x * 16u;
+    const auto place = [&](auto *row, int first) {
+        using P = decltype(row);
+        return reinterpret_cast<P>(reinterpret_cast<std::conditional_t<std::is_const_v<std::remove_pointer_t<P>>, const char, char> *>(row) +
+                                   static_cast<int64_t>(first) * 16 + mine);
+    };
+    u4 w[KV];
+#pragma unroll
+    for (int k = 0; k < KV; ++k) {
+        w[k] = u4{E::kNothing, E::kNothing, E::kNothing, E::kNothing};
+        if (k * threads + static_cast<int>(threadIdx.x) < vectors) w[k] = load16<E>(place(z, k * threads));
+    }
+    const bool has_tail = static_cast<int>(threadIdx.x) < tail;
+    const float z_tail = has_tail ? E::widen(z[static_cast<int64_t>(vectors) * E::kPer16 + threadIdx.x]) : -__builtin_inff();
+    keep_target(a, n, threadIdx.x, own, to);
+    keep_others(a, n, to);
+    const float c = soft_factor(a);
+    Stats all{kLowest, 0.0f, 0.0f};
+    {
+        float high[2] = {z_tail, z_tail};
+#pragma unroll
+        for (int k = 0; k < KV; ++k) {
+            float v[E::kPer16];
+            E::unpack(w[k], v);
+#pragma unroll
+            for (int j = 0; j < E::kPer16; ++j) high[j & 1] = fmaxf(high[j & 1], v[j]);
+        }
+        all.m = fmaxf(all.m, fmaxf(high[0], high[1]));
+    }
+#pragma unroll
+    for (int k = 0; k < KV; ++k) {
+        float v[E::kPer16];
+        forget_widened(w[k]);
+        E::unpack(w[k], v);
+        add_terms<X>(all, v, c, kLog2e);
+    }
+    const float last[1] = {z_tail};
+    add_terms<X>(all, last, c, kLog2e);
+    all = join_workgroup<X>(all, lds, c, kLog2e, threads / kWave);
+    if (!two_sums(X)) all.u = all.s;                    // one sum serves both
+    if (threadIdx.x < kWave) settle(a, all, to);
+    __syncthreads();
+    if (threadIdx.x == 0) write_loss(a, n, all, to);
+    if (!a.dz) return;
+    const RowGradient<E, X> gradient(a, n, all, to);
+    typename E::T *dz = a.dz + n * a.ld_dz;
+#pragma unroll
+    for (int k = 0; k < KV; ++k) {
+        forget_widened(w[k]);
+        if (k * threads + static_cast<int>(threadIdx.x) < vectors) store16<E>(place(dz, k * threads), gradient.idle ? u4{} : gradient.share_of(w[k]));
+    }
+    if (has_tail) dz[static_cast<int64_t>(vectors) * E::kPer16 + threadIdx.x] = gradient.idle ? E::narrow(0.0f) : E::narrow(gradient.share(z_tail));
+    __syncthreads();
+    if (!gradient.idle) gradient.write_targets(a, n, 0, a.V, to);
+}
+
 enum Source { kHere, kParts, kSaved };                  // where a row's statistics come from
 
-// Grid (parts, N).  kHere: one part.
+// Grid (parts, N).  kHere: one part, read a second time for the gradient, its end first: what the caches still hold.
 template <class E, Extra X, Source FROM>
 __global__ __launch_bounds__(kRowThreads) void distill_kernel(const DistillArgs<E> a)
 {
@@ -135,68 +265,36 @@ __global__ __launch_bounds__(kRowThreads) void distill_kernel(const DistillArgs<
     const int part = FROM == kHere ? 0 : blockIdx.x, parts = FROM == kHere ? 1 : a.parts;
     const int64_t n = blockIdx.y, lo = part_begin(a.V, parts, part, E::kPer16), hi = part_begin(a.V, parts, part + 1, E::kPer16);
     const Slice<E> slice(a.z + n * a.ld, lo, hi);
-    const float c = soft_factor(a);
+    keep_target(a, n, threadIdx.x, load_target(a, n, threadIdx.x), to);
     Stats all;
     if constexpr (FROM == kHere) {
-        all = slice_stats<E, X>(slice, c, lds);
+        all = slice_stats<E, X>(slice, soft_factor(a), lds);
     } else if constexpr (FROM == kParts) {
         all = a.part_stats[n * parts];
-        for (int k = 1; k < parts; ++k) all = join<X>(all, a.part_stats[n * parts + k], c, kLog2e);
+        for (int k = 1; k < parts; ++k) all = join<X>(all, a.part_stats[n * parts + k], soft_factor(a), kLog2e);
     } else {
         all = {a.stats[n * 4], a.stats[n * 4 + 1], a.stats[n * 4 + 2]};
     }
-    if (FROM != kSaved && !two_sums(X)) all.u = all.s;    // one sum serves both
-    if (threadIdx.x < kWave) {
-        const bool want_loss = FROM != kSaved && part == 0 && a.loss;
-        row_targets<E>(a, n, all, want_loss, to);
-        if (want_loss && threadIdx.x == 0) {
-            a.loss[n] = to.loss;
-            if (a.stats) {
-                a.stats[n * 4] = all.m; a.stats[n * 4 + 1] = all.s; a.stats[n * 4 + 2] = all.u; a.stats[n * 4 + 3] = 0.0f;
-            }
-        }
-    }
+    if (FROM != kSaved && !two_sums(X)) all.u = all.s;
+    __syncthreads();
+    if (threadIdx.x < kWave) settle(a, all, to);
+    __syncthreads();
+    if (FROM != kSaved && part == 0 && threadIdx.x == 0) write_loss(a, n, all, to);
     if (!a.dz) return;
-    __syncthreads();
-    // the few elements that have a target: their logits before anything is written (dz may be z)
-    const int k = threadIdx.x;
-    const int id = k <= a.K ? to.id[k] : -1;
-    const bool target = id >= lo && id < hi;
-    float z_target = 0.0f, q = 0.0f;
-    if (target) {
-        z_target = E::widen(a.z[n * a.ld + id]);
-        for (int i = 0; i <= a.K; ++i) q += to.id[i] == id ? to.q[i] : 0.0f;
-    }
-    __syncthreads();
-    const float gout = a.gout[n], soft = to.soft == 0.0f ? 0.0f : gout * to.soft / all.s, hard = to.hard == 0.0f ? 0.0f : gout * to.hard / all.u;
-    const auto share = [&](float z) {
-        const float d = z - all.m, e = exp2_fast(d * c);
-        if (X == kDual) return __builtin_fmaf(soft, e, hard * second<X>(d, e, kLog2e));
-        if (X == kSquare) return e * __builtin_fmaf(hard, e, soft);
-        if (X == kFourth) return e * __builtin_fmaf(hard * e, e * e, soft);
-        return (soft + hard) * e;
-    };
+    const RowGradient<E, X> gradient(a, n, all, to);
     typename E::T *dz = a.dz + n * a.ld_dz + lo;
-    if (to.soft == 0.0f && to.hard == 0.0f) {           // a row without targets has no gradient, whatever its logits are
-        if (slice.has_tail()) dz[slice.tail_at()] = E::narrow(0.0f);
-        for (int at = threadIdx.x; at < slice.vectors; at += kRowThreads) store16<E>(dz + static_cast<int64_t>(at) * E::kPer16, u4{});
-        return;
-    }
-    if (slice.has_tail()) dz[slice.tail_at()] = E::narrow(share(E::widen(slice.z[slice.tail_at()])));
+    if (slice.has_tail()) dz[slice.tail_at()] = gradient.idle ? E::narrow(0.0f) : E::narrow(gradient.share(E::widen(slice.z[slice.tail_at()])));
     for (int round = slice.rounds() - 1; round >= 0; --round) {
-        float v[kAhead * E::kPer16];
-        slice.load(round, v);
+        u4 w[kAhead];
+        slice.load(round, w);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            float g[E::kPer16];
-#pragma unroll
-            for (int j = 0; j < E::kPer16; ++j) g[j] = share(v[i * E::kPer16 + j]);
             const int at = slice.vector_of(round, i);
-            if (at < slice.vectors) store16<E>(dz + static_cast<int64_t>(at) * E::kPer16, E::pack(g));
+            if (at < slice.vectors) store16<E>(dz + static_cast<int64_t>(at) * E::kPer16, gradient.idle ? u4{} : gradient.share_of(w[i]));
         }
     }
     __syncthreads();
-    if (target) dz[id - lo] = E::narrow(__builtin_fmaf(-gout, q, share(z_target)));
+    if (!gradient.idle) gradient.write_targets(a, n, lo, hi, to);
 }
 
 struct DistillSpace {
@@ -267,7 +365,12 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
             if (from_saved) {
                 hipLaunchKernelGGL((distill_kernel<E, X, kSaved>), parted, block, 0, st, b);
             } else if (space.parts == 1) {
-                hipLaunchKernelGGL((distill_kernel<E, X, kHere>), whole, block, 0, st, b);
+                const int64_t vectors = a.V / E::kPer16;
+                const auto threads = [&](int64_t each) { return dim3(static_cast<unsigned>(vectors < each ? kWave : round_up(ceil_div(vectors, each), kWave))); };
+                if (vectors > 16 * kMostThreads) hipLaunchKernelGGL((distill_kernel<E, X, kHere>), whole, block, 0, st, b);
+                else if (vectors > 8 * kMostThreads) hipLaunchKernelGGL((row_kernel<E, X, 16>), dim3(rows), threads(16), 0, st, b);
+                else if (vectors > 4 * kMostThreads) hipLaunchKernelGGL((row_kernel<E, X, 8>), dim3(rows), threads(8), 0, st, b);
+                else hipLaunchKernelGGL((row_kernel<E, X, 4>), dim3(rows), threads(4), 0, st, b);
             } else {                                    // few rows: one slice of them
                 hipLaunchKernelGGL((part_kernel<E, X>), parted, block, 0, st, b);
                 if (want_dz && static_cast<const void *>(a.dz) == a.z) {

@@ -28,6 +28,7 @@ struct F32 {
     using T = float;
     using Vec = u4_at4;
     static constexpr int kPer16 = 4;
+    static constexpr unsigned kNothing = 0xff800000u;      // -inf, as often as a word holds it
     static __device__ __forceinline__ float widen(T v) { return v; }
     static __device__ __forceinline__ T narrow(float v) { return v; }
     static __device__ __forceinline__ void unpack(const u4 &w, float (&out)[4])
@@ -45,6 +46,7 @@ struct Bf16 {
     using T = uint16_t;
     using Vec = u4_at2;
     static constexpr int kPer16 = 8;
+    static constexpr unsigned kNothing = 0xff80ff80u;
     typedef __bf16 pair __attribute__((ext_vector_type(2)));
     typedef float f2 __attribute__((ext_vector_type(2)));
     static __device__ __forceinline__ float widen(T v) { return __uint_as_float(static_cast<unsigned>(v) << 16); }
@@ -70,6 +72,7 @@ struct F16 {
     using T = uint16_t;
     using Vec = u4_at2;
     static constexpr int kPer16 = 8;
+    static constexpr unsigned kNothing = 0xfc00fc00u;
     static __device__ __forceinline__ float widen(T v) { return static_cast<float>(__builtin_bit_cast(_Float16, v)); }
     static __device__ __forceinline__ float low(unsigned w) { return widen(static_cast<T>(w)); }
     static __device__ __forceinline__ float high(unsigned w) { return widen(static_cast<T>(w >> 16)); }

@@ -55,13 +55,10 @@ __device__ __forceinline__ Stats join(Stats a, Stats b, float c, float c2)
     return {m, a.s + b.s, a.u + b.u};
 }
 
+// Terms of elements that a.m is the maximum of already.
 template <Extra X, int N>
-__device__ __forceinline__ float accumulate(Stats &a, const float (&z)[N], float c, float c2)
+__device__ __forceinline__ void add_terms(Stats &a, const float (&z)[N], float c, float c2)
 {
-    float top = z[0];
-#pragma unroll
-    for (int j = 1; j < N; ++j) top = fmaxf(top, z[j]);
-    rebase<X>(a, fmaxf(a.m, top), c, c2);
     float s[2] = {}, u[2] = {};
 #pragma unroll
     for (int j = 0; j < N; ++j) {
@@ -72,12 +69,22 @@ __device__ __forceinline__ float accumulate(Stats &a, const float (&z)[N], float
     }
     a.s += s[0] + s[1];
     a.u += u[0] + u[1];
+}
+
+template <Extra X, int N>
+__device__ __forceinline__ float accumulate(Stats &a, const float (&z)[N], float c, float c2)
+{
+    float top = z[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) top = fmaxf(top, z[j]);
+    rebase<X>(a, fmaxf(a.m, top), c, c2);
+    add_terms<X>(a, z, c, c2);
     return top;
 }
 
 // The statistics of all threads of the workgroup, in every thread.
-template <Extra X>
-__device__ __forceinline__ Stats join_workgroup(Stats a, Stats (&lds)[kRowWaves], float c, float c2)
+template <Extra X, int WAVES>
+__device__ __forceinline__ Stats join_workgroup(Stats a, Stats (&lds)[WAVES], float c, float c2, int waves = WAVES)
 {
 #pragma unroll
     for (int d = kWave / 2; d > 0; d /= 2)
@@ -85,8 +92,7 @@ __device__ __forceinline__ Stats join_workgroup(Stats a, Stats (&lds)[kRowWaves]
     if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = a;
     __syncthreads();
     a = lds[0];
-#pragma unroll
-    for (int k = 1; k < kRowWaves; ++k) a = join<X>(a, lds[k], c, c2);
+    for (int k = 1; k < waves; ++k) a = join<X>(a, lds[k], c, c2);
     return a;
 }
 
@@ -101,27 +107,25 @@ struct Slice {
     __device__ __forceinline__ int rounds() const { return (vectors + kRowThreads * kAhead - 1) / (kRowThreads * kAhead); }
     static __device__ __forceinline__ int vector_of(int round, int k) { return (round * kAhead + k) * kRowThreads + static_cast<int>(threadIdx.x); }
     // the thread's kAhead vectors of a round; what lies beyond the slice counts as -inf
-    __device__ __forceinline__ void load(int round, float (&v)[kAhead * E::kPer16]) const
+    __device__ __forceinline__ void load(int round, u4 (&w)[kAhead]) const
     {
-        u4 w[kAhead];
         if ((round + 1) * kAhead * kRowThreads <= vectors) {
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) w[k] = load16<E>(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) unpack(w[k], v, k);
         } else {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k)
-                if (vector_of(round, k) < vectors) w[k] = load16<E>(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
-                else w[k] = u4{};
-#pragma unroll
             for (int k = 0; k < kAhead; ++k) {
-                unpack(w[k], v, k);
-                if (vector_of(round, k) >= vectors)
-#pragma unroll
-                    for (int j = 0; j < E::kPer16; ++j) v[k * E::kPer16 + j] = -__builtin_inff();
+                w[k] = u4{E::kNothing, E::kNothing, E::kNothing, E::kNothing};
+                if (vector_of(round, k) < vectors) w[k] = load16<E>(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
             }
         }
+    }
+    __device__ __forceinline__ void load(int round, float (&v)[kAhead * E::kPer16]) const
+    {
+        u4 w[kAhead];
+        load(round, w);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) unpack(w[k], v, k);
     }
     static __device__ __forceinline__ void unpack(const u4 &w, float (&v)[kAhead * E::kPer16], int k)
     {
