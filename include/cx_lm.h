@@ -94,7 +94,8 @@ int cx_embed_grad_f16(const uint16_t *dout, int64_t ld_dout, const int32_t *toke
  *   h_last   float [B][D] or NULL: receives the state after the last one; may be h0 (generation: T = 1, state in place)
  *   states   float [B][ceil(T / CX_SCAN_CHUNK)][D] or NULL: receives the state that enters every CX_SCAN_CHUNK-th step, which
  *            the gradient needs
- * Long sequences are computed as compositions of affine maps, so an infinite state may turn into a NaN.
+ * Long sequences are computed as compositions of affine maps, so an infinite state may turn into a NaN.  Sequences of no more than
+ * CX_SCAN_CHUNK steps need no workspace.
  */
 int cx_scan_workspace(int64_t B, int64_t T, int32_t D, int64_t *bytes);
 int cx_gated_scan(const float *f, int64_t ldf, const float *x, int64_t ldx, float *y, int64_t ldy, int64_t B, int64_t T,

@@ -302,9 +302,18 @@ struct DistillSpace {
     int64_t bytes;
 };
 
+// The gradient alone needs nothing of a row but its statistics: as many workgroups to a row as give a CU two.
+int grad_parts(int64_t N, int64_t V, int per16)
+{
+    const int64_t fit = ceil_div(V, static_cast<int64_t>(kRowThreads) * per16 * 2), wanted = ceil_div(512, N);
+    return static_cast<int>(N >= 512 ? 1 : fit < wanted ? fit : wanted);
+}
+
+constexpr int64_t kRegisterVectors = 16 * kMostThreads;         // of a row that one workgroup's registers hold
+
 DistillSpace distill_space(int64_t N, int64_t V, int per16)
 {
-    const int parts = parts_of(N, V, per16);
+    const int parts = V / per16 > kRegisterVectors ? parts_of(N, V, per16) : 1;
     return {parts, parts > 1 ? N * parts * static_cast<int64_t>(sizeof(Stats)) : 0};
 }
 
@@ -323,7 +332,8 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
     if (N == 0) return CX_OK;
     if (!a.z || (a.K > 0 && (!a.ids || !a.t)) || (want_dz && (!a.dz || !a.gout)) || (!from_saved && !a.loss) || (from_saved && !a.stats)) return CX_ERR_NULL;
     if (bad_matrix(N, a.ld, a.V) || (want_dz && bad_matrix(N, a.ld_dz, a.V))) return CX_ERR_SHAPE;
-    const DistillSpace space = distill_space(N, a.V, E::kPer16);
+    DistillSpace space = distill_space(N, a.V, E::kPer16);
+    if (from_saved) space.parts = grad_parts(N, a.V, E::kPer16);
     const int64_t need = from_saved ? 0 : space.bytes;
     if (need > 0 && !workspace) return CX_ERR_NULL;
     if (need > 0 && workspace_bytes < need) return CX_ERR_SHAPE;
@@ -367,7 +377,7 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
             } else if (space.parts == 1) {
                 const int64_t vectors = a.V / E::kPer16;
                 const auto threads = [&](int64_t each) { return dim3(static_cast<unsigned>(vectors < each ? kWave : round_up(ceil_div(vectors, each), kWave))); };
-                if (vectors > 16 * kMostThreads) hipLaunchKernelGGL((distill_kernel<E, X, kHere>), whole, block, 0, st, b);
+                if (vectors > kRegisterVectors) hipLaunchKernelGGL((distill_kernel<E, X, kHere>), whole, block, 0, st, b);
                 else if (vectors > 8 * kMostThreads) hipLaunchKernelGGL((row_kernel<E, X, 16>), dim3(rows), threads(16), 0, st, b);
                 else if (vectors > 4 * kMostThreads) hipLaunchKernelGGL((row_kernel<E, X, 8>), dim3(rows), threads(8), 0, st, b);
                 else hipLaunchKernelGGL((row_kernel<E, X, 4>), dim3(rows), threads(4), 0, st, b);

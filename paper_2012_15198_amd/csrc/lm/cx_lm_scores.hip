@@ -15,8 +15,7 @@ namespace {
 
 constexpr int kMaxTop = CX_MAX_TOP;
 constexpr int kGroups = 4;                              // subsets of a thread
-constexpr int kRoundKeys = 1024;                        // elements looked at between two checks of the list's length
-constexpr int kList = 2048 + kMaxTop;
+constexpr int kTurnKeys = 1024;                         // elements looked at between two checks of the list's length, at most
 constexpr int kRankable = 256;                          // a list of this length is ranked by counting, a longer one cut to K first
 
 typedef unsigned long long Key;
@@ -35,61 +34,65 @@ __device__ __forceinline__ float value_of(Key key)
 __device__ __forceinline__ Key key_of(float v, int64_t id) { return static_cast<Key>(ordered(v)) << 32 | (0xffffffffu - static_cast<unsigned>(id)); }
 __device__ __forceinline__ int id_of(Key key) { return static_cast<int>(0xffffffffu - static_cast<unsigned>(key)); }
 
+template <int THREADS>
 struct TopSpace {
+    static constexpr int kTurn = THREADS * 8 < kTurnKeys ? THREADS * 8 : kTurnKeys, kList = 2 * kTurn + kMaxTop;
     union {
-        float maxima[kGroups][kRowThreads];             // first pass
+        float maxima[kGroups][THREADS];                 // first pass
         Key list[kList];                                // second
     };
-    uint16_t subsets[kGroups * kRowThreads];
+    uint16_t subsets[kGroups * THREADS];
     Key kept[kMaxTop];
+    int reach[2][THREADS / kWave];
     Key least;                                          // keys below it are out
     unsigned count, subset_count;
 };
 
-// One wavefront: the largest key of which the list holds at least K that reach it (K <= count: the K-th largest).
-__device__ Key kth_largest(const Key *list, unsigned count, int K)
-{
-    const unsigned lane = threadIdx.x & (kWave - 1);
-    Key found = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-        const Key probe = found | (1ull << bit);
-        int reach = 0;
-        for (unsigned i = 0; i < count; i += kWave) reach += __popcll(__ballot(i + lane < count && list[i + lane] >= probe));
-        if (reach >= K) found = probe;
-    }
-    return found;
-}
-
 // Cuts the list to its K largest keys and raises `least`.  All threads, after a barrier; count > K.
-__device__ void cut_list(TopSpace &s, int K)
+template <int THREADS>
+__device__ void cut_list(TopSpace<THREADS> &s, int K)
 {
+    constexpr int kEach = (TopSpace<THREADS>::kList + THREADS - 1) / THREADS, kWaves = THREADS / kWave;
     const unsigned count = s.count;
-    __syncthreads();                                    // everyone has read it
-    if (threadIdx.x < kWave) {
-        const Key kth = kth_largest(s.list, count, K);
-        if (threadIdx.x == 0) { s.least = kth; s.count = 0; }
+    Key own[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) own[i] = i * THREADS + threadIdx.x < count ? s.list[i * THREADS + threadIdx.x] : 0;
+    Key kth = 0;                                        // the K-th largest, bit after bit
+#pragma unroll 1
+    for (int bit = 63; bit >= 0; --bit) {
+        const Key probe = kth | (1ull << bit);
+        int reach = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) reach += __popcll(__ballot(own[i] >= probe));
+        if (kWaves > 1) {
+            if ((threadIdx.x & (kWave - 1)) == 0) s.reach[bit & 1][threadIdx.x / kWave] = reach;
+            __syncthreads();
+            reach = 0;
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) reach += s.reach[bit & 1][k];
+        }
+        if (reach >= K) kth = probe;
     }
+    __syncthreads();                                    // everyone has the list in registers and the count read
+    if (threadIdx.x == 0) { s.least = kth + 1; s.count = 0; }           // keys are unique: those that follow have to beat the K-th
     __syncthreads();
-    const Key least = s.least;
-    for (unsigned i = threadIdx.x; i < count; i += blockDim.x)
-        if (s.list[i] >= least) s.kept[atomicAdd(&s.count, 1u)] = s.list[i];
-    __syncthreads();
-    for (unsigned i = threadIdx.x; i < s.count; i += blockDim.x) s.list[i] = s.kept[i];
-    __syncthreads();
-    if (threadIdx.x == 0) s.least = least + 1;          // keys are unique: those that follow have to beat the K-th
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        if (own[i] >= kth && own[i]) s.list[atomicAdd(&s.count, 1u)] = own[i];
     __syncthreads();
 }
 
 // The K largest keys of the list to kept[], the largest first; absent ones are 0.  All threads.
-__device__ void rank_list(TopSpace &s, int K)
+template <int THREADS>
+__device__ void rank_list(TopSpace<THREADS> &s, int K)
 {
     __syncthreads();
     if (s.count > kRankable) cut_list(s, K);
     const unsigned count = s.count;
     if (static_cast<int>(threadIdx.x) < K) s.kept[threadIdx.x] = 0;
     __syncthreads();
-    if (threadIdx.x < count) {
-        const Key mine = s.list[threadIdx.x];
+    for (unsigned at = threadIdx.x; at < count; at += THREADS) {
+        const Key mine = s.list[at];
         int rank = 0;
         for (unsigned i = 0; i < count; ++i) rank += s.list[i] > mine;
         if (rank < K) s.kept[rank] = mine;
@@ -98,15 +101,15 @@ __device__ void rank_list(TopSpace &s, int K)
 }
 
 // The K largest keys of a slice, after the first pass has noted the maxima.  `rounds_each` rounds make a subset.
-template <class E>
-__device__ void top_of_slice(TopSpace &s, const Slice<E> &slice, int64_t lo, int rounds_each, int K)
+template <class E, int THREADS>
+__device__ void top_of_slice(TopSpace<THREADS> &s, const Slice<E, THREADS> &slice, int64_t lo, int rounds_each, int K)
 {
     __syncthreads();
     // wavefront 0: the largest 16-bit prefix of a value that the maxima of K threads reach
     if (threadIdx.x < kWave) {
-        unsigned own[kRowWaves];
+        unsigned own[THREADS / kWave];
 #pragma unroll
-        for (int k = 0; k < kRowWaves; ++k) {
+        for (int k = 0; k < THREADS / kWave; ++k) {
             float top = s.maxima[0][k * kWave + threadIdx.x];
 #pragma unroll
             for (int g = 1; g < kGroups; ++g) top = fmaxf(top, s.maxima[g][k * kWave + threadIdx.x]);
@@ -118,7 +121,7 @@ __device__ void top_of_slice(TopSpace &s, const Slice<E> &slice, int64_t lo, int
             const unsigned probe = prefix | (1u << bit);
             int reach = 0;
 #pragma unroll
-            for (int k = 0; k < kRowWaves; ++k) reach += __popcll(__ballot(own[k] >= probe));
+            for (int k = 0; k < THREADS / kWave; ++k) reach += __popcll(__ballot(own[k] >= probe));
             if (reach >= K) prefix = probe;
         }
         if (threadIdx.x == 0) { s.least = static_cast<Key>(prefix) << 48; s.subset_count = 0; }
@@ -128,8 +131,8 @@ __device__ void top_of_slice(TopSpace &s, const Slice<E> &slice, int64_t lo, int
     const int each = rounds_each * kAhead;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
-        if (g * each * kRowThreads + static_cast<int>(threadIdx.x) < slice.vectors && ordered(s.maxima[g][threadIdx.x]) >> 16 >= prefix)
-            s.subsets[atomicAdd(&s.subset_count, 1u)] = static_cast<uint16_t>(g * kRowThreads + threadIdx.x);
+        if (g * each * THREADS + static_cast<int>(threadIdx.x) < slice.vectors && ordered(s.maxima[g][threadIdx.x]) >> 16 >= prefix)
+            s.subsets[atomicAdd(&s.subset_count, 1u)] = static_cast<uint16_t>(g * THREADS + threadIdx.x);
     if (threadIdx.x == 0) s.count = 0;
     __syncthreads();                                    // the maxima are dead from here on: their place is the list's
     const auto offer = [&](float v, int64_t at, Key least) {
@@ -138,17 +141,17 @@ __device__ void top_of_slice(TopSpace &s, const Slice<E> &slice, int64_t lo, int
     };
     if (slice.has_tail()) offer(E::widen(slice.z[slice.tail_at()]), slice.tail_at(), s.least);
     const int pieces = static_cast<int>(s.subset_count) * each;
-    constexpr int kPieces = kRoundKeys / E::kPer16;     // vectors looked at in a turn
+    constexpr int kTurn = TopSpace<THREADS>::kTurn, kPieces = kTurn / E::kPer16 < THREADS ? kTurn / E::kPer16 : THREADS;      // vectors looked at in a turn
     for (int p0 = 0; p0 < pieces; p0 += kPieces) {
         __syncthreads();
-        if (s.count + kRoundKeys > kList) cut_list(s, K);
+        if (s.count + kTurn > TopSpace<THREADS>::kList) cut_list(s, K);
         __syncthreads();
         const Key least = s.least;
         const int p = p0 + static_cast<int>(threadIdx.x);
         if (static_cast<int>(threadIdx.x) < kPieces && p < pieces) {
             const unsigned subset = s.subsets[p / each];
-            const int in = p % each, group = subset / kRowThreads, thread = subset % kRowThreads;
-            const int q = (group * each + in) * kRowThreads + thread;
+            const int in = p % each, group = subset / THREADS, thread = subset % THREADS;
+            const int q = (group * each + in) * THREADS + thread;
             if (q < slice.vectors) {
                 float v[E::kPer16];
                 E::unpack(load16<E>(slice.z + static_cast<int64_t>(q) * E::kPer16), v);
@@ -197,14 +200,14 @@ __device__ __forceinline__ void write_row(const ScoreArgs<E> &a, int64_t n, cons
 }
 
 // Grid (parts, N): one part of one row.
-template <class E, bool TOP>
-__global__ __launch_bounds__(kRowThreads) void scores_kernel(const ScoreArgs<E> a)
+template <class E, bool TOP, int THREADS>
+__global__ __launch_bounds__(THREADS) void scores_kernel(const ScoreArgs<E> a)
 {
-    __shared__ Stats lds[kRowWaves];
-    __shared__ TopSpace top;
+    __shared__ Stats lds[THREADS / kWave];
+    __shared__ TopSpace<THREADS> top;
     const int part = blockIdx.x;
     const int64_t n = blockIdx.y, lo = part_begin(a.V, a.parts, part, E::kPer16), hi = part_begin(a.V, a.parts, part + 1, E::kPer16);
-    const Slice<E> slice(a.z + n * a.ld, lo, hi);
+    const Slice<E, THREADS> slice(a.z + n * a.ld, lo, hi);
     const float c = a.scale * kLog2e;
     const int rounds = slice.rounds(), rounds_each = (rounds + kGroups - 1) / kGroups;
     Stats own{kLowest, 0.0f, 0.0f};
@@ -222,7 +225,7 @@ __global__ __launch_bounds__(kRowThreads) void scores_kernel(const ScoreArgs<E> 
         accumulate<kEntropy>(own, v, c, 0.0f);
     }
     const Stats all = join_workgroup<kEntropy>(own, lds, c, 0.0f);
-    if (TOP) top_of_slice<E>(top, slice, lo, rounds_each, a.K);
+    if (TOP) top_of_slice<E, THREADS>(top, slice, lo, rounds_each, a.K);
     if (a.parts == 1) {
         write_row<E>(a, n, all, top.kept);
     } else {
@@ -234,23 +237,26 @@ __global__ __launch_bounds__(kRowThreads) void scores_kernel(const ScoreArgs<E> 
 template <class E, bool TOP>
 __global__ __launch_bounds__(kRowThreads) void join_kernel(const ScoreArgs<E> a)
 {
-    __shared__ TopSpace top;
+    __shared__ TopSpace<kRowThreads> top;
     const int64_t n = blockIdx.x;
     const float c = a.scale * kLog2e;
     Stats all = a.part_stats[n * a.parts];
     for (int k = 1; k < a.parts; ++k) all = join<kEntropy>(all, a.part_stats[n * a.parts + k], c, 0.0f);
     if (TOP) {
-        // each part's K-th key is reached by K keys: the largest of them leaves little more than K
+        // K keys reach a part's K-th one, and K keys reach the least of all parts' (K / parts)-th ones: the larger bound leaves little more than K
         const Key *keys = a.part_keys + n * a.parts * a.K;
         if (threadIdx.x == 0) top.count = 0;
         if (threadIdx.x < kWave) {
-            Key least = static_cast<int>(threadIdx.x) < a.parts ? keys[(threadIdx.x + 1) * a.K - 1] : 0;
+            const bool here = static_cast<int>(threadIdx.x) < a.parts;
+            const int share = (a.K + a.parts - 1) / a.parts;
+            Key most = here ? keys[(threadIdx.x + 1) * a.K - 1] : 0, least = here ? keys[threadIdx.x * a.K + share - 1] : ~0ull;
 #pragma unroll
             for (int d = kWave / 2; d > 0; d /= 2) {
-                const Key other = __shfl_xor(least, d);
-                least = other > least ? other : least;
+                const Key m = __shfl_xor(most, d), l = __shfl_xor(least, d);
+                most = m > most ? m : most;
+                least = l < least ? l : least;
             }
-            if (threadIdx.x == 0) top.least = least;
+            if (threadIdx.x == 0) top.least = most > least ? most : least;
         }
         __syncthreads();
         for (int i = threadIdx.x; i < a.parts * a.K; i += kRowThreads) {
@@ -319,8 +325,17 @@ int scores(const typename E::T *z, int64_t ld, int64_t N, int32_t V, const int32
         if (b.logp) b.logp += n0;
         if (b.entropy) b.entropy += n0;
         if (K > 0) { b.top_ids += n0 * K; b.top_logp += n0 * K; }
-        if (K > 0) hipLaunchKernelGGL((scores_kernel<E, true>), dim3(space.parts, rows), dim3(kRowThreads), 0, st, b);
-        else hipLaunchKernelGGL((scores_kernel<E, false>), dim3(space.parts, rows), dim3(kRowThreads), 0, st, b);
+        const auto launch = [&](auto size) {
+            constexpr int THREADS = decltype(size)::value;
+            if (K > 0) hipLaunchKernelGGL((scores_kernel<E, true, THREADS>), dim3(space.parts, rows), dim3(THREADS), 0, st, b);
+            else hipLaunchKernelGGL((scores_kernel<E, false, THREADS>), dim3(space.parts, rows), dim3(THREADS), 0, st, b);
+        };
+        // threads of a row by its length: 8,192 rows of 1,000 bfloat16 logits take 37 us with 256 each and 75 with 512, 4,096 rows of 50,003
+        // 106 and 109, 2,048 rows of 262,144 219 and 204; with 1,024 all but the longest rows take twice as long
+        const int64_t vectors = ceil_div(V / space.parts, E::kPer16);
+        if (vectors <= 512) launch(std::integral_constant<int, 64>{});
+        else if (vectors <= 8192) launch(std::integral_constant<int, 256>{});
+        else launch(std::integral_constant<int, 512>{});
         if (launched() != CX_OK) return CX_ERR_HIP;
     }
     if (space.parts == 1) return CX_OK;                 // split rows are few: one slice

@@ -98,18 +98,18 @@ __device__ __forceinline__ Stats join_workgroup(Stats a, Stats (&lds)[WAVES], fl
 
 // A slice of a row: `vectors` whole 16-byte vectors from its first element on (which need not be aligned to more than an
 // element), then `tail` elements.
-template <class E>
+template <class E, int THREADS = kRowThreads>
 struct Slice {
     const typename E::T *z;
     int vectors, tail;
     __device__ __forceinline__ Slice(const typename E::T *row, int64_t lo, int64_t hi)
         : z(row + lo), vectors(static_cast<int>((hi - lo) / E::kPer16)), tail(static_cast<int>((hi - lo) % E::kPer16)) {}
-    __device__ __forceinline__ int rounds() const { return (vectors + kRowThreads * kAhead - 1) / (kRowThreads * kAhead); }
-    static __device__ __forceinline__ int vector_of(int round, int k) { return (round * kAhead + k) * kRowThreads + static_cast<int>(threadIdx.x); }
+    __device__ __forceinline__ int rounds() const { return (vectors + THREADS * kAhead - 1) / (THREADS * kAhead); }
+    static __device__ __forceinline__ int vector_of(int round, int k) { return (round * kAhead + k) * THREADS + static_cast<int>(threadIdx.x); }
     // the thread's kAhead vectors of a round; what lies beyond the slice counts as -inf
     __device__ __forceinline__ void load(int round, u4 (&w)[kAhead]) const
     {
-        if ((round + 1) * kAhead * kRowThreads <= vectors) {
+        if ((round + 1) * kAhead * THREADS <= vectors) {
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) w[k] = load16<E>(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
         } else {
@@ -138,14 +138,16 @@ struct Slice {
     __device__ __forceinline__ int64_t tail_at() const { return static_cast<int64_t>(vectors) * E::kPer16 + threadIdx.x; }
 };
 
-// How many workgroups share a row: where rows alone leave CUs idle, as many as give each CU two, and no part shorter than
-// a workgroup's first loads.
+// How many workgroups share a row.  One, up to 8,192 vectors (128 KB): 128 rows of 65,536 bfloat16 logits take 13 us whole and 15 in
+// four parts with their join, one row of 32,768 9 and 10.  Longer ones are cut where rows are few, into parts of 2,048 vectors and
+// no more than give a CU two: one row of 131,072 12.6 us in eight parts, 18 whole; 64 such rows 15 in four parts, 20 whole.
 [[maybe_unused]] int parts_of(int64_t N, int64_t V, int per16)
 {
-    constexpr int64_t kWanted = 512, kMost = 32;
-    int64_t parts = N < kWanted ? ceil_div(kWanted, N) : 1;
-    const int64_t fit = ceil_div(V, static_cast<int64_t>(kRowThreads) * per16 * 2);
-    parts = parts < fit ? parts : fit;
+    constexpr int64_t kWhole = 8192, kPart = 2048, kMost = 16, kWanted = 512;
+    const int64_t vectors = V / per16;
+    if (vectors <= kWhole || 2 * N > kWanted) return 1;
+    int64_t parts = ceil_div(vectors, kPart);
+    parts = parts < kWanted / N ? parts : kWanted / N;
     return static_cast<int>(parts < kMost ? parts : kMost);
 }
 

@@ -78,66 +78,80 @@ def _ok(fn: str, status: int) -> None:
 
 
 # ------------------------------------------------------------------------------------------------------------- checks
-class _Checks:
-    """The tensors of one call: each is checked as it is handed in; done() looks at the devices."""
+# The binding's share of a call is what bounds the smallest ones, so that the checks are plain functions with few queries each:
+# cx_embed_lookup_bf16 of 32 tokens, call after call, 7.8 us with an object for every call's checks, 7.1 us with these, of which
+# 3.7 us are the library's.
+def _matrix(name, arg, t, dtype, rows, columns, device):
+    """Row stride of a row-major matrix of the call's type on its device; rows or columns of None: any."""
+    shape, stride = t.shape, t.stride()
+    if (len(shape) == 2 and t.dtype is dtype and stride[1] == 1 and stride[0] >= shape[1] and (rows is None or shape[0] == rows)
+            and (columns is None or shape[1] == columns) and t.get_device() == device):
+        return stride[0]
+    return _unusual_matrix(name, arg, t, dtype, rows, columns, device)
 
-    def __init__(self, name, suffix):
-        lib()
-        self.name, self.dtype, self.device, self.host = name, _dtypes[suffix], None, False
 
-    def _seen(self, arg, t):
-        if self.device is None:
-            self.device, self.host = t.device, not t.is_cuda
-        elif t.device != self.device:
-            raise ValueError(f"{self.name}: buffers on different devices: {t.device} and {self.device}")
+def _unusual_matrix(name, arg, t, dtype, rows, columns, device):
+    """The same for single rows and columns, whose strides mean nothing; raises what does not fit."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: {arg}: expected {dtype}, got {t.dtype}")
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (columns is not None and shape[1] != columns):
+        raise ValueError(f"{name}: {arg}: expected [{'any' if rows is None else rows}][{'any' if columns is None else columns}], got {list(shape)}")
+    if t.numel() > 0 and ((shape[1] > 1 and stride[1] != 1) or (shape[0] > 1 and stride[0] < shape[1])):
+        raise ValueError(f"{name}: {arg}: expected row-major elements (rows that do not overlap)")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: {arg}: on another device than the call's first buffer: {t.device}")
+    return max(stride[0], shape[1], 1) if shape[0] > 1 else max(shape[1], 1)
+
+
+def _dense(name, arg, t, dtype, shape, device):
+    """Address of a contiguous tensor of exactly this type and shape on the call's device."""
+    if t is not None and t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == device:
         return t.data_ptr()
+    if t is None:
+        raise ValueError(f"{name}: {arg} is missing")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: {arg}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: {arg}: expected a contiguous tensor {list(shape)}, got {list(t.shape)}, strides {t.stride()}")
+    raise ValueError(f"{name}: {arg}: on another device than the call's first buffer: {t.device}")
 
-    def matrix(self, arg, t, rows=None, columns=None):
-        """(address, row stride) of a row-major matrix of the call's type."""
-        shape = t.shape
-        if t.dtype != self.dtype:
-            raise ValueError(f"{self.name}: {arg}: expected {self.dtype}, got {t.dtype}")
-        if len(shape) != 2 or (rows is not None and shape[0] != rows) or (columns is not None and shape[1] != columns):
-            raise ValueError(f"{self.name}: {arg}: expected [{'any' if rows is None else rows}][{'any' if columns is None else columns}], "
-                             f"got {list(shape)}")
-        stride = t.stride()
-        if (shape[1] > 1 and stride[1] != 1) or (shape[0] > 1 and stride[0] < shape[1]):
-            raise ValueError(f"{self.name}: {arg}: expected row-major elements (rows that do not overlap)")
-        return self._seen(arg, t), max(stride[0], shape[1]) if shape[0] > 1 else max(shape[1], 1)
 
-    def dense(self, arg, t, dtype, *shape, optional=False):
-        """Address of a contiguous tensor of exactly this type and shape."""
-        if t is None:
-            if optional:
-                return None
-            raise ValueError(f"{self.name}: {arg} is missing")
-        if t.dtype != dtype:
-            raise ValueError(f"{self.name}: {arg}: expected {dtype}, got {t.dtype}")
-        if t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{self.name}: {arg}: expected a contiguous tensor {list(shape)}, got {list(t.shape)}, strides {t.stride()}")
-        return self._seen(arg, t)
+def _optional(name, arg, t, dtype, shape, device):
+    return None if t is None else _dense(name, arg, t, dtype, shape, device)
 
-    def done(self):
-        if self.host:
-            raise ValueError(f"{self.name}: expected device tensors")
 
-    def scratch(self, workspace, needed, stream):
-        """(tensor to keep alive, address, bytes) of the workspace; all checks are done when this is called."""
-        self.done()
-        if workspace is None:
-            if needed == 0:
-                return None, None, 0
-            if stream is not None and getattr(stream, "cuda_stream", stream) != cxmix._stream(None):
-                raise ValueError(f"{self.name}: a call on a stream that is not the current one brings its own workspace ({needed} bytes)")
-            workspace = _torch.empty(needed, dtype=_torch.uint8, device=self.device)
-        elif workspace.dtype != _torch.uint8 or not workspace.is_contiguous():
-            raise ValueError(f"{self.name}: workspace: expected a contiguous uint8 tensor")
-        return workspace, self._seen("workspace", workspace), workspace.numel()
+def _on_device(name, device):
+    """Last check before the call."""
+    if device < 0:
+        raise ValueError(f"{name}: expected device tensors")
+
+
+def _scratch(name, workspace, size, args, device, stream):
+    """The workspace: the caller's, or from torch's allocator what the library's function `size` asks for (None: no call needs one)."""
+    _on_device(name, device)
+    if size is None and workspace is None:
+        return None
+    if workspace is not None:
+        if workspace.dtype is not _torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != device:
+            raise ValueError(f"{name}: workspace: expected a contiguous uint8 tensor on the call's device")
+        return workspace
+    needed = _size(size, *args)
+    if needed == 0:
+        return None
+    if stream is not None and getattr(stream, "cuda_stream", stream) != cxmix._stream(None):
+        raise ValueError(f"{name}: a call on a stream that is not the current one brings its own workspace ({needed} bytes)")
+    return _torch.empty(needed, dtype=_torch.uint8, device=device)
+
+
+def _span(work):
+    return (None, 0) if work is None else (work.data_ptr(), work.numel())
 
 
 def _size(fn, *args) -> int:
+    L = _lib or lib()
     n = ctypes.c_int64()
-    _ok(fn, getattr(lib(), fn)(*args, ctypes.byref(n)))
+    _ok(fn, getattr(L, fn)(*args, ctypes.byref(n)))
     return n.value
 
 
@@ -166,70 +180,70 @@ def cx_distill_workspace(N: int, V: int) -> int:
 
 
 # ---------------------------------------------------------------------------------------------------------- embeddings
-def _lookup(suffix, x, tokens, out, offset, V, scale, stream):
-    name = "cx_embed_lookup" + suffix
-    k = _Checks(name, suffix)
-    if tokens.dim() != 2:
+def _lookup(name, suffix, x, tokens, out, offset, V, scale, stream):
+    L = _lib or lib()
+    dtype, device = _dtypes[suffix], x.get_device()
+    if len(tokens.shape) != 2:
         raise ValueError(f"{name}: tokens: expected int32 [W][N]")
     W, N = tokens.shape
-    xp, ld = k.matrix("x", x, W)
-    op, ld_out = k.matrix("out", out, W * N)
+    ld = _matrix(name, "x", x, dtype, W, None, device)
+    ld_out = _matrix(name, "out", out, dtype, W * N, None, device)
     D = out.shape[1]
     if offset < 0 or offset + V * D > x.shape[1]:
         raise ValueError(f"{name}: a table of {V} x {D} at {offset} does not fit rows of {x.shape[1]}")
-    tp = k.dense("tokens", tokens, _torch.int32, W, N)
-    k.done()
-    _ok(name, getattr(_lib, name)(xp, ld, W, offset, V, D, tp, N, scale, op, ld_out, cxmix._stream(stream)))
+    tp = _dense(name, "tokens", tokens, _torch.int32, (W, N), device)
+    _on_device(name, device)
+    _ok(name, getattr(L, name)(x.data_ptr(), ld, W, offset, V, D, tp, N, scale, out.data_ptr(), ld_out, cxmix._stream(stream)))
 
 
 def cx_embed_lookup(x, tokens, out, offset: int, V: int, scale: float = 1.0, stream=None):
     """x: [W][ld] flat rows; tokens: int32 [W][N]; out: [W * N][D].  The table of worker w is x[w, offset : offset + V * D]."""
-    _lookup("", x, tokens, out, offset, V, scale, stream)
+    _lookup("cx_embed_lookup", "", x, tokens, out, offset, V, scale, stream)
 
 
 def cx_embed_lookup_bf16(x, tokens, out, offset: int, V: int, scale: float = 1.0, stream=None):
-    _lookup("_bf16", x, tokens, out, offset, V, scale, stream)
+    _lookup("cx_embed_lookup_bf16", "_bf16", x, tokens, out, offset, V, scale, stream)
 
 
 def cx_embed_lookup_f16(x, tokens, out, offset: int, V: int, scale: float = 1.0, stream=None):
-    _lookup("_f16", x, tokens, out, offset, V, scale, stream)
+    _lookup("cx_embed_lookup_f16", "_f16", x, tokens, out, offset, V, scale, stream)
 
 
-def _embed_grad(suffix, dout, tokens, g_in, g_out, offset, V, scale, workspace, stream):
-    name = "cx_embed_grad" + suffix
-    k = _Checks(name, suffix)
-    if tokens.dim() != 2:
+def _embed_grad(name, suffix, dout, tokens, g_in, g_out, offset, V, scale, workspace, stream):
+    L = _lib or lib()
+    dtype, device = _dtypes[suffix], g_out.get_device()
+    if len(tokens.shape) != 2:
         raise ValueError(f"{name}: tokens: expected int32 [W][N]")
     W, N = tokens.shape
-    dp, ld_dout = k.matrix("dout", dout, W * N)
+    ld_dout = _matrix(name, "dout", dout, dtype, W * N, None, device)
     D = dout.shape[1]
-    gp, ld = k.matrix("g_out", g_out, W)
+    ld = _matrix(name, "g_out", g_out, dtype, W, None, device)
     fits = g_out.shape[1]
-    ip = None
     if g_in is not None:
-        ip, ld_in = k.matrix("g_in", g_in, W)
+        ld_in = _matrix(name, "g_in", g_in, dtype, W, None, device)
         if W > 1 and ld_in != ld:
             raise ValueError(f"{name}: g_in: row stride {ld_in} differs from g_out's {ld}")
         fits = min(fits, g_in.shape[1])
     if offset < 0 or offset + V * D > fits:
         raise ValueError(f"{name}: a table of {V} x {D} at {offset} does not fit rows of {fits}")
-    tp = k.dense("tokens", tokens, _torch.int32, W, N)
-    keep, wp, wn = k.scratch(workspace, 0 if workspace is not None else cx_embed_workspace(W, N, V, D), stream)
-    _ok(name, getattr(_lib, name)(dp, ld_dout, tp, W, N, ip, gp, ld, offset, V, D, scale, wp, wn, cxmix._stream(stream)))
+    tp = _dense(name, "tokens", tokens, _torch.int32, (W, N), device)
+    work = _scratch(name, workspace, "cx_embed_workspace", (W, N, V, D), device, stream)
+    _ok(name, getattr(L, name)(dout.data_ptr(), ld_dout, tp, W, N, None if g_in is None else g_in.data_ptr(), g_out.data_ptr(), ld, offset, V, D,
+                               scale, *_span(work), cxmix._stream(stream)))
 
 
 def cx_embed_grad(dout, tokens, g_in, g_out, offset: int, V: int, scale: float = 1.0, workspace=None, stream=None):
     """dout: [W * N][D]; tokens: int32 [W][N]; g_out: [W][ld] flat gradient rows.  g_in: None (rows that no token names become
     zeros), g_out itself (added in place) or a second matrix with the same row stride."""
-    _embed_grad("", dout, tokens, g_in, g_out, offset, V, scale, workspace, stream)
+    _embed_grad("cx_embed_grad", "", dout, tokens, g_in, g_out, offset, V, scale, workspace, stream)
 
 
 def cx_embed_grad_bf16(dout, tokens, g_in, g_out, offset: int, V: int, scale: float = 1.0, workspace=None, stream=None):
-    _embed_grad("_bf16", dout, tokens, g_in, g_out, offset, V, scale, workspace, stream)
+    _embed_grad("cx_embed_grad_bf16", "_bf16", dout, tokens, g_in, g_out, offset, V, scale, workspace, stream)
 
 
 def cx_embed_grad_f16(dout, tokens, g_in, g_out, offset: int, V: int, scale: float = 1.0, workspace=None, stream=None):
-    _embed_grad("_f16", dout, tokens, g_in, g_out, offset, V, scale, workspace, stream)
+    _embed_grad("cx_embed_grad_f16", "_f16", dout, tokens, g_in, g_out, offset, V, scale, workspace, stream)
 
 
 # ----------------------------------------------------------------------------------------------------- gated recurrence
@@ -240,196 +254,196 @@ def scan_states(f, T: int):
     return torch.empty((B, -(-T // CX_SCAN_CHUNK), f.shape[1]), dtype=torch.float32, device=f.device)
 
 
-def _sequences(name, f, T, *ends):
-    """B of a matrix of B * T rows; of empty sequences, what the states at their ends say."""
-    if T > 0 and f.shape[0] % T == 0:
-        return f.shape[0] // T
-    if T == 0 and f.shape[0] == 0:
+def _sequences(name, rows, T, *ends):
+    """B of B * T rows; of empty sequences, what the states at their ends say."""
+    if T > 0 and rows % T == 0:
+        return rows // T
+    if T == 0 and rows == 0:
         return next((t.shape[0] for t in ends if t is not None), 0)
-    raise ValueError(f"{name}: {f.shape[0]} rows are no sequences of {T} steps")
+    raise ValueError(f"{name}: {rows} rows are no sequences of {T} steps")
 
 
-def _scan(suffix, f, x, y, T, h0, h_last, reset, states, workspace, stream):
-    name = "cx_gated_scan" + suffix
-    k = _Checks(name, suffix)
-    fp, ldf = k.matrix("f", f)
+def _scan(name, suffix, f, x, y, T, h0, h_last, reset, states, workspace, stream):
+    L = _lib or lib()
+    dtype, device, f32 = _dtypes[suffix], f.get_device(), _torch.float32
+    ldf = _matrix(name, "f", f, dtype, None, None, device)
     rows, D = f.shape
-    B = _sequences(name, f, T, h0, h_last)
-    xp, ldx = k.matrix("x", x, rows, D)
-    yp, ldy = k.matrix("y", y, rows, D)
-    f32 = _torch.float32
-    hp = k.dense("h0", h0, f32, B, D, optional=True)
-    lp = k.dense("h_last", h_last, f32, B, D, optional=True)
-    sp = k.dense("states", states, f32, B, -(-T // CX_SCAN_CHUNK), D, optional=True)
-    rp = k.dense("reset", reset, _torch.uint8, B, T, optional=True)
-    keep, wp, wn = k.scratch(workspace, 0 if workspace is not None else cx_scan_workspace(B, T, D), stream)
-    _ok(name, getattr(_lib, name)(fp, ldf, xp, ldx, yp, ldy, B, T, D, rp, hp, lp, sp, wp, wn, cxmix._stream(stream)))
+    B = _sequences(name, rows, T, h0, h_last)
+    ldx = _matrix(name, "x", x, dtype, rows, D, device)
+    ldy = _matrix(name, "y", y, dtype, rows, D, device)
+    hp = _optional(name, "h0", h0, f32, (B, D), device)
+    lp = _optional(name, "h_last", h_last, f32, (B, D), device)
+    sp = _optional(name, "states", states, f32, (B, -(-T // CX_SCAN_CHUNK), D), device)
+    rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    work = _scratch(name, workspace, None if T <= CX_SCAN_CHUNK else "cx_scan_workspace", (B, T, D), device, stream)
+    _ok(name, getattr(L, name)(f.data_ptr(), ldf, x.data_ptr(), ldx, y.data_ptr(), ldy, B, T, D, rp, hp, lp, sp, *_span(work),
+                               cxmix._stream(stream)))
 
 
 def cx_gated_scan(f, x, y, T: int, h0=None, h_last=None, reset=None, states=None, workspace=None, stream=None):
     """f, x, y: [B * T][D]; h0, h_last: float32 [B][D] (may be one tensor); reset: uint8 [B][T]; states: see scan_states()."""
-    _scan("", f, x, y, T, h0, h_last, reset, states, workspace, stream)
+    _scan("cx_gated_scan", "", f, x, y, T, h0, h_last, reset, states, workspace, stream)
 
 
 def cx_gated_scan_bf16(f, x, y, T: int, h0=None, h_last=None, reset=None, states=None, workspace=None, stream=None):
-    _scan("_bf16", f, x, y, T, h0, h_last, reset, states, workspace, stream)
+    _scan("cx_gated_scan_bf16", "_bf16", f, x, y, T, h0, h_last, reset, states, workspace, stream)
 
 
 def cx_gated_scan_f16(f, x, y, T: int, h0=None, h_last=None, reset=None, states=None, workspace=None, stream=None):
-    _scan("_f16", f, x, y, T, h0, h_last, reset, states, workspace, stream)
+    _scan("cx_gated_scan_f16", "_f16", f, x, y, T, h0, h_last, reset, states, workspace, stream)
 
 
-def _scan_grad(suffix, f, x, dy, df, dx, T, states, dh_last, dh0, reset, workspace, stream):
-    name = "cx_gated_scan_grad" + suffix
-    k = _Checks(name, suffix)
-    fp, ldf = k.matrix("f", f)
+def _scan_grad(name, suffix, f, x, dy, df, dx, T, states, dh_last, dh0, reset, workspace, stream):
+    L = _lib or lib()
+    dtype, device, f32 = _dtypes[suffix], f.get_device(), _torch.float32
+    ldf = _matrix(name, "f", f, dtype, None, None, device)
     rows, D = f.shape
-    B = _sequences(name, f, T, dh_last, dh0)
-    xp, ldx = k.matrix("x", x, rows, D)
-    yp, lddy = k.matrix("dy", dy, rows, D)
-    dfp, lddf = k.matrix("df", df, rows, D)
-    dxp, lddx = k.matrix("dx", dx, rows, D)
-    f32 = _torch.float32
-    sp = k.dense("states", states, f32, B, -(-T // CX_SCAN_CHUNK), D, optional=T == 0)
-    lp = k.dense("dh_last", dh_last, f32, B, D, optional=True)
-    hp = k.dense("dh0", dh0, f32, B, D, optional=True)
-    rp = k.dense("reset", reset, _torch.uint8, B, T, optional=True)
-    keep, wp, wn = k.scratch(workspace, 0 if workspace is not None else cx_scan_workspace(B, T, D), stream)
-    _ok(name, getattr(_lib, name)(fp, ldf, xp, ldx, yp, lddy, dfp, lddf, dxp, lddx, B, T, D, rp, sp, lp, hp, wp, wn, cxmix._stream(stream)))
+    B = _sequences(name, rows, T, dh_last, dh0)
+    ldx = _matrix(name, "x", x, dtype, rows, D, device)
+    lddy = _matrix(name, "dy", dy, dtype, rows, D, device)
+    lddf = _matrix(name, "df", df, dtype, rows, D, device)
+    lddx = _matrix(name, "dx", dx, dtype, rows, D, device)
+    sp = (_dense if T > 0 else _optional)(name, "states", states, f32, (B, -(-T // CX_SCAN_CHUNK), D), device)
+    lp = _optional(name, "dh_last", dh_last, f32, (B, D), device)
+    hp = _optional(name, "dh0", dh0, f32, (B, D), device)
+    rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    work = _scratch(name, workspace, None if T <= CX_SCAN_CHUNK else "cx_scan_workspace", (B, T, D), device, stream)
+    _ok(name, getattr(L, name)(f.data_ptr(), ldf, x.data_ptr(), ldx, dy.data_ptr(), lddy, df.data_ptr(), lddf, dx.data_ptr(), lddx, B, T, D, rp, sp,
+                               lp, hp, *_span(work), cxmix._stream(stream)))
 
 
 def cx_gated_scan_grad(f, x, dy, df, dx, T: int, states, dh_last=None, dh0=None, reset=None, workspace=None, stream=None):
     """f, x, dy, df, dx: [B * T][D]; states: as cx_gated_scan filled them; dh_last, dh0: float32 [B][D]; reset: uint8 [B][T]."""
-    _scan_grad("", f, x, dy, df, dx, T, states, dh_last, dh0, reset, workspace, stream)
+    _scan_grad("cx_gated_scan_grad", "", f, x, dy, df, dx, T, states, dh_last, dh0, reset, workspace, stream)
 
 
 def cx_gated_scan_grad_bf16(f, x, dy, df, dx, T: int, states, dh_last=None, dh0=None, reset=None, workspace=None, stream=None):
-    _scan_grad("_bf16", f, x, dy, df, dx, T, states, dh_last, dh0, reset, workspace, stream)
+    _scan_grad("cx_gated_scan_grad_bf16", "_bf16", f, x, dy, df, dx, T, states, dh_last, dh0, reset, workspace, stream)
 
 
 def cx_gated_scan_grad_f16(f, x, dy, df, dx, T: int, states, dh_last=None, dh0=None, reset=None, workspace=None, stream=None):
-    _scan_grad("_f16", f, x, dy, df, dx, T, states, dh_last, dh0, reset, workspace, stream)
+    _scan_grad("cx_gated_scan_grad_f16", "_f16", f, x, dy, df, dx, T, states, dh_last, dh0, reset, workspace, stream)
 
 
 # ------------------------------------------------------------------------------------------------------------ token scores
-def _scores(suffix, z, tokens, logp, entropy, top_ids, top_logp, scale, workspace, stream):
-    name = "cx_token_scores" + suffix
-    k = _Checks(name, suffix)
-    zp, ld = k.matrix("z", z)
+def _scores(name, suffix, z, tokens, logp, entropy, top_ids, top_logp, scale, workspace, stream):
+    L = _lib or lib()
+    device, f32, i32 = z.get_device(), _torch.float32, _torch.int32
+    ld = _matrix(name, "z", z, _dtypes[suffix], None, None, device)
     N, V = z.shape
-    f32, i32 = _torch.float32, _torch.int32
-    tp = k.dense("tokens", tokens, i32, N, optional=logp is None)
-    lp = k.dense("logp", logp, f32, N, optional=True)
-    ep = k.dense("entropy", entropy, f32, N, optional=True)
+    tp = (_dense if logp is not None else _optional)(name, "tokens", tokens, i32, (N,), device)
+    lp = _optional(name, "logp", logp, f32, (N,), device)
+    ep = _optional(name, "entropy", entropy, f32, (N,), device)
     K = 0
     ip = pp = None
     if top_ids is not None or top_logp is not None:
-        if top_ids is None or top_ids.dim() != 2:
+        if top_ids is None or len(top_ids.shape) != 2:
             raise ValueError(f"{name}: top_ids: expected int32 [N][K] beside top_logp")
         K = top_ids.shape[1]
-        ip = k.dense("top_ids", top_ids, i32, N, K)
-        pp = k.dense("top_logp", top_logp, f32, N, K)
-    keep, wp, wn = k.scratch(workspace, 0 if workspace is not None else cx_scores_workspace(N, V, K), stream)
-    _ok(name, getattr(_lib, name)(zp, ld, N, V, tp, scale, lp, ep, K, ip, pp, wp, wn, cxmix._stream(stream)))
+        ip = _dense(name, "top_ids", top_ids, i32, (N, K), device)
+        pp = _dense(name, "top_logp", top_logp, f32, (N, K), device)
+    work = _scratch(name, workspace, "cx_scores_workspace", (N, V, K), device, stream)
+    _ok(name, getattr(L, name)(z.data_ptr(), ld, N, V, tp, scale, lp, ep, K, ip, pp, *_span(work), cxmix._stream(stream)))
 
 
 def cx_token_scores(z, tokens, logp, entropy=None, top_ids=None, top_logp=None, scale: float = 1.0, workspace=None, stream=None):
     """z: [N][V] logits; tokens: int32 [N]; logp, entropy: float32 [N]; top_ids: int32 [N][K]; top_logp: float32 [N][K]; what is
     None is not computed.  scale: 1 / temperature."""
-    _scores("", z, tokens, logp, entropy, top_ids, top_logp, scale, workspace, stream)
+    _scores("cx_token_scores", "", z, tokens, logp, entropy, top_ids, top_logp, scale, workspace, stream)
 
 
 def cx_token_scores_bf16(z, tokens, logp, entropy=None, top_ids=None, top_logp=None, scale: float = 1.0, workspace=None, stream=None):
-    _scores("_bf16", z, tokens, logp, entropy, top_ids, top_logp, scale, workspace, stream)
+    _scores("cx_token_scores_bf16", "_bf16", z, tokens, logp, entropy, top_ids, top_logp, scale, workspace, stream)
 
 
 def cx_token_scores_f16(z, tokens, logp, entropy=None, top_ids=None, top_logp=None, scale: float = 1.0, workspace=None, stream=None):
-    _scores("_f16", z, tokens, logp, entropy, top_ids, top_logp, scale, workspace, stream)
+    _scores("cx_token_scores_f16", "_f16", z, tokens, logp, entropy, top_ids, top_logp, scale, workspace, stream)
 
 
 # ------------------------------------------------------------------------------------------------------------- distillation
-def _targets(k, z, ids, t, labels):
-    zp, ld = k.matrix("z", z)
+def _targets(name, suffix, z, ids, t, labels, device):
+    """The first arguments of the three calls."""
+    ld = _matrix(name, "z", z, _dtypes[suffix], None, None, device)
     N, V = z.shape
-    if ids.dim() != 2:
-        raise ValueError(f"{k.name}: ids: expected int32 [N][K]")
+    if len(ids.shape) != 2:
+        raise ValueError(f"{name}: ids: expected int32 [N][K]")
     K = ids.shape[1]
-    ip = k.dense("ids", ids, _torch.int32, N, K)
-    tp = k.dense("t", t, _torch.float32, N, K)
-    lp = k.dense("labels", labels, _torch.int32, N, optional=True)
-    return (zp, ld, N, V, K, ip, tp, lp)
+    ip = _dense(name, "ids", ids, _torch.int32, (N, K), device)
+    tp = _dense(name, "t", t, _torch.float32, (N, K), device)
+    lp = _optional(name, "labels", labels, _torch.int32, (N,), device)
+    return z.data_ptr(), ld, N, V, K, ip, tp, lp
 
 
-def _distill_loss(suffix, z, ids, t, labels, loss, stats, tau, w_kl, w_ce, workspace, stream):
-    name = "cx_distill_loss" + suffix
-    k = _Checks(name, suffix)
-    head = _targets(k, z, ids, t, labels)
-    N, V = z.shape
-    lp = k.dense("loss", loss, _torch.float32, N)
-    sp = k.dense("stats", stats, _torch.float32, N, 4, optional=True)
-    keep, wp, wn = k.scratch(workspace, 0 if workspace is not None else cx_distill_workspace(N, V), stream)
-    _ok(name, getattr(_lib, name)(*head, tau, w_kl, w_ce, lp, sp, wp, wn, cxmix._stream(stream)))
+def _distill_loss(name, suffix, z, ids, t, labels, loss, stats, tau, w_kl, w_ce, workspace, stream):
+    L = _lib or lib()
+    device = z.get_device()
+    head = _targets(name, suffix, z, ids, t, labels, device)
+    N, V = head[2:4]
+    lp = _dense(name, "loss", loss, _torch.float32, (N,), device)
+    sp = _optional(name, "stats", stats, _torch.float32, (N, 4), device)
+    work = _scratch(name, workspace, "cx_distill_workspace", (N, V), device, stream)
+    _ok(name, getattr(L, name)(*head, tau, w_kl, w_ce, lp, sp, *_span(work), cxmix._stream(stream)))
 
 
 def cx_distill_loss(z, ids, t, labels, loss, stats, tau: float, w_kl: float, w_ce: float, workspace=None, stream=None):
     """z: [N][V] logits; ids: int32 [N][K] and t: float32 [N][K], the teacher's top tokens and their logits; labels: int32 [N] or
     None; loss: float32 [N]; stats: float32 [N][4] for the gradient, or None."""
-    _distill_loss("", z, ids, t, labels, loss, stats, tau, w_kl, w_ce, workspace, stream)
+    _distill_loss("cx_distill_loss", "", z, ids, t, labels, loss, stats, tau, w_kl, w_ce, workspace, stream)
 
 
 def cx_distill_loss_bf16(z, ids, t, labels, loss, stats, tau: float, w_kl: float, w_ce: float, workspace=None, stream=None):
-    _distill_loss("_bf16", z, ids, t, labels, loss, stats, tau, w_kl, w_ce, workspace, stream)
+    _distill_loss("cx_distill_loss_bf16", "_bf16", z, ids, t, labels, loss, stats, tau, w_kl, w_ce, workspace, stream)
 
 
 def cx_distill_loss_f16(z, ids, t, labels, loss, stats, tau: float, w_kl: float, w_ce: float, workspace=None, stream=None):
-    _distill_loss("_f16", z, ids, t, labels, loss, stats, tau, w_kl, w_ce, workspace, stream)
+    _distill_loss("cx_distill_loss_f16", "_f16", z, ids, t, labels, loss, stats, tau, w_kl, w_ce, workspace, stream)
 
 
-def _distill_grad(suffix, z, ids, t, labels, stats, gout, dz, tau, w_kl, w_ce, stream):
-    name = "cx_distill_grad" + suffix
-    k = _Checks(name, suffix)
-    head = _targets(k, z, ids, t, labels)
-    N, V = z.shape
-    sp = k.dense("stats", stats, _torch.float32, N, 4)
-    gp = k.dense("gout", gout, _torch.float32, N)
-    dp, ld_dz = k.matrix("dz", dz, N, V)
-    k.done()
-    _ok(name, getattr(_lib, name)(*head, tau, w_kl, w_ce, sp, gp, dp, ld_dz, cxmix._stream(stream)))
+def _distill_grad(name, suffix, z, ids, t, labels, stats, gout, dz, tau, w_kl, w_ce, stream):
+    L = _lib or lib()
+    device = z.get_device()
+    head = _targets(name, suffix, z, ids, t, labels, device)
+    N, V = head[2:4]
+    sp = _dense(name, "stats", stats, _torch.float32, (N, 4), device)
+    gp = _dense(name, "gout", gout, _torch.float32, (N,), device)
+    ld_dz = _matrix(name, "dz", dz, _dtypes[suffix], N, V, device)
+    _on_device(name, device)
+    _ok(name, getattr(L, name)(*head, tau, w_kl, w_ce, sp, gp, dz.data_ptr(), ld_dz, cxmix._stream(stream)))
 
 
 def cx_distill_grad(z, ids, t, labels, stats, gout, dz, tau: float, w_kl: float, w_ce: float, stream=None):
     """As cx_distill_loss, with its stats; gout: float32 [N]; dz: [N][V], may be z."""
-    _distill_grad("", z, ids, t, labels, stats, gout, dz, tau, w_kl, w_ce, stream)
+    _distill_grad("cx_distill_grad", "", z, ids, t, labels, stats, gout, dz, tau, w_kl, w_ce, stream)
 
 
 def cx_distill_grad_bf16(z, ids, t, labels, stats, gout, dz, tau: float, w_kl: float, w_ce: float, stream=None):
-    _distill_grad("_bf16", z, ids, t, labels, stats, gout, dz, tau, w_kl, w_ce, stream)
+    _distill_grad("cx_distill_grad_bf16", "_bf16", z, ids, t, labels, stats, gout, dz, tau, w_kl, w_ce, stream)
 
 
 def cx_distill_grad_f16(z, ids, t, labels, stats, gout, dz, tau: float, w_kl: float, w_ce: float, stream=None):
-    _distill_grad("_f16", z, ids, t, labels, stats, gout, dz, tau, w_kl, w_ce, stream)
+    _distill_grad("cx_distill_grad_f16", "_f16", z, ids, t, labels, stats, gout, dz, tau, w_kl, w_ce, stream)
 
 
-def _distill_step(suffix, z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream):
-    name = "cx_distill_step" + suffix
-    k = _Checks(name, suffix)
-    head = _targets(k, z, ids, t, labels)
-    N, V = z.shape
-    gp = k.dense("gout", gout, _torch.float32, N)
-    lp = k.dense("loss", loss, _torch.float32, N)
-    dp, ld_dz = k.matrix("dz", dz, N, V)
-    keep, wp, wn = k.scratch(workspace, 0 if workspace is not None else cx_distill_workspace(N, V), stream)
-    _ok(name, getattr(_lib, name)(*head, tau, w_kl, w_ce, gp, lp, dp, ld_dz, wp, wn, cxmix._stream(stream)))
+def _distill_step(name, suffix, z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream):
+    L = _lib or lib()
+    device = z.get_device()
+    head = _targets(name, suffix, z, ids, t, labels, device)
+    N, V = head[2:4]
+    gp = _dense(name, "gout", gout, _torch.float32, (N,), device)
+    lp = _dense(name, "loss", loss, _torch.float32, (N,), device)
+    ld_dz = _matrix(name, "dz", dz, _dtypes[suffix], N, V, device)
+    work = _scratch(name, workspace, "cx_distill_workspace", (N, V), device, stream)
+    _ok(name, getattr(L, name)(*head, tau, w_kl, w_ce, gp, lp, dz.data_ptr(), ld_dz, *_span(work), cxmix._stream(stream)))
 
 
 def cx_distill_step(z, ids, t, labels, gout, loss, dz, tau: float, w_kl: float, w_ce: float, workspace=None, stream=None):
     """cx_distill_loss and cx_distill_grad in one call."""
-    _distill_step("", z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream)
+    _distill_step("cx_distill_step", "", z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream)
 
 
 def cx_distill_step_bf16(z, ids, t, labels, gout, loss, dz, tau: float, w_kl: float, w_ce: float, workspace=None, stream=None):
-    _distill_step("_bf16", z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream)
+    _distill_step("cx_distill_step_bf16", "_bf16", z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream)
 
 
 def cx_distill_step_f16(z, ids, t, labels, gout, loss, dz, tau: float, w_kl: float, w_ce: float, workspace=None, stream=None):
-    _distill_step("_f16", z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream)
+    _distill_step("cx_distill_step_f16", "_f16", z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream)

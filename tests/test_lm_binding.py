@@ -103,7 +103,9 @@ def test_scores_and_distill_refusals(suffix):
     for bad in (dict(N=-1), dict(V=0), dict(K=-1), dict(K=lm.CX_MAX_TOP + 1), dict(K=51, V=50), dict(ld=49), dict(scale=0.0), dict(scale=-1.0),
                 dict(scale=float("nan")), dict(scale=float("inf"))):
         assert call(**bad) == -2, bad
-    assert call(N=1, V=60_000, ld=60_000) == -1 and call(N=1, V=60_000, ld=60_000, ws=S, wn=8) == -2
+    long = dict(N=1, V=4_000_000, ld=4_000_000)                           # split, so that a workspace is needed
+    assert lm.cx_scores_workspace(1, 4_000_000, 4) > 0 and lm.cx_distill_workspace(1, 4_000_000) > 0
+    assert call(**long) == -1 and call(**long, ws=S, wn=8) == -2
     assert call(z=A + 1) == -5 and call(logp=C + 2) == -5
     assert call(logp=A) == -6 and call(ent=C) == -6 and call(top=E) == -6 and call(ids=B) == -6
     assert call(N=0, z=None) == 0
@@ -124,8 +126,8 @@ def test_scores_and_distill_refusals(suffix):
     assert loss(loss=None) == -1 and grad(stats=None) == -1 and grad(dz=None) == -1 and grad(gout=None) == -1 and step(loss=None) == -1
     assert loss(loss=A) == -6 and loss(stats=E) == -6 and grad(dz=B) == -6 and step(dz=F) == -6 and step(loss=E) == -6
     assert grad(dz=A + 100) == -6 and step(dz=A, lddz=51) == -6           # in place means exactly there
-    assert step(lddz=49) == -2 and step(N=1, V=60_000, ld=60_000, lddz=60_000) == -1
-    assert step(N=1, V=60_000, ld=60_000, lddz=60_000, ws=S, wn=8) == -2
+    assert step(lddz=49) == -2 and step(**long, lddz=4_000_000) == -1 and loss(**long) == -1
+    assert step(**long, lddz=4_000_000, ws=S, wn=8) == -2 and loss(**long, ws=S, wn=8) == -2
 
 
 def test_workspace_sizes():
@@ -136,7 +138,7 @@ def test_workspace_sizes():
     assert lm.cx_embed_workspace(2, 100, 10, 8) >= 2 * 11 * 4 + 2 * 100 * 4 + 2 * 2 * 2 * 8 * 4
     assert lm.cx_scan_workspace(4, 1, 64) == 0 and lm.cx_scan_workspace(1, 100_000, 64) > 0 and lm.cx_scan_workspace(0, 5, 1) == 0
     assert lm.cx_scores_workspace(10_000, 50_000, 4) == 0 and lm.cx_distill_workspace(10_000, 50_000) == 0
-    assert lm.cx_scores_workspace(1, 50_000, 4) > 0 and lm.cx_distill_workspace(1, 50_000) > 0
+    assert lm.cx_scores_workspace(1, 4_000_000, 4) > 0 and lm.cx_distill_workspace(1, 4_000_000) > 0
     with pytest.raises(lm.CxError, match="CX_ERR_SHAPE"):
         lm.cx_scores_workspace(1, 10, 11)
 
