@@ -7,9 +7,9 @@
 // a lane composes the maps of its piece in registers, the pieces' maps are joined through LDS, and the lane then walks its
 // piece once more with the state that enters it.  So the data are read once, whatever the length.
 //
-//   lane       kCols neighbouring columns (4 bytes of every row) and 8 (gradient: 16) consecutive steps: 64 lanes read whole lines
-//              of a row, and a walk needs no exchange between lanes
-//   workgroup  16 (gradient: 8) wavefronts, one piece each = a tile of 128 steps, tile after tile; the loads of the next tile are
+//   lane       the columns of 4 bytes of every row (16-bit rows: two) and 16 consecutive steps: 64 lanes read whole lines of a row,
+//              and a walk needs no exchange between lanes
+//   workgroup  8 wavefronts, one piece each = a tile of 128 steps, tile after tile; the loads of the next tile are
 //              issued before the present one is computed, into a second set of registers
 //   split      where columns are few (workgroups < kSplitBelow) the steps are also split over workgroups: a first launch composes
 //              the map of each span (it reads what the second reads again, from the last-level cache where the call fits there)
@@ -22,8 +22,8 @@
 namespace {
 
 constexpr int kTile = 128;                              // steps of a full tile
-constexpr int kForward = 8, kGrad = CX_SCAN_CHUNK;      // steps of a piece
-static_assert(CX_SCAN_CHUNK % kForward == 0, "pieces begin where states are kept");
+constexpr int kSteps = CX_SCAN_CHUNK;                   // steps of a piece: one begins where a state is kept
+constexpr int kWaves = kTile / kSteps;
 constexpr int kMaxSpans = 64;                           // workgroups that the steps of one column are split over
 constexpr int64_t kMaxColumns = CX_MAX_WIDTH, kMaxSeq = CX_MAX_TOKENS;
 
@@ -116,8 +116,8 @@ struct ScanArgs {
     float *h_last, *dh0, *states;
     const float *states_in;
     float *maps;                                        // split: [B][spans][2][D] (A, S) of each span, [B][D] what enters the first one
-    int64_t T_;
-    int32_t D, spans;
+    int64_t B, T_;
+    int32_t D, spans, slabs;
     int64_t span_steps;                                 // a multiple of kTile; the steps of one workgroup
 };
 
@@ -136,14 +136,14 @@ struct alignas(8 * N) Maps {                            // of a lane's columns
     Map of[N];
 };
 
-template <int N, int STEPS>
+template <int N>
 struct Exchange {                                       // the maps of the pieces of a tile, two tiles in turn
-    Maps<N> map[2][kTile / STEPS][kWave];
+    Maps<N> map[2][kWaves][kWave];
 };
 
 // What enters this wavefront's piece, and what leaves the tile, in the order of the walk.  One barrier.
-template <bool RESETS, int N, int STEPS>
-__device__ __forceinline__ void join_pieces(Exchange<N, STEPS> &lds, int turn, int place, int pieces, const Map (&mine)[N], float (&carry)[N],
+template <bool RESETS, int N>
+__device__ __forceinline__ void join_pieces(Exchange<N> &lds, int turn, int place, int pieces, const Map (&mine)[N], float (&carry)[N],
                                             float (&enters)[N])
 {
     const int lane = threadIdx.x & (kWave - 1);
@@ -170,8 +170,8 @@ __device__ __forceinline__ void join_pieces(Exchange<N, STEPS> &lds, int turn, i
 }
 
 // The map of a tile behind those of the tiles before it (in the order of the walk).  One barrier.
-template <int N, int STEPS>
-__device__ __forceinline__ void compose_pieces(Exchange<N, STEPS> &lds, int turn, int place, int pieces, const Map (&mine)[N], Map (&whole)[N])
+template <int N>
+__device__ __forceinline__ void compose_pieces(Exchange<N> &lds, int turn, int place, int pieces, const Map (&mine)[N], Map (&whole)[N])
 {
     const int lane = threadIdx.x & (kWave - 1);
     if (pieces > 1) {
@@ -193,8 +193,8 @@ __device__ __forceinline__ void compose_pieces(Exchange<N, STEPS> &lds, int turn
 
 // What enters this workgroup's span: the maps of the spans on the way to it, applied to what enters the first.  The wavefronts
 // compose a part of them each.  Nothing is left in LDS that a later tile's first exchange could meet: a barrier ends it.
-template <class E, int N, int STEPS>
-__device__ __forceinline__ void entering(const ScanArgs<E> &a, Exchange<N, STEPS> &lds, const LaneColumns<E, N> &c, int64_t b, int span, bool backwards,
+template <class E, int N>
+__device__ __forceinline__ void entering(const ScanArgs<E> &a, Exchange<N> &lds, const LaneColumns<E, N> &c, int64_t b, int span, bool backwards,
                                          const float *first, float (&h)[N])
 {
     if (a.spans == 1) {
@@ -204,10 +204,10 @@ __device__ __forceinline__ void entering(const ScanArgs<E> &a, Exchange<N, STEPS
             for (int j = 0; j < N; ++j) h[j] = 0.0f;
         return;
     }
-    constexpr int kEach = kMaxSpans * STEPS / kTile;    // a split call has all its wavefronts
+    constexpr int kEach = kMaxSpans / kWaves;    // a split call has all its wavefronts
     const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1);
     const float *maps = a.maps + b * a.spans * 2 * a.D;
-    c.load_wide(a.maps + (static_cast<int64_t>(gridDim.x) * a.spans * 2 + b) * a.D, h);
+    c.load_wide(a.maps + (a.B * a.spans * 2 + b) * a.D, h);
     const int before = backwards ? a.spans - 1 - span : span;
     float A[kEach][N], S[kEach][N];
 #pragma unroll
@@ -239,24 +239,23 @@ __device__ __forceinline__ void entering(const ScanArgs<E> &a, Exchange<N, STEPS
     __syncthreads();
 }
 
-template <int STEPS>
 __device__ __forceinline__ int steps_at(int64_t t, int64_t end)
 {
     const int64_t left = end - t;
-    return left >= STEPS ? STEPS : left > 0 ? static_cast<int>(left) : 0;
+    return left >= kSteps ? kSteps : left > 0 ? static_cast<int>(left) : 0;
 }
 
 // The first `steps` rows of a piece, at row `row` of the matrix.
-template <class E, int N, int STEPS>
-__device__ __forceinline__ void load_piece(const LaneColumns<E, N> &c, const typename E::T *m, int64_t ld, int64_t row, int steps, Word<E, N> (&v)[STEPS])
+template <class E, int N>
+__device__ __forceinline__ void load_piece(const LaneColumns<E, N> &c, const typename E::T *m, int64_t ld, int64_t row, int steps, Word<E, N> (&v)[kSteps])
 {
     const typename E::T *p = m + row * ld;
-    if (steps >= STEPS) {
+    if (steps >= kSteps) {
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) v[i] = c.load(p + i * ld);
+        for (int i = 0; i < kSteps; ++i) v[i] = c.load(p + i * ld);
     } else {
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) v[i] = i < steps ? c.load(p + i * ld) : 0;
+        for (int i = 0; i < kSteps; ++i) v[i] = i < steps ? c.load(p + i * ld) : 0;
     }
 }
 
@@ -277,28 +276,27 @@ __device__ __forceinline__ void keep_first(const ScanArgs<E> &a, const LaneColum
 {
     float h[N] = {};
     if (first) c.load_wide(first + b * a.D, h);
-    c.store_wide(a.maps + (static_cast<int64_t>(gridDim.x) * a.spans * 2 + b) * a.D, h);
+    c.store_wide(a.maps + (a.B * a.spans * 2 + b) * a.D, h);
 }
 
 template <bool V>
 using Flag = std::integral_constant<bool, V>;
 
-// Grid (sequences, spans, slabs of columns).  ONLY_MAP: the first launch of a split call.
+// Grid (slabs of columns of sequences, spans): workgroups that run together read whole rows.  ONLY_MAP: the first launch of a split call.
 template <class E, int N, bool RESETS, bool ONLY_MAP>
-__global__ __launch_bounds__(kTile / kForward *kWave) void scan_kernel(const ScanArgs<E> a)
+__global__ __launch_bounds__(kWaves *kWave) void scan_kernel(const ScanArgs<E> a)
 {
-    constexpr int STEPS = kForward;
-    __shared__ Exchange<N, STEPS> lds;
+    __shared__ Exchange<N> lds;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
-    const int64_t b = blockIdx.x;
-    const int span = blockIdx.y;
-    const LaneColumns<E, N> c((static_cast<int>(blockIdx.z) * kWave + lane) * N, a.D);
+    const int64_t b = blockIdx.x / a.slabs;
+    const int span = blockIdx.y, slab = static_cast<int>(blockIdx.x) % a.slabs;
+    const LaneColumns<E, N> c((slab * kWave + lane) * N, a.D);
     const bool whole_lanes = __ballot(c.whole()) == ~0ull;
     const int64_t row0 = b * a.T_, begin = span * a.span_steps, end = begin + a.span_steps < a.T_ ? begin + a.span_steps : a.T_;
-    const int tile = waves * STEPS;
-    Word<E, N> fw[2][STEPS], xw[2][STEPS];
-    int64_t t = begin + wave * STEPS;                   // of the piece whose rows were loaded last
-    int steps = steps_at<STEPS>(t, end);
+    const int tile = waves * kSteps;
+    Word<E, N> fw[2][kSteps], xw[2][kSteps];
+    int64_t t = begin + wave * kSteps;                   // of the piece whose rows were loaded last
+    int steps = steps_at(t, end);
     load_piece(c, a.f, a.ldf, row0 + t, steps, fw[0]);
     load_piece(c, a.x, a.ldx, row0 + t, steps, xw[0]);
     float carry[N];
@@ -316,16 +314,16 @@ __global__ __launch_bounds__(kTile / kForward *kWave) void scan_kernel(const Sca
         const int steps_now = steps;
         const unsigned resets = reset_bits<RESETS>(a.reset, row0 + t_now, steps_now);
         t += tile;
-        steps = steps_at<STEPS>(t, end);
+        steps = steps_at(t, end);
         load_piece(c, a.f, a.ldf, row0 + t, steps, fw[!turn]);
         load_piece(c, a.x, a.ldx, row0 + t, steps, xw[!turn]);
-        float keep[STEPS][N], in[STEPS][N];
+        float keep[kSteps][N], in[kSteps][N];
         Map mine[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) mine[j] = {1.0f, 0.0f};
         const auto maps = [&](auto full) {
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
+            for (int i = 0; i < kSteps; ++i) {
                 if (!decltype(full)::value && i >= steps_now) break;
                 const bool cut = RESETS && ((resets >> i) & 1u);
 #pragma unroll
@@ -338,18 +336,18 @@ __global__ __launch_bounds__(kTile / kForward *kWave) void scan_kernel(const Sca
                 }
             }
         };
-        if (steps_now == STEPS) maps(Flag<true>{}); else maps(Flag<false>{});
+        if (steps_now == kSteps) maps(Flag<true>{}); else maps(Flag<false>{});
         if constexpr (ONLY_MAP) {
             compose_pieces(lds, turn, wave, waves, mine, whole);
         } else {
             float h[N];
             join_pieces<RESETS>(lds, turn, wave, waves, mine, carry, h);
-            if (a.states && steps_now > 0 && t_now % CX_SCAN_CHUNK == 0)
-                c.store_wide(a.states + (b * ceil_div(a.T_, CX_SCAN_CHUNK) + t_now / CX_SCAN_CHUNK) * a.D, h);
+            if (a.states && steps_now > 0)
+                c.store_wide(a.states + (b * ceil_div(a.T_, kSteps) + t_now / kSteps) * a.D, h);
             typename E::T *out = a.y + (row0 + t_now) * a.ldy;
             const auto walk = [&](auto full) {
 #pragma unroll
-                for (int i = 0; i < STEPS; ++i) {
+                for (int i = 0; i < kSteps; ++i) {
                     if (!decltype(full)::value && i >= steps_now) break;
                     const bool cut = RESETS && ((resets >> i) & 1u);
 #pragma unroll
@@ -357,7 +355,7 @@ __global__ __launch_bounds__(kTile / kForward *kWave) void scan_kernel(const Sca
                     if (decltype(full)::value) c.store_whole(out + i * a.ldy, h); else c.store(out + i * a.ldy, h);
                 }
             };
-            if (steps_now == STEPS && whole_lanes) walk(Flag<true>{}); else walk(Flag<false>{});
+            if (steps_now == kSteps && whole_lanes) walk(Flag<true>{}); else walk(Flag<false>{});
         }
     };
     for (int64_t tile0 = begin; tile0 < end; tile0 += 2 * tile) {
@@ -373,21 +371,20 @@ __global__ __launch_bounds__(kTile / kForward *kWave) void scan_kernel(const Sca
 
 // The gradient, from the last step to the first.  What a piece hands to the one before it is keep a r of its first step.
 template <class E, int N, bool RESETS, bool ONLY_MAP>
-__global__ __launch_bounds__(kTile / kGrad *kWave) void scan_grad_kernel(const ScanArgs<E> a)
+__global__ __launch_bounds__(kWaves *kWave) void scan_grad_kernel(const ScanArgs<E> a)
 {
-    constexpr int STEPS = kGrad;
-    __shared__ Exchange<N, STEPS> lds;
+    __shared__ Exchange<N> lds;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
-    const int64_t b = blockIdx.x;
-    const int span = blockIdx.y;
-    const LaneColumns<E, N> c((static_cast<int>(blockIdx.z) * kWave + lane) * N, a.D);
+    const int64_t b = blockIdx.x / a.slabs;
+    const int span = blockIdx.y, slab = static_cast<int>(blockIdx.x) % a.slabs;
+    const LaneColumns<E, N> c((slab * kWave + lane) * N, a.D);
     const bool whole_lanes = __ballot(c.whole()) == ~0ull;
     const int64_t row0 = b * a.T_, begin = span * a.span_steps, end = begin + a.span_steps < a.T_ ? begin + a.span_steps : a.T_;
-    const int tile = waves * STEPS;
-    Word<E, N> fw[2][STEPS], xw[2][STEPS], gw[2][STEPS];
+    const int tile = waves * kSteps;
+    Word<E, N> fw[2][kSteps], xw[2][kSteps], gw[2][kSteps];
     int64_t tile0 = begin + (end - 1 - begin) / tile * tile;
-    int64_t t = tile0 + wave * STEPS;
-    int steps = steps_at<STEPS>(t, end);
+    int64_t t = tile0 + wave * kSteps;
+    int steps = steps_at(t, end);
     float entered[2][N];                                // the state before the piece
     const auto load = [&](auto turn_flag) {
         constexpr int turn = decltype(turn_flag)::value;
@@ -395,7 +392,7 @@ __global__ __launch_bounds__(kTile / kGrad *kWave) void scan_grad_kernel(const S
         load_piece(c, a.dy, a.lddy, row0 + t, steps, gw[turn]);
         if constexpr (!ONLY_MAP) {
             load_piece(c, a.x, a.ldx, row0 + t, steps, xw[turn]);
-            if (steps > 0) c.load_wide(a.states_in + (b * ceil_div(a.T_, CX_SCAN_CHUNK) + t / CX_SCAN_CHUNK) * a.D, entered[turn]);
+            if (steps > 0) c.load_wide(a.states_in + (b * ceil_div(a.T_, kSteps) + t / kSteps) * a.D, entered[turn]);
         }
     };
     load(Flag<false>{});
@@ -414,9 +411,9 @@ __global__ __launch_bounds__(kTile / kGrad *kWave) void scan_grad_kernel(const S
         const int steps_now = steps;
         const unsigned resets = reset_bits<RESETS>(a.reset, row0 + t_now, steps_now);
         t -= tile;
-        steps = tile0 > begin ? STEPS : 0;
+        steps = tile0 > begin ? kSteps : 0;
         load(Flag<!turn>{});
-        float keep[STEPS][N], open[STEPS][N], pull[STEPS][N];     // pull: a (keep h - x)
+        float keep[kSteps][N], open[kSteps][N], pull[kSteps][N];     // pull: a (keep h - x)
         Map mine[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) mine[j] = {1.0f, 0.0f};
@@ -425,7 +422,7 @@ __global__ __launch_bounds__(kTile / kGrad *kWave) void scan_grad_kernel(const S
 #pragma unroll
             for (int j = 0; j < N; ++j) h[j] = ONLY_MAP ? 0.0f : entered[turn][j];
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
+            for (int i = 0; i < kSteps; ++i) {
                 if (!decltype(full)::value && i >= steps_now) break;
                 const bool cut = RESETS && ((resets >> i) & 1u);
 #pragma unroll
@@ -441,7 +438,7 @@ __global__ __launch_bounds__(kTile / kGrad *kWave) void scan_grad_kernel(const S
                 }
             }
 #pragma unroll
-            for (int i = STEPS - 1; i >= 0; --i) {
+            for (int i = kSteps - 1; i >= 0; --i) {
                 if (!decltype(full)::value && i >= steps_now) continue;
                 const bool cut = RESETS && ((resets >> i) & 1u);
 #pragma unroll
@@ -451,7 +448,7 @@ __global__ __launch_bounds__(kTile / kGrad *kWave) void scan_grad_kernel(const S
                 }
             }
         };
-        if (steps_now == STEPS) maps(Flag<true>{}); else maps(Flag<false>{});
+        if (steps_now == kSteps) maps(Flag<true>{}); else maps(Flag<false>{});
         if constexpr (ONLY_MAP) {
             compose_pieces(lds, turn, waves - 1 - wave, waves, mine, whole);
         } else {
@@ -460,7 +457,7 @@ __global__ __launch_bounds__(kTile / kGrad *kWave) void scan_grad_kernel(const S
             typename E::T *df = a.df + (row0 + t_now) * a.lddf, *dx = a.dx + (row0 + t_now) * a.lddx;
             const auto walk = [&](auto full) {
 #pragma unroll
-                for (int i = STEPS - 1; i >= 0; --i) {
+                for (int i = kSteps - 1; i >= 0; --i) {
                     if (!decltype(full)::value && i >= steps_now) continue;
                     const bool cut = RESETS && ((resets >> i) & 1u);
                     float f_out[N], x_out[N];
@@ -480,7 +477,7 @@ __global__ __launch_bounds__(kTile / kGrad *kWave) void scan_grad_kernel(const S
                     }
                 }
             };
-            if (steps_now == STEPS && whole_lanes) walk(Flag<true>{}); else walk(Flag<false>{});
+            if (steps_now == kSteps && whole_lanes) walk(Flag<true>{}); else walk(Flag<false>{});
         }
         tile0 -= tile;
     };
@@ -512,12 +509,12 @@ struct Split {
 };
 
 // Fewer workgroups than this leave CUs idle for longer than a second reading takes.
-constexpr int64_t kSplitBelow = 128, kSplitTo = 512;
+constexpr int64_t kSplitBelow = 128, kSplitTo = 256;
 
 Split split_of(int64_t B, int64_t T, int32_t D, int lane_columns)
 {
     const int64_t groups = B * ceil_div(D, kWave * lane_columns), tiles = ceil_div(T, kTile);
-    int64_t spans = groups < kSplitBelow ? ceil_div(kSplitTo, groups) : 1;
+    int64_t spans = groups < kSplitBelow ? kSplitTo / groups : 1;
     spans = spans < tiles ? spans : tiles;
     spans = spans < kMaxSpans ? spans : kMaxSpans;
     if (spans <= 1) return {1, round_up(T, kTile), 0};
@@ -540,7 +537,7 @@ bool share(const typename E::T *a, int64_t lda, const typename E::T *b, int64_t 
 
 int check_sizes(int64_t B, int64_t T, int32_t D)
 {
-    return B < 0 || B > CX_MAX_SEQUENCES || T < 0 || T > kMaxSeq || D < 1 || D > kMaxColumns ? CX_ERR_SHAPE : CX_OK;
+    return B < 0 || B > CX_MAX_SEQUENCES || B * D > (int64_t(1) << 31) || T < 0 || T > kMaxSeq || D < 1 || D > kMaxColumns ? CX_ERR_SHAPE : CX_OK;
 }
 
 template <class E>
@@ -567,7 +564,7 @@ int scan(const typename E::T *f, int64_t ldf, const typename E::T *x, int64_t ld
     if (split.bytes > 0 && workspace_bytes < split.bytes) return CX_ERR_SHAPE;
     if (misaligned_to(f, kElem) || misaligned_to(x, kElem) || misaligned_to(y, kElem) || misaligned_to(states, 4) ||
         misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const uint64_t y_bytes = span(B * T, ldy, D, kElem), states_bytes = B * ceil_div(T, CX_SCAN_CHUNK) * D * 4;
+    const uint64_t y_bytes = span(B * T, ldy, D, kElem), states_bytes = B * ceil_div(T, kSteps) * D * 4;
     if (share<E>(y, ldy, f, ldf, B * T, D) || share<E>(y, ldy, x, ldx, B * T, D) || overlap(y, y_bytes, reset, B * T) ||
         overlap(y, y_bytes, h0, state_bytes) || overlap(y, y_bytes, h_last, state_bytes) || overlap(y, y_bytes, states, states_bytes) ||
         overlap(states, states_bytes, h0, state_bytes) || overlap(states, states_bytes, h_last, state_bytes)) return CX_ERR_ALIAS;
@@ -575,10 +572,11 @@ int scan(const typename E::T *f, int64_t ldf, const typename E::T *x, int64_t ld
     a.f = f; a.ldf = ldf; a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy;
     a.reset = reset; a.h0 = h0; a.h_last = h_last; a.states = states;
     a.maps = static_cast<float *>(workspace);
-    a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
-    const int64_t pieces = ceil_div(T, kForward);
-    const dim3 grid(static_cast<unsigned>(B), split.spans, static_cast<unsigned>(ceil_div(D, kWave * columns_of_lane<E>(D))));
-    const dim3 block(static_cast<unsigned>(pieces < kTile / kForward ? pieces : kTile / kForward) * kWave);
+    a.B = B; a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
+    a.slabs = static_cast<int32_t>(ceil_div(D, kWave * columns_of_lane<E>(D)));
+    const int64_t pieces = ceil_div(T, kSteps);
+    const dim3 grid(static_cast<unsigned>(B * a.slabs), split.spans);
+    const dim3 block(static_cast<unsigned>(pieces < kWaves ? pieces : kWaves) * kWave);
     const auto launch = [&](auto lane_columns) -> int {
         constexpr int N = decltype(lane_columns)::value;
         if (split.spans > 1) {
@@ -621,7 +619,7 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
     if (split.bytes > 0 && workspace_bytes < split.bytes) return CX_ERR_SHAPE;
     if (misaligned_to(f, kElem) || misaligned_to(x, kElem) || misaligned_to(dy, kElem) || misaligned_to(df, kElem) ||
         misaligned_to(dx, kElem) || misaligned_to(states, 4) || misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const uint64_t states_bytes = B * ceil_div(T, CX_SCAN_CHUNK) * D * 4;
+    const uint64_t states_bytes = B * ceil_div(T, kSteps) * D * 4;
     const typename E::T *outs[2] = {df, dx};
     const int64_t lds[2] = {lddf, lddx};
     for (int k = 0; k < 2; ++k) {
@@ -635,10 +633,11 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
     a.f = f; a.ldf = ldf; a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.df = df; a.lddf = lddf; a.dx = dx; a.lddx = lddx;
     a.reset = reset; a.states_in = states; a.dh_last = dh_last; a.dh0 = dh0;
     a.maps = static_cast<float *>(workspace);
-    a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
-    const int64_t pieces = ceil_div(T, kGrad);
-    const dim3 grid(static_cast<unsigned>(B), split.spans, static_cast<unsigned>(ceil_div(D, kWave * columns_of_lane<E>(D))));
-    const dim3 block(static_cast<unsigned>(pieces < kTile / kGrad ? pieces : kTile / kGrad) * kWave);
+    a.B = B; a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
+    a.slabs = static_cast<int32_t>(ceil_div(D, kWave * columns_of_lane<E>(D)));
+    const int64_t pieces = ceil_div(T, kSteps);
+    const dim3 grid(static_cast<unsigned>(B * a.slabs), split.spans);
+    const dim3 block(static_cast<unsigned>(pieces < kWaves ? pieces : kWaves) * kWave);
     const auto launch = [&](auto lane_columns) -> int {
         constexpr int N = decltype(lane_columns)::value;
         if (split.spans > 1) {
