@@ -45,10 +45,11 @@ struct Columns {                            // the columns of a row that a lane 
         return w;
     }
     __device__ __forceinline__ void load(const typename E::T *row, float (&v)[E::kPer16]) const { E::unpack(raw(row), v); }
+    template <bool THROUGH = false>
     __device__ __forceinline__ void store(typename E::T *row, const float (&v)[E::kPer16]) const
     {
         if (n == E::kPer16) {
-            store16<E>(row + first, E::pack(v));
+            if (THROUGH) store16_through<E>(row + first, E::pack(v)); else store16<E>(row + first, E::pack(v));
         } else {
 #pragma unroll
             for (int j = 0; j < E::kPer16; ++j)
@@ -58,6 +59,13 @@ struct Columns {                            // the columns of a row that a lane 
 };
 
 template <class E>
+__device__ __forceinline__ typename E::T element(const u4 &w, int j)
+{
+    if constexpr (E::kPer16 == 4) return __uint_as_float(w[j]);
+    else return static_cast<typename E::T>(w[j / 2] >> (16 * (j & 1)));
+}
+
+template <class E>
 __device__ __forceinline__ Columns<E> columns_of(int lane, int lanes, int slab, int D)
 {
     const int64_t first = (static_cast<int64_t>(slab) * lanes + lane) * E::kPer16;
@@ -65,8 +73,8 @@ __device__ __forceinline__ Columns<E> columns_of(int lane, int lanes, int slab, 
     return {first, left >= E::kPer16 ? E::kPer16 : left > 0 ? static_cast<int>(left) : 0};
 }
 
-// ROWS tokens a group of lanes: as many reads of the table in flight.
-template <class E, int ROWS>
+// ROWS tokens a group of lanes: as many reads of the table in flight.  THROUGH: the results are larger than the caches.
+template <class E, int ROWS, bool THROUGH>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(const typename E::T *table, int64_t ld, int32_t V, int32_t D, const int32_t *tokens,
                                                           int64_t N, float scale, typename E::T *out, int64_t ld_out, int shift)
 {
@@ -93,7 +101,7 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const typename E::T *t
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
-        if (n0 + r < N) c.store(out + (w * N + n0 + r) * ld_out, v[r]);
+        if (n0 + r < N) c.template store<THROUGH>(out + (w * N + n0 + r) * ld_out, v[r]);
 }
 
 struct Sorted {
@@ -217,6 +225,7 @@ struct GradArgs {
     int64_t ld, N, piece_ld;                // piece_ld: D in whole vectors
     int32_t V, D, chunks, chunk_blocks;
     float scale;
+    uint32_t per_row;                       // 2^32 / D, rounded down
     int shift, piece, slabs, fills, turn;   // lanes of a group (log2), tokens of a piece, groups to a row, workgroups to 64 rows
 };
 
@@ -327,6 +336,11 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const GradArgs<E> a)
         const typename E::T *from = a.g_in ? a.g_in + w * a.ld + v0 * a.D : nullptr;
         typename E::T *to = a.g_out + w * a.ld + v0 * a.D;
         constexpr int kPer = E::kPer16, kAhead = 4;
+        // at / D by a product that is at most one too small
+        const auto row_of = [&](int at) {
+            const int r = static_cast<int>(__umulhi(static_cast<unsigned>(at), a.per_row));
+            return (r + 1) * a.D <= at ? r + 1 : r;
+        };
         const int vectors = (elements + kPer - 1) / kPer, each = (vectors + a.fills - 1) / a.fills;
         int q = block % a.fills * each;
         const int end = q + each < vectors ? q + each : vectors;
@@ -341,14 +355,45 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const GradArgs<E> a)
                 for (int k = 0; k < kAhead; ++k) store16<E>(to + (q + k * kThreads) * kPer, v[k]);
             }
         }
-        for (; q < end; q += kThreads) {
-            const int first = q * kPer, last = (first + kPer < elements ? first + kPer : elements) - 1;
-            const int r0 = first / a.D, r1 = last / a.D;
-            if (first + kPer <= elements && ((word >> r0) & ((2ull << (r1 - r0)) - 1)) == 0) {
-                store16<E>(to + first, from ? load16<E>(from + first) : u4{});
-            } else {
-                for (int at = first; at <= last; ++at)
-                    if (!((word >> (at / a.D)) & 1)) to[at] = from ? from[at] : E::narrow(0.0f);
+        for (; q < end; q += kAhead * kThreads) {
+            u4 v[kAhead];
+            unsigned wanted[kAhead];                    // bit j: element j of the vector is of a row that no token names
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int first = (q + k * kThreads) * kPer, left = elements - first;
+                v[k] = u4{};
+                wanted[k] = 0;
+                if (q + k * kThreads >= end) continue;
+                if (left >= kPer) {
+                    if (from) v[k] = load16<E>(from + first);
+                    wanted[k] = (1u << kPer) - 1;
+                } else {                                // the last vector hangs over the rows' end
+                    if (from) v[k] = Columns<E>{first, left}.raw(from);
+                    wanted[k] = (1u << left) - 1;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int first = (q + k * kThreads) * kPer;
+                if (wanted[k] == 0) continue;
+                const int r0 = row_of(first), r1 = first + kPer <= (r0 + 1) * a.D ? r0 : row_of((first + kPer < elements ? first + kPer : elements) - 1);
+                const uint64_t rows_of_it = (2ull << (r1 - r0)) - 1, hit = (word >> r0) & rows_of_it;
+                if (hit == rows_of_it) continue;
+                if (hit != 0) {
+                    int row = 0, next = (r0 + 1) * a.D;
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) {
+                        if (first + j == next) { ++row; next += a.D; }
+                        if ((hit >> row) & 1) wanted[k] &= ~(1u << j);
+                    }
+                }
+                if (wanted[k] == (1u << kPer) - 1) {
+                    store16<E>(to + first, v[k]);
+                } else if (wanted[k] != 0) {
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j)
+                        if ((wanted[k] >> j) & 1) to[first + j] = element<E>(v[k], j);
+                }
             }
         }
     }
@@ -450,13 +495,18 @@ int lookup(const typename E::T *x, int64_t ld, int32_t W, int64_t offset, int32_
     if (overlap(out, out_bytes, x, span(W, ld, offset + static_cast<int64_t>(V) * D, kElem)) || overlap(out, out_bytes, tokens, W * N * 4)) return CX_ERR_ALIAS;
     const int shift = lanes_shift<E>(D), groups = kThreads >> shift;
     const int64_t slabs = ceil_div(ceil_div(D, E::kPer16), 1 << shift);
-    // Four rows a group from 4,096 workgroups of one row on
-    const bool many = W * N * slabs >= int64_t(4096) * groups;
-    const int64_t blocks = ceil_div(N, static_cast<int64_t>(groups) * (many ? 4 : 1));
-    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(slabs), W);
+    // Four rows a group from 4,096 workgroups of one row on; from 64 MB on, results that go past the caches: 16 x 4,096 tokens of 768 columns
+    // take 35 us with ordinary stores and 26 without in bfloat16, 63 and 59 in float32
+    const bool many = W * N * slabs >= int64_t(4096) * groups, large = many && W * N * D * kElem >= int64_t(64) << 20;
+    const dim3 grid(static_cast<unsigned>(ceil_div(N, static_cast<int64_t>(groups) * (many ? 4 : 1))), static_cast<unsigned>(slabs), W);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (many) hipLaunchKernelGGL((lookup_kernel<E, 4>), grid, dim3(kThreads), 0, st, x + offset, ld, V, D, tokens, N, scale, out, ld_out, shift);
-    else hipLaunchKernelGGL((lookup_kernel<E, 1>), grid, dim3(kThreads), 0, st, x + offset, ld, V, D, tokens, N, scale, out, ld_out, shift);
+    const auto launch = [&](auto rows, auto through) {
+        hipLaunchKernelGGL((lookup_kernel<E, decltype(rows)::value, decltype(through)::value>), grid, dim3(kThreads), 0, st, x + offset, ld, V, D,
+                           tokens, N, scale, out, ld_out, shift);
+    };
+    if (large) launch(std::integral_constant<int, 4>{}, std::true_type{});
+    else if (many) launch(std::integral_constant<int, 4>{}, std::false_type{});
+    else launch(std::integral_constant<int, 1>{}, std::false_type{});
     return launched();
 }
 
@@ -468,8 +518,9 @@ struct GradSpace {
 GradSpace grad_space(int32_t W, int64_t N, int32_t V, int32_t D)
 {
     GradSpace s{};
-    // tokens of a piece: few, so that there are many; more of them where a list of all tokens would leave thousands of sums to join
-    s.piece = N <= 16384 ? 16 : 64;
+    // tokens of a piece: few, so that there are many (1,000 tokens of four workers, 129 columns: sums in 9.5 us with 8, 13.6 with 16); more of
+    // them where a list of all tokens would leave thousands of sums to join
+    s.piece = N <= 2048 ? 8 : N <= 16384 ? 16 : 64;
     s.chunks = ceil_div(N, s.piece);
     s.named = 0;
     s.total = round_up(W * ceil_div(V, 64) * 8, 256);
@@ -505,7 +556,7 @@ int grad(const typename E::T *dout, int64_t ld_dout, const int32_t *tokens, int3
     int32_t *total = reinterpret_cast<int32_t *>(base + space.total);
     Crossing *crossing = reinterpret_cast<Crossing *>(base + space.crossing);
     GradArgs<E> a{dout, ld_dout, sorted, named, total, crossing, reinterpret_cast<float *>(base + space.pieces), g_in ? g_in + offset : nullptr, g_out + offset,
-                  ld, N, round_up(D, 8), V, D, static_cast<int32_t>(space.chunks), 0, scale, lanes_shift<E>(D), space.piece, 0, 1, 1};
+                  ld, N, round_up(D, 8), V, D, static_cast<int32_t>(space.chunks), 0, scale, static_cast<uint32_t>(0xffffffffu / static_cast<uint32_t>(D)), lanes_shift<E>(D), space.piece, 0, 1, 1};
     const int groups = kThreads >> a.shift;
     a.slabs = static_cast<int>(ceil_div(ceil_div(D, E::kPer16), 1 << a.shift));
     const hipStream_t st = static_cast<hipStream_t>(stream);

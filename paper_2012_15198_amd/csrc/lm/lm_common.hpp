@@ -97,6 +97,10 @@ __device__ __forceinline__ u4 load16(const typename E::T *p) { return *reinterpr
 template <class E>
 __device__ __forceinline__ void store16(typename E::T *p, const u4 &v) { *reinterpret_cast<typename E::Vec *>(p) = v; }
 
+// For results so large that no cache keeps them for their reader: they do not push out what is being read.
+template <class E>
+__device__ __forceinline__ void store16_through(typename E::T *p, const u4 &v) { __builtin_nontemporal_store(v, reinterpret_cast<typename E::Vec *>(p)); }
+
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }     // one instruction, 1 ulp
 __device__ __forceinline__ float rcp_fast(float v) { return __builtin_amdgcn_rcpf(v); }       // likewise

@@ -30,6 +30,7 @@ EXPORTS = ["cx_lm_abi_version", "cx_embed_workspace", "cx_scan_workspace", "cx_s
 _lib = None
 _torch = None
 _dtypes = {}                     # "", "_bf16", "_f16" -> the torch type of the matrices
+_calls = {}                      # name -> the library's function
 
 
 def lib() -> ctypes.CDLL:
@@ -67,6 +68,7 @@ def lib() -> ctypes.CDLL:
             getattr(L, name + suffix).argtypes = args
     for name in EXPORTS:
         getattr(L, name).restype = ctypes.c_int
+        _calls[name] = getattr(L, name)
     _dtypes.update({"": torch.float32, "_bf16": torch.bfloat16, "_f16": torch.float16})
     _lib, _torch = L, torch
     return L
@@ -75,6 +77,12 @@ def lib() -> ctypes.CDLL:
 def _ok(fn: str, status: int) -> None:
     if status != 0:
         raise CxError(fn, status)
+
+
+def _call(name, *args) -> None:
+    status = _calls[name](*args)
+    if status != 0:
+        raise CxError(name, status)
 
 
 # ------------------------------------------------------------------------------------------------------------- checks
@@ -181,7 +189,8 @@ def cx_distill_workspace(N: int, V: int) -> int:
 
 # ---------------------------------------------------------------------------------------------------------- embeddings
 def _lookup(name, suffix, x, tokens, out, offset, V, scale, stream):
-    L = _lib or lib()
+    if _lib is None:
+        lib()
     dtype, device = _dtypes[suffix], x.get_device()
     if len(tokens.shape) != 2:
         raise ValueError(f"{name}: tokens: expected int32 [W][N]")
@@ -193,7 +202,7 @@ def _lookup(name, suffix, x, tokens, out, offset, V, scale, stream):
         raise ValueError(f"{name}: a table of {V} x {D} at {offset} does not fit rows of {x.shape[1]}")
     tp = _dense(name, "tokens", tokens, _torch.int32, (W, N), device)
     _on_device(name, device)
-    _ok(name, getattr(L, name)(x.data_ptr(), ld, W, offset, V, D, tp, N, scale, out.data_ptr(), ld_out, cxmix._stream(stream)))
+    _call(name, x.data_ptr(), ld, W, offset, V, D, tp, N, scale, out.data_ptr(), ld_out, cxmix._stream(stream))
 
 
 def cx_embed_lookup(x, tokens, out, offset: int, V: int, scale: float = 1.0, stream=None):
@@ -210,7 +219,8 @@ def cx_embed_lookup_f16(x, tokens, out, offset: int, V: int, scale: float = 1.0,
 
 
 def _embed_grad(name, suffix, dout, tokens, g_in, g_out, offset, V, scale, workspace, stream):
-    L = _lib or lib()
+    if _lib is None:
+        lib()
     dtype, device = _dtypes[suffix], g_out.get_device()
     if len(tokens.shape) != 2:
         raise ValueError(f"{name}: tokens: expected int32 [W][N]")
@@ -228,8 +238,8 @@ def _embed_grad(name, suffix, dout, tokens, g_in, g_out, offset, V, scale, works
         raise ValueError(f"{name}: a table of {V} x {D} at {offset} does not fit rows of {fits}")
     tp = _dense(name, "tokens", tokens, _torch.int32, (W, N), device)
     work = _scratch(name, workspace, "cx_embed_workspace", (W, N, V, D), device, stream)
-    _ok(name, getattr(L, name)(dout.data_ptr(), ld_dout, tp, W, N, None if g_in is None else g_in.data_ptr(), g_out.data_ptr(), ld, offset, V, D,
-                               scale, *_span(work), cxmix._stream(stream)))
+    _call(name, dout.data_ptr(), ld_dout, tp, W, N, None if g_in is None else g_in.data_ptr(), g_out.data_ptr(), ld, offset, V, D,
+                               scale, *_span(work), cxmix._stream(stream))
 
 
 def cx_embed_grad(dout, tokens, g_in, g_out, offset: int, V: int, scale: float = 1.0, workspace=None, stream=None):
@@ -264,7 +274,8 @@ def _sequences(name, rows, T, *ends):
 
 
 def _scan(name, suffix, f, x, y, T, h0, h_last, reset, states, workspace, stream):
-    L = _lib or lib()
+    if _lib is None:
+        lib()
     dtype, device, f32 = _dtypes[suffix], f.get_device(), _torch.float32
     ldf = _matrix(name, "f", f, dtype, None, None, device)
     rows, D = f.shape
@@ -276,8 +287,8 @@ def _scan(name, suffix, f, x, y, T, h0, h_last, reset, states, workspace, stream
     sp = _optional(name, "states", states, f32, (B, -(-T // CX_SCAN_CHUNK), D), device)
     rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
     work = _scratch(name, workspace, None if T <= CX_SCAN_CHUNK else "cx_scan_workspace", (B, T, D), device, stream)
-    _ok(name, getattr(L, name)(f.data_ptr(), ldf, x.data_ptr(), ldx, y.data_ptr(), ldy, B, T, D, rp, hp, lp, sp, *_span(work),
-                               cxmix._stream(stream)))
+    _call(name, f.data_ptr(), ldf, x.data_ptr(), ldx, y.data_ptr(), ldy, B, T, D, rp, hp, lp, sp, *_span(work),
+                               cxmix._stream(stream))
 
 
 def cx_gated_scan(f, x, y, T: int, h0=None, h_last=None, reset=None, states=None, workspace=None, stream=None):
@@ -294,7 +305,8 @@ def cx_gated_scan_f16(f, x, y, T: int, h0=None, h_last=None, reset=None, states=
 
 
 def _scan_grad(name, suffix, f, x, dy, df, dx, T, states, dh_last, dh0, reset, workspace, stream):
-    L = _lib or lib()
+    if _lib is None:
+        lib()
     dtype, device, f32 = _dtypes[suffix], f.get_device(), _torch.float32
     ldf = _matrix(name, "f", f, dtype, None, None, device)
     rows, D = f.shape
@@ -308,8 +320,8 @@ def _scan_grad(name, suffix, f, x, dy, df, dx, T, states, dh_last, dh0, reset, w
     hp = _optional(name, "dh0", dh0, f32, (B, D), device)
     rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
     work = _scratch(name, workspace, None if T <= CX_SCAN_CHUNK else "cx_scan_workspace", (B, T, D), device, stream)
-    _ok(name, getattr(L, name)(f.data_ptr(), ldf, x.data_ptr(), ldx, dy.data_ptr(), lddy, df.data_ptr(), lddf, dx.data_ptr(), lddx, B, T, D, rp, sp,
-                               lp, hp, *_span(work), cxmix._stream(stream)))
+    _call(name, f.data_ptr(), ldf, x.data_ptr(), ldx, dy.data_ptr(), lddy, df.data_ptr(), lddf, dx.data_ptr(), lddx, B, T, D, rp, sp,
+                               lp, hp, *_span(work), cxmix._stream(stream))
 
 
 def cx_gated_scan_grad(f, x, dy, df, dx, T: int, states, dh_last=None, dh0=None, reset=None, workspace=None, stream=None):
@@ -327,7 +339,8 @@ def cx_gated_scan_grad_f16(f, x, dy, df, dx, T: int, states, dh_last=None, dh0=N
 
 # ------------------------------------------------------------------------------------------------------------ token scores
 def _scores(name, suffix, z, tokens, logp, entropy, top_ids, top_logp, scale, workspace, stream):
-    L = _lib or lib()
+    if _lib is None:
+        lib()
     device, f32, i32 = z.get_device(), _torch.float32, _torch.int32
     ld = _matrix(name, "z", z, _dtypes[suffix], None, None, device)
     N, V = z.shape
@@ -343,7 +356,7 @@ def _scores(name, suffix, z, tokens, logp, entropy, top_ids, top_logp, scale, wo
         ip = _dense(name, "top_ids", top_ids, i32, (N, K), device)
         pp = _dense(name, "top_logp", top_logp, f32, (N, K), device)
     work = _scratch(name, workspace, "cx_scores_workspace", (N, V, K), device, stream)
-    _ok(name, getattr(L, name)(z.data_ptr(), ld, N, V, tp, scale, lp, ep, K, ip, pp, *_span(work), cxmix._stream(stream)))
+    _call(name, z.data_ptr(), ld, N, V, tp, scale, lp, ep, K, ip, pp, *_span(work), cxmix._stream(stream))
 
 
 def cx_token_scores(z, tokens, logp, entropy=None, top_ids=None, top_logp=None, scale: float = 1.0, workspace=None, stream=None):
@@ -375,14 +388,15 @@ def _targets(name, suffix, z, ids, t, labels, device):
 
 
 def _distill_loss(name, suffix, z, ids, t, labels, loss, stats, tau, w_kl, w_ce, workspace, stream):
-    L = _lib or lib()
+    if _lib is None:
+        lib()
     device = z.get_device()
     head = _targets(name, suffix, z, ids, t, labels, device)
     N, V = head[2:4]
     lp = _dense(name, "loss", loss, _torch.float32, (N,), device)
     sp = _optional(name, "stats", stats, _torch.float32, (N, 4), device)
     work = _scratch(name, workspace, "cx_distill_workspace", (N, V), device, stream)
-    _ok(name, getattr(L, name)(*head, tau, w_kl, w_ce, lp, sp, *_span(work), cxmix._stream(stream)))
+    _call(name, *head, tau, w_kl, w_ce, lp, sp, *_span(work), cxmix._stream(stream))
 
 
 def cx_distill_loss(z, ids, t, labels, loss, stats, tau: float, w_kl: float, w_ce: float, workspace=None, stream=None):
@@ -400,7 +414,8 @@ def cx_distill_loss_f16(z, ids, t, labels, loss, stats, tau: float, w_kl: float,
 
 
 def _distill_grad(name, suffix, z, ids, t, labels, stats, gout, dz, tau, w_kl, w_ce, stream):
-    L = _lib or lib()
+    if _lib is None:
+        lib()
     device = z.get_device()
     head = _targets(name, suffix, z, ids, t, labels, device)
     N, V = head[2:4]
@@ -408,7 +423,7 @@ def _distill_grad(name, suffix, z, ids, t, labels, stats, gout, dz, tau, w_kl, w
     gp = _dense(name, "gout", gout, _torch.float32, (N,), device)
     ld_dz = _matrix(name, "dz", dz, _dtypes[suffix], N, V, device)
     _on_device(name, device)
-    _ok(name, getattr(L, name)(*head, tau, w_kl, w_ce, sp, gp, dz.data_ptr(), ld_dz, cxmix._stream(stream)))
+    _call(name, *head, tau, w_kl, w_ce, sp, gp, dz.data_ptr(), ld_dz, cxmix._stream(stream))
 
 
 def cx_distill_grad(z, ids, t, labels, stats, gout, dz, tau: float, w_kl: float, w_ce: float, stream=None):
@@ -425,7 +440,8 @@ def cx_distill_grad_f16(z, ids, t, labels, stats, gout, dz, tau: float, w_kl: fl
 
 
 def _distill_step(name, suffix, z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream):
-    L = _lib or lib()
+    if _lib is None:
+        lib()
     device = z.get_device()
     head = _targets(name, suffix, z, ids, t, labels, device)
     N, V = head[2:4]
@@ -433,7 +449,7 @@ def _distill_step(name, suffix, z, ids, t, labels, gout, loss, dz, tau, w_kl, w_
     lp = _dense(name, "loss", loss, _torch.float32, (N,), device)
     ld_dz = _matrix(name, "dz", dz, _dtypes[suffix], N, V, device)
     work = _scratch(name, workspace, "cx_distill_workspace", (N, V), device, stream)
-    _ok(name, getattr(L, name)(*head, tau, w_kl, w_ce, gp, lp, dz.data_ptr(), ld_dz, *_span(work), cxmix._stream(stream)))
+    _call(name, *head, tau, w_kl, w_ce, gp, lp, dz.data_ptr(), ld_dz, *_span(work), cxmix._stream(stream))
 
 
 def cx_distill_step(z, ids, t, labels, gout, loss, dz, tau: float, w_kl: float, w_ce: float, workspace=None, stream=None):
