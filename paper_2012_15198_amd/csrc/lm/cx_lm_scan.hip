@@ -282,9 +282,10 @@ __device__ __forceinline__ void keep_first(const ScanArgs<E> &a, const LaneColum
 template <bool V>
 using Flag = std::integral_constant<bool, V>;
 
-// Grid (slabs of columns of sequences, spans): workgroups that run together read whole rows.  ONLY_MAP: the first launch of a split call.
+// Grid (slabs of columns of sequences, spans): workgroups that run together read whole rows.  ONLY_MAP: the first launch of a split call,
+// over the spans that another one follows.
 template <class E, int N, bool RESETS, bool ONLY_MAP>
-__global__ __launch_bounds__(kWaves *kWave) void scan_kernel(const ScanArgs<E> a)
+__global__ __launch_bounds__(kWaves *kWave, N == 1 ? 4 : 2) void scan_kernel(const ScanArgs<E> a)
 {
     __shared__ Exchange<N> lds;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_kernel(const ScanArgs<E> a
     float carry[N];
     Map whole[N];
     if constexpr (ONLY_MAP) {
-        if (span == 0 && wave == 0) keep_first<E, N>(a, c, b, a.h0);
+        if (blockIdx.y == 0 && wave == 0) keep_first<E, N>(a, c, b, a.h0);
 #pragma unroll
         for (int j = 0; j < N; ++j) whole[j] = {1.0f, 0.0f};
     } else {
@@ -376,7 +377,7 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_grad_kernel(const ScanArgs
     __shared__ Exchange<N> lds;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
     const int64_t b = blockIdx.x / a.slabs;
-    const int span = blockIdx.y, slab = static_cast<int>(blockIdx.x) % a.slabs;
+    const int span = blockIdx.y + (ONLY_MAP ? 1 : 0), slab = static_cast<int>(blockIdx.x) % a.slabs;
     const LaneColumns<E, N> c((slab * kWave + lane) * N, a.D);
     const bool whole_lanes = __ballot(c.whole()) == ~0ull;
     const int64_t row0 = b * a.T_, begin = span * a.span_steps, end = begin + a.span_steps < a.T_ ? begin + a.span_steps : a.T_;
@@ -399,7 +400,7 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_grad_kernel(const ScanArgs
     float carry[N];
     Map whole[N];
     if constexpr (ONLY_MAP) {
-        if (span == 0 && wave == 0) keep_first<E, N>(a, c, b, a.dh_last);
+        if (blockIdx.y == 0 && wave == 0) keep_first<E, N>(a, c, b, a.dh_last);
 #pragma unroll
         for (int j = 0; j < N; ++j) whole[j] = {1.0f, 0.0f};
     } else {
@@ -508,13 +509,17 @@ struct Split {
     int64_t span_steps, bytes;
 };
 
-// Fewer workgroups than this leave CUs idle for longer than a second reading takes.
-constexpr int64_t kSplitBelow = 128, kSplitTo = 256;
+// Fewer workgroups than kSplitBelow leave CUs idle for longer than a second reading takes.  They become as many as the CUs take at once, one
+// each, or two of the forward pass on float32 columns: one sequence of 16,381 x 1,024 takes 43 us forward in bfloat16 with 256 and 51
+// with 512, in float32 68 and 63.
+constexpr int64_t kSplitBelow = 128;
 
-Split split_of(int64_t B, int64_t T, int32_t D, int lane_columns)
+template <class E>
+Split split_of(int64_t B, int64_t T, int32_t D, bool forward)
 {
+    const int lane_columns = columns_of_lane<E>(D);
     const int64_t groups = B * ceil_div(D, kWave * lane_columns), tiles = ceil_div(T, kTile);
-    int64_t spans = groups < kSplitBelow ? kSplitTo / groups : 1;
+    int64_t spans = groups < kSplitBelow ? (forward && lane_columns == 1 ? 512 : 256) / groups : 1;
     spans = spans < tiles ? spans : tiles;
     spans = spans < kMaxSpans ? spans : kMaxSpans;
     if (spans <= 1) return {1, round_up(T, kTile), 0};
@@ -559,7 +564,7 @@ int scan(const typename E::T *f, int64_t ldf, const typename E::T *x, int64_t ld
     }
     if (!f || !x || !y) return CX_ERR_NULL;
     if (bad_matrix(B * T, ldf, D) || bad_matrix(B * T, ldx, D) || bad_matrix(B * T, ldy, D)) return CX_ERR_SHAPE;
-    const Split split = split_of(B, T, D, columns_of_lane<E>(D));
+    const Split split = split_of<E>(B, T, D, true);
     if (split.bytes > 0 && !workspace) return CX_ERR_NULL;
     if (split.bytes > 0 && workspace_bytes < split.bytes) return CX_ERR_SHAPE;
     if (misaligned_to(f, kElem) || misaligned_to(x, kElem) || misaligned_to(y, kElem) || misaligned_to(states, 4) ||
@@ -575,13 +580,13 @@ int scan(const typename E::T *f, int64_t ldf, const typename E::T *x, int64_t ld
     a.B = B; a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
     a.slabs = static_cast<int32_t>(ceil_div(D, kWave * columns_of_lane<E>(D)));
     const int64_t pieces = ceil_div(T, kSteps);
-    const dim3 grid(static_cast<unsigned>(B * a.slabs), split.spans);
+    const dim3 grid(static_cast<unsigned>(B * a.slabs), split.spans), maps(grid.x, split.spans - 1);
     const dim3 block(static_cast<unsigned>(pieces < kWaves ? pieces : kWaves) * kWave);
     const auto launch = [&](auto lane_columns) -> int {
         constexpr int N = decltype(lane_columns)::value;
         if (split.spans > 1) {
-            if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, true>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((scan_kernel<E, N, false, true>), grid, block, 0, st, a);
+            if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, true>), maps, block, 0, st, a);
+            else hipLaunchKernelGGL((scan_kernel<E, N, false, true>), maps, block, 0, st, a);
             if (launched() != CX_OK) return CX_ERR_HIP;
         }
         if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, false>), grid, block, 0, st, a);
@@ -614,7 +619,7 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
     if (!f || !x || !dy || !df || !dx || !states) return CX_ERR_NULL;
     if (bad_matrix(B * T, ldf, D) || bad_matrix(B * T, ldx, D) || bad_matrix(B * T, lddy, D) || bad_matrix(B * T, lddf, D) ||
         bad_matrix(B * T, lddx, D)) return CX_ERR_SHAPE;
-    const Split split = split_of(B, T, D, columns_of_lane<E>(D));
+    const Split split = split_of<E>(B, T, D, false);
     if (split.bytes > 0 && !workspace) return CX_ERR_NULL;
     if (split.bytes > 0 && workspace_bytes < split.bytes) return CX_ERR_SHAPE;
     if (misaligned_to(f, kElem) || misaligned_to(x, kElem) || misaligned_to(dy, kElem) || misaligned_to(df, kElem) ||
@@ -636,13 +641,13 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
     a.B = B; a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
     a.slabs = static_cast<int32_t>(ceil_div(D, kWave * columns_of_lane<E>(D)));
     const int64_t pieces = ceil_div(T, kSteps);
-    const dim3 grid(static_cast<unsigned>(B * a.slabs), split.spans);
+    const dim3 grid(static_cast<unsigned>(B * a.slabs), split.spans), maps(grid.x, split.spans - 1);
     const dim3 block(static_cast<unsigned>(pieces < kWaves ? pieces : kWaves) * kWave);
     const auto launch = [&](auto lane_columns) -> int {
         constexpr int N = decltype(lane_columns)::value;
         if (split.spans > 1) {
-            if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, true>), grid, block, 0, st, a);
-            else hipLaunchKernelGGL((scan_grad_kernel<E, N, false, true>), grid, block, 0, st, a);
+            if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, true>), maps, block, 0, st, a);
+            else hipLaunchKernelGGL((scan_grad_kernel<E, N, false, true>), maps, block, 0, st, a);
             if (launched() != CX_OK) return CX_ERR_HIP;
         }
         if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, false>), grid, block, 0, st, a);
@@ -684,8 +689,9 @@ int cx_scan_workspace(int64_t B, int64_t T, int32_t D, int64_t *bytes)
     *bytes = 0;
     const int rc = check_sizes(B, T, D);
     if (rc != CX_OK || B == 0 || T == 0) return rc;
-    const int64_t wide = split_of(B, T, D, columns_of_lane<F32>(D)).bytes, narrow = split_of(B, T, D, columns_of_lane<Bf16>(D)).bytes;
-    *bytes = wide > narrow ? wide : narrow;
+    for (const int64_t n : {split_of<F32>(B, T, D, true).bytes, split_of<F32>(B, T, D, false).bytes, split_of<Bf16>(B, T, D, true).bytes,
+                            split_of<Bf16>(B, T, D, false).bytes})
+        *bytes = n > *bytes ? n : *bytes;
     return CX_OK;
 }
 
