@@ -149,6 +149,7 @@ struct RowGradient {
         const float d = z - m, e = exp2_fast(d * c);
         if (X == kDual) return __builtin_fmaf(soft, e, hard * second<X>(d, e, kLog2e));
         if (X == kSquare) return e * __builtin_fmaf(hard, e, soft);
+        if (X == kCube) return e * __builtin_fmaf(hard * e, e, soft);
         if (X == kFourth) return e * __builtin_fmaf(hard * e, e * e, soft);
         return (soft + hard) * e;
     }
@@ -356,7 +357,7 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
     a.parts = space.parts;
     a.part_stats = static_cast<Stats *>(workspace);
     const bool dual = a.w_kl != 0.0f && a.w_ce != 0.0f && a.tau != 1.0f;
-    const Extra sums = !dual ? kNone : a.tau == 2.0f ? kSquare : a.tau == 4.0f ? kFourth : kDual;
+    const Extra sums = !dual ? kNone : a.tau == 2.0f ? kSquare : a.tau == 3.0f ? kCube : a.tau == 4.0f ? kFourth : kDual;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     for (int64_t n0 = 0; n0 < N; n0 += 65535) {         // rows in slices of a grid's second dimension
         const unsigned rows = static_cast<unsigned>(N - n0 < 65535 ? N - n0 : 65535);
@@ -396,6 +397,7 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
         switch (sums) {
         case kDual: launch(std::integral_constant<Extra, kDual>{}); break;
         case kSquare: launch(std::integral_constant<Extra, kSquare>{}); break;
+        case kCube: launch(std::integral_constant<Extra, kCube>{}); break;
         case kFourth: launch(std::integral_constant<Extra, kFourth>{}); break;
         default: launch(std::integral_constant<Extra, kNone>{});
         }

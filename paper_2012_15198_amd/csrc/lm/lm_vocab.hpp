@@ -17,17 +17,18 @@ constexpr float kVanish = -200.0f;                      // exponents (base 2) fr
 
 // With e = 2^((z - m) c), s is the sum of e, and u
 //   kEntropy          the sum of e * log2(e)
-//   kDual             the sum of 2^((z - m) c2);  kSquare, kFourth: the same where c2 is 2 c or 4 c: a power of e by
-//                     multiplications.  A kernel whose loop has two exponentials an element is bound by them, not by memory.
-enum Extra { kNone, kEntropy, kDual, kSquare, kFourth };
-__host__ __device__ constexpr bool two_sums(Extra x) { return x == kDual || x == kSquare || x == kFourth; }
+//   kDual             the sum of 2^((z - m) c2);  kSquare, kCube, kFourth: the same where c2 is 2, 3 or 4 times c: a power of e by
+//                     multiplications.  Two exponentials an element bound the loop before memory does: loss and gradient of
+//                     8,192 x 65,536 bfloat16 logits take 403 us with one, 473 with two, 445 with one and its square.
+enum Extra { kNone, kEntropy, kDual, kSquare, kCube, kFourth };
+__host__ __device__ constexpr bool two_sums(Extra x) { return x == kDual || x == kSquare || x == kCube || x == kFourth; }
 
 // 2^((z - m) c2), d = z - m, e = 2^(d c)
 template <Extra X>
 __device__ __forceinline__ float second(float d, float e, float c2)
 {
     if (X == kDual) return __builtin_amdgcn_exp2f(d * c2);
-    return X == kFourth ? (e * e) * (e * e) : e * e;
+    return X == kFourth ? (e * e) * (e * e) : X == kCube ? e * e * e : e * e;
 }
 
 struct Stats {

@@ -80,6 +80,15 @@ def test_weights_and_temperatures(suffix, N, tau, w_kl, w_ce):
 
 
 @pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("tau", [2.0, 3.0, 4.0, 1.7])
+@pytest.mark.parametrize("N,V,K", [(3, 5_003, 7), (520, 901, 256), (2, 140_001, 20)])
+def test_both_terms_at_whole_and_other_temperatures(suffix, N, V, K, tau):
+    """Whole temperatures take powers of one exponential; rows of few and of many vectors, and beyond one workgroup's registers."""
+    z, ids, t, labels, gout = make(N, V, K, R.TYPES[suffix], 17)
+    compare(suffix, z, ids, t, labels, gout, tau, 0.6, 0.4, offset=1)
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
 @pytest.mark.parametrize("N,V", [(12, 6_000), (12, 30), (530, 700)])
 def test_masks_empty_rows_and_repeated_ids(suffix, N, V):
     dtype = R.TYPES[suffix]
