@@ -7,8 +7,8 @@
 // a lane composes the maps of its piece in registers, the pieces' maps are joined through LDS, and the lane then walks its
 // piece once more with the state that enters it.  So the data are read once, whatever the length.
 //
-//   lane       the columns of 4 bytes of every row (16-bit rows: two) and 16 consecutive steps: 64 lanes read whole lines of a row,
-//              and a walk needs no exchange between lanes
+//   lane       a column of every row (16-bit rows: two where there are enough) and 16 consecutive steps: 64 lanes read whole lines of a
+//              row, and a walk needs no exchange between lanes
 //   workgroup  8 wavefronts, one piece each = a tile of 128 steps, tile after tile; the loads of the next tile are
 //              issued before the present one is computed, into a second set of registers
 //   split      where columns are few (workgroups < kSplitBelow) the steps are also split over workgroups: a first launch composes
@@ -500,26 +500,36 @@ __global__ __launch_bounds__(256) void pass_kernel(const float *from, float *to,
     if (i < n) to[i] = from ? from[i] : 0.0f;
 }
 
-// Columns of a lane.
+// Workgroups from which the steps are not split: fewer leave CUs idle for longer than a second reading takes.
+constexpr int64_t kSplitBelow = 128, kUnits = 256;
+
+// Columns of a lane.  Two of 16 bits halve the loads.  One makes twice the workgroups, which is more where even those do not fill the card:
+// forward 16 sequences of 2,048 x 1,024 take 56 us in bfloat16 against 74 with two, 6 of 1,111 x 515 19 against 25; more than kUnits gain
+// nothing (18 sequences: 76 and 75).  The gradient's split costs less, so that it gains only where one column fills the card without a
+// split (16 sequences 90 us against 103, 12: 83 against 87, but 10: 83 against 69).  Up to 64 columns two would leave half the lanes idle
+// (64 sequences of 1,024 x 64: 16 us against 22, gradient 21 against 26).
 template <class E>
-int columns_of_lane(int32_t D) { return sizeof(typename E::T) == 2 && D > 1 ? 2 : 1; }
+int columns_of_lane(int64_t B, int32_t D, bool forward)
+{
+    if (sizeof(typename E::T) == 4 || D <= kWave) return 1;
+    const int64_t groups = B * ceil_div(D, kWave);
+    return groups > kUnits || (!forward && groups < kUnits * 3 / 4) ? 2 : 1;
+}
 
 struct Split {
     int spans;
     int64_t span_steps, bytes;
 };
 
-// Fewer workgroups than kSplitBelow leave CUs idle for longer than a second reading takes.  They become as many as the CUs take at once, one
-// each, or two of the forward pass on float32 columns: one sequence of 16,381 x 1,024 takes 43 us forward in bfloat16 with 256 and 51
-// with 512, in float32 68 and 63.
-constexpr int64_t kSplitBelow = 128;
-
+// Split calls become as many workgroups as the CUs take at once, one each, or two of the forward pass on single columns: one sequence of
+// 16,381 x 1,024 takes 40 us forward in bfloat16 with 512 and 49 with 256, in float32 63 and 68.
 template <class E>
 Split split_of(int64_t B, int64_t T, int32_t D, bool forward)
 {
-    const int lane_columns = columns_of_lane<E>(D);
+    const int lane_columns = columns_of_lane<E>(B, D, forward);
+    const bool two = forward && lane_columns == 1;
     const int64_t groups = B * ceil_div(D, kWave * lane_columns), tiles = ceil_div(T, kTile);
-    int64_t spans = groups < kSplitBelow ? (forward && lane_columns == 1 ? 512 : 256) / groups : 1;
+    int64_t spans = groups < kSplitBelow || (two && groups == kSplitBelow) ? (two ? 2 * kUnits : kUnits) / groups : 1;
     spans = spans < tiles ? spans : tiles;
     spans = spans < kMaxSpans ? spans : kMaxSpans;
     if (spans <= 1) return {1, round_up(T, kTile), 0};
@@ -578,23 +588,25 @@ int scan(const typename E::T *f, int64_t ldf, const typename E::T *x, int64_t ld
     a.reset = reset; a.h0 = h0; a.h_last = h_last; a.states = states;
     a.maps = static_cast<float *>(workspace);
     a.B = B; a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
-    a.slabs = static_cast<int32_t>(ceil_div(D, kWave * columns_of_lane<E>(D)));
+    a.slabs = static_cast<int32_t>(ceil_div(D, kWave * columns_of_lane<E>(B, D, true)));
     const int64_t pieces = ceil_div(T, kSteps);
     const dim3 grid(static_cast<unsigned>(B * a.slabs), split.spans), maps(grid.x, split.spans - 1);
     const dim3 block(static_cast<unsigned>(pieces < kWaves ? pieces : kWaves) * kWave);
     const auto launch = [&](auto lane_columns) -> int {
         constexpr int N = decltype(lane_columns)::value;
-        if (split.spans > 1) {
-            if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, true>), maps, block, 0, st, a);
-            else hipLaunchKernelGGL((scan_kernel<E, N, false, true>), maps, block, 0, st, a);
-            if (launched() != CX_OK) return CX_ERR_HIP;
+        if constexpr (N == 1) {                         // two columns are taken by calls of too many workgroups for a split
+            if (split.spans > 1) {
+                if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, true>), maps, block, 0, st, a);
+                else hipLaunchKernelGGL((scan_kernel<E, N, false, true>), maps, block, 0, st, a);
+                if (launched() != CX_OK) return CX_ERR_HIP;
+            }
         }
         if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, false>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((scan_kernel<E, N, false, false>), grid, block, 0, st, a);
         return launched();
     };
     if constexpr (sizeof(typename E::T) == 2)
-        if (D > 1) return launch(std::integral_constant<int, 2>{});
+        if (columns_of_lane<E>(B, D, true) == 2) return launch(std::integral_constant<int, 2>{});
     return launch(std::integral_constant<int, 1>{});
 }
 
@@ -639,7 +651,7 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
     a.reset = reset; a.states_in = states; a.dh_last = dh_last; a.dh0 = dh0;
     a.maps = static_cast<float *>(workspace);
     a.B = B; a.T_ = T; a.D = D; a.spans = split.spans; a.span_steps = split.span_steps;
-    a.slabs = static_cast<int32_t>(ceil_div(D, kWave * columns_of_lane<E>(D)));
+    a.slabs = static_cast<int32_t>(ceil_div(D, kWave * columns_of_lane<E>(B, D, false)));
     const int64_t pieces = ceil_div(T, kSteps);
     const dim3 grid(static_cast<unsigned>(B * a.slabs), split.spans), maps(grid.x, split.spans - 1);
     const dim3 block(static_cast<unsigned>(pieces < kWaves ? pieces : kWaves) * kWave);
@@ -655,7 +667,7 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
         return launched();
     };
     if constexpr (sizeof(typename E::T) == 2)
-        if (D > 1) return launch(std::integral_constant<int, 2>{});
+        if (columns_of_lane<E>(B, D, false) == 2) return launch(std::integral_constant<int, 2>{});
     return launch(std::integral_constant<int, 1>{});
 }
 

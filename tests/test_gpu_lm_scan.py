@@ -71,6 +71,13 @@ def test_both_directions(suffix, packed, strided, B, T, D):
 
 
 @pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("packed,strided", [(False, False), (True, True)])
+@pytest.mark.parametrize("B,T,D", [(300, 1, 65), (140, 37, 129), (66, 131, 200), (50, 259, 258), (260, 20, 2), (70, 300, 3)])
+def test_columns_of_a_lane_at_many_and_few_sequences(suffix, packed, strided, B, T, D):
+    test_both_directions(suffix, packed, strided, B, T, D)
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
 def test_defaults_and_halves_of_one_projection(suffix):
     """No states at the ends; gates and inputs (and their gradients) as the two halves of the rows of one matrix."""
     dtype, B, T, D = R.TYPES[suffix], 2, 70, 33

@@ -47,4 +47,4 @@ def test_rows_in_registers_leave_room_for_a_second_workgroup(kernels):
 
 def test_recurrence_keeps_two_wavefronts_a_simd(kernels):
     scans = [(name, vgpr) for name, vgpr, _ in kernels if "scan_kernel" in name or "scan_grad_kernel" in name]
-    assert len(scans) >= 40 and all(vgpr <= 256 for _, vgpr in scans)
+    assert len(scans) >= 36 and all(vgpr <= 256 for _, vgpr in scans)
