@@ -17,6 +17,7 @@ constexpr int kMaxTop = CX_MAX_TOP;
 constexpr int kGroups = 4;                              // subsets of a thread
 constexpr int kTurnKeys = 1024;                         // elements looked at between two checks of the list's length, at most
 constexpr int kRankable = 256;                          // a list of this length is ranked by counting, a longer one cut to K first
+constexpr unsigned kRankStep = 8;                       // keys of the list compared at once
 
 typedef unsigned long long Key;
 
@@ -90,11 +91,14 @@ __device__ void rank_list(TopSpace<THREADS> &s, int K)
     if (s.count > kRankable) cut_list(s, K);
     const unsigned count = s.count;
     if (static_cast<int>(threadIdx.x) < K) s.kept[threadIdx.x] = 0;
+    if (threadIdx.x < kRankStep) s.list[count + threadIdx.x] = 0;       // so that whole steps are compared
     __syncthreads();
     for (unsigned at = threadIdx.x; at < count; at += THREADS) {
         const Key mine = s.list[at];
         int rank = 0;
-        for (unsigned i = 0; i < count; ++i) rank += s.list[i] > mine;
+        for (unsigned i = 0; i < count; i += kRankStep)
+#pragma unroll
+            for (unsigned k = 0; k < kRankStep; ++k) rank += s.list[i + k] > mine;
         if (rank < K) s.kept[rank] = mine;
     }
     __syncthreads();
@@ -331,9 +335,11 @@ int scores(const typename E::T *z, int64_t ld, int64_t N, int32_t V, const int32
             else hipLaunchKernelGGL((scores_kernel<E, false, THREADS>), dim3(space.parts, rows), dim3(THREADS), 0, st, b);
         };
         // threads of a row by its length: 8,192 rows of 1,000 bfloat16 logits take 37 us with 256 each and 75 with 512, 4,096 rows of 50,003
-        // 106 and 109, 2,048 rows of 262,144 219 and 204; with 1,024 all but the longest rows take twice as long
+        // 106 and 109, 2,048 rows of 262,144 219 and 204; with 1,024 all but the longest rows take twice as long.  The K-th largest of
+        // as many maxima as threads is a sharp threshold only where K is well below their number: with 64 threads 8,192 rows of 1,000 take
+        // 16 us for 5 tokens against 37 with 256, 22 against 44 for 32, but 72 against 54 for 64, and 5 rows of 3,557 29 against 10
         const int64_t vectors = ceil_div(V / space.parts, E::kPer16);
-        if (vectors <= 512) launch(std::integral_constant<int, 64>{});
+        if (vectors <= 512 && K <= kWave / 2) launch(std::integral_constant<int, 64>{});
         else if (vectors <= 8192) launch(std::integral_constant<int, 256>{});
         else launch(std::integral_constant<int, 512>{});
         if (launched() != CX_OK) return CX_ERR_HIP;
