@@ -188,8 +188,9 @@ __device__ __forceinline__ void write_loss(const DistillArgs<E> &a, int64_t n, c
 __device__ __forceinline__ void forget_widened(u4 &w) { asm volatile("" : "+v"(w)); }
 
 // Loss and, if it is wanted, gradient of a row that fits the registers of one workgroup, KV vectors to a thread: it is read once.  The caches do
-// not hold the rows of all workgroups, so a second reading would cross the same path as the first and the writing.
-template <class E, Extra X, int KV>
+// not hold the rows of all workgroups, so a second reading would cross the same path as the first and the writing.  SAVED: the gradient alone,
+// from the statistics that the loss left.
+template <class E, Extra X, int KV, bool SAVED = false>
 __global__ __launch_bounds__(kMostThreads, KV > 8 ? 4 : 8) void row_kernel(const DistillArgs<E> a)
 {
     __shared__ Stats lds[kMostThreads / kWave];
@@ -217,31 +218,36 @@ __global__ __launch_bounds__(kMostThreads, KV > 8 ? 4 : 8) void row_kernel(const
     keep_others(a, n, to);
     const float c = soft_factor(a);
     Stats all{kLowest, 0.0f, 0.0f};
-    {
-        float high[2] = {z_tail, z_tail};
-#pragma unroll
+    if constexpr (SAVED) {
+        all = {a.stats[n * 4], a.stats[n * 4 + 1], a.stats[n * 4 + 2]};
+        __syncthreads();
+    } else {
+        {
+            float high[2] = {z_tail, z_tail};
+    #pragma unroll
+            for (int k = 0; k < KV; ++k) {
+                float v[E::kPer16];
+                E::unpack(w[k], v);
+    #pragma unroll
+                for (int j = 0; j < E::kPer16; ++j) high[j & 1] = fmaxf(high[j & 1], v[j]);
+            }
+            all.m = fmaxf(all.m, fmaxf(high[0], high[1]));
+        }
+    #pragma unroll
         for (int k = 0; k < KV; ++k) {
             float v[E::kPer16];
+            forget_widened(w[k]);
             E::unpack(w[k], v);
-#pragma unroll
-            for (int j = 0; j < E::kPer16; ++j) high[j & 1] = fmaxf(high[j & 1], v[j]);
+            add_terms<X>(all, v, c, kLog2e);
         }
-        all.m = fmaxf(all.m, fmaxf(high[0], high[1]));
+        const float last[1] = {z_tail};
+        add_terms<X>(all, last, c, kLog2e);
+        all = join_workgroup<X>(all, lds, c, kLog2e, threads / kWave);
+        if (!two_sums(X)) all.u = all.s;                    // one sum serves both
     }
-#pragma unroll
-    for (int k = 0; k < KV; ++k) {
-        float v[E::kPer16];
-        forget_widened(w[k]);
-        E::unpack(w[k], v);
-        add_terms<X>(all, v, c, kLog2e);
-    }
-    const float last[1] = {z_tail};
-    add_terms<X>(all, last, c, kLog2e);
-    all = join_workgroup<X>(all, lds, c, kLog2e, threads / kWave);
-    if (!two_sums(X)) all.u = all.s;                    // one sum serves both
     if (threadIdx.x < kWave) settle(a, all, to);
     __syncthreads();
-    if (threadIdx.x == 0) write_loss(a, n, all, to);
+    if (!SAVED && threadIdx.x == 0) write_loss(a, n, all, to);
     if (!a.dz) return;
     const RowGradient<E, X> gradient(a, n, all, to);
     typename E::T *dz = a.dz + n * a.ld_dz;
@@ -303,18 +309,25 @@ struct DistillSpace {
     int64_t bytes;
 };
 
+// From so many rows on the gradient alone takes a row in registers too, if it fits 4 vectors of a thread: workgroups as large as the row is long take
+// 11 us for 8,192 rows of 500 bfloat16 logits against 40 with the others' 256 threads, 50 against 58 for 4,096 of 16,000.
+constexpr int64_t kManyRows = 512;
+
 // The gradient alone needs nothing of a row but its statistics: as many workgroups to a row as give a CU two.
 int grad_parts(int64_t N, int64_t V, int per16)
 {
     const int64_t fit = ceil_div(V, static_cast<int64_t>(kRowThreads) * per16 * 2), wanted = ceil_div(512, N);
-    return static_cast<int>(N >= 512 ? 1 : fit < wanted ? fit : wanted);
+    return static_cast<int>(N >= kManyRows ? 1 : fit < wanted ? fit : wanted);
 }
 
 constexpr int64_t kRegisterVectors = 16 * kMostThreads;         // of a row that one workgroup's registers hold
+// Up to so many rows the long ones are split even if they would fit, as a workgroup to a row leaves CUs idle: loss and gradient of 4 rows of 131,072
+// bfloat16 logits take 14 us against 25, of 128 rows 26 against 31, but of 200 36 against 33.
+constexpr int64_t kFewRows = 128;
 
 DistillSpace distill_space(int64_t N, int64_t V, int per16)
 {
-    const int parts = V / per16 > kRegisterVectors ? parts_of(N, V, per16) : 1;
+    const int parts = V / per16 > kRegisterVectors || N <= kFewRows ? parts_of(N, V, per16) : 1;
     return {parts, parts > 1 ? N * parts * static_cast<int64_t>(sizeof(Stats)) : 0};
 }
 
@@ -373,11 +386,13 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
         const dim3 whole(1, rows), parted(space.parts, rows), block(kRowThreads);
         const auto launch = [&](auto kind) {
             constexpr Extra X = decltype(kind)::value;
-            if (from_saved) {
+            const int64_t vectors = a.V / E::kPer16;
+            const auto threads = [&](int64_t each) { return dim3(static_cast<unsigned>(vectors < each ? kWave : round_up(ceil_div(vectors, each), kWave))); };
+            if (from_saved && N >= kManyRows && vectors <= 4 * kMostThreads) {
+                hipLaunchKernelGGL((row_kernel<E, X, 4, true>), dim3(rows), threads(4), 0, st, b);
+            } else if (from_saved) {
                 hipLaunchKernelGGL((distill_kernel<E, X, kSaved>), parted, block, 0, st, b);
             } else if (space.parts == 1) {
-                const int64_t vectors = a.V / E::kPer16;
-                const auto threads = [&](int64_t each) { return dim3(static_cast<unsigned>(vectors < each ? kWave : round_up(ceil_div(vectors, each), kWave))); };
                 if (vectors > kRegisterVectors) hipLaunchKernelGGL((distill_kernel<E, X, kHere>), whole, block, 0, st, b);
                 else if (vectors > 8 * kMostThreads) hipLaunchKernelGGL((row_kernel<E, X, 16>), dim3(rows), threads(16), 0, st, b);
                 else if (vectors > 4 * kMostThreads) hipLaunchKernelGGL((row_kernel<E, X, 8>), dim3(rows), threads(8), 0, st, b);

@@ -60,7 +60,7 @@ def compare(suffix, z, ids, t, labels, gout, tau, w_kl, w_ce, **kw):
 @pytest.mark.parametrize("suffix", R.SUFFIXES)
 @pytest.mark.parametrize("in_place", [False, True])
 @pytest.mark.parametrize("N,V,K", [(1, 1, 1), (2, 3, 2), (3, 17, 5), (1, 4096, 32), (2, 4097, 256), (5, 1000, 0), (700, 70, 9), (515, 4_111, 64),
-                                   (1, 50_001, 64), (3, 20_000, 100)])
+                                   (1, 50_001, 64), (3, 20_000, 100), (4, 70_001, 20), (129, 66_003, 5), (520, 16_390, 40)])
 def test_rows(suffix, in_place, N, V, K):
     z, ids, t, labels, gout = make(N, V, K, R.TYPES[suffix], N + V + K)
     if N > 2:
