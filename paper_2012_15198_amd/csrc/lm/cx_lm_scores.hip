@@ -17,7 +17,7 @@ constexpr int kMaxTop = CX_MAX_TOP;
 constexpr int kGroups = 4;                              // subsets of a thread
 constexpr int kTurnKeys = 1024;                         // elements looked at between two checks of the list's length, at most
 constexpr int kRankable = 256;                          // a list of this length is ranked by counting, a longer one cut to K first
-constexpr unsigned kRankStep = 8;                       // keys of the list compared at once
+constexpr unsigned kRankStep = 4;                       // keys of the list compared at once: eight take the kernel from 52 to 80 registers (4,096 float32 rows of 50,003: 145 to 160 us)
 
 typedef unsigned long long Key;
 
@@ -337,7 +337,7 @@ int scores(const typename E::T *z, int64_t ld, int64_t N, int32_t V, const int32
         // threads of a row by its length: 8,192 rows of 1,000 bfloat16 logits take 37 us with 256 each and 75 with 512, 4,096 rows of 50,003
         // 106 and 109, 2,048 rows of 262,144 219 and 204; with 1,024 all but the longest rows take twice as long.  The K-th largest of
         // as many maxima as threads is a sharp threshold only where K is well below their number: with 64 threads 8,192 rows of 1,000 take
-        // 16 us for 5 tokens against 37 with 256, 22 against 44 for 32, but 72 against 54 for 64, and 5 rows of 3,557 29 against 10
+        // 16 us for 5 tokens against 37 with 256, 22 against 44 for 32, but 70 against 53 for 64, and 5 rows of 3,557 27 against 9
         const int64_t vectors = ceil_div(V / space.parts, E::kPer16);
         if (vectors <= 512 && K <= kWave / 2) launch(std::integral_constant<int, 64>{});
         else if (vectors <= 8192) launch(std::integral_constant<int, 256>{});

@@ -48,3 +48,8 @@ def test_rows_in_registers_leave_room_for_a_second_workgroup(kernels):
 def test_recurrence_keeps_two_wavefronts_a_simd(kernels):
     scans = [(name, vgpr) for name, vgpr, _ in kernels if "scan_kernel" in name or "scan_grad_kernel" in name]
     assert len(scans) >= 36 and all(vgpr <= 256 for _, vgpr in scans)
+
+
+def test_scores_keep_eight_wavefronts_a_simd(kernels):
+    scores = [(name, vgpr) for name, vgpr, _ in kernels if "scores_kernel" in name]
+    assert len(scores) >= 18 and all(vgpr <= 64 for _, vgpr in scores)
