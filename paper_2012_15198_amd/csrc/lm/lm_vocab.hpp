@@ -98,13 +98,14 @@ __device__ __forceinline__ Stats join_workgroup(Stats a, Stats (&lds)[WAVES], fl
 }
 
 // A slice of a row: `vectors` whole 16-byte vectors from its first element on (which need not be aligned to more than an
-// element), then `tail` elements.
-template <class E, int THREADS = kRowThreads>
+// element), then `tail` elements.  LAST: nothing of the call reads (most of) it again.
+template <class E, int THREADS = kRowThreads, bool LAST = false>
 struct Slice {
     const typename E::T *z;
     int vectors, tail;
     __device__ __forceinline__ Slice(const typename E::T *row, int64_t lo, int64_t hi)
         : z(row + lo), vectors(static_cast<int>((hi - lo) / E::kPer16)), tail(static_cast<int>((hi - lo) % E::kPer16)) {}
+    static __device__ __forceinline__ u4 read(const typename E::T *p) { return LAST ? load16_last<E>(p) : load16<E>(p); }
     __device__ __forceinline__ int rounds() const { return (vectors + THREADS * kAhead - 1) / (THREADS * kAhead); }
     static __device__ __forceinline__ int vector_of(int round, int k) { return (round * kAhead + k) * THREADS + static_cast<int>(threadIdx.x); }
     // the thread's kAhead vectors of a round; what lies beyond the slice counts as -inf
@@ -112,12 +113,12 @@ struct Slice {
     {
         if ((round + 1) * kAhead * THREADS <= vectors) {
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) w[k] = load16<E>(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
+            for (int k = 0; k < kAhead; ++k) w[k] = read(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
         } else {
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
                 w[k] = u4{E::kNothing, E::kNothing, E::kNothing, E::kNothing};
-                if (vector_of(round, k) < vectors) w[k] = load16<E>(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
+                if (vector_of(round, k) < vectors) w[k] = read(z + static_cast<int64_t>(vector_of(round, k)) * E::kPer16);
             }
         }
     }
