@@ -3,7 +3,7 @@
 //
 //   out[w][n] = round(scale * table_w[token[w][n]])               g[w][v] = round(g_in[w][v] + scale * sum_{n: token = v} dout[w][n])
 //
-// Both are bound by memory: 16 workers' 4,096 tokens of 768 float32 columns take 50 us (5.9 TB/s), the gradient of as many in bfloat16 into
+// Both are bound by memory: 16 workers' 4,096 tokens of 768 float32 columns take 48 us (6.1 TB/s), the gradient of as many in bfloat16 into
 // tables of 32,768 rows 168 us for the sums and the filling (5.4 TB/s), 14 for the sort before and 8 for the joining behind.  A group of lanes (a power of two, as many as one row's 16-byte vectors, 64 at most) handles one
 // vector column each of one row, so a short row does not leave a wavefront's lanes idle.
 //
@@ -29,23 +29,42 @@ constexpr int kFewPieces = 8;               // a list of no more is joined by on
 constexpr int64_t kMaxTokens = CX_MAX_TOKENS;
 constexpr int32_t kMaxVocab = CX_MAX_VOCAB, kMaxWidth = CX_MAX_WIDTH;
 
+// Elements [0, n) of a vector.
+template <class E>
+__device__ __forceinline__ u4 load_part(const typename E::T *p, int n)
+{
+    u4 w{};
+#pragma unroll
+    for (int j = 0; j < E::kPer16; ++j)
+        if (j < n) {
+            if constexpr (E::kPer16 == 4) w[j] = __float_as_uint(p[j]);
+            else w[j / 2] |= static_cast<unsigned>(p[j]) << (16 * (j & 1));
+        }
+    return w;
+}
+
 template <class E>
 struct Columns {                            // the columns of a row that a lane handles
     int64_t first;
     int n;                                  // of kPer16; 0 beyond the row
+    int back;                               // the row's last columns are read as a whole vector that begins so many columns earlier
+    bool narrow;                            // unless the row is shorter than a vector
+    // Reads a row's columns; place() before their use moves those of a row's end where they belong, so that no read waits for another: read
+    // one by one, 3 workers' 2,438 tokens of 503 binary16 columns were added up in 23 us instead of 13.
     __device__ __forceinline__ u4 raw(const typename E::T *row) const
     {
-        if (n == E::kPer16) return load16<E>(row + first);
-        u4 w{};
-#pragma unroll
-        for (int j = 0; j < E::kPer16; ++j)
-            if (j < n) {
-                if constexpr (E::kPer16 == 4) w[j] = __float_as_uint(row[first + j]);
-                else w[j / 2] |= static_cast<unsigned>(row[first + j]) << (16 * (j & 1));
-            }
-        return w;
+        return narrow ? load_part<E>(row + first, n) : load16<E>(row + (first - back));
     }
-    __device__ __forceinline__ void load(const typename E::T *row, float (&v)[E::kPer16]) const { E::unpack(raw(row), v); }
+    __device__ __forceinline__ void place(u4 &w) const
+    {
+        if (back == 0) return;
+        uint64_t lo = static_cast<uint64_t>(w[1]) << 32 | w[0], hi = static_cast<uint64_t>(w[3]) << 32 | w[2];
+        int bits = back * 8 * static_cast<int>(sizeof(typename E::T));
+        if (bits >= 64) { lo = hi; hi = 0; bits -= 64; }
+        lo = lo >> bits | hi << 1 << (63 - bits);
+        hi >>= bits;
+        w = u4{static_cast<unsigned>(lo), static_cast<unsigned>(lo >> 32), static_cast<unsigned>(hi), static_cast<unsigned>(hi >> 32)};
+    }
     template <bool THROUGH = false>
     __device__ __forceinline__ void store(typename E::T *row, const float (&v)[E::kPer16]) const
     {
@@ -71,7 +90,9 @@ __device__ __forceinline__ Columns<E> columns_of(int lane, int lanes, int slab, 
 {
     const int64_t first = (static_cast<int64_t>(slab) * lanes + lane) * E::kPer16;
     const int64_t left = D - first;
-    return {first, left >= E::kPer16 ? E::kPer16 : left > 0 ? static_cast<int>(left) : 0};
+    const int n = left >= E::kPer16 ? E::kPer16 : left > 0 ? static_cast<int>(left) : 0;
+    const bool narrow = D < E::kPer16;
+    return {first, n, narrow || n == 0 ? 0 : E::kPer16 - n, narrow};
 }
 
 // ROWS tokens a group of lanes: as many reads of the table in flight.  THROUGH: the results are larger than the caches.
@@ -88,17 +109,22 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(const typename E::T *t
     int token[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) token[r] = n0 + r < N ? tokens[w * N + n0 + r] : -1;
+    u4 rows[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        rows[r] = u4{};
+        if (static_cast<uint32_t>(token[r]) < static_cast<uint32_t>(V)) rows[r] = c.raw(table + static_cast<int64_t>(token[r]) * D);
+    }
+    if (c.back > 0)
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) c.place(rows[r]);
     float v[ROWS][E::kPer16];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
-        if (static_cast<uint32_t>(token[r]) < static_cast<uint32_t>(V)) {
-            c.load(table + static_cast<int64_t>(token[r]) * D, v[r]);
+        const bool known = static_cast<uint32_t>(token[r]) < static_cast<uint32_t>(V);
+        E::unpack(rows[r], v[r]);
 #pragma unroll
-            for (int j = 0; j < E::kPer16; ++j) v[r][j] *= scale;
-        } else {
-#pragma unroll
-            for (int j = 0; j < E::kPer16; ++j) v[r][j] = 0.0f;
-        }
+        for (int j = 0; j < E::kPer16; ++j) v[r][j] = known ? v[r][j] * scale : 0.0f;
     }
 #pragma unroll
     for (int r = 0; r < ROWS; ++r)
@@ -257,9 +283,10 @@ __device__ __forceinline__ int64_t place_of(const GradArgs<E> &a, int64_t w, int
 
 // g: the row of g_in, where there is one
 template <class E>
-__device__ __forceinline__ void finish(const GradArgs<E> &a, const Columns<E> &c, int64_t w, int32_t v, const float (&sum)[E::kPer16], const u4 &g_row)
+__device__ __forceinline__ void finish(const GradArgs<E> &a, const Columns<E> &c, int64_t w, int32_t v, const float (&sum)[E::kPer16], u4 g_row)
 {
     float g[E::kPer16];
+    c.place(g_row);
     E::unpack(g_row, g);
 #pragma unroll
     for (int j = 0; j < E::kPer16; ++j) g[j] = a.g_in ? __builtin_fmaf(a.scale, sum[j], g[j]) : a.scale * sum[j];
@@ -287,6 +314,7 @@ __device__ __forceinline__ void sum_piece(const GradArgs<E> &a, const Columns<E>
         for (int k = 0; k < kRows; ++k) {
             if (i + k >= tokens) break;
             float one[E::kPer16];
+            c.place(v[k]);
             E::unpack(v[k], one);
 #pragma unroll
             for (int j = 0; j < E::kPer16; ++j) sum[j] += one[j];
@@ -369,7 +397,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(const GradArgs<E> a)
                     if (from) v[k] = load16<E>(from + first);
                     wanted[k] = (1u << kPer) - 1;
                 } else {                                // the last vector hangs over the rows' end
-                    if (from) v[k] = Columns<E>{first, left}.raw(from);
+                    if (from) v[k] = load_part<E>(from + first, left);
                     wanted[k] = (1u << left) - 1;
                 }
             }
@@ -496,16 +524,16 @@ int lookup(const typename E::T *x, int64_t ld, int32_t W, int64_t offset, int32_
     if (overlap(out, out_bytes, x, span(W, ld, offset + static_cast<int64_t>(V) * D, kElem)) || overlap(out, out_bytes, tokens, W * N * 4)) return CX_ERR_ALIAS;
     const int shift = lanes_shift<E>(D), groups = kThreads >> shift;
     const int64_t slabs = ceil_div(ceil_div(D, E::kPer16), 1 << shift);
-    // Four rows a group from 4,096 workgroups of one row on; from 64 MB on, results that go past the caches: 16 x 4,096 tokens of 768 columns
-    // take 35 us with ordinary stores and 26 without in bfloat16, 63 and 59 in float32
+    // Four rows a group from 4,096 workgroups of one row on; from 64 MB on, results that go past the caches, and two rows: 16 x 4,096 tokens
+    // of 768 columns take 35 us with ordinary stores and 26 without in bfloat16, in float32 63 and 61, 56 with two rows, 65 with one
     const bool many = W * N * slabs >= int64_t(4096) * groups, large = many && W * N * D * kElem >= int64_t(64) << 20;
-    const dim3 grid(static_cast<unsigned>(ceil_div(N, static_cast<int64_t>(groups) * (many ? 4 : 1))), static_cast<unsigned>(slabs), W);
+    const dim3 grid(static_cast<unsigned>(ceil_div(N, static_cast<int64_t>(groups) * (large ? 2 : many ? 4 : 1))), static_cast<unsigned>(slabs), W);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const auto launch = [&](auto rows, auto through) {
         hipLaunchKernelGGL((lookup_kernel<E, decltype(rows)::value, decltype(through)::value>), grid, dim3(kThreads), 0, st, x + offset, ld, V, D,
                            tokens, N, scale, out, ld_out, shift);
     };
-    if (large) launch(std::integral_constant<int, 4>{}, std::true_type{});
+    if (large) launch(std::integral_constant<int, 2>{}, std::true_type{});
     else if (many) launch(std::integral_constant<int, 4>{}, std::false_type{});
     else launch(std::integral_constant<int, 1>{}, std::false_type{});
     return launched();

@@ -31,7 +31,8 @@ def tokens_of(kind, W, N, V, gen):
 SHAPES = [  # W, N, V, D, offset, extra row length, tokens
     (1, 1, 1, 1, 0, 0, "any"), (1, 1, 5, 8, 0, 0, "any"), (2, 7, 11, 3, 5, 3, "any"), (3, 64, 40, 33, 1, 0, "zipf"),
     (2, 65, 513, 16, 7, 1, "zipf"), (1, 300, 512, 129, 0, 5, "one"), (2, 1000, 1025, 65, 3, 0, "two"), (1, 200, 3, 520, 9, 2, "any"),
-    (4, 129, 700, 7, 0, 0, "none"), (1, 5000, 2000, 31, 0, 0, "zipf"), (2, 33, 90, 1030, 11, 0, "any"), (1, 513, 1, 64, 0, 0, "any")]
+    (4, 129, 700, 7, 0, 0, "none"), (1, 5000, 2000, 31, 0, 0, "zipf"), (2, 33, 90, 1030, 11, 0, "any"), (1, 513, 1, 64, 0, 0, "any"),
+    (2, 70, 50, 13, 2, 0, "any"), (1, 90, 30, 26, 0, 1, "zipf"), (2, 300, 60, 527, 4, 0, "zipf"), (1, 40, 20, 9, 1, 0, "two")]
 
 
 def rows(gen, W, ld, dtype):
@@ -50,6 +51,12 @@ def test_lookup(suffix, W, N, V, D, offset, extra, kind):
     ref = R.lookup(x, tokens, offset, V, D, scale)
     R.check(out[:, 2:2 + D], ref, 2 * R.U * ref.abs())                # scale as fp32, the product's rounding
     assert (out[:, :2] == 7).all() and (out[:, 2 + D:] == 7).all()
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("W,N,D", [(1, 262_150, 13), (2, 70_001, 131), (1, 40_003, 1001)])
+def test_lookup_of_many_tokens(suffix, W, N, D):
+    test_lookup(suffix, W, N, 300, D, 3, 0, "any")
 
 
 @pytest.mark.parametrize("suffix", R.SUFFIXES)
