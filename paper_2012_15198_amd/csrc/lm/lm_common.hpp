@@ -28,6 +28,7 @@ struct F32 {
     using T = float;
     using Vec = u4_at4;
     static constexpr int kPer16 = 4;
+    static constexpr int kBits = 32;                       // of a value widened to fp32, from the top: the others are zero
     static constexpr unsigned kNothing = 0xff800000u;      // -inf, as often as a word holds it
     static __device__ __forceinline__ float widen(T v) { return v; }
     static __device__ __forceinline__ T narrow(float v) { return v; }
@@ -46,6 +47,7 @@ struct Bf16 {
     using T = uint16_t;
     using Vec = u4_at2;
     static constexpr int kPer16 = 8;
+    static constexpr int kBits = 16;
     static constexpr unsigned kNothing = 0xff80ff80u;
     typedef __bf16 pair __attribute__((ext_vector_type(2)));
     typedef float f2 __attribute__((ext_vector_type(2)));
@@ -72,6 +74,7 @@ struct F16 {
     using T = uint16_t;
     using Vec = u4_at2;
     static constexpr int kPer16 = 8;
+    static constexpr int kBits = 19;
     static constexpr unsigned kNothing = 0xfc00fc00u;
     static __device__ __forceinline__ float widen(T v) { return static_cast<float>(__builtin_bit_cast(_Float16, v)); }
     static __device__ __forceinline__ float low(unsigned w) { return widen(static_cast<T>(w)); }

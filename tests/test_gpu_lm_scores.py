@@ -34,7 +34,7 @@ def compare(suffix, z, tokens, K, scale=1.0, offset=0):
 @pytest.mark.parametrize("suffix", R.SUFFIXES)
 @pytest.mark.parametrize("N,V,K", [(1, 1, 1), (1, 2, 2), (3, 7, 7), (2, 9, 0), (5, 64, 64), (4, 300, 60), (2, 1000, 5), (3, 4097, 64),
                                    (700, 515, 3), (2, 8192, 20), (1, 33_333, 64), (600, 17_001, 9), (1, 131_073, 20), (513, 40, 40),
-                                   (130, 219, 28), (5, 3557, 63), (40, 900, 32), (40, 900, 33)])
+                                   (130, 219, 28), (5, 3557, 63), (40, 900, 32), (40, 900, 33), (30, 318, 54), (3, 512, 64)])
 def test_rows(suffix, N, V, K):
     gen = torch.Generator().manual_seed(N + V)
     z = (torch.randn((N, V), generator=gen) * 3).to(R.TYPES[suffix])
