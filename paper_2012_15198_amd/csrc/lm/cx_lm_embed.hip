@@ -3,7 +3,7 @@
 //
 //   out[w][n] = round(scale * table_w[token[w][n]])               g[w][v] = round(g_in[w][v] + scale * sum_{n: token = v} dout[w][n])
 //
-// Both are bound by memory: 16 workers' 4,096 tokens of 768 float32 columns take 48 us (6.1 TB/s), the gradient of as many in bfloat16 into
+// Both are bound by memory: 16 workers' 4,096 tokens of 768 float32 columns take 50 us (5.9 TB/s), the gradient of as many in bfloat16 into
 // tables of 32,768 rows 168 us for the sums and the filling (5.4 TB/s), 14 for the sort before and 8 for the joining behind.  A group of lanes (a power of two, as many as one row's 16-byte vectors, 64 at most) handles one
 // vector column each of one row, so a short row does not leave a wavefront's lanes idle.
 //
