@@ -32,7 +32,8 @@ SHAPES = [  # W, N, V, D, offset, extra row length, tokens
     (1, 1, 1, 1, 0, 0, "any"), (1, 1, 5, 8, 0, 0, "any"), (2, 7, 11, 3, 5, 3, "any"), (3, 64, 40, 33, 1, 0, "zipf"),
     (2, 65, 513, 16, 7, 1, "zipf"), (1, 300, 512, 129, 0, 5, "one"), (2, 1000, 1025, 65, 3, 0, "two"), (1, 200, 3, 520, 9, 2, "any"),
     (4, 129, 700, 7, 0, 0, "none"), (1, 5000, 2000, 31, 0, 0, "zipf"), (2, 33, 90, 1030, 11, 0, "any"), (1, 513, 1, 64, 0, 0, "any"),
-    (2, 70, 50, 13, 2, 0, "any"), (1, 90, 30, 26, 0, 1, "zipf"), (2, 300, 60, 527, 4, 0, "zipf"), (1, 40, 20, 9, 1, 0, "two")]
+    (2, 70, 50, 13, 2, 0, "any"), (1, 90, 30, 26, 0, 1, "zipf"), (2, 300, 60, 527, 4, 0, "zipf"), (1, 40, 20, 9, 1, 0, "two"),
+    (2, 40, 700, 33, 3, 2, "zipf"), (1, 5, 90, 7, 1, 0, "any"), (3, 300, 5000, 65, 5, 3, "two"), (2, 33, 1500, 130, 1, 1, "none")]
 
 
 def rows(gen, W, ld, dtype):
