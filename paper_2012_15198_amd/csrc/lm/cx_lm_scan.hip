@@ -571,18 +571,6 @@ Split split_of(int64_t B, int64_t T, int32_t D, bool forward)
     return {static_cast<int>(spans), span_tiles * kTile, spans > 1 ? (B * spans * 2 + B) * D * 4 : 0};
 }
 
-// Whether two matrices of the same number of rows share an element.  Halves of the rows of one wider matrix do not.
-template <class E>
-bool share(const typename E::T *a, int64_t lda, const typename E::T *b, int64_t ldb, int64_t rows, int64_t columns)
-{
-    constexpr int kElem = sizeof(typename E::T);
-    if (!a || !b || !overlap(a, span(rows, lda, columns, kElem), b, span(rows, ldb, columns, kElem))) return false;
-    if (lda != ldb) return true;
-    const uintptr_t lo = reinterpret_cast<uintptr_t>(a < b ? a : b), hi = reinterpret_cast<uintptr_t>(a < b ? b : a);
-    const uint64_t off = (hi - lo) % (static_cast<uint64_t>(lda) * kElem), width = static_cast<uint64_t>(columns) * kElem;
-    return off < width || off + width > static_cast<uint64_t>(lda) * kElem;
-}
-
 int check_sizes(int64_t B, int64_t T, int32_t D)
 {
     return B < 0 || B > CX_MAX_SEQUENCES || B * D > (int64_t(1) << 31) || T < 0 || T > kMaxSeq || D < 1 || D > kMaxColumns ? CX_ERR_SHAPE : CX_OK;
@@ -612,10 +600,10 @@ int scan(const typename E::T *f, int64_t ldf, const typename E::T *x, int64_t ld
     if (split.bytes > 0 && workspace_bytes < split.bytes) return CX_ERR_SHAPE;
     if (misaligned_to(f, kElem) || misaligned_to(x, kElem) || misaligned_to(y, kElem) || misaligned_to(states, 4) ||
         misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const uint64_t y_bytes = span(B * T, ldy, D, kElem), states_bytes = B * ceil_div(T, kSteps) * D * 4;
-    if (share<E>(y, ldy, f, ldf, B * T, D) || share<E>(y, ldy, x, ldx, B * T, D) || overlap(y, y_bytes, reset, B * T) ||
-        overlap(y, y_bytes, h0, state_bytes) || overlap(y, y_bytes, h_last, state_bytes) || overlap(y, y_bytes, states, states_bytes) ||
-        overlap(states, states_bytes, h0, state_bytes) || overlap(states, states_bytes, h_last, state_bytes)) return CX_ERR_ALIAS;
+    const Extent in[4] = {matrix_of(f, B * T, ldf, D, kElem), matrix_of(x, B * T, ldx, D, kElem), dense_of(reset, B * T), dense_of(h0, state_bytes)};
+    const Extent out[4] = {matrix_of(y, B * T, ldy, D, kElem), dense_of(h_last, state_bytes), dense_of(states, B * ceil_div(T, kSteps) * D * 4),
+                           dense_of(workspace, split.bytes)};
+    if (outputs_share(in, out, 1, 3)) return CX_ERR_ALIAS;
     ScanArgs<E> a{};
     a.f = f; a.ldf = ldf; a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy;
     a.reset = reset; a.h0 = h0; a.h_last = h_last; a.states = states;
@@ -678,16 +666,11 @@ int scan_grad(const typename E::T *f, int64_t ldf, const typename E::T *x, int64
     if (split.bytes > 0 && workspace_bytes < split.bytes) return CX_ERR_SHAPE;
     if (misaligned_to(f, kElem) || misaligned_to(x, kElem) || misaligned_to(dy, kElem) || misaligned_to(df, kElem) ||
         misaligned_to(dx, kElem) || misaligned_to(states, 4) || misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const uint64_t states_bytes = B * ceil_div(T, kSteps) * D * 4;
-    const typename E::T *outs[2] = {df, dx};
-    const int64_t lds[2] = {lddf, lddx};
-    for (int k = 0; k < 2; ++k) {
-        const uint64_t bytes = span(B * T, lds[k], D, kElem);
-        if (share<E>(outs[k], lds[k], f, ldf, B * T, D) || share<E>(outs[k], lds[k], x, ldx, B * T, D) ||
-            share<E>(outs[k], lds[k], dy, lddy, B * T, D) || overlap(outs[k], bytes, reset, B * T) || overlap(outs[k], bytes, states, states_bytes) ||
-            overlap(outs[k], bytes, dh_last, state_bytes) || overlap(outs[k], bytes, dh0, state_bytes)) return CX_ERR_ALIAS;
-    }
-    if (share<E>(df, lddf, dx, lddx, B * T, D) || overlap(dh0, state_bytes, states, states_bytes)) return CX_ERR_ALIAS;
+    const Extent in[6] = {matrix_of(f, B * T, ldf, D, kElem), matrix_of(x, B * T, ldx, D, kElem), matrix_of(dy, B * T, lddy, D, kElem), dense_of(reset, B * T),
+                          dense_of(states, B * ceil_div(T, kSteps) * D * 4), dense_of(dh_last, state_bytes)};
+    const Extent out[4] = {matrix_of(df, B * T, lddf, D, kElem), matrix_of(dx, B * T, lddx, D, kElem), dense_of(dh0, state_bytes),
+                           dense_of(workspace, split.bytes)};
+    if (outputs_share(in, out, 2, 5)) return CX_ERR_ALIAS;
     ScanArgs<E> a{};
     a.f = f; a.ldf = ldf; a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.df = df; a.lddf = lddf; a.dx = dx; a.lddx = lddx;
     a.reset = reset; a.states_in = states; a.dh_last = dh_last; a.dh0 = dh0;

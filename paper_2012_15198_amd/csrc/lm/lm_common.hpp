@@ -131,6 +131,46 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
     return rows < 1 || columns < 1 ? 0 : (static_cast<uint64_t>(rows - 1) * ld + columns) * elem;
 }
 
+// An array of a call for the question whether two of them share an element: rows of `width` bytes, `pitch` bytes from row to row.
+struct Extent {
+    const void *first;
+    uint64_t rows, width, pitch;
+};
+[[maybe_unused]] Extent matrix_of(const void *first, int64_t rows, int64_t ld, int64_t columns, int elem)
+{
+    const uint64_t width = static_cast<uint64_t>(columns) * elem;
+    return {first, static_cast<uint64_t>(rows), width, rows > 1 ? static_cast<uint64_t>(ld) * elem : width};
+}
+[[maybe_unused]] Extent dense_of(const void *first, uint64_t bytes) { return {first, 1, bytes, bytes}; }
+
+// Exact where the pitches are equal or one of them is a single row: parts of the rows of one wider matrix share nothing.  Of other pitches
+// whatever lies between the first and the last element counts.
+[[maybe_unused]] bool share(const Extent &a, const Extent &b)
+{
+    if (a.rows < 1 || b.rows < 1 || !overlap(a.first, (a.rows - 1) * a.pitch + a.width, b.first, (b.rows - 1) * b.pitch + b.width)) return false;
+    if (a.rows > 1 && b.rows > 1 && a.pitch != b.pitch) return true;
+    const bool in_order = a.first <= b.first;
+    const Extent &lo = in_order ? a : b, &hi = in_order ? b : a;
+    if (lo.rows == 1) return true;                       // the other one begins inside it
+    const uint64_t off = (reinterpret_cast<uintptr_t>(hi.first) - reinterpret_cast<uintptr_t>(lo.first)) % lo.pitch;
+    return off < lo.width || off + hi.width > lo.pitch;
+}
+
+// Whether an output shares an element with an input or with another output.  may_out may be may_in, element for element (-1: none may).
+template <int INS, int OUTS>
+[[maybe_unused]] bool outputs_share(const Extent (&in)[INS], const Extent (&out)[OUTS], int may_out, int may_in)
+{
+    for (int i = 0; i < OUTS; ++i) {
+        for (int k = 0; k < INS; ++k) {
+            if (i == may_out && k == may_in && out[i].first == in[k].first && out[i].pitch == in[k].pitch) continue;
+            if (share(out[i], in[k])) return true;
+        }
+        for (int k = i + 1; k < OUTS; ++k)
+            if (share(out[i], out[k])) return true;
+    }
+    return false;
+}
+
 // Sizes whose products stay far inside 64 bits.
 constexpr int64_t kMaxExtent = int64_t(1) << 40;
 [[maybe_unused]] bool bad_matrix(int64_t rows, int64_t ld, int64_t columns)
