@@ -21,7 +21,9 @@
  *              sizes (of any element type; 0: NULL will do).  Nothing has to be cleared, nothing is kept in it from call to
  *              call; calls that may run at the same time need one each.
  *   results    depend on the arguments alone: no atomics on memory, sums in a fixed order.
- *   overlap    outputs overlap neither inputs nor each other (CX_ERR_ALIAS) except where a call says so.
+ *   overlap    outputs overlap neither inputs nor each other (CX_ERR_ALIAS) except where a call says so.  Parts of the rows of one wider
+ *              matrix do not overlap; a flat row counts from its first column to its table's end, and of two matrices of several rows
+ *              and of different ld everything between the first and the last element.
  *   empty      sizes of zero tokens, rows, steps or sequences are valid; pointers to empty arrays may be NULL.
  *   return     CX_OK or a negative cx_status of cx_mix.h.  Argument errors are detected on the host before anything is
  *              enqueued: CX_ERR_NULL, CX_ERR_SHAPE (a size, a stride, a weight or the workspace's size out of range),

@@ -355,18 +355,12 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
     constexpr int kElem = sizeof(typename E::T);
     if (misaligned_to(a.z, kElem) || misaligned_to(a.dz, kElem) || misaligned_to(a.ids, 4) || misaligned_to(a.labels, 4) || misaligned_to(a.t, 4) ||
         misaligned_to(a.gout, 4) || misaligned_to(a.loss, 4) || misaligned_to(a.stats, 4) || misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const uint64_t z_bytes = span(N, a.ld, a.V, kElem), row_bytes = N * 4, top_bytes = N * a.K * 4;
-    const struct { const void *p; uint64_t bytes; } in[5] = {{a.z, z_bytes}, {a.ids, top_bytes}, {a.t, top_bytes}, {a.labels, row_bytes}, {a.gout, row_bytes}};
-    const struct { const void *p; uint64_t bytes; } out[4] = {{a.dz, want_dz ? span(N, a.ld_dz, a.V, kElem) : 0}, {a.loss, from_saved ? 0 : row_bytes},
-                                                              {a.stats, row_bytes * 4}, {workspace, static_cast<uint64_t>(need)}};
-    for (int i = 0; i < 4; ++i) {
-        for (int k = 0; k < 5; ++k) {
-            if (i == 0 && k == 0 && static_cast<const void *>(a.dz) == a.z && a.ld_dz == a.ld) continue;     // in place
-            if (overlap(out[i].p, out[i].bytes, in[k].p, in[k].bytes)) return CX_ERR_ALIAS;
-        }
-        for (int k = i + 1; k < 4; ++k)
-            if (overlap(out[i].p, out[i].bytes, out[k].p, out[k].bytes)) return CX_ERR_ALIAS;
-    }
+    const uint64_t row_bytes = N * 4, top_bytes = N * a.K * 4;
+    const Extent in[5] = {matrix_of(a.z, N, a.ld, a.V, kElem), dense_of(a.ids, top_bytes), dense_of(a.t, top_bytes), dense_of(a.labels, row_bytes),
+                          dense_of(a.gout, row_bytes)};
+    const Extent out[4] = {matrix_of(a.dz, want_dz ? N : 0, a.ld_dz, a.V, kElem), dense_of(a.loss, from_saved ? 0 : row_bytes),
+                           dense_of(a.stats, row_bytes * 4), dense_of(workspace, need)};
+    if (outputs_share(in, out, 0, 0)) return CX_ERR_ALIAS;
     if (!want_dz) a.dz = nullptr;
     a.parts = space.parts;
     a.part_stats = static_cast<Stats *>(workspace);

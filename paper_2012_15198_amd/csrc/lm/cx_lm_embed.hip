@@ -548,8 +548,9 @@ int lookup(const typename E::T *x, int64_t ld, int32_t W, int64_t offset, int32_
     if (bad_matrix(W * N, ld_out, D)) return CX_ERR_SHAPE;
     constexpr int kElem = sizeof(typename E::T);
     if (misaligned_to(x, kElem) || misaligned_to(out, kElem) || misaligned_to(tokens, 4)) return CX_ERR_ALIGN;
-    const uint64_t out_bytes = span(W * N, ld_out, D, kElem);
-    if (overlap(out, out_bytes, x, span(W, ld, offset + static_cast<int64_t>(V) * D, kElem)) || overlap(out, out_bytes, tokens, W * N * 4)) return CX_ERR_ALIAS;
+    const Extent in[2] = {matrix_of(x, W, ld, offset + static_cast<int64_t>(V) * D, kElem), dense_of(tokens, W * N * 4)};
+    const Extent result[1] = {matrix_of(out, W * N, ld_out, D, kElem)};
+    if (outputs_share(in, result, -1, -1)) return CX_ERR_ALIAS;
     const int shift = lanes_shift<E>(D), groups = kThreads >> shift;
     const int64_t slabs = ceil_div(ceil_div(D, E::kPer16), 1 << shift);
     // Four rows a group from 4,096 workgroups of one row on; from 64 MB on, results that go past the caches, and two rows: 16 x 4,096 tokens
@@ -602,11 +603,10 @@ int grad(const typename E::T *dout, int64_t ld_dout, const int32_t *tokens, int3
     constexpr int kElem = sizeof(typename E::T);
     if (misaligned_to(dout, kElem) || misaligned_to(g_in, kElem) || misaligned_to(g_out, kElem) || misaligned_to(tokens, 4) ||
         misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const uint64_t g_bytes = span(W, ld, offset + static_cast<int64_t>(V) * D, kElem), dout_bytes = span(W * N, ld_dout, D, kElem), token_bytes = W * N * 4;
-    if (overlap(g_out, g_bytes, dout, dout_bytes) || overlap(g_out, g_bytes, tokens, token_bytes) ||
-        (g_in != g_out && overlap(g_out, g_bytes, g_in, g_bytes))) return CX_ERR_ALIAS;
-    if (overlap(workspace, space.bytes, g_out, g_bytes) || overlap(workspace, space.bytes, dout, dout_bytes) ||
-        overlap(workspace, space.bytes, g_in, g_bytes) || overlap(workspace, space.bytes, tokens, token_bytes)) return CX_ERR_ALIAS;
+    const int64_t columns = offset + static_cast<int64_t>(V) * D;
+    const Extent in[3] = {matrix_of(dout, W * N, ld_dout, D, kElem), dense_of(tokens, W * N * 4), matrix_of(g_in, W, ld, columns, kElem)};
+    const Extent out[2] = {matrix_of(g_out, W, ld, columns, kElem), dense_of(workspace, space.bytes)};
+    if (outputs_share(in, out, 0, 2)) return CX_ERR_ALIAS;
     char *base = static_cast<char *>(workspace);
     Sorted *sorted = reinterpret_cast<Sorted *>(base + space.sorted);
     uint64_t *named = reinterpret_cast<uint64_t *>(base + space.named);

@@ -337,14 +337,11 @@ int scores(const typename E::T *z, int64_t ld, int64_t N, int32_t V, const int32
     constexpr int kElem = sizeof(typename E::T);
     if (misaligned_to(z, kElem) || misaligned_to(tokens, 4) || misaligned_to(logp, 4) || misaligned_to(entropy, 4) || misaligned_to(top_ids, 4) ||
         misaligned_to(top_logp, 4) || misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const uint64_t z_bytes = span(N, ld, V, kElem), row_bytes = N * 4, top_bytes = N * K * 4;
-    const struct { const void *p; uint64_t bytes; } outs[5] = {{logp, row_bytes}, {entropy, row_bytes}, {top_ids, top_bytes},
-                                                               {top_logp, top_bytes}, {workspace, static_cast<uint64_t>(space.bytes)}};
-    for (int i = 0; i < 5; ++i) {
-        if (overlap(outs[i].p, outs[i].bytes, z, z_bytes) || overlap(outs[i].p, outs[i].bytes, tokens, row_bytes)) return CX_ERR_ALIAS;
-        for (int k = i + 1; k < 5; ++k)
-            if (overlap(outs[i].p, outs[i].bytes, outs[k].p, outs[k].bytes)) return CX_ERR_ALIAS;
-    }
+    const uint64_t row_bytes = N * 4, top_bytes = N * K * 4;
+    const Extent in[2] = {matrix_of(z, N, ld, V, kElem), dense_of(tokens, row_bytes)};
+    const Extent out[5] = {dense_of(logp, row_bytes), dense_of(entropy, row_bytes), dense_of(top_ids, top_bytes), dense_of(top_logp, top_bytes),
+                           dense_of(workspace, space.bytes)};
+    if (outputs_share(in, out, -1, -1)) return CX_ERR_ALIAS;
     char *base = static_cast<char *>(workspace);
     const ScoreArgs<E> a{z, tokens, logp, entropy, top_logp, top_ids, ld, V, K, space.parts, scale, reinterpret_cast<Stats *>(base),
                          reinterpret_cast<Key *>(base + space.keys)};

@@ -125,12 +125,6 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
     return a && b && a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
 }
 
-// Bytes from a matrix' first element to its last one.
-[[maybe_unused]] uint64_t span(int64_t rows, int64_t ld, int64_t columns, int elem)
-{
-    return rows < 1 || columns < 1 ? 0 : (static_cast<uint64_t>(rows - 1) * ld + columns) * elem;
-}
-
 // An array of a call for the question whether two of them share an element: rows of `width` bytes, `pitch` bytes from row to row.
 struct Extent {
     const void *first;
