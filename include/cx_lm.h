@@ -132,7 +132,7 @@ int cx_gated_scan_grad_f16(const uint16_t *f, int64_t ldf, const uint16_t *x, in
                            void *stream);
 
 /* ------------------------------------------------------------------------------------
- * cx_token_scores -- of N rows of V logits (scale = 1 / temperature > 0), p = softmax(scale * z):
+ * cx_token_scores -- of N rows of V logits (scale = 1 / temperature > 0, log2(e) scale finite), p = softmax(scale * z):
  *     logp[n] = log p[tokens[n]]  (0 for a token outside [0, V)) ;  entropy[n] = -sum_v p_v log p_v
  *     top_ids[n][k], top_logp[n][k]: the K largest logits, largest first, the lower id first among equal ones, and their log p
  *   logp (with tokens, int32 [N]) and entropy: float [N] or NULL;  top_ids int32, top_logp float: [N][K], 0 <= K <= CX_MAX_TOP, K <= V

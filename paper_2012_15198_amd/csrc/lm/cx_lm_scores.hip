@@ -327,7 +327,7 @@ int scores(const typename E::T *z, int64_t ld, int64_t N, int32_t V, const int32
 {
     const int rc = check_sizes(N, V, K);
     if (rc != CX_OK) return rc;
-    if (!(scale > 0.0f) || !(scale <= 3.0e38f)) return CX_ERR_SHAPE;
+    if (!(scale > 0.0f) || !(scale * kLog2e <= kLargest)) return CX_ERR_SHAPE;      // an infinite factor would make the maximum's term 0 * inf
     if (N == 0) return CX_OK;
     if (!z || (logp && !tokens) || (K > 0 && (!top_ids || !top_logp))) return CX_ERR_NULL;
     if (bad_matrix(N, ld, V)) return CX_ERR_SHAPE;

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kRowThreads = 512, kRowWaves = kRowThreads / kWave;
 constexpr int kAhead = 4;                               // 16-byte loads a thread has in flight
-constexpr float kLowest = -3.40282346638528859812e38f;
+constexpr float kLargest = 3.40282346638528859812e38f, kLowest = -kLargest;
 constexpr float kVanish = -200.0f;                      // exponents (base 2) from here on give 0; keeps 0 * inf out of the sums
 
 // With e = 2^((z - m) c), s is the sum of e, and u

@@ -114,3 +114,23 @@ def test_outputs_that_are_not_wanted_and_no_rows():
     lm.cx_token_scores(z, None, None, None, ids, top)
     assert torch.equal(ids.cpu(), R.order(z.cpu())[:, :4].int())
     lm.cx_token_scores(torch.empty((0, 50), device=DEV), torch.empty(0, dtype=torch.int32, device=DEV), torch.empty(0, device=DEV))
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("V", [700, 70_000])
+def test_scales_at_the_ends_of_their_range(suffix, V):
+    """The largest scale leaves the maximum alone, shared by the logits that equal it; the smallest makes every row uniform."""
+    z = torch.randn((3, V), generator=torch.Generator().manual_seed(V)).to(R.TYPES[suffix])
+    z[1, 100], z[1, 650] = 20.0, 20.0
+    best = z.double().amax(1, keepdim=True)
+    at = (z.double() == best).double()
+    tokens = at.argmax(1).int()
+    tokens[2] = int(z[2].double().argmin())
+    for scale, count in ((2.3e38, at.sum(1)), (1e-38, torch.full((3,), float(V), dtype=torch.float64))):
+        logp, entropy, ids, _ = run(suffix, z, tokens, 2, scale)
+        want = -count.log()
+        if scale > 1:
+            want[2] = -torch.inf
+        R.check(logp, want, R.U * (64 + V / 256) * 20)
+        R.check(entropy, count.log(), R.U * (64 + V / 256) * 20)
+        assert torch.equal(ids.cpu(), R.order(z)[:, :2].int())
