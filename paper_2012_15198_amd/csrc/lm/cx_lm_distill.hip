@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kRowThreads) void part_kernel(const DistillArgs<E> 
 
 struct Targets {                                        // of a row: the teacher's tokens, then the label
     int id[kMaxTeacher + 1];                            // -1: none
-    float t[kMaxTeacher + 1];                           // t / tau (-inf: none), later log q
+    float t[kMaxTeacher + 1];                           // the teacher's logits (-inf: none)
     float z[kMaxTeacher + 1];                           // their logits
     float q[kMaxTeacher + 1];                           // weight of the gradient's target, without gout: w_kl tau q, w_ce
     float soft, hard, loss;                             // w_kl tau, w_ce if these terms count in this row; the row's loss
@@ -90,7 +90,7 @@ __device__ __forceinline__ void keep_target(const DistillArgs<E> &a, int64_t n, 
     if (k > a.K) return;
     const bool valid = own.id >= 0 && own.id < a.V;
     to.id[k] = valid ? own.id : -1;
-    to.t[k] = valid && k < a.K ? own.t / a.tau : -__builtin_inff();
+    to.t[k] = valid && k < a.K ? own.t : -__builtin_inff();
     to.z[k] = valid ? E::widen(a.z[n * a.ld + own.id]) : 0.0f;
 }
 template <class E>
@@ -100,7 +100,9 @@ __device__ __forceinline__ void keep_others(const DistillArgs<E> &a, int64_t n, 
 }
 
 // Wavefront 0, behind a barrier: the teacher's distribution, and the loss from the row's statistics.  The row's own logits at
-// the targets count for the loss alone.
+// the targets count for the loss alone.  Only differences of logits are divided by tau, and the loss is taken as
+//   w_kl tau sum_k q_k ((t_k - max t) - (z_k - m) + tau (log s - log sum_t)):
+// a quotient such as the lowest value / 0.5 is infinite, and tau^2 times an infinite log p would be no loss where tau^2 log p is one.
 template <class E>
 __device__ __forceinline__ void settle(const DistillArgs<E> &a, const Stats &all, Targets &to)
 {
@@ -109,23 +111,23 @@ __device__ __forceinline__ void settle(const DistillArgs<E> &a, const Stats &all
     for (int k = threadIdx.x; k < a.K; k += kWave) high = fmaxf(high, to.t[k]);
 #pragma unroll
     for (int d = kWave / 2; d > 0; d /= 2) high = fmaxf(high, __shfl_xor(high, d));
-    for (int k = threadIdx.x; k < a.K; k += kWave) sum += to.t[k] == lowest ? 0.0f : expf(to.t[k] - high);
+    for (int k = threadIdx.x; k < a.K; k += kWave) sum += to.t[k] == lowest ? 0.0f : expf((to.t[k] - high) / a.tau);
 #pragma unroll
     for (int d = kWave / 2; d > 0; d /= 2) sum += __shfl_xor(sum, d);
     const bool row = all.s != 0.0f;                     // a row of -inf alone has no distribution: it counts for nothing
     const bool soft = row && a.w_kl != 0.0f && sum != 0.0f;
-    const float log_sum = logf(sum), log_s = logf(all.s);
+    const float log_sum = logf(sum), sums = a.tau * (logf(all.s) - log_sum);
     for (int k = threadIdx.x; k < a.K; k += kWave) {
-        const float log_q = to.t[k] - high - log_sum;
-        const float q = soft && to.t[k] != lowest ? expf(log_q) : 0.0f;
-        if (q != 0.0f) loss += q * (log_q - ((to.z[k] - all.m) / a.tau - log_s));
+        const float below = to.t[k] - high;
+        const float q = soft && to.t[k] != lowest ? expf(below / a.tau - log_sum) : 0.0f;
+        if (q != 0.0f) loss += q * (below - (to.z[k] - all.m) + sums);
         to.q[k] = a.w_kl * a.tau * q;
     }
 #pragma unroll
     for (int d = kWave / 2; d > 0; d /= 2) loss += __shfl_xor(loss, d);
     if (threadIdx.x == 0) {
         const bool hard = row && to.id[a.K] >= 0;
-        loss = soft ? a.w_kl * a.tau * a.tau * loss : 0.0f;
+        loss = soft ? a.w_kl * a.tau * loss : 0.0f;
         if (hard) loss -= a.w_ce * ((to.z[a.K] - all.m) - logf(all.u));
         to.q[a.K] = hard ? a.w_ce : 0.0f;
         to.soft = soft ? a.w_kl * a.tau : 0.0f;

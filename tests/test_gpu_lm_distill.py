@@ -165,3 +165,38 @@ def test_no_rows_and_top_scores_of_a_teacher():
     loss, dz = e(6), torch.empty_like(z)
     lm.cx_distill_step(z, ids, top, None, torch.ones(6, device=DEV), loss, dz, 1.0, 1.0, 0.0)
     assert loss.abs().max() < 200 * R.U * 10 and dz.abs().max() < 200 * R.U
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("N,V", [(5, 600), (520, 600), (5, 140_001)])
+def test_targets_of_extreme_values_at_low_temperatures(suffix, N, V):
+    """What divided by the temperature leaves float32's range: teachers whose logits are all the lowest value (uniform) or share the
+    largest one, and a student that masks a teacher's token with the lowest value."""
+    dtype = R.TYPES[suffix]
+    z, ids, t, labels, gout = make(N, V, 6, dtype, N + V)
+    t[0] = torch.finfo(torch.float32).min
+    t[1, :2], t[1, 2:] = 3e38, -3e38
+    t[2, 3:] = torch.finfo(torch.float32).min
+    z[3, ids[3, 1].long()] = torch.finfo(dtype).min
+    labels[3] = ids[3, 0]
+    below = t.double() - t.double().amax(1, keepdim=True)             # changes nothing, but beside 3e38 even 64 bits hold no log 6
+    for tau in (0.5, 0.25):
+        loss, dz = run(suffix, z, ids, t, labels, gout, tau, 0.7, 0.3)
+        ref, grad, slack, grad_slack = R.distill(z, ids, below, labels, gout, tau, 0.7, 0.3)
+        assert ref.isfinite().all() and (ref.abs() < torch.finfo(torch.float32).max).all()
+        R.check(loss, ref, slack, "loss")
+        R.check(dz, grad, grad_slack, "dz")
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("N,V", [(5, 600), (520, 600), (5, 140_001)])
+def test_the_lowest_temperatures(suffix, N, V):
+    """Loss and gradient of the first term vanish with the temperature; the second term is what it is alone."""
+    z, ids, t, labels, gout = make(N, V, 6, R.TYPES[suffix], N + V)
+    want, grad, slack, grad_slack = R.distill(z, ids, t, labels, gout, 1.0, 0.0, 0.3)
+    for tau in (1e-38, 1e-30):
+        loss, dz = run(suffix, z, ids, t, labels, gout, tau, 0.7, 0.0)
+        assert (loss.abs() <= 1e3 * tau).all() and (dz.float().abs() <= 4 * tau).all()
+        loss, dz = run(suffix, z, ids, t, labels, gout, tau, 0.7, 0.3)
+        R.check(loss, want, slack)
+        R.check(dz, grad, grad_slack)
