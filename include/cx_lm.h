@@ -163,8 +163,8 @@ int cx_token_scores_f16(const uint16_t *z, int64_t ld, int64_t N, int32_t V, con
  *   stats    float [N][4]: written by _loss (may be NULL there), read by _grad with the same tau, w_kl and w_ce
  *   loss     float [N];  dz [N][ld_dz], may be z (with the same ld)
  * _loss computes the loss, _grad the gradient from the statistics that _loss left, _step both in one call.
- * tau > 0, w_kl >= 0, w_ce >= 0, finite.  A row that no term counts in has loss 0 and gradient 0, whatever its logits; so has a row
- * of -inf alone.  NaN and +inf in a row that counts make its loss and gradient NaN.
+ * tau > 0, w_kl >= 0, w_ce >= 0; they, log2(e) / tau and w_kl tau are finite.  A row that no term counts in has loss 0 and gradient 0,
+ * whatever its logits; so has a row of -inf alone.  NaN and +inf in a row that counts make its loss and gradient NaN.
  */
 int cx_distill_workspace(int64_t N, int32_t V, int64_t *bytes);
 int cx_distill_loss(const float *z, int64_t ld, int64_t N, int32_t V, int32_t K, const int32_t *ids, const float *t,

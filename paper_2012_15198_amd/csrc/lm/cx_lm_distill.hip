@@ -346,6 +346,7 @@ int distill(DistillArgs<E> a, int64_t N, bool from_saved, bool want_dz, void *wo
     const int rc = check_sizes(N, static_cast<int32_t>(a.V), a.K);
     if (rc != CX_OK) return rc;
     if (!(a.tau > 0.0f) || !(a.tau <= 3.0e38f) || !(a.w_kl >= 0.0f) || !(a.w_ce >= 0.0f) || !(a.w_kl <= 3.0e38f) || !(a.w_ce <= 3.0e38f)) return CX_ERR_SHAPE;
+    if (!(kLog2e / a.tau <= kLargest) || !(a.w_kl * a.tau <= kLargest)) return CX_ERR_SHAPE;        // factors of every element
     if (N == 0) return CX_OK;
     if (!a.z || (a.K > 0 && (!a.ids || !a.t)) || (want_dz && (!a.dz || !a.gout)) || (!from_saved && !a.loss) || (from_saved && !a.stats)) return CX_ERR_NULL;
     if (bad_matrix(N, a.ld, a.V) || (want_dz && bad_matrix(N, a.ld_dz, a.V))) return CX_ERR_SHAPE;

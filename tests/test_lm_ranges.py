@@ -15,3 +15,12 @@ LOG2E = math.log2(math.e)
 @pytest.mark.parametrize("scale", [LARGEST / LOG2E * 1.0001, 2.9e38, LARGEST, math.inf])
 def test_a_scale_whose_base_two_factor_overflows(suffix, scale):
     assert getattr(lm.lib(), "cx_token_scores" + suffix)(A, 50, 600, 50, B, scale, C, D, 4, E, F, None, 0, None) == -2
+
+
+@pytest.mark.parametrize("suffix", SUFFIXES)
+@pytest.mark.parametrize("tau,w_kl", [(4.2e-39, 1.0), (1e-45, 1.0), (2e38, 2.0), (1e20, 1e20)])
+def test_a_temperature_whose_factors_overflow(suffix, tau, w_kl):
+    head = (A, 50, 600, 50, 4, B, C, D, tau, w_kl, 0.5)
+    assert getattr(lm.lib(), "cx_distill_loss" + suffix)(*head, E, F, None, 0, None) == -2
+    assert getattr(lm.lib(), "cx_distill_grad" + suffix)(*head, F, E, G, 50, None) == -2
+    assert getattr(lm.lib(), "cx_distill_step" + suffix)(*head, E, F, G, 50, None, 0, None) == -2
