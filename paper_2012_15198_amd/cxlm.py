@@ -27,6 +27,8 @@ _TYPED = ["cx_embed_lookup", "cx_embed_grad", "cx_gated_scan", "cx_gated_scan_gr
 EXPORTS = ["cx_lm_abi_version", "cx_embed_workspace", "cx_scan_workspace", "cx_scores_workspace", "cx_distill_workspace",
            *(name + suffix for name in _TYPED for suffix in ("", "_bf16", "_f16"))]
 
+_INT32 = 2**31 - 1
+_CX_ERR_SHAPE = -2
 _lib = None
 _torch = None
 _dtypes = {}                     # "", "_bf16", "_f16" -> the torch type of the matrices
@@ -129,6 +131,11 @@ def _optional(name, arg, t, dtype, shape, device):
     return None if t is None else _dense(name, arg, t, dtype, shape, device)
 
 
+def _too_wide(name):
+    """A size that a 32-bit argument cannot hold, of which ctypes would drop the upper bits: refused as the library refuses what is beyond its limits."""
+    raise CxError(name, _CX_ERR_SHAPE)
+
+
 def _on_device(name, device):
     """Last check before the call."""
     if device < 0:
@@ -158,6 +165,8 @@ def _span(work):
 
 def _size(fn, *args) -> int:
     L = _lib or lib()
+    if max(args) > _INT32 or min(args) < -_INT32:        # the 64-bit ones have limits below 2^31 too
+        _too_wide(fn)
     n = ctypes.c_int64()
     _ok(fn, getattr(L, fn)(*args, ctypes.byref(n)))
     return n.value
@@ -198,6 +207,8 @@ def _lookup(name, suffix, x, tokens, out, offset, V, scale, stream):
     ld = _matrix(name, "x", x, dtype, W, None, device)
     ld_out = _matrix(name, "out", out, dtype, W * N, None, device)
     D = out.shape[1]
+    if V > _INT32 or V < -_INT32 or D > _INT32 or W > _INT32:
+        _too_wide(name)
     if offset < 0 or offset + V * D > x.shape[1]:
         raise ValueError(f"{name}: a table of {V} x {D} at {offset} does not fit rows of {x.shape[1]}")
     tp = _dense(name, "tokens", tokens, _torch.int32, (W, N), device)
@@ -227,6 +238,8 @@ def _embed_grad(name, suffix, dout, tokens, g_in, g_out, offset, V, scale, works
     W, N = tokens.shape
     ld_dout = _matrix(name, "dout", dout, dtype, W * N, None, device)
     D = dout.shape[1]
+    if V > _INT32 or V < -_INT32 or D > _INT32 or W > _INT32:
+        _too_wide(name)
     ld = _matrix(name, "g_out", g_out, dtype, W, None, device)
     fits = g_out.shape[1]
     if g_in is not None:
@@ -279,6 +292,8 @@ def _scan(name, suffix, f, x, y, T, h0, h_last, reset, states, workspace, stream
     dtype, device, f32 = _dtypes[suffix], f.get_device(), _torch.float32
     ldf = _matrix(name, "f", f, dtype, None, None, device)
     rows, D = f.shape
+    if D > _INT32:
+        _too_wide(name)
     B = _sequences(name, rows, T, h0, h_last)
     ldx = _matrix(name, "x", x, dtype, rows, D, device)
     ldy = _matrix(name, "y", y, dtype, rows, D, device)
@@ -310,6 +325,8 @@ def _scan_grad(name, suffix, f, x, dy, df, dx, T, states, dh_last, dh0, reset, w
     dtype, device, f32 = _dtypes[suffix], f.get_device(), _torch.float32
     ldf = _matrix(name, "f", f, dtype, None, None, device)
     rows, D = f.shape
+    if D > _INT32:
+        _too_wide(name)
     B = _sequences(name, rows, T, dh_last, dh0)
     ldx = _matrix(name, "x", x, dtype, rows, D, device)
     lddy = _matrix(name, "dy", dy, dtype, rows, D, device)
@@ -355,6 +372,8 @@ def _scores(name, suffix, z, tokens, logp, entropy, top_ids, top_logp, scale, wo
         K = top_ids.shape[1]
         ip = _dense(name, "top_ids", top_ids, i32, (N, K), device)
         pp = _dense(name, "top_logp", top_logp, f32, (N, K), device)
+    if V > _INT32 or K > _INT32:
+        _too_wide(name)
     work = _scratch(name, workspace, "cx_scores_workspace", (N, V, K), device, stream)
     _call(name, z.data_ptr(), ld, N, V, tp, scale, lp, ep, K, ip, pp, *_span(work), cxmix._stream(stream))
 
@@ -381,6 +400,8 @@ def _targets(name, suffix, z, ids, t, labels, device):
     if len(ids.shape) != 2:
         raise ValueError(f"{name}: ids: expected int32 [N][K]")
     K = ids.shape[1]
+    if V > _INT32 or K > _INT32:
+        _too_wide(name)
     ip = _dense(name, "ids", ids, _torch.int32, (N, K), device)
     tp = _dense(name, "t", t, _torch.float32, (N, K), device)
     lp = _optional(name, "labels", labels, _torch.int32, (N,), device)
