@@ -67,7 +67,8 @@ int cx_embed_lookup_f16(const uint16_t *x, int64_t ld, int32_t W, int64_t offset
 /* ------------------------------------------------------------------------------------
  * cx_embed_grad -- its gradient by sorted tokens, into the same columns of the workers' flat gradient rows:
  *     g_out[w][v] = round(g_in[w][v] + scale * sum over n with tokens[w][n] = v of dout[w * N + n])
- * summed in fp32 in an order that the tokens alone fix (ascending n, in pieces where a token occurs more than 64 times).
+ * summed in fp32 in an order that the tokens, the sizes and the element type alone fix: by ascending n, in parts where a token's
+ * places cross one of the cuts that the sorted tokens have at equal distances, so that two occurrences may be in two parts.
  *   g_in     NULL: nothing is added, and rows that no token names become zeros;
  *            = g_out: added in place, rows that no token names are not touched (the gradient of a table that is
  *            also the output projection);  otherwise a second matrix with the same ld
@@ -164,7 +165,8 @@ int cx_token_scores_f16(const uint16_t *z, int64_t ld, int64_t N, int32_t V, con
  *   loss     float [N];  dz [N][ld_dz], may be z (with the same ld)
  * _loss computes the loss, _grad the gradient from the statistics that _loss left, _step both in one call.
  * tau > 0, w_kl >= 0, w_ce >= 0; they, log2(e) / tau and w_kl tau are finite.  A row that no term counts in has loss 0 and gradient 0,
- * whatever its logits; so has a row of -inf alone.  NaN and +inf in a row that counts make its loss and gradient NaN.
+ * whatever its logits; so has a row of -inf alone.  NaN and +inf in a row that counts make its loss and gradient NaN.  A probability
+ * below 2^-126 is 0 in the gradient.
  */
 int cx_distill_workspace(int64_t N, int32_t V, int64_t *bytes);
 int cx_distill_loss(const float *z, int64_t ld, int64_t N, int32_t V, int32_t K, const int32_t *ids, const float *t,

@@ -8,7 +8,8 @@
 // Bound by memory where the exponentials allow it: loss and gradient together read a row of logits once, into registers, as long as it
 // fits there.  q and the label touch K + 1 elements: every element is written with its share of p and p1, and behind a
 // barrier those few are written again with their targets.
-// 8,192 bfloat16 rows of 65,536 take 416 us (5.2 TB/s, what a copy of the logits takes), 4,096 float32 rows of 50,257 336 us (4.9 TB/s).
+// 8,192 bfloat16 rows of 65,536 take 419 us at tau = 2 (5.1 TB/s, what a copy of the logits takes), 431 in rows of twenty calls and up to 490
+// there under the profiler; 4,096 float32 rows of 50,257 330 us (5.0 TB/s).
 // Where rows are few, several workgroups share one: part_kernel leaves the parts' statistics in the workspace, and each
 // workgroup of the second launch joins them for itself.
 #include "lm_vocab.hpp"

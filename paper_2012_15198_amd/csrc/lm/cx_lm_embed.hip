@@ -3,8 +3,9 @@
 //
 //   out[w][n] = round(scale * table_w[token[w][n]])               g[w][v] = round(g_in[w][v] + scale * sum_{n: token = v} dout[w][n])
 //
-// Both are bound by memory: 16 workers' 4,096 tokens of 768 float32 columns take 50 us (5.9 TB/s), the gradient of as many in bfloat16 into
-// tables of 32,768 rows 168 us for the sums and the filling (5.4 TB/s), 14 for the sort before and 8 for the joining behind.  A group of lanes
+// Both are bound by memory: 16 workers' 4,096 tokens of 768 float32 columns take 49 to 51 us (5.7 to 6.0 TB/s), the gradient of as many in bfloat16 into
+// tables of 32,768 rows 166 to 190 us for the sums and the filling, by where the buffers lie (medians of 169 and 178, 5.4 and 5.1 TB/s), 14 for
+// the sort before and 8 for the joining behind.  A group of lanes
 // (a power of two, as many as one row's 16-byte vectors, 64 at most) handles one vector column each of one row, so a short row does not leave a wavefront's lanes idle.
 //
 // The gradient adds in a fixed order, which atomics would not, and writes each row of the table once (where nearly all are zeros, the others twice).
@@ -576,8 +577,11 @@ struct GradSpace {
 GradSpace grad_space(int32_t W, int64_t N, int32_t V, int32_t D)
 {
     GradSpace s{};
-    // tokens of a piece: few, so that there are many (1,000 tokens of four workers, 129 columns: sums in 9.5 us with 8, 13.6 with 16); more of
-    // them where a list of all tokens would leave thousands of sums to join
+    // tokens of a piece: few, so that there are many; more of them where long lists would leave thousands of sums to join.  Calls of 8, 16, 32 and
+    // 64 tokens a piece, us, 768 bfloat16 columns and tables of 32,768 rows unless noted: four workers' 1,000 (129 float32 columns) 18, 20, 26, 39;
+    // one worker's 4,096 28, 29, 36, 49, sixteen's 193, 191, 195, 211; one worker's 16,000 (129 float32 columns) 43, 39, 42, 54; 32,768 82, 72,
+    // 72, 82, all of them one token 383, 233, 155, 123; sixteen workers' 32,768 491, 435, 414, 414; one worker's 131,072 (float32) 384, 322, 283,
+    // 275.  Above 16,384 it is the frequent token that 64 are for: one worker's ordinary text would take less with 16 or 32
     s.piece = N <= 2048 ? 8 : N <= 16384 ? 16 : 64;
     s.chunks = ceil_div(N, s.piece);
     s.named = 0;

@@ -14,7 +14,7 @@
 //   split      where columns are few (workgroups < kSplitBelow) the steps are also split over workgroups: a first launch composes
 //              the map of each span (it reads what the second reads again, from the last-level cache where the call fits there)
 //
-// Bound by memory in long calls (32 sequences of 2,048 x 1,024 in bfloat16: 90 us, 4.5 TB/s; gradient 124 us, 5.4 TB/s; the forward pass's
+// Bound by memory in long calls (32 sequences of 2,048 x 1,024 in bfloat16: 86 to 90 us, 4.5 TB/s; gradient 139 us, 4.8 TB/s; the forward pass's
 // two transcendental instructions an element take half as long as its loads), by the launches' latency and by the second reading where few
 // columns are split (one sequence of 16,381 x 1,024: 40 us, 2.5 TB/s), and by the launch for single steps.
 //
@@ -293,8 +293,8 @@ template <bool V>
 using Flag = std::integral_constant<bool, V>;
 
 // What a launch does: a whole call, or of a split one the spans' maps or the spans.  Reading past the caches is for the whole call: 32 sequences of
-// 2,048 x 1,024 take 90 us in bfloat16 against 98, their gradient 124 against 147; in a split one, whose two launches read the same, one
-// sequence of 16,381 x 1,024 would take 47 against 40.
+// 2,048 x 1,024 take 86 us in bfloat16 against 99, their gradient 139 against 150 (float32 164 and 171, 276 and 279); in a split one, whose
+// two launches read the same, one sequence of 16,381 x 1,024 would take 47 against 40.
 enum Pass { kWhole, kMaps, kSpans };
 
 // Grid (slabs of columns of sequences, spans): workgroups that run together read whole rows.  kMaps: the first launch of a split call,
@@ -518,7 +518,7 @@ __global__ __launch_bounds__(256) void pass_kernel(const float *from, float *to,
 }
 
 // One step, as decoding takes them: an element to a thread, all loads at once, where a walk waits for the state that enters and then steps
-// over 15 absent ones.  64 sequences of 2,048 columns take 2.5 us in bfloat16 against a walk's 4.3, 4,096 of 4,096 63 against 212 (3.7 TB/s).
+// over 15 absent ones.  64 sequences of 2,048 columns take 2.5 us in bfloat16 against a walk's 4.3, 4,096 of 4,096 56 to 63 against 212 (4 TB/s).
 template <class E>
 __global__ __launch_bounds__(256) void step_kernel(const ScanArgs<E> a)
 {

@@ -8,8 +8,8 @@
 // the threads' maxima is a threshold that at least K elements reach, and few more than K do; only the subsets whose maximum
 // reaches it are read again.  Elements are compared by a 64-bit key (value, then lower id first), so ties are decided and the
 // result does not depend on the order in which threads find them.
-// Bound by memory: 4,096 float32 rows of 50,003 with 5 tokens take 138 us (5.9 TB/s).  Few rows are bound by the chain of waits: 16 bfloat16 rows of
-// 131,072 with 20 tokens take 9 us, and 4 for joining the parts.
+// Bound by memory: 4,096 float32 rows of 50,003 with 5 tokens take 139 us (5.9 TB/s).  Few rows are bound by the chain of waits: 16 bfloat16 rows of
+// 131,072 with 20 tokens take 8 us, and 5 for joining the parts.
 // Rows are split over workgroups where there are few; join_kernel then joins statistics and keys of the parts.
 #include "lm_vocab.hpp"
 
@@ -232,7 +232,7 @@ __device__ __forceinline__ void write_row(const ScoreArgs<E> &a, int64_t n, cons
     }
 }
 
-// Grid (parts, N): one part of one row.  The first pass reads past the caches (4,096 float32 rows of 50,003: 143 us against 148).
+// Grid (parts, N): one part of one row.  The first pass reads past the caches (4,096 float32 rows of 50,003: 139 us against 149).
 template <class E, bool TOP, int THREADS>
 __global__ __launch_bounds__(THREADS) void scores_kernel(const ScoreArgs<E> a)
 {
