@@ -6,6 +6,10 @@
  *   cx_gated_scan, cx_gated_scan_grad   a gated linear recurrence over long sequences; its single-token step
  *   cx_token_scores                     log probabilities of given tokens, entropy, the largest logits
  *   cx_distill_loss / _grad / _step     distillation from a teacher's top logits, with the label's cross entropy
+ *   cx_dropout                          dropout whose mask a counter-based generator names and nothing stores
+ *   cx_add_norm, cx_add_norm_grad       residual addition (with dropout) and root-mean-square norm; output in 8 bits with scales
+ *   cx_short_conv, cx_short_conv_grad   short causal convolution of every column; its single-token step
+ *   cx_select_scan, cx_select_scan_grad selective state space scan over long sequences; its single-token step
  *
  * Common conventions
  *   types      every operator has three entry points: float32, bfloat16 (suffix _bf16) and IEEE binary16 (suffix _f16);
@@ -44,7 +48,10 @@ extern "C" {
 #define CX_MAX_WIDTH (1 << 20)
 #define CX_MAX_TOP 64               /* alternatives of cx_token_scores */
 #define CX_MAX_TEACHER 256          /* teacher's logits a row of cx_distill_* */
-#define CX_SCAN_CHUNK 16            /* steps between two states that cx_gated_scan keeps for its gradient */
+#define CX_SCAN_CHUNK 16            /* steps between two states that cx_gated_scan and cx_select_scan keep for their gradients */
+#define CX_MAX_NORM_WIDTH 16384     /* columns of cx_add_norm */
+#define CX_MAX_TAPS 4               /* inputs that a step of cx_short_conv sees */
+#define CX_MAX_STATES 16            /* states of a column of cx_select_scan */
 
 /* Version of this header (bumped on any signature change): 1. */
 int cx_lm_abi_version(void);
@@ -196,6 +203,165 @@ int cx_distill_step_bf16(const uint16_t *z, int64_t ld, int64_t N, int32_t V, in
 int cx_distill_step_f16(const uint16_t *z, int64_t ld, int64_t N, int32_t V, int32_t K, const int32_t *ids, const float *t,
                         const int32_t *labels, float tau, float w_kl, float w_ce, const float *gout, float *loss,
                         uint16_t *dz, int64_t ld_dz, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * cx_dropout -- dropout, added to a residual where there is one:
+ *     out = round(residual + keep x s)     s = 2^16 / (2^16 - k),  k = round(p 2^16) <= 65535, 0 <= p < 1
+ * keep of row n and column d: at least k is the 16-bit half (d mod 8) of block (n ceil(D / 8) + floor(d / 8), rng[1]) of Philox4x32 with ten
+ * rounds (Salmon et al. 2011) and key rng[0]: halves of the four words in turn, the lower one first; of each 64-bit number the lower word first.
+ *   x, out   [N][D], N <= 2^31; residual: the same or NULL.  out may be x or residual
+ *   rng      int64 [2] DEVICE: key and draw; another draw is another mask.  Read when the kernel runs, so that a captured call whose
+ *            caller adds to rng[1] between replays draws anew
+ * The gradient is the same call on the result's gradient, with the same rng.  A dropped element counts for nothing, NaN and infinities included.
+ */
+int cx_dropout(const float *x, int64_t ldx, const float *residual, int64_t ldr, float *out, int64_t ldo, int64_t N, int32_t D,
+               const int64_t *rng, float p, void *stream);
+int cx_dropout_bf16(const uint16_t *x, int64_t ldx, const uint16_t *residual, int64_t ldr, uint16_t *out, int64_t ldo, int64_t N,
+                    int32_t D, const int64_t *rng, float p, void *stream);
+int cx_dropout_f16(const uint16_t *x, int64_t ldx, const uint16_t *residual, int64_t ldr, uint16_t *out, int64_t ldo, int64_t N, int32_t D,
+                   const int64_t *rng, float p, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * cx_add_norm -- residual addition and root-mean-square norm of N rows of each of W workers:
+ *     t = residual + drop(x) ;  s = round(t) ;  inv = 1 / sqrt(mean(t^2) + eps) ;  y = round(t inv w)
+ *     scale = max(max |t inv w| / 448, 2^-126) ;  q = (t inv w / scale) rounded to e4m3 (4 exponent, 3 mantissa bits, largest 448)
+ * drop as cx_dropout with p, rng and the row's number in 0 .. W N - 1 (p = 0: nothing is dropped, rng may be NULL); t is not rounded between.
+ * w is [D] in columns [offset, offset + D) of the worker's flat row weights[w].
+ *   x        [W * N][D], D <= CX_MAX_NORM_WIDTH; residual: the same or NULL (zeros)
+ *   s, y     the same or NULL; s may be x or residual, y may be x;  inv: float [W * N] or NULL, which the gradient needs
+ *   q, scale bytes [W * N][ldq], D columns, with float [W * N]; or both NULL.  One of s, y and q at least is wanted
+ * 0 <= eps < infinity.  Squares whose sum leaves float32's range make inv and the row's y 0; an infinity's own y is NaN.  A NaN in a row makes
+ * all of its y NaN, and so does eps = 0 in a row of zeros.  A NaN among a row's y makes its scale and its q NaN.
+ */
+int cx_add_norm(const float *x, int64_t ldx, const float *residual, int64_t ldr, const float *weights, int64_t ldw, int32_t W,
+                int64_t offset, int64_t N, int32_t D, float eps, const int64_t *rng, float p, float *s, int64_t lds, float *y, int64_t ldy,
+                float *inv, uint8_t *q, int64_t ldq, float *scale, void *stream);
+int cx_add_norm_bf16(const uint16_t *x, int64_t ldx, const uint16_t *residual, int64_t ldr, const uint16_t *weights, int64_t ldw,
+                     int32_t W, int64_t offset, int64_t N, int32_t D, float eps, const int64_t *rng, float p, uint16_t *s, int64_t lds,
+                     uint16_t *y, int64_t ldy, float *inv, uint8_t *q, int64_t ldq, float *scale, void *stream);
+int cx_add_norm_f16(const uint16_t *x, int64_t ldx, const uint16_t *residual, int64_t ldr, const uint16_t *weights, int64_t ldw, int32_t W,
+                    int64_t offset, int64_t N, int32_t D, float eps, const int64_t *rng, float p, uint16_t *s, int64_t lds, uint16_t *y,
+                    int64_t ldy, float *inv, uint8_t *q, int64_t ldq, float *scale, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * cx_add_norm_grad -- its gradient.  With g = dy w and the s and inv that the forward call left:
+ *     ds = round(inv (g - s inv mean(g s inv)) + ds_in) ;  dx = round(drop of the same before its rounding)
+ *     dw = round(g_in + sum over the worker's rows of dy s inv), into columns [offset, offset + D) of its flat gradient row g_out[w]
+ *   ds_in    gradient of s from elsewhere (the residual path behind the norm), or NULL
+ *   ds       gradient of residual; dx: gradient of x; one of them may be NULL.  Each may be dy or ds_in
+ *   g_in     NULL (nothing is added), g_out (added in place) or a second matrix with the same ld
+ * Sums are fp32 in an order that the sizes fix.
+ */
+int cx_norm_workspace(int32_t W, int64_t N, int32_t D, int64_t *bytes);
+int cx_add_norm_grad(const float *dy, int64_t lddy, const float *s, int64_t lds, const float *inv, const float *weights, int64_t ldw,
+                     int32_t W, int64_t offset, int64_t N, int32_t D, const float *ds_in, int64_t ldi, const int64_t *rng, float p,
+                     float *ds, int64_t ldds, float *dx, int64_t lddx, const float *g_in, float *g_out, int64_t ldg, void *workspace,
+                     int64_t workspace_bytes, void *stream);
+int cx_add_norm_grad_bf16(const uint16_t *dy, int64_t lddy, const uint16_t *s, int64_t lds, const float *inv, const uint16_t *weights,
+                          int64_t ldw, int32_t W, int64_t offset, int64_t N, int32_t D, const uint16_t *ds_in, int64_t ldi,
+                          const int64_t *rng, float p, uint16_t *ds, int64_t ldds, uint16_t *dx, int64_t lddx, const uint16_t *g_in,
+                          uint16_t *g_out, int64_t ldg, void *workspace, int64_t workspace_bytes, void *stream);
+int cx_add_norm_grad_f16(const uint16_t *dy, int64_t lddy, const uint16_t *s, int64_t lds, const float *inv, const uint16_t *weights,
+                         int64_t ldw, int32_t W, int64_t offset, int64_t N, int32_t D, const uint16_t *ds_in, int64_t ldi,
+                         const int64_t *rng, float p, uint16_t *ds, int64_t ldds, uint16_t *dx, int64_t lddx, const uint16_t *g_in,
+                         uint16_t *g_out, int64_t ldg, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * cx_short_conv -- causal convolution of every column with K taps of its own, B sequences of T steps and D columns:
+ *     v_t = bias + sum_{k < K} w[k] x_{t - K + 1 + k} ;  y_t = round(silu != 0 ? v_t sigmoid(v_t) : v_t)
+ * 1 <= K <= CX_MAX_TAPS.  W workers have B / W sequences each (B a multiple of W); a worker's taps [D][K] and, behind them, biases [D] are in
+ * columns [offset, offset + D (K + 1)) of its flat row.
+ *   reset    uint8 [B][T] or NULL: nonzero where a document begins; its steps see nothing of the steps before
+ *   before   [B][K - 1][D] or NULL (zeros): the inputs before the first step, the oldest first
+ *   after    [B][K - 1][D] or NULL: receives what the step after the last one sees of these inputs, zeros where a reset lies between;
+ *            may be before (generation: T = 1, state in place)
+ */
+int cx_short_conv(const float *x, int64_t ldx, const float *weights, int64_t ldw, int32_t W, int64_t offset, float *y, int64_t ldy,
+                  int64_t B, int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const float *before, float *after,
+                  void *stream);
+int cx_short_conv_bf16(const uint16_t *x, int64_t ldx, const uint16_t *weights, int64_t ldw, int32_t W, int64_t offset, uint16_t *y,
+                       int64_t ldy, int64_t B, int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const uint16_t *before,
+                       uint16_t *after, void *stream);
+int cx_short_conv_f16(const uint16_t *x, int64_t ldx, const uint16_t *weights, int64_t ldw, int32_t W, int64_t offset, uint16_t *y,
+                      int64_t ldy, int64_t B, int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const uint16_t *before,
+                      uint16_t *after, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * cx_short_conv_grad -- its gradient over x, and over taps and biases into the same columns of the workers' flat gradient rows (g_in as
+ * in cx_add_norm_grad).  v is computed again; `before` is a constant.  dx is [B * T][lddx].
+ */
+int cx_conv_workspace(int32_t W, int64_t B, int64_t T, int32_t D, int32_t K, int64_t *bytes);
+int cx_short_conv_grad(const float *x, int64_t ldx, const float *dy, int64_t lddy, const float *weights, int64_t ldw, int32_t W,
+                       int64_t offset, float *dx, int64_t lddx, const float *g_in, float *g_out, int64_t ldg, int64_t B, int64_t T,
+                       int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const float *before, void *workspace,
+                       int64_t workspace_bytes, void *stream);
+int cx_short_conv_grad_bf16(const uint16_t *x, int64_t ldx, const uint16_t *dy, int64_t lddy, const uint16_t *weights, int64_t ldw,
+                            int32_t W, int64_t offset, uint16_t *dx, int64_t lddx, const uint16_t *g_in, uint16_t *g_out, int64_t ldg,
+                            int64_t B, int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const uint16_t *before,
+                            void *workspace, int64_t workspace_bytes, void *stream);
+int cx_short_conv_grad_f16(const uint16_t *x, int64_t ldx, const uint16_t *dy, int64_t lddy, const uint16_t *weights, int64_t ldw,
+                           int32_t W, int64_t offset, uint16_t *dx, int64_t lddx, const uint16_t *g_in, uint16_t *g_out, int64_t ldg,
+                           int64_t B, int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const uint16_t *before,
+                           void *workspace, int64_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * cx_select_scan -- selective state space scan of B sequences of T steps, D columns and N states a column:
+ *     delta_t = softplus(dt_t + bias) ;  a_t[n] = exp(-delta_t exp(A_log[n]))
+ *     h_t[n] = a_t[n] (reset_t ? 0 : h_{t-1}[n]) + delta_t B_t[n] u_t
+ *     y_t = round((sum_n C_t[n] h_t[n] + skip u_t) (z ? z_t sigmoid(z_t) : 1))
+ * u, dt, z, y are matrices of B * T rows and D columns, bm (B) and cm (C) of N columns, each with its own ld; 1 <= N <= CX_MAX_STATES.
+ * W workers have B / W sequences each (B a multiple of W); A_log [D][N], bias [D] and skip [D] lie one behind the other in columns
+ * [offset, offset + D (N + 2)) of the worker's flat row.
+ *   z        NULL: no gate
+ *   reset    uint8 [B][T] or NULL: nonzero where a document begins; nothing of the state before it is used, NaN and infinities included
+ *   h0       float [B][D][N] or NULL (zeros);  h_last: the same or NULL, may be h0 (generation: T = 1, state in place)
+ *   states   float [B][ceil(T / CX_SCAN_CHUNK)][D][N] or NULL: the state that enters every CX_SCAN_CHUNK-th step, which the gradient needs
+ * A dt of -inf (padding) leaves the state as it is.  Long sequences are computed as compositions of maps, so an infinite state may turn into a
+ * NaN.  A single step needs no workspace.
+ */
+int cx_select_workspace(int64_t B, int64_t T, int32_t D, int32_t N, int64_t *bytes);
+int cx_select_scan(const float *u, int64_t ldu, const float *dt, int64_t lddt, const float *bm, int64_t ldb, const float *cm, int64_t ldc,
+                   const float *z, int64_t ldz, const float *params, int64_t ldp, int32_t W, int64_t offset, float *y, int64_t ldy,
+                   int64_t B, int64_t T, int32_t D, int32_t N, const uint8_t *reset, const float *h0, float *h_last, float *states,
+                   void *workspace, int64_t workspace_bytes, void *stream);
+int cx_select_scan_bf16(const uint16_t *u, int64_t ldu, const uint16_t *dt, int64_t lddt, const uint16_t *bm, int64_t ldb,
+                        const uint16_t *cm, int64_t ldc, const uint16_t *z, int64_t ldz, const uint16_t *params, int64_t ldp, int32_t W,
+                        int64_t offset, uint16_t *y, int64_t ldy, int64_t B, int64_t T, int32_t D, int32_t N, const uint8_t *reset,
+                        const float *h0, float *h_last, float *states, void *workspace, int64_t workspace_bytes, void *stream);
+int cx_select_scan_f16(const uint16_t *u, int64_t ldu, const uint16_t *dt, int64_t lddt, const uint16_t *bm, int64_t ldb,
+                       const uint16_t *cm, int64_t ldc, const uint16_t *z, int64_t ldz, const uint16_t *params, int64_t ldp, int32_t W,
+                       int64_t offset, uint16_t *y, int64_t ldy, int64_t B, int64_t T, int32_t D, int32_t N, const uint8_t *reset,
+                       const float *h0, float *h_last, float *states, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------
+ * cx_select_scan_grad -- its gradient over u, dt, B, C, z and, into the same columns of the workers' flat gradient rows (g_in as in
+ * cx_add_norm_grad), over A_log, bias and skip.  States between those kept are computed again in fp32; y is not read.
+ *   states   as the forward call left them for the same inputs
+ *   z, dz    both or neither
+ *   dh_last  float [B][D][N] or NULL (zeros);  dh0: float [B][D][N] or NULL (not wanted); may be dh_last
+ * Gradients of what columns and sequences share (B, C and the parameters) are sums in fp32, in an order that the sizes fix.
+ */
+int cx_select_grad_workspace(int64_t B, int64_t T, int32_t D, int32_t N, int64_t *bytes);
+int cx_select_scan_grad(const float *u, int64_t ldu, const float *dt, int64_t lddt, const float *bm, int64_t ldb, const float *cm,
+                        int64_t ldc, const float *z, int64_t ldz, const float *params, int64_t ldp, int32_t W, int64_t offset,
+                        const float *dy, int64_t lddy, float *du, int64_t lddu, float *ddt, int64_t ldddt, float *dbm, int64_t lddb,
+                        float *dcm, int64_t lddc, float *dz, int64_t lddz, const float *g_in, float *g_out, int64_t ldg, int64_t B,
+                        int64_t T, int32_t D, int32_t N, const uint8_t *reset, const float *states, const float *dh_last, float *dh0,
+                        void *workspace, int64_t workspace_bytes, void *stream);
+int cx_select_scan_grad_bf16(const uint16_t *u, int64_t ldu, const uint16_t *dt, int64_t lddt, const uint16_t *bm, int64_t ldb,
+                             const uint16_t *cm, int64_t ldc, const uint16_t *z, int64_t ldz, const uint16_t *params, int64_t ldp,
+                             int32_t W, int64_t offset, const uint16_t *dy, int64_t lddy, uint16_t *du, int64_t lddu, uint16_t *ddt,
+                             int64_t ldddt, uint16_t *dbm, int64_t lddb, uint16_t *dcm, int64_t lddc, uint16_t *dz, int64_t lddz,
+                             const uint16_t *g_in, uint16_t *g_out, int64_t ldg, int64_t B, int64_t T, int32_t D, int32_t N,
+                             const uint8_t *reset, const float *states, const float *dh_last, float *dh0, void *workspace,
+                             int64_t workspace_bytes, void *stream);
+int cx_select_scan_grad_f16(const uint16_t *u, int64_t ldu, const uint16_t *dt, int64_t lddt, const uint16_t *bm, int64_t ldb,
+                            const uint16_t *cm, int64_t ldc, const uint16_t *z, int64_t ldz, const uint16_t *params, int64_t ldp,
+                            int32_t W, int64_t offset, const uint16_t *dy, int64_t lddy, uint16_t *du, int64_t lddu, uint16_t *ddt,
+                            int64_t ldddt, uint16_t *dbm, int64_t lddb, uint16_t *dcm, int64_t lddc, uint16_t *dz, int64_t lddz,
+                            const uint16_t *g_in, uint16_t *g_out, int64_t ldg, int64_t B, int64_t T, int32_t D, int32_t N,
+                            const uint8_t *reset, const float *states, const float *dh_last, float *dh0, void *workspace,
+                            int64_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -19,9 +19,10 @@ HEADERS = [os.path.join(ROOT, "include", "cx_mix.h")] + [os.path.join(CSRC, h) f
     "cx_columns.hpp", "cx_schedule.hpp", "cx_tile.hpp", "cx_ops.hpp", "cx_ops16.hpp", "cx_kernels.hpp", "cx_launch.hpp")]
 LM_LIB = os.path.join(HERE, "libcxlm.so")
 LM_CSRC = os.path.join(CSRC, "lm")
-LM_SOURCES = [os.path.join(LM_CSRC, f) for f in ("cx_lm_embed.hip", "cx_lm_scan.hip", "cx_lm_scores.hip", "cx_lm_distill.hip")]
+LM_SOURCES = [os.path.join(LM_CSRC, f) for f in ("cx_lm_embed.hip", "cx_lm_scan.hip", "cx_lm_scores.hip", "cx_lm_distill.hip",
+                                                 "cx_lm_norm.hip", "cx_lm_conv.hip", "cx_lm_select.hip", "cx_lm_select_grad.hip")]
 LM_HEADERS = [os.path.join(ROOT, "include", h) for h in ("cx_lm.h", "cx_mix.h")] + [os.path.join(LM_CSRC, h) for h in (
-    "lm_common.hpp", "lm_vocab.hpp")]
+    "lm_common.hpp", "lm_vocab.hpp", "lm_block.hpp", "lm_select.hpp")]
 OBJDIR = os.path.join(HERE, "_build")
 
 HIPCC_FLAGS = [

@@ -1,0 +1,204 @@
+// What the operators of a residual block share (internal header): eight columns of a row at a time, random bits of a counter,
+// and sums of a worker's parameter gradients over the parts that workgroups leave.
+#ifndef CX_LM_BLOCK_HPP
+#define CX_LM_BLOCK_HPP
+#include "lm_common.hpp"
+
+#include <cmath>
+
+namespace {
+
+// ---------------------------------------------------------------------------------
+// Eight columns of a row: 16 bytes of a 16-bit type, two times 16 bytes of float32.
+// ---------------------------------------------------------------------------------
+template <class E>
+struct Eight {
+    static constexpr int kWords = sizeof(typename E::T) / 2;
+    u4 w[kWords];
+};
+
+// `left`: columns from p to the row's end; those behind it are zeros.
+template <class E, bool LAST = false>
+__device__ __forceinline__ Eight<E> load_eight(const typename E::T *p, int left)
+{
+    Eight<E> r;
+    if (left >= 8) {
+#pragma unroll
+        for (int k = 0; k < Eight<E>::kWords; ++k) r.w[k] = LAST ? load16_last<E>(p + k * E::kPer16) : load16<E>(p + k * E::kPer16);
+    } else {
+#pragma unroll
+        for (int k = 0; k < Eight<E>::kWords; ++k) r.w[k] = u4{};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < left) {
+                if constexpr (sizeof(typename E::T) == 4) r.w[j / 4][j % 4] = __float_as_uint(p[j]);
+                else r.w[0][j / 2] |= static_cast<unsigned>(p[j]) << (16 * (j & 1));
+            }
+    }
+    return r;
+}
+
+template <class E>
+__device__ __forceinline__ void widen(const Eight<E> &r, float (&v)[8])
+{
+    if constexpr (sizeof(typename E::T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r.w[j / 4][j % 4]);
+    } else {
+        E::unpack(r.w[0], v);
+    }
+}
+
+template <class E>
+__device__ __forceinline__ void store_eight(typename E::T *p, int left, const float (&v)[8])
+{
+    if (left >= 8) {
+        if constexpr (sizeof(typename E::T) == 4) {
+            store16<E>(p, u4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+            store16<E>(p + 4, u4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+        } else {
+            store16<E>(p, E::pack(v));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < left) p[j] = E::narrow(v[j]);
+    }
+}
+
+// ---------------------------------------------------------------------------------
+// Dropout's bits: Philox4x32 of ten rounds (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011),
+// eight times 16 bits a block.  The counter names the place, so nothing is stored and every pass finds the same bits.
+// ---------------------------------------------------------------------------------
+struct Drop {
+    const int64_t *rng;                                 // device: key, draw
+    uint32_t border;                                    // bits below it are dropped: share * 2^16
+    float scale;                                        // 2^16 / (2^16 - border)
+};
+
+__device__ __forceinline__ u4 random_block(uint64_t key, uint64_t draw, uint64_t block)
+{
+    uint32_t c0 = static_cast<uint32_t>(block), c1 = static_cast<uint32_t>(block >> 32), c2 = static_cast<uint32_t>(draw), c3 = static_cast<uint32_t>(draw >> 32);
+    uint32_t k0 = static_cast<uint32_t>(key), k1 = static_cast<uint32_t>(key >> 32);
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint32_t h0 = __umulhi(0xD2511F53u, c0), l0 = 0xD2511F53u * c0, h1 = __umulhi(0xCD9E8D57u, c2), l1 = 0xCD9E8D57u * c2;
+        c0 = h1 ^ c1 ^ k0;
+        c1 = l1;
+        c2 = h0 ^ c3 ^ k1;
+        c3 = l0;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return u4{c0, c1, c2, c3};
+}
+
+// A dropped element is 0 whatever it held.
+__device__ __forceinline__ void drop(const u4 &bits, uint32_t border, float scale, float (&v)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t b = (j & 1) ? bits[j / 2] >> 16 : bits[j / 2] & 0xffffu;
+        v[j] = b >= border ? v[j] * scale : 0.0f;
+    }
+}
+
+// The share p in [0, 1) to a multiple of 2^-16; false if it has none.
+[[maybe_unused]] bool drop_of(float p, const int64_t *rng, Drop &d)
+{
+    if (!(p >= 0.0f && p < 1.0f)) return false;
+    d.border = static_cast<uint32_t>(std::nearbyint(static_cast<double>(p) * 65536.0));
+    if (d.border > 65535u) return false;
+    d.scale = 65536.0f / static_cast<float>(65536u - d.border);
+    d.rng = rng;
+    return true;
+}
+
+// 0 and 1 far out, to the last bit.
+__device__ __forceinline__ float sigmoid(float v) { return rcp_fast(1.0f + exp2_fast(v * -kLog2e)); }
+// -inf as the lowest number: its product with a sigmoid of 0 is 0.  A NaN passes the comparison.
+__device__ __forceinline__ float finite_below(float v) { return v < -3.0e38f ? -3.0e38f : v; }
+// e = sigmoid(v), v from finite_below()
+__device__ __forceinline__ float silu_slope(float v, float e) { return e * __builtin_fmaf(v, 1.0f - e, 1.0f); }
+
+// ---------------------------------------------------------------------------------
+// Sums over lanes
+// ---------------------------------------------------------------------------------
+__device__ __forceinline__ float sum_lanes(float v, int lanes)
+{
+    for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor(v, o);
+    return v;
+}
+__device__ __forceinline__ unsigned max_lanes(unsigned v, int lanes)
+{
+    for (int o = 1; o < lanes; o <<= 1) {
+        const unsigned u = __shfl_xor(v, o);
+        v = u > v ? u : v;
+    }
+    return v;
+}
+
+// ---------------------------------------------------------------------------------
+// Parameter gradients: parts float [W][parts][columns] added in a fixed order, to g_in where there is one, into columns of flat rows.
+// ---------------------------------------------------------------------------------
+constexpr int kSumSlices = 16;
+
+template <class E>
+__global__ __launch_bounds__(kWave *kSumSlices) void sum_parts_kernel(const float *parts, int64_t count, int64_t columns, const typename E::T *g_in,
+                                                                      typename E::T *g_out, int64_t ld)
+{
+    __shared__ float sums[kSumSlices][kWave];
+    const int lane = threadIdx.x & (kWave - 1), slice = threadIdx.x / kWave;
+    const int64_t column = static_cast<int64_t>(blockIdx.x) * kWave + lane, w = blockIdx.y;
+    float v = 0.0f;
+    if (column < columns) {
+        const float *p = parts + w * count * columns + column;
+#pragma unroll 4
+        for (int64_t k = slice; k < count; k += kSumSlices) v += p[k * columns];
+    }
+    sums[slice][lane] = v;
+    __syncthreads();
+    if (slice > 0 || column >= columns) return;
+#pragma unroll
+    for (int k = 1; k < kSumSlices; ++k) v += sums[k][lane];
+    if (g_in) v += E::widen(g_in[w * ld + column]);
+    g_out[w * ld + column] = E::narrow(v);
+}
+
+template <class E>
+[[maybe_unused]] int sum_parts(const float *parts, int64_t count, int64_t columns, const typename E::T *g_in, typename E::T *g_out, int64_t ld, int32_t W,
+                               hipStream_t st)
+{
+    hipLaunchKernelGGL(sum_parts_kernel<E>, dim3(static_cast<unsigned>(ceil_div(columns, kWave)), W), dim3(kWave * kSumSlices), 0, st, parts, count, columns,
+                       g_in, g_out, ld);
+    return launched();
+}
+
+// Pairs of an output and an input that may be the same array, element for element.
+struct Same {
+    int out, in;
+};
+template <int INS, int OUTS, int PAIRS>
+[[maybe_unused]] bool outputs_share_but(const Extent (&in)[INS], const Extent (&out)[OUTS], const Same (&same)[PAIRS])
+{
+    for (int i = 0; i < OUTS; ++i) {
+        for (int k = 0; k < INS; ++k) {
+            bool may = false;
+            for (const Same &s : same) may = may || (s.out == i && s.in == k && out[i].first == in[k].first && out[i].pitch == in[k].pitch);
+            if (!may && share(out[i], in[k])) return true;
+        }
+        for (int k = i + 1; k < OUTS; ++k)
+            if (share(out[i], out[k])) return true;
+    }
+    return false;
+}
+
+// Flat rows of W workers with `columns` parameters from `offset` on.
+[[maybe_unused]] bool bad_rows(int32_t W, int64_t ld, int64_t offset, int64_t columns)
+{
+    return W < 1 || W > CX_MAX_ROWS || offset < 0 || offset > kMaxExtent || bad_matrix(W, ld, offset + columns);
+}
+
+}  // namespace
+
+#endif  // CX_LM_BLOCK_HPP

@@ -21,10 +21,13 @@ LIB_PATH = os.path.join(_HERE, "libcxlm.so")
 
 CX_MAX_TOKENS, CX_MAX_SEQUENCES, CX_MAX_VOCAB, CX_MAX_WIDTH = 1 << 26, 1 << 22, 1 << 26, 1 << 20
 CX_MAX_TOP, CX_MAX_TEACHER, CX_SCAN_CHUNK = 64, 256, 16
+CX_MAX_NORM_WIDTH, CX_MAX_TAPS, CX_MAX_STATES = 16384, 4, 16
 
 _TYPED = ["cx_embed_lookup", "cx_embed_grad", "cx_gated_scan", "cx_gated_scan_grad", "cx_token_scores", "cx_distill_loss",
-          "cx_distill_grad", "cx_distill_step"]
+          "cx_distill_grad", "cx_distill_step", "cx_dropout", "cx_add_norm", "cx_add_norm_grad", "cx_short_conv", "cx_short_conv_grad",
+          "cx_select_scan", "cx_select_scan_grad"]
 EXPORTS = ["cx_lm_abi_version", "cx_embed_workspace", "cx_scan_workspace", "cx_scores_workspace", "cx_distill_workspace",
+           "cx_norm_workspace", "cx_conv_workspace", "cx_select_workspace", "cx_select_grad_workspace",
            *(name + suffix for name in _TYPED for suffix in ("", "_bf16", "_f16"))]
 
 _INT32 = 2**31 - 1
@@ -52,6 +55,10 @@ def lib() -> ctypes.CDLL:
     L.cx_scan_workspace.argtypes = [i64, i64, i32, size]
     L.cx_scores_workspace.argtypes = [i64, i32, i32, size]
     L.cx_distill_workspace.argtypes = [i64, i32, size]
+    L.cx_norm_workspace.argtypes = [i32, i64, i32, size]
+    L.cx_conv_workspace.argtypes = [i32, i64, i64, i32, i32, size]
+    L.cx_select_workspace.argtypes = [i64, i64, i32, i32, size]
+    L.cx_select_grad_workspace.argtypes = [i64, i64, i32, i32, size]
     row = [vp, i64]
     targets = [i64, i32, i32, vp, vp, vp, f32, f32, f32]
     scratch = [vp, i64, vp]
@@ -64,6 +71,14 @@ def lib() -> ctypes.CDLL:
         "cx_distill_loss": [*row, *targets, vp, vp, *scratch],
         "cx_distill_grad": [*row, *targets, vp, vp, *row, vp],
         "cx_distill_step": [*row, *targets, vp, vp, *row, *scratch],
+        "cx_dropout": [*row, *row, *row, i64, i32, vp, f32, vp],
+        "cx_add_norm": [*row, *row, *row, i32, i64, i64, i32, f32, vp, f32, *row, *row, vp, *row, vp, vp],
+        "cx_add_norm_grad": [*row, *row, vp, *row, i32, i64, i64, i32, *row, vp, f32, *row, *row, vp, *row, *scratch],
+        "cx_short_conv": [*row, *row, i32, i64, *row, i64, i64, i32, i32, i32, vp, vp, vp, vp],
+        "cx_short_conv_grad": [*row, *row, *row, i32, i64, *row, vp, *row, i64, i64, i32, i32, i32, vp, vp, *scratch],
+        "cx_select_scan": [*row, *row, *row, *row, *row, *row, i32, i64, *row, i64, i64, i32, i32, vp, vp, vp, vp, *scratch],
+        "cx_select_scan_grad": [*row, *row, *row, *row, *row, *row, i32, i64, *row, *row, *row, *row, *row, *row, vp, *row, i64, i64, i32, i32, vp, vp,
+                                vp, vp, *scratch],
     }
     for name, args in typed.items():
         for suffix in ("", "_bf16", "_f16"):
@@ -194,6 +209,26 @@ def cx_scores_workspace(N: int, V: int, K: int) -> int:
 def cx_distill_workspace(N: int, V: int) -> int:
     """Bytes of workspace of cx_distill_loss* and cx_distill_step*."""
     return _size("cx_distill_workspace", N, V)
+
+
+def cx_norm_workspace(W: int, N: int, D: int) -> int:
+    """Bytes of workspace of cx_add_norm_grad*."""
+    return _size("cx_norm_workspace", W, N, D)
+
+
+def cx_conv_workspace(W: int, B: int, T: int, D: int, K: int) -> int:
+    """Bytes of workspace of cx_short_conv_grad*."""
+    return _size("cx_conv_workspace", W, B, T, D, K)
+
+
+def cx_select_workspace(B: int, T: int, D: int, N: int) -> int:
+    """Bytes of workspace of cx_select_scan*."""
+    return _size("cx_select_workspace", B, T, D, N)
+
+
+def cx_select_grad_workspace(B: int, T: int, D: int, N: int) -> int:
+    """Bytes of workspace of cx_select_scan_grad*."""
+    return _size("cx_select_grad_workspace", B, T, D, N)
 
 
 # ---------------------------------------------------------------------------------------------------------- embeddings
@@ -484,3 +519,317 @@ def cx_distill_step_bf16(z, ids, t, labels, gout, loss, dz, tau: float, w_kl: fl
 
 def cx_distill_step_f16(z, ids, t, labels, gout, loss, dz, tau: float, w_kl: float, w_ce: float, workspace=None, stream=None):
     _distill_step("cx_distill_step_f16", "_f16", z, ids, t, labels, gout, loss, dz, tau, w_kl, w_ce, workspace, stream)
+
+
+# ------------------------------------------------------------------------------------------------- dropout, residual and norm
+def _spread(name, arg, t, dtype, rows, columns, device):
+    """(address, row stride) of a matrix that may be absent."""
+    if t is None:
+        return None, 0
+    return t.data_ptr(), _matrix(name, arg, t, dtype, rows, columns, device)
+
+
+def _rng(name, rng, p, device):
+    """Address of the generator's two numbers, which a call that drops something needs."""
+    return (_dense if p else _optional)(name, "rng", rng, _torch.int64, (2,), device)
+
+
+def _flat(name, arg, rows, dtype, W, offset, count, device):
+    """Row stride of flat rows that hold `count` parameters from `offset` on."""
+    ld = _matrix(name, arg, rows, dtype, W, None, device)
+    if offset < 0 or offset + count > rows.shape[1]:
+        raise ValueError(f"{name}: {arg}: {count} parameters at {offset} do not fit rows of {rows.shape[1]}")
+    return ld
+
+
+def _gradients(name, g_in, g_out, dtype, W, offset, count, device):
+    """(address of g_in, address and row stride of g_out) of flat gradient rows."""
+    ld = _flat(name, "g_out", g_out, dtype, W, offset, count, device)
+    if g_in is not None:
+        ld_in = _flat(name, "g_in", g_in, dtype, W, offset, count, device)
+        if W > 1 and ld_in != ld:
+            raise ValueError(f"{name}: g_in: row stride {ld_in} differs from g_out's {ld}")
+    return None if g_in is None else g_in.data_ptr(), g_out.data_ptr(), ld
+
+
+def _narrow(name, *sizes):
+    if max(sizes) > _INT32 or min(sizes) < -_INT32:
+        _too_wide(name)
+
+
+def _dropout(name, suffix, x, rng, out, p, residual, stream):
+    if _lib is None:
+        lib()
+    dtype, device = _dtypes[suffix], x.get_device()
+    ldx = _matrix(name, "x", x, dtype, None, None, device)
+    N, D = x.shape
+    _narrow(name, D)
+    residual_at = _spread(name, "residual", residual, dtype, N, D, device)
+    ldo = _matrix(name, "out", out, dtype, N, D, device)
+    rp = _dense(name, "rng", rng, _torch.int64, (2,), device)
+    _on_device(name, device)
+    _call(name, x.data_ptr(), ldx, *residual_at, out.data_ptr(), ldo, N, D, rp, p, cxmix._stream(stream))
+
+
+def cx_dropout(x, rng, out, p: float, residual=None, stream=None):
+    """x, residual, out: [N][D] (out may be one of the others); rng: int64 [2] on the device, key and draw; p: share that is dropped."""
+    _dropout("cx_dropout", "", x, rng, out, p, residual, stream)
+
+
+def cx_dropout_bf16(x, rng, out, p: float, residual=None, stream=None):
+    _dropout("cx_dropout_bf16", "_bf16", x, rng, out, p, residual, stream)
+
+
+def cx_dropout_f16(x, rng, out, p: float, residual=None, stream=None):
+    _dropout("cx_dropout_f16", "_f16", x, rng, out, p, residual, stream)
+
+
+def _add_norm(name, suffix, x, residual, weights, offset, s, y, eps, inv, q, scale, p, rng, stream):
+    if _lib is None:
+        lib()
+    dtype, device = _dtypes[suffix], x.get_device()
+    ldx = _matrix(name, "x", x, dtype, None, None, device)
+    rows, D = x.shape
+    W = weights.shape[0] if len(weights.shape) == 2 else 0
+    ldw = _flat(name, "weights", weights, dtype, None, offset, D, device)
+    _narrow(name, D, W)
+    if W == 0 or rows % W:
+        raise ValueError(f"{name}: {rows} rows are not the same number of each of {W} workers")
+    residual_at, s_at, y_at = (_spread(name, arg, t, dtype, rows, D, device) for arg, t in (("residual", residual), ("s", s), ("y", y)))
+    ip = _optional(name, "inv", inv, _torch.float32, (rows,), device)
+    q_at, sp = (None, 0), None
+    if q is not None or scale is not None:
+        if q is None or q.dtype not in (_torch.uint8, _torch.float8_e4m3fn):
+            raise ValueError(f"{name}: q: expected uint8 or float8_e4m3fn [{rows}][{D}] beside scale")
+        q_at = _spread(name, "q", q, q.dtype, rows, D, device)
+        sp = _dense(name, "scale", scale, _torch.float32, (rows,), device)
+    rp = _rng(name, rng, p, device)
+    _on_device(name, device)
+    _call(name, x.data_ptr(), ldx, *residual_at, weights.data_ptr(), ldw, W, offset, rows // W, D, eps, rp, p, *s_at, *y_at, ip, *q_at, sp,
+          cxmix._stream(stream))
+
+
+def cx_add_norm(x, residual, weights, offset: int, s, y, eps: float, inv=None, q=None, scale=None, p: float = 0.0, rng=None, stream=None):
+    """x, residual, s, y: [W * N][D], all but x may be None; weights: [W][ld] flat rows, a worker's at weights[w, offset : offset + D]; inv,
+    scale: float32 [W * N]; q: uint8 or float8_e4m3fn [W * N][D]; p, rng: as cx_dropout, on x."""
+    _add_norm("cx_add_norm", "", x, residual, weights, offset, s, y, eps, inv, q, scale, p, rng, stream)
+
+
+def cx_add_norm_bf16(x, residual, weights, offset: int, s, y, eps: float, inv=None, q=None, scale=None, p: float = 0.0, rng=None, stream=None):
+    _add_norm("cx_add_norm_bf16", "_bf16", x, residual, weights, offset, s, y, eps, inv, q, scale, p, rng, stream)
+
+
+def cx_add_norm_f16(x, residual, weights, offset: int, s, y, eps: float, inv=None, q=None, scale=None, p: float = 0.0, rng=None, stream=None):
+    _add_norm("cx_add_norm_f16", "_f16", x, residual, weights, offset, s, y, eps, inv, q, scale, p, rng, stream)
+
+
+def _add_norm_grad(name, suffix, dy, s, inv, weights, offset, ds_in, ds, g_in, g_out, dx, p, rng, workspace, stream):
+    if _lib is None:
+        lib()
+    dtype, device = _dtypes[suffix], dy.get_device()
+    lddy = _matrix(name, "dy", dy, dtype, None, None, device)
+    rows, D = dy.shape
+    W = weights.shape[0] if len(weights.shape) == 2 else 0
+    ldw = _flat(name, "weights", weights, dtype, None, offset, D, device)
+    _narrow(name, D, W)
+    if W == 0 or rows % W:
+        raise ValueError(f"{name}: {rows} rows are not the same number of each of {W} workers")
+    lds = _matrix(name, "s", s, dtype, rows, D, device)
+    ip = _dense(name, "inv", inv, _torch.float32, (rows,), device)
+    in_at, ds_at, dx_at = (_spread(name, arg, t, dtype, rows, D, device) for arg, t in (("ds_in", ds_in), ("ds", ds), ("dx", dx)))
+    grads = _gradients(name, g_in, g_out, dtype, W, offset, D, device)
+    rp = _rng(name, rng, p, device)
+    work = _scratch(name, workspace, "cx_norm_workspace", (W, rows // W, D), device, stream)
+    _call(name, dy.data_ptr(), lddy, s.data_ptr(), lds, ip, weights.data_ptr(), ldw, W, offset, rows // W, D, *in_at, rp, p, *ds_at, *dx_at, *grads,
+          *_span(work), cxmix._stream(stream))
+
+
+def cx_add_norm_grad(dy, s, inv, weights, offset: int, ds_in, ds, g_in, g_out, dx=None, p: float = 0.0, rng=None, workspace=None, stream=None):
+    """s, inv: as cx_add_norm left them; ds_in: gradient of s from elsewhere, or None; ds, dx: gradients of residual and x, one of them may be
+    None; g_out: [W][ld] flat gradient rows; g_in: None, g_out itself (added in place) or a second matrix with the same row stride."""
+    _add_norm_grad("cx_add_norm_grad", "", dy, s, inv, weights, offset, ds_in, ds, g_in, g_out, dx, p, rng, workspace, stream)
+
+
+def cx_add_norm_grad_bf16(dy, s, inv, weights, offset: int, ds_in, ds, g_in, g_out, dx=None, p: float = 0.0, rng=None, workspace=None,
+                          stream=None):
+    _add_norm_grad("cx_add_norm_grad_bf16", "_bf16", dy, s, inv, weights, offset, ds_in, ds, g_in, g_out, dx, p, rng, workspace, stream)
+
+
+def cx_add_norm_grad_f16(dy, s, inv, weights, offset: int, ds_in, ds, g_in, g_out, dx=None, p: float = 0.0, rng=None, workspace=None,
+                         stream=None):
+    _add_norm_grad("cx_add_norm_grad_f16", "_f16", dy, s, inv, weights, offset, ds_in, ds, g_in, g_out, dx, p, rng, workspace, stream)
+
+
+# --------------------------------------------------------------------------------------------------------- short convolution
+def _by_worker(name, rows, T, W, *ends):
+    """B of B * T rows, as many sequences of each of W workers."""
+    B = _sequences(name, rows, T, *ends)
+    if W == 0 or B % W:
+        raise ValueError(f"{name}: {B} sequences are not the same number of each of {W} workers")
+    return B
+
+
+def _short_conv(name, suffix, x, weights, offset, y, T, K, silu, before, after, reset, stream):
+    if _lib is None:
+        lib()
+    dtype, device = _dtypes[suffix], x.get_device()
+    ldx = _matrix(name, "x", x, dtype, None, None, device)
+    rows, D = x.shape
+    W = weights.shape[0] if len(weights.shape) == 2 else 0
+    _narrow(name, D, W, K)
+    B = _by_worker(name, rows, T, W, before, after)
+    ldw = _flat(name, "weights", weights, dtype, None, offset, D * (K + 1), device)
+    ldy = _matrix(name, "y", y, dtype, rows, D, device)
+    bp = _optional(name, "before", before, dtype, (B, K - 1, D), device)
+    ap = _optional(name, "after", after, dtype, (B, K - 1, D), device)
+    rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    _on_device(name, device)
+    _call(name, x.data_ptr(), ldx, weights.data_ptr(), ldw, W, offset, y.data_ptr(), ldy, B, T, D, K, int(bool(silu)), rp, bp, ap, cxmix._stream(stream))
+
+
+def cx_short_conv(x, weights, offset: int, y, T: int, K: int, silu: bool = True, before=None, after=None, reset=None, stream=None):
+    """x, y: [B * T][D]; weights: [W][ld] flat rows with taps [D][K] and biases [D] at offset; before, after: [B][K - 1][D] (may be one tensor);
+    reset: uint8 [B][T]."""
+    _short_conv("cx_short_conv", "", x, weights, offset, y, T, K, silu, before, after, reset, stream)
+
+
+def cx_short_conv_bf16(x, weights, offset: int, y, T: int, K: int, silu: bool = True, before=None, after=None, reset=None, stream=None):
+    _short_conv("cx_short_conv_bf16", "_bf16", x, weights, offset, y, T, K, silu, before, after, reset, stream)
+
+
+def cx_short_conv_f16(x, weights, offset: int, y, T: int, K: int, silu: bool = True, before=None, after=None, reset=None, stream=None):
+    _short_conv("cx_short_conv_f16", "_f16", x, weights, offset, y, T, K, silu, before, after, reset, stream)
+
+
+def _short_conv_grad(name, suffix, x, dy, weights, offset, dx, g_in, g_out, T, K, silu, before, reset, workspace, stream):
+    if _lib is None:
+        lib()
+    dtype, device = _dtypes[suffix], x.get_device()
+    ldx = _matrix(name, "x", x, dtype, None, None, device)
+    rows, D = x.shape
+    W = weights.shape[0] if len(weights.shape) == 2 else 0
+    _narrow(name, D, W, K)
+    B = _by_worker(name, rows, T, W, before)
+    ldw = _flat(name, "weights", weights, dtype, None, offset, D * (K + 1), device)
+    lddy = _matrix(name, "dy", dy, dtype, rows, D, device)
+    lddx = _matrix(name, "dx", dx, dtype, rows, D, device)
+    grads = _gradients(name, g_in, g_out, dtype, W, offset, D * (K + 1), device)
+    bp = _optional(name, "before", before, dtype, (B, K - 1, D), device)
+    rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    work = _scratch(name, workspace, "cx_conv_workspace", (W, B, T, D, K), device, stream)
+    _call(name, x.data_ptr(), ldx, dy.data_ptr(), lddy, weights.data_ptr(), ldw, W, offset, dx.data_ptr(), lddx, *grads, B, T, D, K, int(bool(silu)), rp, bp,
+          *_span(work), cxmix._stream(stream))
+
+
+def cx_short_conv_grad(x, dy, weights, offset: int, dx, g_in, g_out, T: int, K: int, silu: bool = True, before=None, reset=None,
+                       workspace=None, stream=None):
+    """x, dy, dx: [B * T][D]; the others as cx_short_conv; g_in, g_out: as cx_add_norm_grad."""
+    _short_conv_grad("cx_short_conv_grad", "", x, dy, weights, offset, dx, g_in, g_out, T, K, silu, before, reset, workspace, stream)
+
+
+def cx_short_conv_grad_bf16(x, dy, weights, offset: int, dx, g_in, g_out, T: int, K: int, silu: bool = True, before=None, reset=None,
+                            workspace=None, stream=None):
+    _short_conv_grad("cx_short_conv_grad_bf16", "_bf16", x, dy, weights, offset, dx, g_in, g_out, T, K, silu, before, reset, workspace, stream)
+
+
+def cx_short_conv_grad_f16(x, dy, weights, offset: int, dx, g_in, g_out, T: int, K: int, silu: bool = True, before=None, reset=None,
+                           workspace=None, stream=None):
+    _short_conv_grad("cx_short_conv_grad_f16", "_f16", x, dy, weights, offset, dx, g_in, g_out, T, K, silu, before, reset, workspace, stream)
+
+
+# ------------------------------------------------------------------------------------------------------------ selective scan
+def select_states(u, T: int, N: int):
+    """An empty tensor for the `states` of a selective scan over u ([B * T][D]) with N states that is to have a gradient."""
+    import torch
+    B = u.shape[0] // T if T > 0 else 0
+    return torch.empty((B, -(-T // CX_SCAN_CHUNK), u.shape[1], N), dtype=torch.float32, device=u.device)
+
+
+def _select_inputs(name, dtype, u, dt, bm, cm, z, params, offset, T, device, *ends):
+    """(the first arguments of both calls, B, D, N, W)"""
+    ldu = _matrix(name, "u", u, dtype, None, None, device)
+    rows, D = u.shape
+    lddt = _matrix(name, "dt", dt, dtype, rows, D, device)
+    ldb = _matrix(name, "bm", bm, dtype, rows, None, device)
+    N = bm.shape[1]
+    ldc = _matrix(name, "cm", cm, dtype, rows, N, device)
+    z_at = _spread(name, "z", z, dtype, rows, D, device)
+    W = params.shape[0] if len(params.shape) == 2 else 0
+    _narrow(name, D, W, N)
+    B = _by_worker(name, rows, T, W, *ends)
+    ldp = _flat(name, "params", params, dtype, None, offset, D * (N + 2), device)
+    head = (u.data_ptr(), ldu, dt.data_ptr(), lddt, bm.data_ptr(), ldb, cm.data_ptr(), ldc, *z_at, params.data_ptr(), ldp, W, offset)
+    return head, B, D, N, W
+
+
+def _select_scan(name, suffix, u, dt, bm, cm, params, offset, y, T, z, h0, h_last, reset, states, workspace, stream):
+    if _lib is None:
+        lib()
+    dtype, device, f32 = _dtypes[suffix], u.get_device(), _torch.float32
+    head, B, D, N, _ = _select_inputs(name, dtype, u, dt, bm, cm, z, params, offset, T, device, h0, h_last)
+    ldy = _matrix(name, "y", y, dtype, u.shape[0], D, device)
+    hp = _optional(name, "h0", h0, f32, (B, D, N), device)
+    lp = _optional(name, "h_last", h_last, f32, (B, D, N), device)
+    sp = _optional(name, "states", states, f32, (B, -(-T // CX_SCAN_CHUNK), D, N), device)
+    rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    work = _scratch(name, workspace, None if T <= 1 else "cx_select_workspace", (B, T, D, N), device, stream)
+    _call(name, *head, y.data_ptr(), ldy, B, T, D, N, rp, hp, lp, sp, *_span(work), cxmix._stream(stream))
+
+
+def cx_select_scan(u, dt, bm, cm, params, offset: int, y, T: int, z=None, h0=None, h_last=None, reset=None, states=None, workspace=None,
+                   stream=None):
+    """u, dt, z, y: [B * T][D]; bm, cm: [B * T][N]; params: [W][ld] flat rows with A_log [D][N], bias [D] and skip [D] at offset; h0, h_last:
+    float32 [B][D][N] (may be one tensor); reset: uint8 [B][T]; states: see select_states()."""
+    _select_scan("cx_select_scan", "", u, dt, bm, cm, params, offset, y, T, z, h0, h_last, reset, states, workspace, stream)
+
+
+def cx_select_scan_bf16(u, dt, bm, cm, params, offset: int, y, T: int, z=None, h0=None, h_last=None, reset=None, states=None, workspace=None,
+                        stream=None):
+    _select_scan("cx_select_scan_bf16", "_bf16", u, dt, bm, cm, params, offset, y, T, z, h0, h_last, reset, states, workspace, stream)
+
+
+def cx_select_scan_f16(u, dt, bm, cm, params, offset: int, y, T: int, z=None, h0=None, h_last=None, reset=None, states=None, workspace=None,
+                       stream=None):
+    _select_scan("cx_select_scan_f16", "_f16", u, dt, bm, cm, params, offset, y, T, z, h0, h_last, reset, states, workspace, stream)
+
+
+def _select_scan_grad(name, suffix, u, dt, bm, cm, params, offset, dy, du, ddt, dbm, dcm, g_in, g_out, T, states, z, dz, dh_last, dh0, reset, workspace,
+                      stream):
+    if _lib is None:
+        lib()
+    dtype, device, f32 = _dtypes[suffix], u.get_device(), _torch.float32
+    head, B, D, N, W = _select_inputs(name, dtype, u, dt, bm, cm, z, params, offset, T, device, dh_last, dh0)
+    rows = u.shape[0]
+    if (z is None) != (dz is None):
+        raise ValueError(f"{name}: z and dz go together")
+    outs = [(t.data_ptr(), _matrix(name, arg, t, dtype, rows, columns, device))
+            for arg, t, columns in (("dy", dy, D), ("du", du, D), ("ddt", ddt, D), ("dbm", dbm, N), ("dcm", dcm, N))]
+    dz_at = _spread(name, "dz", dz, dtype, rows, D, device)
+    grads = _gradients(name, g_in, g_out, dtype, W, offset, D * (N + 2), device)
+    sp = (_dense if T > 0 else _optional)(name, "states", states, f32, (B, -(-T // CX_SCAN_CHUNK), D, N), device)
+    lp = _optional(name, "dh_last", dh_last, f32, (B, D, N), device)
+    hp = _optional(name, "dh0", dh0, f32, (B, D, N), device)
+    rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    work = _scratch(name, workspace, "cx_select_grad_workspace", (B, T, D, N), device, stream)
+    _call(name, *head, *(v for at in outs for v in at), *dz_at, *grads, B, T, D, N, rp, sp, lp, hp, *_span(work), cxmix._stream(stream))
+
+
+def cx_select_scan_grad(u, dt, bm, cm, params, offset: int, dy, du, ddt, dbm, dcm, g_in, g_out, T: int, states, z=None, dz=None,
+                        dh_last=None, dh0=None, reset=None, workspace=None, stream=None):
+    """Gradients beside their inputs: dy, du, ddt, dz: [B * T][D]; dbm, dcm: [B * T][N]; states: as cx_select_scan filled them; dh_last, dh0:
+    float32 [B][D][N]; g_in, g_out: as cx_add_norm_grad."""
+    _select_scan_grad("cx_select_scan_grad", "", u, dt, bm, cm, params, offset, dy, du, ddt, dbm, dcm, g_in, g_out, T, states, z, dz,
+                      dh_last, dh0, reset, workspace, stream)
+
+
+def cx_select_scan_grad_bf16(u, dt, bm, cm, params, offset: int, dy, du, ddt, dbm, dcm, g_in, g_out, T: int, states, z=None, dz=None,
+                             dh_last=None, dh0=None, reset=None, workspace=None, stream=None):
+    _select_scan_grad("cx_select_scan_grad_bf16", "_bf16", u, dt, bm, cm, params, offset, dy, du, ddt, dbm, dcm, g_in, g_out, T, states, z,
+                      dz, dh_last, dh0, reset, workspace, stream)
+
+
+def cx_select_scan_grad_f16(u, dt, bm, cm, params, offset: int, dy, du, ddt, dbm, dcm, g_in, g_out, T: int, states, z=None, dz=None,
+                            dh_last=None, dh0=None, reset=None, workspace=None, stream=None):
+    _select_scan_grad("cx_select_scan_grad_f16", "_f16", u, dt, bm, cm, params, offset, dy, du, ddt, dbm, dcm, g_in, g_out, T, states, z, dz,
+                      dh_last, dh0, reset, workspace, stream)
+

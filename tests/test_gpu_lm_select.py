@@ -1,0 +1,231 @@
+"""cx_select_scan and cx_select_scan_grad against the scan in 64 bits, step by step."""
+import math
+
+import pytest
+import torch
+
+import lm_block_reference as BR
+import lm_reference as R
+from lm_block_util import DEV, edges, flat_rows, gradient_rows, place, untouched
+from paper_2012_15198_amd import cxlm as lm
+
+pytestmark = pytest.mark.gpu
+OFFSET = 3
+
+
+class Case:
+    def __init__(self, suffix, W, B, T, D, N, packed=False, gated=True, seed=0):
+        gen = torch.Generator().manual_seed(seed + B * T + D * N)
+        self.gen, self.dtype, self.suffix, self.sizes = gen, R.TYPES[suffix], suffix, (W, B, T, D, N)
+        matrix = lambda columns, s=1.0: (torch.randn((B * T, columns), generator=gen) * s).to(self.dtype)
+        self.u, self.dt, self.z, self.dy = matrix(D), matrix(D, 0.7), matrix(D) if gated else None, matrix(D)
+        self.bm, self.cm = matrix(N), matrix(N)
+        rates = (torch.arange(N) + 1.0).log().repeat(D).expand(W, D * N) + torch.randn((W, D * N), generator=gen) * 0.1
+        steps = (torch.rand((W, D), generator=gen) * math.log(300.0) + math.log(1e-3)).exp()
+        self.rows = flat_rows([rates, steps + (-(-steps).expm1()).log(), 1 + 0.2 * torch.randn((W, D), generator=gen)], OFFSET, self.dtype, gen)
+        of = lambda begin, n, *shape: self.rows[:, OFFSET + begin:OFFSET + begin + n].repeat_interleave(B // W, 0).view(B, *shape)
+        self.A_log, self.bias, self.skip = of(0, D * N, D, N), of(D * N, D, D), of(D * (N + 1), D, D)
+        self.h0, self.dh = (torch.randn((B, D, N), generator=gen) for _ in range(2))
+        self.reset = None
+        if packed:
+            self.reset = (torch.rand((B, T), generator=gen) < 0.1).to(torch.uint8) * 3
+            self.reset[0, 0] = 1
+            if B > 1:
+                self.reset[1] = 1
+            self.reset[B - 1, T - 1] = 1
+
+    def reference(self, grad=False):
+        args = (self.u, self.dt, self.bm, self.cm, self.z, self.sizes[2], self.A_log, self.bias, self.skip, self.h0, self.reset)
+        return BR.select_grad(*args, self.dy, self.dh) if grad else BR.select(*args)
+
+    def on(self, strided=False):
+        to = lambda t: None if t is None else place(t, strided)
+        return {k: to(getattr(self, k)) for k in ("u", "dt", "z", "dy", "bm", "cm")}
+
+    def forward(self, d, y, states=None, h0=None, h_last=None, reset=None):
+        getattr(lm, "cx_select_scan" + self.suffix)(d["u"], d["dt"], d["bm"], d["cm"], self.rows.to(DEV), OFFSET, y, self.sizes[2], z=d["z"], h0=h0, h_last=h_last,
+                                                    reset=reset, states=states)
+
+    def backward(self, d, states, g_in, g_out, dh_last=None, dh0=None, reset=None, strided=False):
+        grads = {k: None if d[k] is None else place(torch.full_like(getattr(self, k), 9.0), strided) for k in ("u", "dt", "bm", "cm", "z")}
+        getattr(lm, "cx_select_scan_grad" + self.suffix)(d["u"], d["dt"], d["bm"], d["cm"], self.rows.to(DEV), OFFSET, d["dy"], grads["u"], grads["dt"], grads["bm"],
+                                                         grads["cm"], g_in, g_out, self.sizes[2], states, z=d["z"], dz=grads["z"], dh_last=dh_last, dh0=dh0, reset=reset)
+        return grads
+
+
+SHAPES = [  # W, B, T, D, N
+    (1, 1, 1, 1, 1), (1, 2, 1, 70, 16), (2, 4, 2, 5, 3), (1, 1, 15, 64, 4), (1, 2, 16, 65, 5), (3, 3, 17, 9, 8), (1, 1, 40, 129, 16), (2, 2, 63, 12, 9),
+    (1, 1, 64, 3, 16), (1, 2, 130, 20, 2), (1, 1, 300, 70, 16), (1, 1, 1111, 7, 10), (2, 2, 500, 33, 7)]
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("packed,strided,gated,mode", [(False, False, True, "alone"), (True, True, True, "in place"), (True, False, False, "added"),
+                                                       (False, True, False, "alone")])
+@pytest.mark.parametrize("W,B,T,D,N", SHAPES)
+def test_both_directions(suffix, packed, strided, gated, mode, W, B, T, D, N):
+    c = Case(suffix, W, B, T, D, N, packed, gated)
+    d, on = c.on(strided), lambda t: None if t is None else t.to(DEV)
+    y, h_last = place(torch.full_like(c.u, 9.0), strided), torch.full((B, D, N), 9.0, device=DEV)
+    states = torch.full_like(lm.select_states(d["u"], T, N), 9.0)
+    c.forward(d, y, states, on(c.h0), h_last, on(c.reset))
+    ref = c.reference()
+    R.check(y.reshape(B, T, D), ref["y"], ref["y_err"], "y")
+    R.check(h_last, ref["h_last"], ref["h_last_err"], "h_last")
+    if not packed:
+        R.check(states, ref["before"][:, ::16], ref["before_err"][:, ::16], "states")
+    count, dh0 = D * (N + 2), torch.full((B, D, N), 9.0, device=DEV)
+    g_in, g_out, base = gradient_rows(mode, c.rows, c.dtype, c.gen)
+    around = edges(g_out, OFFSET, count)
+    grads = c.backward(d, states, g_in, g_out, on(c.dh), dh0, on(c.reset), strided)
+    ref = c.reference(grad=True)
+    for key, name, columns in (("u", "du", D), ("dt", "ddt", D), ("bm", "db", N), ("cm", "dc", N), ("z", "dz", D)):
+        if grads[key] is not None:
+            R.check(grads[key].reshape(B, T, columns), ref[name], ref[name + "_err"], name)
+            assert not strided or untouched(grads[key])
+    R.check(dh0, ref["dh0"], ref["dh0_err"], "dh0")
+    begin = OFFSET
+    for name, n in (("dA", D * N), ("dbias", D), ("dskip", D)):
+        part = None if base is None else base[:, begin:begin + n]
+        R.check(g_out[:, begin:begin + n], *BR.summed(ref[name], ref[name + "_err"], ref[name + "_size"], W, T, part), name)
+        begin += n
+    assert torch.equal(edges(g_out, OFFSET, count), around) and (not strided or untouched(y))
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("N,D", [(1, 1), (7, 130), (16, 65)])
+def test_steps_one_by_one_with_the_state_in_place_equal_the_sequence(suffix, N, D):
+    W, B, T = 1, 3, 37
+    c = Case(suffix, W, B, T, D, N, True)
+    d, state, ref = c.on(), c.h0.to(DEV), c.reference()
+    steps, out, reset = {k: v.view(B, T, -1) for k, v in d.items()}, torch.empty((B, D), dtype=c.dtype, device=DEV), c.reset.to(DEV)
+    for t in range(T):
+        s = {k: v[:, t] for k, v in steps.items()}
+        getattr(lm, "cx_select_scan" + suffix)(s["u"], s["dt"], s["bm"], s["cm"], c.rows.to(DEV), OFFSET, out, 1, z=s["z"], h0=state, h_last=state,
+                                               reset=reset[:, t:t + 1].contiguous())
+        R.check(out, ref["y"][:, t], ref["y_err"][:, t], str(t))
+    R.check(state, ref["h_last"], ref["h_last_err"])
+
+
+@pytest.mark.parametrize("T", [2, 64, 1000])
+def test_state_in_place_over_long_and_split_sequences(T):
+    c = Case("_bf16", 1, 1, T, 65, 16)
+    d, state, dstate, y, ref, back = c.on(), c.h0.to(DEV), c.dh.to(DEV), torch.empty_like(c.u.to(DEV)), c.reference(), c.reference(grad=True)
+    states, g = lm.select_states(d["u"], T, 16), torch.empty_like(c.rows.to(DEV))
+    c.forward(d, y, states, state, state)
+    R.check(y.reshape(1, T, 65), ref["y"], ref["y_err"])
+    R.check(state, ref["h_last"], ref["h_last_err"])
+    c.backward(d, states, None, g, dstate, dstate)
+    R.check(dstate, back["dh0"], back["dh0_err"])
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("T", [9, 200, 900])
+def test_nothing_crosses_a_reset(suffix, T):
+    """NaN and infinities in one document leave the others as they are, forward and backward, where no parameter joins them."""
+    D, N, cut = 40, 9, T * 2 // 3
+    c = Case(suffix, 1, 1, T, D, N)
+    reset = torch.zeros((1, T), dtype=torch.uint8)
+    reset[0, cut] = 1
+    outs = []
+    for dirty in (None, "early", "late"):
+        d = {k: v.clone() for k, v in c.on().items()}
+        last = c.dh.to(DEV)
+        if dirty == "early":
+            d["u"][cut - 1, ::2], d["dt"][cut - 1, 1::3], d["bm"][0, 0], d["u"][0, 3] = torch.inf, torch.nan, torch.inf, torch.nan
+        if dirty == "late":
+            d["dy"][cut, 5], last = torch.nan, torch.full_like(last, torch.inf)
+        y, h_last, g = torch.empty_like(d["u"]), torch.empty((1, D, N), device=DEV), torch.empty_like(c.rows.to(DEV))
+        states = lm.select_states(y, T, N)
+        c.forward(d, y, states, c.h0.to(DEV), h_last, reset.to(DEV))
+        grads = c.backward(d, states, None, g, last, None, reset.to(DEV))
+        outs.append([y, h_last[0].t(), *grads.values()])
+    for k, (clean, early, late) in enumerate(zip(*outs)):
+        if k == 1:
+            assert clean.isfinite().all() and torch.equal(clean, early)
+        else:
+            assert clean.isfinite().all() and torch.equal(clean[cut:], early[cut:]), k
+            assert torch.equal(clean[:cut], late[:cut]), k
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("T", [1, 50])
+def test_padding_steps_leave_the_state(suffix, T):
+    """dt of -inf: nothing decays, nothing enters, and no gradient but the direct path's comes of it."""
+    c = Case(suffix, 1, 2, T, 30, 5)
+    c.dt[:] = -torch.inf
+    d, y, h_last = c.on(), torch.empty_like(c.u.to(DEV)), torch.empty((2, 30, 5), device=DEV)
+    states, dh0, g = lm.select_states(d["u"], T, 5), torch.empty((2, 30, 5), device=DEV), torch.empty_like(c.rows.to(DEV))
+    c.forward(d, y, states, c.h0.to(DEV), h_last)
+    assert torch.equal(h_last.cpu(), c.h0) and y.isfinite().all()
+    grads = c.backward(d, states, None, g, c.dh.to(DEV), dh0)
+    assert (grads["dt"] == 0).all() and (grads["bm"] == 0).all() and all(v.isfinite().all() for v in grads.values())
+
+
+def test_closed_gates():
+    """z of -inf: a result of 0, and gradients of 0 through it."""
+    c = Case("", 1, 1, 20, 10, 3)
+    c.z[3], c.z[:, 4] = -torch.inf, -torch.inf
+    d, y, g = c.on(), torch.empty((20, 10), device=DEV), torch.empty_like(c.rows.to(DEV))
+    states = lm.select_states(y, 20, 3)
+    c.forward(d, y, states)
+    assert (y[3] == 0).all() and (y[:, 4] == 0).all() and y.isfinite().all()
+    grads = c.backward(d, states, None, g)
+    assert all(v.isfinite().all() for v in grads.values()) and (grads["z"][3] == 0).all() and (grads["u"][:, 4] == 0).all()
+
+
+def test_steps_at_their_ends():
+    """Softplus far out on both sides: the state's decay from 1 to 0 to the last bit, small steps with their relative accuracy."""
+    v = torch.tensor([[-87.0], [-40.0], [-16.0], [-8.0], [-1e-3], [0.0], [3.0], [30.0], [88.0], [200.0]])
+    T = v.shape[0]
+    rows, one = torch.zeros((1, 3)), torch.ones((T, 1))
+    y, zero = torch.empty((T, 1), device=DEV), torch.zeros((T, 1), device=DEV)
+    reset = torch.ones((1, T), dtype=torch.uint8, device=DEV)
+    lm.cx_select_scan(one.to(DEV), v.to(DEV), one.to(DEV), one.to(DEV), rows.to(DEV), 0, y, T, reset=reset)      # y = delta
+    want = torch.nn.functional.softplus(v.double(), threshold=700.0)
+    R.check(y, want, want * (3 * v.double().abs() + 24) * R.U)
+    lm.cx_select_scan(zero, v.to(DEV), one.to(DEV), one.to(DEV), rows.to(DEV), 0, y, T, h0=torch.ones((1, 1, 1), device=DEV))
+    want = (-want.cumsum(0)).exp()
+    assert ((y.cpu().double() - want).abs() <= 1e-5 * want + 1e-37).all()
+
+
+def test_no_steps():
+    h0, out = torch.randn((4, 6, 3), device=DEV), torch.empty((4, 6, 3), device=DEV)
+    e, s, rows = torch.empty((0, 6), device=DEV), torch.empty((0, 3), device=DEV), torch.randn((1, 30), device=DEV)
+    lm.cx_select_scan(e, e, s, s, rows, 0, e, 0, h0=h0, h_last=out)
+    assert torch.equal(out, h0)
+    lm.cx_select_scan(e, e, s, s, rows, 0, e, 0, h_last=out)
+    assert (out == 0).all()
+    g = torch.full_like(rows, 2.0)
+    lm.cx_select_scan_grad(e, e, s, s, rows, 0, e, e, e, s, s, g, g, 0, None, dh_last=h0, dh0=out)
+    assert torch.equal(out, h0) and (g == 2).all()
+    lm.cx_select_scan_grad(e, e, s, s, rows, 0, e, e, e, s, s, None, g, 0, None)
+    assert (g == 0).all()
+
+
+def test_gradient_against_differences():
+    """Central differences in 64 bits at drawn places of every input and parameter."""
+    W, B, T, D, N = 2, 2, 40, 3, 4
+    c = Case("", W, B, T, D, N, True)
+    c.reset[1] = 0
+    d, y, dh0, g = c.on(), torch.empty_like(c.u.to(DEV)), torch.empty((B, D, N), device=DEV), torch.empty_like(c.rows.to(DEV))
+    states = lm.select_states(y, T, N)
+    c.forward(d, y, states, c.h0.to(DEV), None, c.reset.to(DEV))
+    grads = c.backward(d, states, None, g, c.dh.to(DEV), dh0, c.reset.to(DEV))
+    names = ("u", "dt", "bm", "cm", "z", "A_log", "bias", "skip", "h0")
+
+    def value(a):
+        f = BR.select(a["u"], a["dt"], a["bm"], a["cm"], a["z"], T, a["A_log"], a["bias"], a["skip"], a["h0"], c.reset)
+        return float((f["y"].reshape(B * T, D) * c.dy.double()).sum() + (f["h_last"] * c.dh.double()).sum())
+
+    args = {k: getattr(c, k).double().clone() for k in names}
+    got = {**{k: grads[k] for k in ("u", "dt", "bm", "cm", "z")}, "A_log": g[:, OFFSET:OFFSET + D * N], "bias": g[:, OFFSET + D * N:OFFSET + D * (N + 1)],
+           "skip": g[:, OFFSET + D * (N + 1):OFFSET + D * (N + 2)], "h0": dh0}
+    for name in names:
+        for at in torch.randint(0, args[name].numel(), (8,), generator=c.gen).tolist():
+            ends = []
+            for sign in (1, -1):
+                moved = {k: v.clone() for k, v in args.items()}
+                moved[name].view(-1)[at] += sign * 1e-5
+                ends.append(value(moved))
+            slope = (ends[0] - ends[1]) / 2e-5
+            assert abs(slope - float(got[name].reshape(-1)[at])) < 3e-5 * (1 + abs(slope)), (name, at)
