@@ -1,4 +1,8 @@
 // C-ABI entry points cx_select_scan*, cx_select_workspace: the selective state space scan (see include/cx_lm.h, lm_select.hpp)
+//
+// Bound by the vector units: with 16 states a column's step takes 64 exponentials, products and sums six issue slots each, and a quarter as many again
+// for what the states share; 94 % of the cycles issue one (16 sequences of 2,048 x 1,024 in bfloat16: 82 us the maps of three spans in four, 7 what
+// enters, 155 the walk).  Without a split they would take 257 us, one wavefront to a SIMD.
 #include "lm_select.hpp"
 
 namespace {
@@ -12,12 +16,17 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
 {
     using T = typename E::T;
     constexpr bool MAPS = PASS == kMaps;
-    __shared__ alignas(16) float2 step[kTile][kColumns];               // delta, delta u
-    __shared__ alignas(16) float both[kTile][2][kMaxStates];           // B, C
-    __shared__ alignas(16) float out[MAPS ? 1 : kTile][kOutPitch];
+    // two tiles in turn: while one is walked the other's elements are computed
+    __shared__ alignas(16) float2 step[2][kTile][kColumns];            // delta, delta u
+    __shared__ alignas(16) float both[2][kTile][2][kMaxStates];        // B, C
+    __shared__ alignas(16) float out[MAPS ? 1 : 2][MAPS ? 1 : kTile][kOutPitch];
     const int64_t b = blockIdx.x / a.slabs, w = b / a.per_worker, row0 = b * a.T_;
-    const int column0 = static_cast<int>(blockIdx.x % a.slabs) * kColumns, span = blockIdx.y;
-    const int64_t begin = span * a.span_steps, end = begin + a.span_steps < a.T_ ? begin + a.span_steps : a.T_;
+    const int column0 = static_cast<int>(blockIdx.x % a.slabs) * kColumns;
+    // maps: piece i of each span; spans may have fewer steps than their pieces' together
+    const int parts = a.pieces / a.spans, span = MAPS ? blockIdx.y / parts : blockIdx.y;
+    const int64_t span_begin = span * a.span_steps, span_end = span_begin + a.span_steps < a.T_ ? span_begin + a.span_steps : a.T_;
+    const int64_t begin = MAPS ? span_begin + (blockIdx.y % parts) * a.piece_steps : span_begin;
+    const int64_t end = MAPS && begin + a.piece_steps < span_end ? begin + a.piece_steps : span_end;
     const T *params = a.params + w * a.ldp;
     // elements
     const int es = threadIdx.x / (kColumns / kEach), ec = threadIdx.x % (kColumns / kEach) * kEach, left = a.D - column0 - ec;
@@ -25,9 +34,10 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
     load_four<E>(params + static_cast<int64_t>(a.D) * a.N + column0 + ec, left, bias);
     load_four<E>(params + static_cast<int64_t>(a.D) * (a.N + 1) + column0 + ec, left, skip);
     // states
-    const int q = threadIdx.x % kQuarters, c = threadIdx.x / kQuarters, n0 = q * NQ;
+    const int q = threadIdx.x / 16 % kQuarters, c = threadIdx.x / kWave * 16 + threadIdx.x % 16, n0 = q * NQ;
     const bool any = column0 + c < a.D;
     const int64_t state = (static_cast<int64_t>(column0) + c) * a.N;   // of a column in [D][N]
+    const int64_t of = static_cast<int64_t>(a.D) * a.N, chunks = ceil_div(a.T_, kTile);
     float rate[NQ], h[NQ], sum = 0.0f;
     bool gone = false;
 #pragma unroll
@@ -35,64 +45,70 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
         rate[i] = any && n0 + i < a.N ? -kLog2e * exp2_fast(kLog2e * E::widen(params[state + n0 + i])) : 0.0f;
         h[i] = 0.0f;
     }
-    const int64_t of = static_cast<int64_t>(a.D) * a.N;
     if constexpr (!MAPS) {
-        if (a.spans > 1) load_states<NQ>(a.maps + (b * a.spans + span) * of + state, n0, a.N, any, h);
+        if (a.spans > 1) load_states<NQ>(a.maps + (b * a.pieces + span * parts) * of + state, n0, a.N, any, h);
         else if (a.h0) load_states<NQ>(a.h0 + b * of + state, n0, a.N, any, h);
     }
-    float u[4], dt[4], z[4], shared_[2];
+    const uint32_t u_at = place_in<T>(a.ldu, es, ec), dt_at = place_in<T>(a.lddt, es, ec), z_at = place_in<T>(a.ldz, es, ec), y_at = place_in<T>(a.ldy, es, ec);
+    const int bs = threadIdx.x / kMaxStates, bn = threadIdx.x % kMaxStates;          // a thread's element of B and of C
+    const uint32_t b_at = place_in<T>(a.ldb, bs, bn), c_at = place_in<T>(a.ldc, bs, bn), state_at = (c * a.N) * 4;
+    const auto steps_from = [&](int64_t t0) { return end - t0 >= kTile ? kTile : end > t0 ? static_cast<int>(end - t0) : 0; };
+    Four<E> u, dt, z{};
+    T b_next, c_next;
     const auto load = [&](int64_t t0) {
-        const int64_t t = t0 + es;
-        const int there = t < end ? left : 0;
-        load_four<E>(a.u + (row0 + t) * a.ldu + column0 + ec, there, u);
-        load_four<E>(a.dt + (row0 + t) * a.lddt + column0 + ec, there, dt);
-        if constexpr (!MAPS)
-            if (a.z) load_four<E>(a.z + (row0 + t) * a.ldz + column0 + ec, there, z);
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int at = threadIdx.x + k * kThreads, n = at % kMaxStates, which = at / kMaxStates % 2;
-            const int64_t s = t0 + at / (2 * kMaxStates);
-            shared_[k] = 0.0f;
-            if (n < a.N && s < end && !(MAPS && which)) shared_[k] = E::widen(which ? a.cm[(row0 + s) * a.ldc + n] : a.bm[(row0 + s) * a.ldb + n]);
+        const int64_t row = row0 + t0;
+        const int steps = steps_from(t0), there = es < steps ? left : 0;
+        const bool has = bn < a.N && bs < steps;
+        u = load_four<E>(at_byte(a.u + row * a.ldu + column0, u_at), there);
+        dt = load_four<E>(at_byte(a.dt + row * a.lddt + column0, dt_at), there);
+        b_next = has ? *at_byte(a.bm + row * a.ldb, b_at) : 0;
+        if constexpr (!MAPS) {
+            if (a.z) z = load_four<E>(at_byte(a.z + row * a.ldz + column0, z_at), there);
+            c_next = has ? *at_byte(a.cm + row * a.ldc, c_at) : 0;
         }
     };
-    load(begin);
-    for (int64_t t0 = begin; t0 < end; t0 += kTile) {
-        const unsigned resets = resets_of<RESETS>(a.reset, row0 + t0, end - t0 < kTile ? static_cast<int>(end - t0) : kTile);
-        const bool there = t0 + es < end;
-        float gate[4], direct[4];
+    float gate[4], direct[4];
+    const auto elements = [&](int64_t t0, int turn, float (&gates)[4], float (&directs)[4]) {
+        const bool there = es < steps_from(t0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float delta = there ? softplus(dt[j] + bias[j]) : 0.0f;            // behind the end: a step that changes nothing
-            step[es][ec + j] = float2{delta, delta * u[j]};
+            const float uj = value_of<E>(u, j), zj = finite_below(value_of<E>(z, j)), soft = softplus(value_of<E>(dt, j) + bias[j]);
+            const float delta = there ? soft : 0.0f;                    // behind the end: a step that changes nothing
+            step[turn][es][ec + j] = float2{delta, delta * uj};
             if constexpr (!MAPS) {
-                direct[j] = skip[j] * u[j];
-                gate[j] = a.z ? finite_below(z[j]) * sigmoid(z[j]) : 1.0f;
+                const float open = zj * sigmoid(zj);
+                directs[j] = skip[j] * uj;
+                gates[j] = a.z ? open : 1.0f;
             }
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) (&both[0][0][0])[threadIdx.x + k * kThreads] = shared_[k];
-        if (t0 + kTile < end) load(t0 + kTile);
-        __syncthreads();
+        both[turn][bs][0][bn] = E::widen(b_next);
+        if constexpr (!MAPS) both[turn][bs][1][bn] = E::widen(c_next);
+    };
+    const auto tile = [&](int64_t t0, auto turn_of) {
+        constexpr int turn = decltype(turn_of)::value;
+        const int steps = steps_from(t0);
+        const unsigned resets = resets_of<RESETS>(a.reset, row0 + t0, steps);
         if constexpr (!MAPS)
-            if (a.states) store_states<NQ>(a.states + (b * ceil_div(a.T_, kTile) + t0 / kTile) * of + state, n0, a.N, any, h);
-        float four[4];
+            if (a.states) store_states<NQ>(at_byte(a.states + (b * chunks + t0 / kTile) * of + static_cast<int64_t>(column0) * a.N, state_at), n0, a.N, any, h);
+        float next_gate[4], next_direct[4], four[4];
+        elements(t0 + kTile, !turn, next_gate, next_direct);
+        load(t0 + 2 * kTile);
 #pragma unroll
         for (int i = 0; i < kTile; ++i) {
-            const float2 s = step[i][c];
+            const float2 s = step[turn][i][c];
             const bool cut = RESETS && ((resets >> i) & 1u);
             float y = 0.0f;
 #pragma unroll
             for (int j = 0; j < NQ; ++j) {
-                const float in = s.y * both[i][0][n0 + j], keep = exp2_fast(rate[j] * s.x);
+                const float in = s.y * both[turn][i][0][n0 + j], keep = exp2_fast(rate[j] * s.x);
                 h[j] = cut ? in : __builtin_fmaf(keep, h[j], in);
-                if constexpr (!MAPS) y = __builtin_fmaf(both[i][1][n0 + j], h[j], y);
+                if constexpr (!MAPS) y = __builtin_fmaf(both[turn][i][1][n0 + j], h[j], y);
             }
             if constexpr (MAPS) {
                 sum += s.x;
             } else {
-                four[i % 4] = quad_sum(y);
-                if (i % 4 == 3) out[i - 3 + q][c] = one_of(q, four[0], four[1], four[2], four[3]);
+                four[i % 4] = y;
+                if (i % 4 == 3) out[turn][i - 3 + quarter_step(q)][c] = quarters_sum(four);
             }
         }
         if (RESETS) gone = gone || resets != 0;
@@ -100,13 +116,27 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
         if constexpr (!MAPS) {
             float v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = (out[es][ec + j] + direct[j]) * gate[j];
-            if (there) store_four<E>(a.y + (row0 + t0 + es) * a.ldy + column0 + ec, left, v);
+            for (int j = 0; j < 4; ++j) {
+                v[j] = (out[turn][es][ec + j] + direct[j]) * gate[j];
+                gate[j] = next_gate[j];
+                direct[j] = next_direct[j];
+            }
+            if (es < steps) store_four<E>(at_byte(a.y + (row0 + t0) * a.ldy + column0, y_at), left, v);
         }
+    };
+    if (begin < end) {
+        load(begin);
+        elements(begin, 0, gate, direct);
+        load(begin + kTile);
+        __syncthreads();
+    }
+    for (int64_t t0 = begin; t0 < end; t0 += 2 * kTile) {
+        tile(t0, std::integral_constant<int, 0>{});
+        if (t0 + kTile < end) tile(t0 + kTile, std::integral_constant<int, 1>{});
     }
     if constexpr (MAPS) {
-        store_states<NQ>(a.maps + (b * a.spans + span) * of + state, n0, a.N, any, h);
-        if (any && q == 0) a.sums[(b * a.spans + span) * a.D + column0 + c] = gone ? -1.0f : sum;
+        store_states<NQ>(a.maps + (b * a.pieces + blockIdx.y) * of + state, n0, a.N, any, h);
+        if (any && q == 0) a.sums[(b * a.pieces + blockIdx.y) * a.D + column0 + c] = gone ? -1.0f : sum;
     } else if (a.h_last && end == a.T_) {
         store_states<NQ>(a.h_last + b * of + state, n0, a.N, any, h);
     }
@@ -117,7 +147,8 @@ template <class E, int NQ>
 __global__ __launch_bounds__(kThreads) void select_step_kernel(const SelectArgs<E> a)
 {
     const int64_t b = blockIdx.x / a.slabs, w = b / a.per_worker;
-    const int d = static_cast<int>(blockIdx.x % a.slabs) * kColumns + threadIdx.x / kQuarters, q = threadIdx.x % kQuarters, n0 = q * NQ;
+    const int q = threadIdx.x / 16 % kQuarters, n0 = q * NQ;
+    const int d = static_cast<int>(blockIdx.x % a.slabs) * kColumns + threadIdx.x / kWave * 16 + threadIdx.x % 16;
     const bool any = d < a.D;
     const int at = any ? d : 0;
     const int64_t of = static_cast<int64_t>(a.D) * a.N, state = static_cast<int64_t>(at) * a.N;
@@ -138,16 +169,17 @@ __global__ __launch_bounds__(kThreads) void select_step_kernel(const SelectArgs<
         y = __builtin_fmaf(read, h[i], y);
     }
     if (a.h_last) store_states<NQ>(a.h_last + b * of + state, n0, a.N, any, h);
-    y = quad_sum(y) + skip * u;
+    y = add32(y, y);
+    y = add16(y, y) + skip * u;
     if (a.z) y *= finite_below(z) * sigmoid(z);
     if (any && q == 0) a.y[b * a.ldy + d] = E::narrow(y);
 }
 
-constexpr int64_t kWanted = 1024, kLeastTiles = 4;      // workgroups of a call; tiles of a span
+constexpr int64_t kAtOnce = 1024;                       // workgroups that run at a time: four to a CU
 
-Spans forward_spans(int64_t B, int64_t T, int32_t D) { return spans_of(B, T, D, kWanted, kLeastTiles); }
+Spans forward_spans(int64_t B, int64_t T, int32_t D) { return spans_of(B, T, D, kAtOnce); }
 
-int64_t maps_bytes(int64_t B, int32_t D, int32_t N, const Spans &s) { return s.spans > 1 ? B * s.spans * D * (N + 1) * 4 : 0; }
+int64_t maps_bytes(int64_t B, int32_t D, int32_t N, const Spans &s) { return s.spans > 1 ? B * s.pieces * D * (N + 1) * 4 : 0; }
 
 template <class E>
 int select_scan(const typename E::T *u, int64_t ldu, const typename E::T *dt, int64_t lddt, const typename E::T *bm, int64_t ldb, const typename E::T *cm,
@@ -170,8 +202,8 @@ int select_scan(const typename E::T *u, int64_t ldu, const typename E::T *dt, in
     }
     if (!u || !dt || !bm || !cm || !params || !y) return CX_ERR_NULL;
     const int64_t rows = B * T;
-    if (bad_matrix(rows, ldu, D) || bad_matrix(rows, lddt, D) || bad_matrix(rows, ldb, N) || bad_matrix(rows, ldc, N) || (z && bad_matrix(rows, ldz, D)) ||
-        bad_matrix(rows, ldy, D)) return CX_ERR_SHAPE;
+    if (bad_strip(rows, ldu, D) || bad_strip(rows, lddt, D) || bad_strip(rows, ldb, N) || bad_strip(rows, ldc, N) || (z && bad_strip(rows, ldz, D)) ||
+        bad_strip(rows, ldy, D)) return CX_ERR_SHAPE;
     const Spans s = forward_spans(B, T, D);
     const int64_t bytes = maps_bytes(B, D, N, s);
     if (bytes > 0 && !workspace) return CX_ERR_NULL;
@@ -188,21 +220,21 @@ int select_scan(const typename E::T *u, int64_t ldu, const typename E::T *dt, in
     SelectArgs<E> a{};
     a.u = u; a.ldu = ldu; a.dt = dt; a.lddt = lddt; a.bm = bm; a.ldb = ldb; a.cm = cm; a.ldc = ldc; a.z = z; a.ldz = ldz; a.params = params + offset;
     a.ldp = ldp; a.y = y; a.ldy = ldy; a.reset = reset; a.h0 = h0; a.h_last = h_last; a.states = states; a.B = B; a.T_ = T; a.per_worker = B / W;
-    a.D = D; a.N = N; a.slabs = s.slabs; a.spans = s.spans; a.span_steps = s.steps;
+    a.D = D; a.N = N; a.slabs = s.slabs; a.spans = s.spans; a.span_steps = s.steps; a.pieces = s.pieces; a.piece_steps = s.piece_steps;
     a.maps = static_cast<float *>(workspace);
-    a.sums = a.maps + B * s.spans * D * N;
+    a.sums = a.maps + B * s.pieces * D * N;
     const unsigned groups = static_cast<unsigned>(B * s.slabs);
     if (T == 1)
         return by_states(N, false, [&](auto nq, auto) {
             hipLaunchKernelGGL((select_step_kernel<E, decltype(nq)::value>), dim3(groups), dim3(kThreads), 0, st, a);
         });
     if (s.spans > 1) {
+        const int composed = s.pieces - s.pieces / s.spans;     // all but the last span's
         const int rc2 = by_states(N, reset != nullptr, [&](auto nq, auto resets) {
-            hipLaunchKernelGGL((select_kernel<E, decltype(nq)::value, decltype(resets)::value, kMaps>), dim3(groups, s.spans - 1), dim3(kThreads), 0, st, a);
+            hipLaunchKernelGGL((select_kernel<E, decltype(nq)::value, decltype(resets)::value, kMaps>), dim3(groups, composed), dim3(kThreads), 0, st, a);
         });
         if (rc2 != CX_OK) return rc2;
-        hipLaunchKernelGGL(enter_kernel<E>, dim3(static_cast<unsigned>(ceil_div(B * D * N, 256))), dim3(256), 0, st, a, h0, false);
-        if (launched() != CX_OK) return CX_ERR_HIP;
+        if (enter<E>(a, h0, false, composed, st) != CX_OK) return CX_ERR_HIP;
     }
     return by_states(N, reset != nullptr, [&](auto nq, auto resets) {
         hipLaunchKernelGGL((select_kernel<E, decltype(nq)::value, decltype(resets)::value, kWalk>), dim3(groups, s.spans), dim3(kThreads), 0, st, a);

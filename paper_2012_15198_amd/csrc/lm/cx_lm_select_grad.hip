@@ -7,7 +7,9 @@
 //   dB_t = sum over columns of r_t delta_t u_t    dC_t = sum over columns of h_t g_t
 //   dA_log = A sum_t r_t delta_t keep_t h_{t-1}    dbias = sum_t ddt    dskip = sum_t g u
 //
-// A tile's states are computed again from the one kept where it begins and stay in registers; the walk back meets them there.
+// A tile's states are computed again from the one kept where it begins and stay in registers with their gates; the walk back meets them there.
+// That takes 250 registers, so two wavefronts to a SIMD, which issue vector instructions in 80 % of the cycles (16 sequences of 2,048 x 1,024 with 16
+// states in bfloat16: 60 us the maps, 7 what enters, 480 the walks, 13 and 6 the sums over columns and parts).
 #include "lm_select.hpp"
 
 namespace {
@@ -17,50 +19,69 @@ enum Pass { kMaps, kWalk };
 constexpr int kOutPitch = kColumns + 16;                // the four steps that a column's lanes write lie in different banks
 constexpr int kWaves = kThreads / kWave;
 
-// The sums of 2 NQ values over the 16 columns of a wavefront (lanes of equal q), each value's in some lanes: two exchanges leave a lane half of
-// the values each, rotations of rows the rest.  `which`: B or C; `j`: the state; `holds`: this lane is the one to write it.
-template <int NQ>
+// The sums of 2 NQ values over the 16 columns of a row of lanes, each in some of its lanes: `which` (B or C) and `j` (the state); `holds`: this lane
+// is the one to write it.  Each stage leaves a lane half of the values, its own and its partner's: partners lie opposite each other in the
+// row, in half of it, in a group of four, beside each other.
 struct Reduced {
     float v;
     int which, j;
     bool holds;
 };
-__device__ __forceinline__ float add32(float x, float y)               // lanes 0 to 31: x of both halves, 32 to 63: y
+constexpr int kMirror = 0x140, kHalfMirror = 0x141, kOppositePair = 0x4e, kBeside = 0xb1;
+template <int PATTERN>
+__device__ __forceinline__ float add_partner(float v)
 {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    return v + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), PATTERN, 0xf, 0xf, true));
 }
-__device__ __forceinline__ float add16(float x, float y)               // even rows of 16 lanes: x of the row and the next, odd ones: y
+// Every lane adds both, then keeps one.
+template <int PATTERN>
+__device__ __forceinline__ float half_of(int second, float x, float y)
 {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-template <int BY>
-__device__ __forceinline__ float add_turned(float v)                   // with the lane BY places on in its row of 16
-{
-    return v + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), 0x120 + BY, 0xf, 0xf, true));
+    const float a = add_partner<PATTERN>(x), b = add_partner<PATTERN>(y);
+    return second ? b : a;
 }
 template <int NQ>
-__device__ __forceinline__ Reduced<NQ> reduce_columns(const float (&pb)[NQ], const float (&pc)[NQ])
+__device__ __forceinline__ Reduced reduce_columns(const float (&pb)[NQ], const float (&pc)[NQ])
 {
-    const int lane = threadIdx.x & (kWave - 1);
-    Reduced<NQ> r;
-    r.which = lane >> 5;
+    const int lane = threadIdx.x & 15;
+    Reduced r;
+    r.which = lane >> 3;
     if constexpr (NQ == 4) {
-        const float first = add_turned<4>(add_turned<8>(add16(add32(pb[0], pc[0]), add32(pb[1], pc[1]))));
-        const float second = add_turned<4>(add_turned<8>(add16(add32(pb[2], pc[2]), add32(pb[3], pc[3]))));
-        r.v = (lane & 8) ? second : first;
-        r.j = ((lane >> 4) & 1) + ((lane >> 2) & 2);
-        r.holds = (lane & 4) == 0;
+        // Two additions a pair: the second value's in all lanes, then the first one's over it in the half of the lanes (banks of four) that keep it.
+        // A value is read across lanes two instructions after it was written at the earliest.
+        float b0 = pb[0], b1 = pb[1], b2 = pb[2], b3 = pb[3], c0 = pc[0], c1 = pc[1], c2 = pc[2], c3 = pc[3];
+        asm("s_nop 1\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_mirror row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %1, %1, %1 row_mirror row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %2, %2, %2 row_mirror row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %3, %3, %3 row_mirror row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %2, %6, %6 row_mirror row_mask:0xf bank_mask:0x3\n\t"
+            "v_add_f32_dpp %3, %7, %7 row_mirror row_mask:0xf bank_mask:0x3\n\t"
+            "v_add_f32_dpp %0, %4, %4 row_mirror row_mask:0xf bank_mask:0x3\n\t"
+            "v_add_f32_dpp %1, %5, %5 row_mirror row_mask:0xf bank_mask:0x3\n\t"
+            "v_add_f32_dpp %2, %2, %2 row_half_mirror row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %3, %3, %3 row_half_mirror row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %2, %0, %0 row_half_mirror row_mask:0xf bank_mask:0x5\n\t"
+            "v_add_f32_dpp %3, %1, %1 row_half_mirror row_mask:0xf bank_mask:0x5\n\t"
+            "s_nop 0\n\t"
+            "v_add_f32_dpp %2, %2, %2 quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %3, %3, %3 quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf"
+            : "+v"(c0), "+v"(c1), "+v"(c2), "+v"(c3)
+            : "v"(b0), "v"(b1), "v"(b2), "v"(b3));
+        r.v = add_partner<kBeside>((lane & 2) ? c3 : c2);
+        r.j = ((lane >> 1) & 1) + ((lane >> 1) & 2);
+        r.holds = (lane & 1) == 0;
     } else if constexpr (NQ == 2) {
-        r.v = add_turned<4>(add_turned<8>(add16(add32(pb[0], pc[0]), add32(pb[1], pc[1]))));
-        r.j = (lane >> 4) & 1;
-        r.holds = (lane & 12) == 0;
+        const float first = half_of<kMirror>(lane & 8, pb[0], pc[0]), second = half_of<kMirror>(lane & 8, pb[1], pc[1]);
+        const float v = half_of<kHalfMirror>(lane & 4, first, second);
+        r.v = add_partner<kBeside>(add_partner<kOppositePair>(v));
+        r.j = (lane >> 2) & 1;
+        r.holds = (lane & 3) == 0;
     } else {
-        const float t = add32(pb[0], pc[0]);
-        r.v = add_turned<4>(add_turned<8>(add16(t, t)));
+        const float v = half_of<kMirror>(lane & 8, pb[0], pc[0]);
+        r.v = add_partner<kBeside>(add_partner<kOppositePair>(add_partner<kHalfMirror>(v)));
         r.j = 0;
-        r.holds = (lane & 28) == 0;
+        r.holds = (lane & 7) == 0;
     }
     return r;
 }
@@ -76,14 +97,18 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
     __shared__ alignas(16) float out[MAPS ? 1 : 3][MAPS ? 1 : kTile][kOutPitch];       // y', into, across
     __shared__ alignas(16) float shares[MAPS ? 1 : kWaves][kTile][2][kMaxStates];      // dB, dC of a wavefront's columns
     const int64_t b = blockIdx.x / a.slabs, w = b / a.per_worker, row0 = b * a.T_;
-    const int slab = static_cast<int>(blockIdx.x % a.slabs), column0 = slab * kColumns, span = blockIdx.y + (MAPS ? 1 : 0);
-    const int64_t begin = span * a.span_steps, end = begin + a.span_steps < a.T_ ? begin + a.span_steps : a.T_;
+    const int slab = static_cast<int>(blockIdx.x % a.slabs), column0 = slab * kColumns;
+    const int parts = a.pieces / a.spans, piece = blockIdx.y + parts, span = MAPS ? piece / parts : blockIdx.y;       // maps: all but the first span's
+    const int64_t span_begin = span * a.span_steps, span_end = span_begin + a.span_steps < a.T_ ? span_begin + a.span_steps : a.T_;
+    const int64_t begin = MAPS ? span_begin + (piece % parts) * a.piece_steps : span_begin;
+    const int64_t end = MAPS && begin + a.piece_steps < span_end ? begin + a.piece_steps : span_end;
     const T *params = a.params + w * a.ldp;
     const int es = threadIdx.x / (kColumns / kEach), ec = threadIdx.x % (kColumns / kEach) * kEach, left = a.D - column0 - ec;
     float bias[4], skip[4], dbias[4] = {}, dskip[4] = {};
+    __shared__ alignas(16) float parked[MAPS ? 1 : 3][MAPS ? 1 : kTile][kColumns];     // u, sigmoid(dt + bias), dy silu'(z): a thread's own, over the walks
     load_four<E>(params + static_cast<int64_t>(a.D) * a.N + column0 + ec, left, bias);
     load_four<E>(params + static_cast<int64_t>(a.D) * (a.N + 1) + column0 + ec, left, skip);
-    const int q = threadIdx.x % kQuarters, c = threadIdx.x / kQuarters, n0 = q * NQ, wave = threadIdx.x / kWave;
+    const int wave = threadIdx.x / kWave, q = threadIdx.x / 16 % kQuarters, c = wave * 16 + threadIdx.x % 16, n0 = q * NQ;
     const bool any = column0 + c < a.D;
     const int64_t state = (static_cast<int64_t>(column0) + c) * a.N, of = static_cast<int64_t>(a.D) * a.N, chunks = ceil_div(a.T_, kTile);
     float rate[NQ], carry[NQ], drate[NQ] = {}, sum = 0.0f;
@@ -94,50 +119,53 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         carry[i] = 0.0f;
     }
     if constexpr (!MAPS) {
-        if (a.spans > 1) load_states<NQ>(a.maps + (b * a.spans + span) * of + state, n0, a.N, any, carry);
+        if (a.spans > 1) load_states<NQ>(a.maps + (b * a.pieces + span * parts + parts - 1) * of + state, n0, a.N, any, carry);
         else if (a.dh_last) load_states<NQ>(a.dh_last + b * of + state, n0, a.N, any, carry);
     }
-    float u[4], dt[4], z[4] = {}, dy[4], shared_[2], entering[NQ];
+    const uint32_t u_at = place_in<T>(a.ldu, es, ec), dt_at = place_in<T>(a.lddt, es, ec), z_at = place_in<T>(a.ldz, es, ec), dy_at = place_in<T>(a.lddy, es, ec);
+    const int bs = threadIdx.x / kMaxStates, bn = threadIdx.x % kMaxStates;          // a thread's element of B and of C
+    const uint32_t b_at = place_in<T>(a.ldb, bs, bn), c_at = place_in<T>(a.ldc, bs, bn), state_at = (c * a.N) * 4;
+    Four<E> u, dt, z{}, dy;
+    T b_next, c_next;
+    float entering[NQ];
     const auto load = [&](int64_t t0) {
-        const int64_t t = t0 + es;
-        const int there = t < end ? left : 0;
-        load_four<E>(a.dt + (row0 + t) * a.lddt + column0 + ec, there, dt);
-        load_four<E>(a.dy + (row0 + t) * a.lddy + column0 + ec, there, dy);
-        if (a.z) load_four<E>(a.z + (row0 + t) * a.ldz + column0 + ec, there, z);
+        const int64_t row = row0 + t0;
+        const int steps = end - t0 < kTile ? static_cast<int>(end - t0) : kTile, there = es < steps ? left : 0;
+        const bool has = bn < a.N && bs < steps;
+        dt = load_four<E>(at_byte(a.dt + row * a.lddt + column0, dt_at), there);
+        dy = load_four<E>(at_byte(a.dy + row * a.lddy + column0, dy_at), there);
+        if (a.z) z = load_four<E>(at_byte(a.z + row * a.ldz + column0, z_at), there);
+        c_next = has ? *at_byte(a.cm + row * a.ldc, c_at) : 0;
         if constexpr (!MAPS) {
-            load_four<E>(a.u + (row0 + t) * a.ldu + column0 + ec, there, u);
-            load_states<NQ>(a.states_in + (b * chunks + t0 / kTile) * of + state, n0, a.N, any, entering);
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int at = threadIdx.x + k * kThreads, n = at % kMaxStates, which = at / kMaxStates % 2;
-            const int64_t s = t0 + at / (2 * kMaxStates);
-            shared_[k] = 0.0f;
-            if (n < a.N && s < end && !(MAPS && !which)) shared_[k] = E::widen(which ? a.cm[(row0 + s) * a.ldc + n] : a.bm[(row0 + s) * a.ldb + n]);
+            u = load_four<E>(at_byte(a.u + row * a.ldu + column0, u_at), there);
+            b_next = has ? *at_byte(a.bm + row * a.ldb, b_at) : 0;
+            load_states<NQ>(at_byte(a.states_in + (b * chunks + t0 / kTile) * of + static_cast<int64_t>(column0) * a.N, state_at), n0, a.N, any, entering);
         }
     };
-    int64_t t0 = begin + (end - 1 - begin) / kTile * kTile;
-    load(t0);
+    int64_t t0 = begin < end ? begin + (end - 1 - begin) / kTile * kTile : begin - kTile;        // a last span may leave its last pieces empty
+    if (begin < end) load(t0);
     for (; t0 >= begin; t0 -= kTile) {
-        const unsigned resets = resets_of<RESETS>(a.reset, row0 + t0, end - t0 < kTile ? static_cast<int>(end - t0) : kTile);
-        const bool there = t0 + es < end;
-        float own_u[4], delta[4], opens[4], g[4], dgate[4];
+        const int steps = end - t0 < kTile ? static_cast<int>(end - t0) : kTile;
+        const unsigned resets = resets_of<RESETS>(a.reset, row0 + t0, steps);
+        const bool there = es < steps;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float v = dt[j] + bias[j], zj = finite_below(z[j]), e = sigmoid(zj);
-            delta[j] = there ? softplus(v) : 0.0f;
-            g[j] = a.z ? dy[j] * (zj * e) : dy[j];
-            if constexpr (!MAPS) {
-                own_u[j] = u[j];
-                opens[j] = sigmoid(v);
-                dgate[j] = dy[j] * silu_slope(zj, e);
+            const float v = value_of<E>(dt, j) + bias[j], zj = finite_below(value_of<E>(z, j)), e = sigmoid(zj), dyj = value_of<E>(dy, j);
+            const float delta = there ? softplus(v) : 0.0f;             // behind the end: a step that changes nothing
+            pull[es][ec + j] = a.z ? dyj * (zj * e) : dyj;
+            if constexpr (MAPS) {
+                step[es][ec + j] = float2{delta, 0.0f};
+            } else {
+                const float uj = value_of<E>(u, j);
+                step[es][ec + j] = float2{delta, delta * uj};
+                parked[0][es][ec + j] = uj;
+                parked[1][es][ec + j] = sigmoid(v);
+                parked[2][es][ec + j] = dyj * silu_slope(zj, e);
             }
-            step[es][ec + j] = float2{delta[j], MAPS ? 0.0f : delta[j] * u[j]};
-            pull[es][ec + j] = g[j];
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) (&both[0][0][0])[threadIdx.x + k * kThreads] = shared_[k];
-        float h[MAPS ? 1 : kTile + 1][NQ];
+        if constexpr (!MAPS) both[bs][0][bn] = E::widen(b_next);
+        both[bs][1][bn] = E::widen(c_next);
+        float h[MAPS ? 1 : kTile + 1][NQ], keep[MAPS ? 1 : kTile][NQ];
         if constexpr (!MAPS)
 #pragma unroll
             for (int j = 0; j < NQ; ++j) h[0][j] = entering[j];
@@ -167,11 +195,12 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
 #pragma unroll
                 for (int j = 0; j < NQ; ++j) {
                     const float in = s.y * both[i][0][n0 + j];
-                    h[i + 1][j] = cut ? in : __builtin_fmaf(exp2_fast(rate[j] * s.x), h[i][j], in);
+                    keep[i][j] = exp2_fast(rate[j] * s.x);
+                    h[i + 1][j] = cut ? in : __builtin_fmaf(keep[i][j], h[i][j], in);
                     y = __builtin_fmaf(both[i][1][n0 + j], h[i + 1][j], y);
                 }
-                four[i % 4] = quad_sum(y);
-                if (i % 4 == 3) out[0][i - 3 + q][c] = one_of(q, four[0], four[1], four[2], four[3]);
+                four[i % 4] = y;
+                if (i % 4 == 3) out[0][i - 3 + quarter_step(q)][c] = quarters_sum(four);
             }
 #pragma unroll
             for (int i = kTile - 1; i >= 0; --i) {
@@ -184,20 +213,22 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
                 for (int j = 0; j < NQ; ++j) {
                     const float r = __builtin_fmaf(both[i][1][n0 + j], g_i, carry[j]);
                     into = __builtin_fmaf(r, both[i][0][n0 + j], into);
-                    const float keep = exp2_fast(rate[j] * s.x), moved = cut ? 0.0f : r * (keep * h[i][j]);
+                    const float moved = cut ? 0.0f : r * (keep[i][j] * h[i][j]);
                     across = __builtin_fmaf(rate[j], moved, across);
                     drate[j] = __builtin_fmaf(s.x, moved, drate[j]);
-                    carry[j] = cut ? 0.0f : keep * r;
+                    carry[j] = cut ? 0.0f : keep[i][j] * r;
                     pb[j] = r * s.y;
                     pc[j] = h[i + 1][j] * g_i;
                 }
-                four[i % 4] = quad_sum(into);
-                other[i % 4] = quad_sum(across);
+                four[i % 4] = into;
+                other[i % 4] = across;
                 if (i % 4 == 0) {
-                    out[1][i + q][c] = one_of(q, four[0], four[1], four[2], four[3]);
-                    out[2][i + q][c] = one_of(q, other[0], other[1], other[2], other[3]);
+                    out[1][i + quarter_step(q)][c] = quarters_sum(four);
+                    out[2][i + quarter_step(q)][c] = quarters_sum(other);
                 }
-                const Reduced<NQ> sums = reduce_columns<NQ>(pb, pc);
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) asm volatile("" : "+v"(drate[j]));       // summed here: 64 products waiting for it would cost as many registers
+                const Reduced sums = reduce_columns<NQ>(pb, pc);
                 if (sums.holds) shares[wave][i][sums.which][n0 + sums.j] = sums.v;
             }
         }
@@ -206,35 +237,37 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
             float du[4], ddt[4], dz[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float y = out[0][es][ec + j] + skip[j] * own_u[j], into = out[1][es][ec + j], across = kLn2 * out[2][es][ec + j];
-                du[j] = __builtin_fmaf(delta[j], into, skip[j] * g[j]);
-                ddt[j] = __builtin_fmaf(own_u[j], into, across) * opens[j];
-                dz[j] = dgate[j] * y;
+                const float uj = parked[0][es][ec + j], g = pull[es][ec + j], delta = step[es][ec + j].x;
+                const float y = out[0][es][ec + j] + skip[j] * uj, into = out[1][es][ec + j], across = kLn2 * out[2][es][ec + j];
+                du[j] = __builtin_fmaf(delta, into, skip[j] * g);
+                ddt[j] = __builtin_fmaf(uj, into, across) * parked[1][es][ec + j];
+                dz[j] = parked[2][es][ec + j] * y;
                 if (there) {
                     dbias[j] += ddt[j];
-                    dskip[j] = __builtin_fmaf(g[j], own_u[j], dskip[j]);
+                    dskip[j] = __builtin_fmaf(g, uj, dskip[j]);
                 }
             }
+            const int64_t row = row0 + t0;
             if (there) {
-                const int64_t row = row0 + t0 + es;
-                store_four<E>(a.du + row * a.lddu + column0 + ec, left, du);
-                store_four<E>(a.ddt + row * a.ldddt + column0 + ec, left, ddt);
-                if (a.dz) store_four<E>(a.dz + row * a.lddz + column0 + ec, left, dz);
+                store_four<E>(at_byte(a.du + row * a.lddu + column0, place_in<T>(a.lddu, es, ec)), left, du);
+                store_four<E>(at_byte(a.ddt + row * a.ldddt + column0, place_in<T>(a.ldddt, es, ec)), left, ddt);
+                if (a.dz) store_four<E>(at_byte(a.dz + row * a.lddz + column0, place_in<T>(a.lddz, es, ec)), left, dz);
             }
+            if (bn < a.N && bs < steps) {
+                float *share = at_byte(a.shared_parts + (slab * a.B * a.T_ + row) * 2 * a.N, (bs * 2 * a.N + bn) * 4);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int at = threadIdx.x + k * kThreads, n = at % kMaxStates, which = at / kMaxStates % 2, i = at / (2 * kMaxStates);
-                if (n >= a.N || t0 + i >= end) continue;
-                float v = 0.0f;
+                for (int which = 0; which < 2; ++which) {
+                    float v = 0.0f;
 #pragma unroll
-                for (int k2 = 0; k2 < kWaves; ++k2) v += shares[k2][i][which][n];
-                a.shared_parts[((slab * a.B * a.T_ + row0 + t0 + i) * 2 + which) * a.N + n] = v;
+                    for (int k = 0; k < kWaves; ++k) v += shares[k][bs][which][bn];
+                    share[which * a.N] = v;
+                }
             }
         }
     }
     if constexpr (MAPS) {
-        store_states<NQ>(a.maps + (b * a.spans + span) * of + state, n0, a.N, any, carry);
-        if (any && q == 0) a.sums[(b * a.spans + span) * a.D + column0 + c] = gone ? -1.0f : sum;
+        store_states<NQ>(a.maps + (b * a.pieces + piece) * of + state, n0, a.N, any, carry);
+        if (any && q == 0) a.sums[(b * a.pieces + piece) * a.D + column0 + c] = gone ? -1.0f : sum;
     } else {
         if (a.dh0 && begin == 0) store_states<NQ>(a.dh0 + b * of + state, n0, a.N, any, carry);
         const int64_t count = static_cast<int64_t>(a.D) * (a.N + 2);
@@ -274,7 +307,7 @@ __global__ __launch_bounds__(256) void share_kernel(const SelectArgs<E> a)
     else a.dcm[row * a.lddc + at - a.N] = E::narrow(v);
 }
 
-constexpr int64_t kWanted = 768, kLeastTiles = 4;       // workgroups of a call; tiles of a span
+constexpr int64_t kAtOnce = 512;                        // workgroups that run at a time: two to a CU, by their registers
 
 struct Space {
     Spans s;
@@ -283,10 +316,10 @@ struct Space {
 Space space_of(int64_t B, int64_t T, int32_t D, int32_t N)
 {
     Space p{};
-    p.s = spans_of(B, T, D, kWanted, kLeastTiles);
+    p.s = spans_of(B, T, D, kAtOnce);
     const bool split = p.s.spans > 1;
-    p.sums = split ? round_up(B * p.s.spans * D * N * 4, 16) : 0;
-    p.shared = p.sums + (split ? round_up(B * p.s.spans * D * 4, 16) : 0);
+    p.sums = split ? round_up(B * p.s.pieces * D * N * 4, 16) : 0;
+    p.shared = p.sums + (split ? round_up(B * p.s.pieces * D * 4, 16) : 0);
     p.parts = p.shared + round_up(p.s.slabs * B * T * 2 * N * 4, 16);
     p.bytes = p.parts + B * p.s.spans * D * (N + 2) * 4;
     return p;
@@ -310,9 +343,9 @@ int select_scan_grad(const typename E::T *u, int64_t ldu, const typename E::T *d
     Space space{};
     if (!none) {
         if (!u || !dt || !bm || !cm || !params || !dy || !du || !ddt || !dbm || !dcm || !states || !workspace || (z && !dz) || (!z && dz)) return CX_ERR_NULL;
-        if (bad_matrix(rows, ldu, D) || bad_matrix(rows, lddt, D) || bad_matrix(rows, ldb, N) || bad_matrix(rows, ldc, N) || (z && bad_matrix(rows, ldz, D)) ||
-            bad_matrix(rows, lddy, D) || bad_matrix(rows, lddu, D) || bad_matrix(rows, ldddt, D) || bad_matrix(rows, lddb, N) || bad_matrix(rows, lddc, N) ||
-            (dz && bad_matrix(rows, lddz, D))) return CX_ERR_SHAPE;
+        if (bad_strip(rows, ldu, D) || bad_strip(rows, lddt, D) || bad_strip(rows, ldb, N) || bad_strip(rows, ldc, N) || (z && bad_strip(rows, ldz, D)) ||
+            bad_strip(rows, lddy, D) || bad_strip(rows, lddu, D) || bad_strip(rows, ldddt, D) || bad_strip(rows, lddb, N) || bad_strip(rows, lddc, N) ||
+            (dz && bad_strip(rows, lddz, D))) return CX_ERR_SHAPE;
         space = space_of(B, T, D, N);
         if (workspace_bytes < space.bytes) return CX_ERR_SHAPE;
     }
@@ -338,7 +371,7 @@ int select_scan_grad(const typename E::T *u, int64_t ldu, const typename E::T *d
         a.u = u; a.ldu = ldu; a.dt = dt; a.lddt = lddt; a.bm = bm; a.ldb = ldb; a.cm = cm; a.ldc = ldc; a.z = z; a.ldz = ldz; a.params = params + offset;
         a.ldp = ldp; a.dy = dy; a.lddy = lddy; a.du = du; a.lddu = lddu; a.ddt = ddt; a.ldddt = ldddt; a.dbm = dbm; a.lddb = lddb; a.dcm = dcm; a.lddc = lddc;
         a.dz = dz; a.lddz = lddz; a.reset = reset; a.states_in = states; a.per_worker = B / W; a.slabs = space.s.slabs; a.spans = space.s.spans;
-        a.span_steps = space.s.steps;
+        a.span_steps = space.s.steps; a.pieces = space.s.pieces; a.piece_steps = space.s.piece_steps;
         a.maps = reinterpret_cast<float *>(base);
         a.sums = reinterpret_cast<float *>(base + space.sums);
         a.shared_parts = reinterpret_cast<float *>(base + space.shared);
@@ -346,12 +379,12 @@ int select_scan_grad(const typename E::T *u, int64_t ldu, const typename E::T *d
         const unsigned groups = static_cast<unsigned>(B * a.slabs);
         int rc2 = CX_OK;
         if (a.spans > 1) {
+            const int composed = a.pieces - a.pieces / a.spans;
             rc2 = by_states(N, reset != nullptr, [&](auto nq, auto resets) {
-                hipLaunchKernelGGL((select_grad_kernel<E, decltype(nq)::value, decltype(resets)::value, kMaps>), dim3(groups, a.spans - 1), dim3(kThreads), 0, st, a);
+                hipLaunchKernelGGL((select_grad_kernel<E, decltype(nq)::value, decltype(resets)::value, kMaps>), dim3(groups, composed), dim3(kThreads), 0, st, a);
             });
             if (rc2 != CX_OK) return rc2;
-            hipLaunchKernelGGL(enter_kernel<E>, dim3(static_cast<unsigned>(ceil_div(B * D * N, 256))), dim3(256), 0, st, a, dh_last, true);
-            if (launched() != CX_OK) return CX_ERR_HIP;
+            if (enter<E>(a, dh_last, true, composed, st) != CX_OK) return CX_ERR_HIP;
         }
         rc2 = by_states(N, reset != nullptr, [&](auto nq, auto resets) {
             hipLaunchKernelGGL((select_grad_kernel<E, decltype(nq)::value, decltype(resets)::value, kWalk>), dim3(groups, a.spans), dim3(kThreads), 0, st, a);

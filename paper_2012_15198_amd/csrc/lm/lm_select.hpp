@@ -7,8 +7,8 @@
 //
 //   elements   a thread has four columns of one step: it reads them in one piece, computes what belongs to a column alone (delta,
 //              the gates) and leaves it in LDS
-//   states     four lanes share a column, each with a quarter of its states in registers; they walk the tile's steps, and their
-//              sums over states are two additions across lanes
+//   states     four lanes share a column, each with a quarter of its states in registers; they walk the tile's steps, and four steps'
+//              sums over states take three exchanges of rows of lanes
 //
 // The states' map over a span of steps is h -> exp(-exp(A_log) sum of delta) h + S: one number and the N of S.
 #ifndef CX_LM_SELECT_HPP
@@ -23,21 +23,18 @@ constexpr int kMaxStates = CX_MAX_STATES;
 constexpr int64_t kMaxSeq = CX_MAX_TOKENS;
 static_assert(kTile * kColumns == kThreads * kEach && kColumns * kQuarters == kThreads && kMaxStates == 16, "the two shapes");
 
-// 1 / (1 + e^-v) and log(1 + e^v), both to a few units in the last place at either end: with e = exp(-|v|) <= 1,
-// softplus = max(v, 0) + log1p(e), log1p(e) = 2 artanh(e / (2 + e)) by its series (argument at most 1/3).  -inf: 0 and 0.
+// log(1 + e^v) to a few units in the last place at either end: with e = exp(-|v|) <= 1 it is max(v, 0) + log1p(e), and log1p(e) = s P(s^2) with
+// s = e / (2 + e) <= 1/3 and P(q) = 2 artanh(sqrt q) / sqrt q.  The coefficients are the polynomial of the least largest relative error on
+// [0, 1/9] (Remez exchange), 8e-9 after their rounding.  -inf gives 0.
 __device__ __forceinline__ float softplus(float v)
 {
     const float e = exp2_fast(-kLog2e * __builtin_fabsf(v)), s = e * rcp_fast(2.0f + e), q = s * s;
-    float p = 2.0f / 17;
-    p = __builtin_fmaf(p, q, 2.0f / 15);
-    p = __builtin_fmaf(p, q, 2.0f / 13);
-    p = __builtin_fmaf(p, q, 2.0f / 11);
-    p = __builtin_fmaf(p, q, 2.0f / 9);
-    p = __builtin_fmaf(p, q, 2.0f / 7);
-    p = __builtin_fmaf(p, q, 2.0f / 5);
-    p = __builtin_fmaf(p, q, 2.0f / 3);
+    float p = 0x1.208bdp-2f;
+    p = __builtin_fmaf(p, q, 0x1.1e510ap-2f);
+    p = __builtin_fmaf(p, q, 0x1.99dae6p-2f);
+    p = __builtin_fmaf(p, q, 0x1.5554ep-1f);
     p = __builtin_fmaf(p, q, 2.0f);
-    return __builtin_fmaf(p, s, v > 0.0f ? v : v != v ? v : 0.0f);
+    return __builtin_fmaf(p, s, __builtin_fmaxf(v, 0.0f));  // a NaN is in s
 }
 
 template <class E>
@@ -49,36 +46,73 @@ struct SelectArgs {
     const uint8_t *reset;
     const float *h0, *states_in, *dh_last;
     float *h_last, *states, *dh0;
-    float *maps;                                        // split: [B][spans][D][N] what a span makes of zeros, then what enters it
-    float *sums;                                        // [B][spans][D] sum of delta; below zero: the span forgets what enters
+    float *maps;                                        // split: [B][pieces][D][N] what a piece of a span makes of zeros, then what enters it
+    float *sums;                                        // [B][pieces][D] sum of delta; below zero: the piece forgets what enters
     float *shared_parts, *parts;                        // gradient: [slabs][B][T][2][N] of B and C; [W][parts][D (N + 2)] of the parameters
     int64_t B, T_, per_worker;
-    int32_t D, N, slabs, spans;
-    int64_t span_steps;                                 // a multiple of kTile
+    int32_t D, N, slabs, spans, pieces;                 // pieces of all spans, as many of each
+    int64_t span_steps, piece_steps;                    // multiples of kTile
 };
 
-// Four columns of a row; `left`: columns from p to the row's end, zeros behind them.
+// Four columns of a row as they lie in memory, widened where they are used: what is loaded ahead is then not waited for.
 template <class E>
-__device__ __forceinline__ void load_four(const typename E::T *p, int left, float (&v)[4])
+struct Four {
+    unsigned w[sizeof(typename E::T)];
+};
+// `left`: columns from p to the row's end, zeros behind them.
+template <class E>
+__device__ __forceinline__ Four<E> load_four(const typename E::T *p, int left)
 {
-    if constexpr (sizeof(typename E::T) == 4) {
-        if (left >= 4) {
+    Four<E> r;
+    constexpr int kWords = sizeof(typename E::T);
+    if (left >= 4) {
+        if constexpr (kWords == 4) {
             const u4 w = load16<E>(p);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(w[j]);
-            return;
-        }
-    } else {
-        if (left >= 4) {
+            for (int j = 0; j < 4; ++j) r.w[j] = w[j];
+        } else {
             typedef unsigned u2 __attribute__((ext_vector_type(2)));
             typedef u2 u2_at2 __attribute__((aligned(2)));
             const u2 w = *reinterpret_cast<const u2_at2 *>(p);
-            v[0] = E::low(w[0]); v[1] = E::high(w[0]); v[2] = E::low(w[1]); v[3] = E::high(w[1]);
-            return;
+            r.w[0] = w[0];
+            r.w[1] = w[1];
         }
-    }
+    } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = j < left ? E::widen(p[j]) : 0.0f;
+        for (int j = 0; j < kWords; ++j) r.w[j] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < left) {
+                if constexpr (kWords == 4) r.w[j] = __float_as_uint(p[j]);
+                else r.w[j / 2] |= static_cast<unsigned>(p[j]) << (16 * (j & 1));
+            }
+    }
+    return r;
+}
+template <class E>
+__device__ __forceinline__ float value_of(const Four<E> &r, int j)
+{
+    if constexpr (sizeof(typename E::T) == 4) return __uint_as_float(r.w[j]);
+    else return (j & 1) ? E::high(r.w[j / 2]) : E::low(r.w[j / 2]);
+}
+// Rows of a tile have uniform addresses, threads a place in them: 32 bits of bytes, which rows of at most kMaxPitch elements leave room for.
+constexpr int64_t kMaxPitch = int64_t(1) << 24;
+template <class T>
+__device__ __forceinline__ T *at_byte(T *base, uint32_t byte)
+{
+    using Byte = std::conditional_t<std::is_const_v<T>, const char, char>;
+    return reinterpret_cast<T *>(reinterpret_cast<Byte *>(base) + byte);
+}
+template <class T>
+__device__ __forceinline__ uint32_t place_in(int64_t ld, int step, int column) { return (static_cast<uint32_t>(step) * static_cast<uint32_t>(ld) + column) * sizeof(T); }
+[[maybe_unused]] bool bad_strip(int64_t rows, int64_t ld, int64_t columns) { return bad_matrix(rows, ld, columns) || ld > kMaxPitch; }
+
+template <class E>
+__device__ __forceinline__ void load_four(const typename E::T *p, int left, float (&v)[4])
+{
+    const Four<E> r = load_four<E>(p, left);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = value_of<E>(r, j);
 }
 template <class E>
 __device__ __forceinline__ void store_four(typename E::T *p, int left, const float (&v)[4])
@@ -98,24 +132,20 @@ __device__ __forceinline__ void store_four(typename E::T *p, int left, const flo
         if (j < left) p[j] = E::narrow(v[j]);
 }
 
-// Sum over the four lanes of a column, in all of them.
-template <int PATTERN>
-__device__ __forceinline__ float from_quad(float v)
+// Lane 16 q + c of a wavefront has quarter q of the states of its column c.  Sums over quarters cross its four rows of 16 lanes.
+__device__ __forceinline__ float add32(float x, float y)               // rows 0 and 1: x of both halves of the wavefront; rows 2 and 3: y
 {
-    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), PATTERN, 0xf, 0xf, true));
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ float quad_sum(float v)
+__device__ __forceinline__ float add16(float x, float y)               // even rows: x of the row and the next; odd rows: y of the row and the one before
 {
-    v += from_quad<0xb1>(v);                            // lanes 1 0 3 2
-    return v + from_quad<0x4e>(v);                      // lanes 2 3 0 1
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-
-// Four steps' sums, one to each of a column's lanes.
-__device__ __forceinline__ float one_of(int q, float a, float b, float c, float d)
-{
-    const float low = (q & 1) ? b : a, high = (q & 1) ? d : c;
-    return (q & 2) ? high : low;
-}
+// Four steps' sums over the quarters: the one of step quarter_step(q) in quarter q's lanes.
+__device__ __forceinline__ float quarters_sum(const float (&v)[4]) { return add16(add32(v[0], v[1]), add32(v[2], v[3])); }
+__device__ __forceinline__ int quarter_step(int q) { return (q & 1) * 2 + q / 2; }
 
 // Bit i: step i of the tile that begins at `row` forgets.
 template <bool RESETS>
@@ -153,37 +183,64 @@ __device__ __forceinline__ void store_states(float *p, int n0, int N, bool any, 
         if (n0 + i < N) p[n0 + i] = h[i];
 }
 
-// What enters each span, in the place of what the span makes of zeros: a thread a state of a column.  `backwards`: the adjoint, from the last
-// span on.  What the span at the end makes is not needed.
+// What enters each piece, in the place of what the piece makes of zeros.  `backwards`: the adjoint, from the last piece on.  `needed` pieces have
+// been composed, in the order of the walk.  A lane has a state of a column; the wavefronts of a workgroup compose a stretch of the pieces each, pass the
+// stretches' maps on through LDS and walk theirs again: one after the other 64 pieces of 16,384 states take 13 us.
+constexpr int kStretches = 8;
 template <class E>
-__global__ __launch_bounds__(256) void enter_kernel(const SelectArgs<E> a, const float *first, bool backwards)
+__global__ __launch_bounds__(kWave *kStretches) void enter_kernel(const SelectArgs<E> a, const float *first, bool backwards, int needed)
 {
-    const int64_t of = static_cast<int64_t>(a.D) * a.N, i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= a.B * of) return;
+    __shared__ float2 maps_of[kStretches][kWave];       // sum of delta (below zero: forgets), S
+    const int lane = threadIdx.x % kWave, stretch = threadIdx.x / kWave, stretches = blockDim.x / kWave;
+    const int64_t of = static_cast<int64_t>(a.D) * a.N, at0 = static_cast<int64_t>(blockIdx.x) * kWave + lane, all = a.B * of;
+    const int64_t i = at0 < all ? at0 : all - 1;
     const int64_t b = i / of, at = i - b * of;
     const int d = static_cast<int>(at / a.N), n = static_cast<int>(at - static_cast<int64_t>(d) * a.N);
     const float rate = -kLog2e * exp2_fast(kLog2e * E::widen(a.params[(b / a.per_worker) * a.ldp + static_cast<int64_t>(d) * a.N + n]));
-    float *maps = a.maps + b * a.spans * of + at;
-    const float *sums = a.sums + b * a.spans * a.D + d;
-    float h = first ? first[i] : 0.0f;
+    float *maps = a.maps + b * a.pieces * of + at;
+    const float *sums = a.sums + b * a.pieces * a.D + d;
+    const int each = (needed + stretches) / stretches, begin = stretch * each;         // of needed + 1 places, the last of which only receives
+    const int end = begin + each < needed + 1 ? begin + each : needed + 1;
+    const auto place = [&](int k) -> int64_t { return backwards ? a.pieces - 1 - k : k; };
     constexpr int kBatch = 8;                           // loads in flight
-    for (int k0 = 0; k0 < a.spans; k0 += kBatch) {
-        float S[kBatch], sum[kBatch];
+    const auto walk = [&](auto &&step) {
+        for (int k0 = begin; k0 < end; k0 += kBatch) {
+            float S[kBatch], sum[kBatch];
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            const int step = k0 + k, span = backwards ? a.spans - 1 - step : step;
-            if (step + 1 < a.spans) {
-                S[k] = maps[span * of];
-                sum[k] = sums[static_cast<int64_t>(span) * a.D];
+            for (int k = 0; k < kBatch; ++k) {
+                S[k] = sum[k] = 0.0f;
+                if (k0 + k < end && k0 + k < needed) {
+                    S[k] = maps[place(k0 + k) * of];
+                    sum[k] = sums[place(k0 + k) * a.D];
+                }
             }
-        }
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            const int step = k0 + k, span = backwards ? a.spans - 1 - step : step;
-            if (step < a.spans) maps[span * of] = h;
-            if (step + 1 < a.spans) h = sum[k] < 0.0f ? S[k] : __builtin_fmaf(exp2_fast(rate * sum[k]), h, S[k]);
+            for (int k = 0; k < kBatch; ++k)
+                if (k0 + k < end) step(k0 + k, S[k], sum[k]);
         }
-    }
+    };
+    const auto apply = [&](float sum, float S, float h) { return sum < 0.0f ? S : __builtin_fmaf(exp2_fast(rate * sum), h, S); };
+    float h = 0.0f, total = 0.0f;
+    walk([&](int, float S, float sum) {
+        h = apply(sum, S, h);
+        total = sum < 0.0f || total < 0.0f ? -1.0f : total + sum;
+    });
+    maps_of[stretch][lane] = float2{total, h};
+    __syncthreads();
+    h = first ? first[i] : 0.0f;
+    for (int k = 0; k < stretch; ++k) h = apply(maps_of[k][lane].x, maps_of[k][lane].y, h);
+    if (at0 >= all) return;
+    walk([&](int k, float S, float sum) {
+        maps[place(k) * of] = h;
+        h = apply(sum, S, h);
+    });
+}
+template <class E>
+[[maybe_unused]] int enter(const SelectArgs<E> &a, const float *first, bool backwards, int needed, hipStream_t st)
+{
+    const int stretches = needed < 8 * kStretches ? needed / 8 + 1 : kStretches;             // short ones only wait for each other
+    hipLaunchKernelGGL(enter_kernel<E>, dim3(static_cast<unsigned>(ceil_div(a.B * a.D * a.N, kWave))), dim3(kWave * stretches), 0, st, a, first, backwards, needed);
+    return launched();
 }
 
 // No steps: the state passes through.
@@ -202,24 +259,32 @@ __global__ __launch_bounds__(256) void pass_states_kernel(const float *from, flo
 }
 
 struct Spans {
-    int32_t slabs, spans;
-    int64_t steps;
+    int32_t slabs, spans, pieces;
+    int64_t steps, piece_steps;
 };
 
-// Workgroups that a call is to have; spans hold at least `least` tiles.
-[[maybe_unused]] Spans spans_of(int64_t B, int64_t T, int32_t D, int64_t wanted, int64_t least)
+// Into how many spans the steps are split: as many as make the rounds of `at_once` workgroups take least, in tiles, with a quarter for the maps' launch
+// where there is one.  Spans have at least kLeastTiles tiles.
+constexpr int64_t kLeastTiles = 4, kMostSpans = 256, kMapsAtOnce = 1536;
+[[maybe_unused]] Spans spans_of(int64_t B, int64_t T, int32_t D, int64_t at_once)
 {
-    Spans s{};
-    s.slabs = static_cast<int32_t>(ceil_div(D, kColumns));
-    const int64_t groups = B * s.slabs, tiles = ceil_div(T, kTile);
-    int64_t spans = groups >= wanted ? 1 : ceil_div(wanted, groups);
-    const int64_t most = tiles / least;
-    spans = spans < most ? spans : most;
-    if (spans < 1) spans = 1;
-    const int64_t span_tiles = ceil_div(tiles, spans);
-    s.spans = static_cast<int32_t>(ceil_div(tiles, span_tiles));
-    s.steps = span_tiles * kTile;
-    return s;
+    const int64_t slabs = ceil_div(D, kColumns), groups = B * slabs, tiles = ceil_div(T, kTile);
+    int64_t best = 1, least = 4 * ceil_div(groups, at_once) * tiles;
+    for (int64_t spans = 2; spans <= kMostSpans && spans * kLeastTiles <= tiles && groups < 8 * at_once; ++spans) {
+        const int64_t each = ceil_div(tiles, spans), cost = 4 * ceil_div(groups * spans, at_once) * each + ceil_div(groups * (spans - 1), at_once) * each + spans;
+        if (cost < least) {
+            least = cost;
+            best = spans;
+        }
+    }
+    // a span's map is composed of pieces of it, where spans alone would leave the maps' launch short of workgroups
+    const int64_t each = ceil_div(tiles, best), spans = ceil_div(tiles, each), others = groups * (spans - 1);
+    int64_t parts = spans > 1 ? kMapsAtOnce / others : 1;
+    parts = parts < each / kLeastTiles ? parts : each / kLeastTiles;
+    if (parts < 1) parts = 1;
+    const int64_t piece = ceil_div(each, parts);
+    parts = ceil_div(each, piece);
+    return {static_cast<int32_t>(slabs), static_cast<int32_t>(spans), static_cast<int32_t>(spans * parts), each * kTile, piece * kTile};
 }
 
 template <class F>
