@@ -11,8 +11,15 @@ projection), one gated recurrence over its rows and a residual connection; a wor
     backward    output projection, cx_gated_scan_grad, projection, cx_embed_grad added to the output projection's gradient
     update      cx_sgd_fused_mix: momentum SGD and segment-wise averaging with the peers
 
+Blocks is the same with residual blocks in the recurrence's place, any number of them: norm, projection, short convolution, selective
+scan with a gate, projection back, dropout on what is added to the residual:
+
+    forward     cx_add_norm, projection, cx_short_conv, projection, cx_select_scan, projection, ..., cx_add_norm, cx_dropout
+    backward    their gradients into the same flat rows, the masks drawn again from the counter
+
 The matrix products in between are torch's.  `python -m paper_2012_15198_amd.codistill` trains on synthetic text (noisy
-arithmetic sequences, packed documents) and prints the loss and the log probability of held-out text.
+arithmetic sequences, packed documents) and prints the loss and the log probability of held-out text; --blocks 2 --dropout 0.1
+trains two blocks with dropout.
 """
 from __future__ import annotations
 
@@ -138,6 +145,150 @@ class Replicas:
         return out
 
 
+class Blocks(Replicas):
+    """W replicas of a model of residual blocks.  A worker's flat row: table V x D; of each block norm D, projection D x 2 D, convolution
+    D x K and D, projection D x (D + 2 S), scan D x S, D and D, projection D x D; norm D."""
+
+    K, S_, EPS = 4, 8, 1e-6                                      # taps, states of a column
+
+    def __init__(self, W, V, D, blocks=2, dropout=0.0, S=4, seed=0, device="cuda:0"):
+        K, N, at = self.K, self.S_, V * D
+        self.blocks, self.p, self.at = blocks, dropout, []
+        for _ in range(blocks):
+            place = {}
+            for name, size in (("norm", D), ("into", 2 * D * D), ("conv", D * (K + 1)), ("steps", D * (D + 2 * N)), ("scan", D * (N + 2)), ("back", D * D)):
+                place[name], at = at, at + size
+            self.at.append(place)
+        self.norm, self.P = at, at + D
+        self.W, self.V, self.D, self.S, self.seed, self.device = W, V, D, S, seed, device
+        gen = torch.Generator(device).manual_seed(seed)
+        row = torch.empty(self.P, device=device).normal_(0.0, 1.0 / math.sqrt(D), generator=gen)
+        row[self.norm:] = 1.0
+        for place in self.at:
+            row[place["norm"]:place["into"]] = 1.0
+            row[place["conv"] + D * K:place["steps"]] = 0.0
+            scan = row[place["scan"]:place["back"]]
+            scan[:D * N] = (torch.arange(N, device=device) + 1.0).log().repeat(D)
+            steps = (torch.rand(D, device=device, generator=gen) * math.log(100.0) + math.log(1e-3)).exp()
+            scan[D * N:D * (N + 1)] = steps + (-(-steps).expm1()).log()          # softplus gives the steps
+            scan[D * (N + 1):] = 1.0
+        self.x = torch.zeros((W, -(-self.P // 8) * 8), device=device)
+        self.x[:, :self.P] = row                                 # replicas begin equal
+        self.v, self.g = torch.zeros_like(self.x), torch.zeros_like(self.x)
+        self.x2, self.v2 = torch.zeros_like(self.x), torch.zeros_like(self.x)
+        offsets = equal_seg_off(self.P, S)
+        cx.cx_check_segments(offsets, self.P)
+        self.offsets, self.round = torch.from_numpy(offsets).to(device), 0
+        # key and draw of each mask: the embedding's, the blocks', the last one; a round's draws follow the round's before
+        self.rng = torch.tensor([[seed, k] for k in range(blocks + 2)], dtype=torch.int64, device=device)
+
+    def part(self, rows, w, at, columns):
+        return rows[w, at:at + self.D * columns].view(self.D, columns)
+
+    def product(self, x, at, columns, a):
+        """a @ the workers' matrices [D][columns] at `at`, each on its own rows."""
+        out, n = torch.empty((a.shape[0], columns), device=a.device), a.shape[0] // x.shape[0]
+        for w in range(x.shape[0]):
+            torch.mm(a[w * n:(w + 1) * n], self.part(x, w, at, columns), out=out[w * n:(w + 1) * n])
+        return out
+
+    def product_grad(self, at, columns, a, d):
+        """Of product(): the gradient of a, and into g that of the matrices."""
+        da, n = torch.empty_like(a), a.shape[0] // self.W
+        for w in range(self.W):
+            rows = slice(w * n, (w + 1) * n)
+            torch.mm(a[rows].t(), d[rows], out=self.part(self.g, w, at, columns))
+            torch.mm(d[rows], self.part(self.x, w, at, columns).t(), out=da[rows])
+        return da
+
+    def block(self, x, place, y, T, reset=None, states=None, before=None, h=None):
+        """What a block adds to the residual, from the norm's output y; before and h: the state of generation, in place."""
+        D, K, N = self.D, self.K, self.S_
+        into = self.product(x, place["into"], 2 * D, y)
+        u, v = torch.empty_like(y), torch.empty_like(y)
+        lm.cx_short_conv(into[:, :D], x, place["conv"], u, T, K, before=before, after=before, reset=reset)
+        steps = self.product(x, place["steps"], D + 2 * N, u)
+        lm.cx_select_scan(u, steps[:, :D], steps[:, D:D + N], steps[:, D + N:], x, place["scan"], v, T, z=into[:, D:], h0=h, h_last=h, reset=reset, states=states)
+        return self.product(x, place["back"], D, v), into, u, steps, v
+
+    def forward(self, x, tokens, reset, keep=False):
+        W, D, n, T = tokens.shape[0], self.D, tokens.shape[1], reset.shape[1]
+        p = self.p if keep else 0.0                              # the teacher and scores drop nothing
+        add, s, kept = torch.empty((W * n, D), device=x.device), None, []
+        lm.cx_embed_lookup(x, tokens, add, 0, self.V, math.sqrt(D))
+        for k, place in enumerate(self.at):
+            total, y, inv = torch.empty_like(add), torch.empty_like(add), torch.empty(W * n, device=x.device)
+            lm.cx_add_norm(add, s, x, place["norm"], total, y, self.EPS, inv=inv, p=p, rng=self.rng[k])
+            states = lm.select_states(y, T, self.S_) if keep else None
+            s, (add, into, u, steps, v) = total, self.block(x, place, y, T, reset, states)
+            kept.append((s, y, inv, into, u, steps, v, states))
+        total, y, inv = torch.empty_like(add), torch.empty_like(add), torch.empty(W * n, device=x.device)
+        lm.cx_add_norm(add, s, x, self.norm, total, y, self.EPS, inv=inv, p=p, rng=self.rng[self.blocks])
+        if p:
+            lm.cx_dropout(y, self.rng[self.blocks + 1], y, p)
+        y /= math.sqrt(D)
+        z = torch.empty((W * n, self.V), device=x.device)
+        for w in range(W):
+            torch.mm(y[w * n:(w + 1) * n], self.table(x, w).t(), out=z[w * n:(w + 1) * n])
+        return (z, (total, y, inv), kept) if keep else z
+
+    def gradient(self, tokens, labels, reset, teacher=None, tau=2.0, w_kl=0.5, w_ce=1.0):
+        W, D, N, n, T, p = self.W, self.D, self.S_, tokens.shape[1], reset.shape[1], self.p
+        z, (s, y, inv), kept = self.forward(self.x, tokens, reset, keep=True)
+        ids, t = teacher or (torch.empty((W * n, 0), dtype=torch.int32, device=z.device), torch.empty((W * n, 0), device=z.device))
+        loss, gout = torch.empty(W * n, device=z.device), torch.full((W * n,), 1.0 / n, device=z.device)
+        lm.cx_distill_step(z, ids, t, labels, gout, loss, z, tau, w_kl, w_ce)          # the gradient takes the logits' place
+        dy = torch.empty_like(y)
+        for w in range(W):
+            rows = slice(w * n, (w + 1) * n)
+            torch.mm(z[rows], self.table(self.x, w), out=dy[rows])
+            torch.mm(z[rows].t(), y[rows], out=self.table(self.g, w))
+        dy /= math.sqrt(D)
+        if p:
+            lm.cx_dropout(dy, self.rng[self.blocks + 1], dy, p)
+        ds, dadd = torch.empty_like(dy), torch.empty_like(dy)
+        lm.cx_add_norm_grad(dy, s, inv, self.x, self.norm, None, ds, None, self.g, dx=dadd, p=p, rng=self.rng[self.blocks])
+        for k in range(self.blocks - 1, -1, -1):
+            place, (s, y, inv, into, u, steps, v, states) = self.at[k], kept[k]
+            dv = self.product_grad(place["back"], D, v, dadd)
+            du, dinto, dsteps = torch.empty_like(u), torch.empty_like(into), torch.empty_like(steps)
+            lm.cx_select_scan_grad(u, steps[:, :D], steps[:, D:D + N], steps[:, D + N:], self.x, place["scan"], dv, du, dsteps[:, :D], dsteps[:, D:D + N],
+                                   dsteps[:, D + N:], None, self.g, T, states, z=into[:, D:], dz=dinto[:, D:], reset=reset)
+            du += self.product_grad(place["steps"], D + 2 * N, u, dsteps)
+            lm.cx_short_conv_grad(into[:, :D], du, self.x, place["conv"], dinto[:, :D], None, self.g, T, self.K, reset=reset)
+            dy = self.product_grad(place["into"], 2 * D, y, dinto)
+            lm.cx_add_norm_grad(dy, s, inv, self.x, place["norm"], ds, ds if k else None, None, self.g, dx=dadd, p=p, rng=self.rng[k])
+        lm.cx_embed_grad(dadd, tokens, self.g, self.g, 0, self.V, math.sqrt(D))
+        return loss.view(W, n).mean(1)
+
+    def step(self, *args, **kw):
+        loss = super().step(*args, **kw)
+        self.rng[:, 1] += self.blocks + 2
+        return loss
+
+    def generate(self, w, prompts, steps):
+        x, D, B = self.x[w:w + 1], self.D, prompts.shape[0]
+        inputs = [torch.zeros((B, self.K - 1, D), device=x.device) for _ in self.at]
+        states = [torch.zeros((B, D, self.S_), device=x.device) for _ in self.at]
+        out, tokens = torch.empty((B, steps), dtype=torch.int32, device=x.device), prompts
+        for k in range(steps):
+            n = tokens.shape[1]
+            add, s = torch.empty((B * n, D), device=x.device), None
+            lm.cx_embed_lookup(x, tokens.reshape(1, -1), add, 0, self.V, math.sqrt(D))
+            for place, before, h in zip(self.at, inputs, states):
+                total, y = torch.empty_like(add), torch.empty_like(add)
+                lm.cx_add_norm(add, s, x, place["norm"], total, y, self.EPS)
+                s, add = total, self.block(x, place, y, n, before=before, h=h)[0]
+            y = torch.empty_like(add)
+            lm.cx_add_norm(add, s, x, self.norm, None, y, self.EPS)
+            z = (y.view(B, n, D)[:, -1] / math.sqrt(D)) @ self.table(x, 0).t()
+            ids, top = torch.empty((B, 1), dtype=torch.int32, device=x.device), torch.empty((B, 1), device=x.device)
+            lm.cx_token_scores(z, None, None, None, ids, top)
+            out[:, k] = ids[:, 0]
+            tokens = ids
+        return out
+
+
 def text(W, B, T, V, seed, device="cuda:0"):
     """Packed documents for every worker: arithmetic sequences modulo V whose step is the document's own, one token in ten
     at random.  tokens int32 [W][B * T], labels int32 [W * B * T] (-1 where a document ends), reset uint8 [W * B][T]."""
@@ -161,8 +312,12 @@ def main(argv=None):
     for name, default in (("workers", 8), ("steps", 100), ("vocab", 97), ("width", 64), ("batch", 4), ("length", 128), ("seed", 1)):
         ap.add_argument("--" + name, type=int, default=default)
     ap.add_argument("--no-codistill", action="store_true", help="labels alone")
+    ap.add_argument("--blocks", type=int, default=0, help="residual blocks in the gated recurrence's place")
+    ap.add_argument("--dropout", type=float, default=0.0, help="share of what blocks add that is dropped")
     a = ap.parse_args(argv)
-    model = Replicas(a.workers, a.vocab, a.width, seed=a.seed)
+    if a.dropout and not a.blocks:
+        ap.error("--dropout: of --blocks")
+    model = Blocks(a.workers, a.vocab, a.width, a.blocks, a.dropout, seed=a.seed) if a.blocks else Replicas(a.workers, a.vocab, a.width, seed=a.seed)
     held_out = text(a.workers, a.batch, a.length, a.vocab, 10**6 + a.seed)
     for k in range(a.steps + 1):
         if k % 20 == 0 or k == a.steps:
