@@ -552,6 +552,13 @@ def _gradients(name, g_in, g_out, dtype, W, offset, count, device):
     return None if g_in is None else g_in.data_ptr(), g_out.data_ptr(), ld
 
 
+def _current(name, device):
+    """Last check before the call: kernels run on the current device."""
+    _on_device(name, device)
+    if device != _torch.cuda.current_device():
+        raise ValueError(f"{name}: tensors on cuda:{device}, which is not the current device")
+
+
 def _narrow(name, *sizes):
     if max(sizes) > _INT32 or min(sizes) < -_INT32:
         _too_wide(name)
@@ -567,7 +574,7 @@ def _dropout(name, suffix, x, rng, out, p, residual, stream):
     residual_at = _spread(name, "residual", residual, dtype, N, D, device)
     ldo = _matrix(name, "out", out, dtype, N, D, device)
     rp = _dense(name, "rng", rng, _torch.int64, (2,), device)
-    _on_device(name, device)
+    _current(name, device)
     _call(name, x.data_ptr(), ldx, *residual_at, out.data_ptr(), ldo, N, D, rp, p, cxmix._stream(stream))
 
 
@@ -604,7 +611,7 @@ def _add_norm(name, suffix, x, residual, weights, offset, s, y, eps, inv, q, sca
         q_at = _spread(name, "q", q, q.dtype, rows, D, device)
         sp = _dense(name, "scale", scale, _torch.float32, (rows,), device)
     rp = _rng(name, rng, p, device)
-    _on_device(name, device)
+    _current(name, device)
     _call(name, x.data_ptr(), ldx, *residual_at, weights.data_ptr(), ldw, W, offset, rows // W, D, eps, rp, p, *s_at, *y_at, ip, *q_at, sp,
           cxmix._stream(stream))
 
@@ -639,6 +646,7 @@ def _add_norm_grad(name, suffix, dy, s, inv, weights, offset, ds_in, ds, g_in, g
     in_at, ds_at, dx_at = (_spread(name, arg, t, dtype, rows, D, device) for arg, t in (("ds_in", ds_in), ("ds", ds), ("dx", dx)))
     grads = _gradients(name, g_in, g_out, dtype, W, offset, D, device)
     rp = _rng(name, rng, p, device)
+    _current(name, device)
     work = _scratch(name, workspace, "cx_norm_workspace", (W, rows // W, D), device, stream)
     _call(name, dy.data_ptr(), lddy, s.data_ptr(), lds, ip, weights.data_ptr(), ldw, W, offset, rows // W, D, *in_at, rp, p, *ds_at, *dx_at, *grads,
           *_span(work), cxmix._stream(stream))
@@ -683,7 +691,7 @@ def _short_conv(name, suffix, x, weights, offset, y, T, K, silu, before, after, 
     bp = _optional(name, "before", before, dtype, (B, K - 1, D), device)
     ap = _optional(name, "after", after, dtype, (B, K - 1, D), device)
     rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
-    _on_device(name, device)
+    _current(name, device)
     _call(name, x.data_ptr(), ldx, weights.data_ptr(), ldw, W, offset, y.data_ptr(), ldy, B, T, D, K, int(bool(silu)), rp, bp, ap, cxmix._stream(stream))
 
 
@@ -716,6 +724,7 @@ def _short_conv_grad(name, suffix, x, dy, weights, offset, dx, g_in, g_out, T, K
     grads = _gradients(name, g_in, g_out, dtype, W, offset, D * (K + 1), device)
     bp = _optional(name, "before", before, dtype, (B, K - 1, D), device)
     rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    _current(name, device)
     work = _scratch(name, workspace, "cx_conv_workspace", (W, B, T, D, K), device, stream)
     _call(name, x.data_ptr(), ldx, dy.data_ptr(), lddy, weights.data_ptr(), ldw, W, offset, dx.data_ptr(), lddx, *grads, B, T, D, K, int(bool(silu)), rp, bp,
           *_span(work), cxmix._stream(stream))
@@ -772,6 +781,7 @@ def _select_scan(name, suffix, u, dt, bm, cm, params, offset, y, T, z, h0, h_las
     lp = _optional(name, "h_last", h_last, f32, (B, D, N), device)
     sp = _optional(name, "states", states, f32, (B, -(-T // CX_SCAN_CHUNK), D, N), device)
     rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    _current(name, device)
     work = _scratch(name, workspace, None if T <= 1 else "cx_select_workspace", (B, T, D, N), device, stream)
     _call(name, *head, y.data_ptr(), ldy, B, T, D, N, rp, hp, lp, sp, *_span(work), cxmix._stream(stream))
 
@@ -810,6 +820,7 @@ def _select_scan_grad(name, suffix, u, dt, bm, cm, params, offset, dy, du, ddt, 
     lp = _optional(name, "dh_last", dh_last, f32, (B, D, N), device)
     hp = _optional(name, "dh0", dh0, f32, (B, D, N), device)
     rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    _current(name, device)
     work = _scratch(name, workspace, "cx_select_grad_workspace", (B, T, D, N), device, stream)
     _call(name, *head, *(v for at in outs for v in at), *dz_at, *grads, B, T, D, N, rp, sp, lp, hp, *_span(work), cxmix._stream(stream))
 
