@@ -10,13 +10,13 @@
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kAhead = 4;                               // rows whose loads are in flight
+constexpr int kAhead = 4, kGradAhead = 2;               // rows whose loads are in flight; spans are whole multiples
 constexpr int64_t kMaxSeq = CX_MAX_TOKENS;
 
 template <class E>
 struct ConvArgs {
     using T = typename E::T;
-    const T *x, *dy, *weights, *before;
+    const T *x, *dy, *wlanes, *before;
     T *y, *dx, *after;
     int64_t ldx, ldy, lddy, lddx, ldw;
     const uint8_t *reset;
@@ -27,70 +27,67 @@ struct ConvArgs {
     bool silu;
 };
 
-template <class E, int K>
-__device__ __forceinline__ void load_taps(const ConvArgs<E> &a, int64_t w, int column, int left, float (&tap)[K][8], float (&bias)[8])
+template <class E, int C, int K>
+__device__ __forceinline__ void load_taps(const ConvArgs<E> &a, int64_t w, int column, int left, float (&tap)[K][C], float (&bias)[C])
 {
-    const typename E::T *p = a.weights + w * a.ldw;
-    widen<E>(load_eight<E>(p + static_cast<int64_t>(a.D) * K + column, left), bias);
-    float flat[K][8];                                   // 8 K elements in a row: column j, tap k at j K + k
+    const typename E::T *p = a.wlanes + w * a.ldw;
+    widen<E, C>(load_columns<E, C>(p + static_cast<int64_t>(a.D) * K + column, left), bias);
+    float flat[K][C];                                   // C K elements in a row: column j, tap k at j K + k
 #pragma unroll
-    for (int i = 0; i < K; ++i) widen<E>(load_eight<E>(p + static_cast<int64_t>(column) * K + i * 8, left * K - i * 8), flat[i]);
+    for (int i = 0; i < K; ++i) widen<E, C>(load_columns<E, C>(p + static_cast<int64_t>(column) * K + i * C, left * K - i * C), flat[i]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < C; ++j)
 #pragma unroll
-        for (int k = 0; k < K; ++k) tap[k][j] = flat[(j * K + k) / 8][(j * K + k) % 8];
+        for (int k = 0; k < K; ++k) tap[k][j] = flat[(j * K + k) / C][(j * K + k) % C];
 }
 
-// The inputs before step t in seen[0 .. K - 2], oldest first: of this sequence's earlier rows or of `before`; zeros from before a reset.
-template <class E, int K>
-__device__ __forceinline__ void enter(const ConvArgs<E> &a, int64_t b, int64_t t, int column, int left, float (&seen)[K][8])
+// seen[0 .. K - 2] before a step, the oldest first, its input behind them; a reset clears what is before it.
+template <int C, int K>
+__device__ __forceinline__ void clear(float (&seen)[K][C], int count = K - 1)
+{
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+        for (int j = 0; j < C; ++j)
+            if (k < count) seen[k][j] = 0.0f;
+}
+template <int C, int K>
+__device__ __forceinline__ void shift_out(float (&seen)[K][C])
+{
+#pragma unroll
+    for (int k = 0; k + 1 < K; ++k)
+#pragma unroll
+        for (int j = 0; j < C; ++j) seen[k][j] = seen[k + 1][j];
+}
+
+// The inputs before step t: of this sequence's earlier rows or of `before`; zeros from before a reset.
+template <class E, int C, int K>
+__device__ __forceinline__ void enter(const ConvArgs<E> &a, int64_t b, int64_t t, int column, int left, float (&seen)[K][C])
 {
 #pragma unroll
     for (int k = 0; k < K - 1; ++k) {
         const int64_t s = t - (K - 1) + k;
         if (s >= 0) {
-            if (a.reset && a.reset[b * a.T_ + s] != 0)
-#pragma unroll
-                for (int i = 0; i < k; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) seen[i][j] = 0.0f;
-            widen<E>(load_eight<E>(a.x + (b * a.T_ + s) * a.ldx + column, left), seen[k]);
+            if (a.reset && a.reset[b * a.T_ + s] != 0) clear<C, K>(seen, k);
+            widen<E, C>(load_columns<E, C>(a.x + (b * a.T_ + s) * a.ldx + column, left), seen[k]);
         } else if (a.before) {
-            widen<E>(load_eight<E>(a.before + (b * (K - 1) + (K - 1 + s)) * a.D + column, left), seen[k]);
+            widen<E, C>(load_columns<E, C>(a.before + (b * (K - 1) + (K - 1 + s)) * a.D + column, left), seen[k]);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) seen[k][j] = 0.0f;
+            for (int j = 0; j < C; ++j) seen[k][j] = 0.0f;
         }
     }
 }
 
-template <class E, int K>
-__device__ __forceinline__ void convolve(const float (&seen)[K][8], const float (&tap)[K][8], const float (&bias)[8], float (&z)[8])
+template <int C, int K>
+__device__ __forceinline__ void convolve(const float (&seen)[K][C], const float (&tap)[K][C], const float (&bias)[C], float (&z)[C])
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < C; ++j) {
         z[j] = bias[j];
 #pragma unroll
         for (int k = 0; k < K; ++k) z[j] = __builtin_fmaf(tap[k][j], seen[k][j], z[j]);
     }
-}
-
-// seen[0 .. K - 2] before the step, its input behind them; a reset clears what is before it.
-template <int K>
-__device__ __forceinline__ void clear(float (&seen)[K][8])
-{
-#pragma unroll
-    for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) seen[k][j] = 0.0f;
-}
-template <int K>
-__device__ __forceinline__ void shift_out(float (&seen)[K][8])
-{
-#pragma unroll
-    for (int k = 0; k + 1 < K; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) seen[k][j] = seen[k + 1][j];
 }
 
 struct Place {
@@ -99,7 +96,7 @@ struct Place {
     bool any;
 };
 // Grid: (slabs of columns of groups of spans, sequences in two dimensions).
-template <class E>
+template <class E, int C>
 __device__ __forceinline__ Place place_of(const ConvArgs<E> &a)
 {
     const int lane = threadIdx.x & ((1 << a.shift) - 1), together = blockDim.x >> a.shift;
@@ -109,119 +106,160 @@ __device__ __forceinline__ Place place_of(const ConvArgs<E> &a)
     p.span = static_cast<int64_t>(blockIdx.x / a.slabs) * together + (threadIdx.x >> a.shift);
     p.begin = p.span * a.span;
     p.end = p.begin + a.span < a.T_ ? p.begin + a.span : a.T_;
-    p.column = ((slab << a.shift) + lane) * 8;
+    p.column = ((slab << a.shift) + lane) * C;
     p.any = p.begin < a.T_ && p.column < a.D && p.b < a.B;
     return p;
 }
 
-template <class E, int K>
+template <class E, int C, int K, bool RESETS>
 __global__ __launch_bounds__(kThreads) void conv_kernel(const ConvArgs<E> a)
 {
-    const Place p = place_of(a);
+    const Place p = place_of<E, C>(a);
     if (!p.any) return;
     const int left = a.D - p.column;
-    float tap[K][8], bias[8], seen[K][8];
-    load_taps<E, K>(a, p.b / a.per_worker, p.column, left, tap, bias);
-    enter<E, K>(a, p.b, p.begin, p.column, left, seen);
-    float last[K][8];
-    const bool first = p.begin == 0;
-    if (K > 1 && first && a.after) {                    // `before` is read by the lanes that write `after`, which may be the same
-        enter<E, K>(a, p.b, a.T_, p.column, left, last);
-    }
-    const typename E::T *x = a.x + p.b * a.T_ * a.ldx + p.column;
-    typename E::T *y = a.y + p.b * a.T_ * a.ldy + p.column;
-    for (int64_t t0 = p.begin; t0 < p.end; t0 += kAhead) {
-        Eight<E> ahead[kAhead];
+    float tap[K][C], bias[C], seen[K][C];
+    load_taps<E, C, K>(a, p.b / a.per_worker, p.column, left, tap, bias);
+    enter<E, C, K>(a, p.b, p.begin, p.column, left, seen);
+    if (K > 1 && p.begin == 0 && a.after) {             // by the lanes that have read `before`, which may be the same
+        float last[K][C];
+        enter<E, C, K>(a, p.b, a.T_, p.column, left, last);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            if (t0 + i < p.end) ahead[i] = load_eight<E>(x + (t0 + i) * a.ldx, left);
+        for (int k = 0; k < K - 1; ++k) store_columns<E, C>(a.after + (p.b * (K - 1) + k) * a.D + p.column, left, last[k]);
+    }
+    const int64_t row0 = p.b * a.T_ + p.begin;
+    const typename E::T *x = a.x + row0 * a.ldx + p.column;
+    typename E::T *y = a.y + row0 * a.ldy + p.column;
+    const int steps = static_cast<int>(p.end - p.begin);
+    const auto some = [&](auto whole, int t0) {         // whole: kAhead steps, all columns
+        constexpr bool WHOLE = decltype(whole)::value;
+        const int columns = WHOLE ? C : left;
+        Columns<E, C> ahead[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) ahead[i] = load_columns<E, C>(x + i * a.ldx, WHOLE || t0 + i < steps ? columns : 0);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (t0 + i >= p.end) break;
-            if (a.reset && a.reset[p.b * a.T_ + t0 + i] != 0) clear<K>(seen);
-            widen<E>(ahead[i], seen[K - 1]);
-            float z[8];
-            convolve<E, K>(seen, tap, bias, z);
+            if (!WHOLE && t0 + i >= steps) break;
+            if (RESETS && a.reset[row0 + t0 + i] != 0) clear<C, K>(seen);
+            widen<E, C>(ahead[i], seen[K - 1]);
+            float z[C];
+            convolve<C, K>(seen, tap, bias, z);
             if (a.silu)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) z[j] = finite_below(z[j]) * sigmoid(z[j]);
-            store_eight<E>(y + (t0 + i) * a.ldy, left, z);
-            shift_out<K>(seen);
+                for (int j = 0; j < C; ++j) z[j] = finite_below(z[j]) * sigmoid(z[j]);
+            store_columns<E, C>(y + i * a.ldy, columns, z);
+            shift_out<C, K>(seen);
         }
+        x += kAhead * a.ldx;
+        y += kAhead * a.ldy;
+    };
+    for (int t0 = 0; t0 < steps; t0 += kAhead) {
+        if (t0 + kAhead <= steps && left >= C) some(std::true_type{}, t0);
+        else some(std::false_type{}, t0);
     }
-    if (K > 1 && first && a.after)
-#pragma unroll
-        for (int k = 0; k < K - 1; ++k) store_eight<E>(a.after + (p.b * (K - 1) + k) * a.D + p.column, left, last[k]);
 }
 
-template <class E, int K, bool RESETS>
+// One step, as decoding takes them: everything is loaded before anything is stored, and no step waits for another.
+template <class E, int C, int K>
+__global__ __launch_bounds__(kWave) void conv_step_kernel(const ConvArgs<E> a)
+{
+    const int column = (static_cast<int>(blockIdx.x % a.slabs) * kWave + threadIdx.x) * C, left = a.D - column;
+    const int64_t b = blockIdx.x / a.slabs;
+    if (left <= 0) return;
+    Columns<E, C> inputs[K];
+    const bool fresh = a.reset && a.reset[b] != 0;
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k) inputs[k] = load_columns<E, C>(a.before + (b * (K - 1) + k) * a.D + column, a.before && !fresh ? left : 0);
+    inputs[K - 1] = load_columns<E, C>(a.x + b * a.ldx + column, left);
+    float tap[K][C], bias[C], seen[K][C], z[C];
+    load_taps<E, C, K>(a, b / a.per_worker, column, left, tap, bias);
+#pragma unroll
+    for (int k = 0; k < K; ++k) widen<E, C>(inputs[k], seen[k]);
+    convolve<C, K>(seen, tap, bias, z);
+    if (a.silu)
+#pragma unroll
+        for (int j = 0; j < C; ++j) z[j] = finite_below(z[j]) * sigmoid(z[j]);
+    store_columns<E, C>(a.y + b * a.ldy + column, left, z);
+    if (a.after)
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k) store_columns<E, C>(a.after + (b * (K - 1) + k) * a.D + column, left, seen[k + 1]);
+}
+
+template <class E, int C, int K, bool RESETS>
 __global__ __launch_bounds__(kThreads) void conv_grad_kernel(const ConvArgs<E> a)
 {
-    __shared__ float sums[kThreads][9];
-    const Place p = place_of(a);
+    __shared__ float sums[kThreads][C + 1];
+    const Place p = place_of<E, C>(a);
     const int lane = threadIdx.x & ((1 << a.shift) - 1), group = threadIdx.x >> a.shift, together = blockDim.x >> a.shift;
     const int left = p.any ? a.D - p.column : 0;
-    float dw[K + 1][8] = {};                            // the bias's behind the taps'
+    float dw[K + 1][C] = {};                            // the bias's behind the taps'
     if (p.any) {
-        float tap[K][8], bias[8], seen[K][8];
-        load_taps<E, K>(a, p.b / a.per_worker, p.column, left, tap, bias);
-        enter<E, K>(a, p.b, p.begin, p.column, left, seen);
-        float open[K][8] = {};                          // gradients of the inputs of steps t - K + 1 .. t, oldest first
+        float tap[K][C], bias[C], seen[K][C];
+        load_taps<E, C, K>(a, p.b / a.per_worker, p.column, left, tap, bias);
+        enter<E, C, K>(a, p.b, p.begin, p.column, left, seen);
+        float open[K][C] = {};                          // gradients of the inputs of steps t - K + 1 .. t, oldest first
         int visible = 0;                                // steps behind that step t's taps see and that belong to this span
-        const typename E::T *x = a.x + p.b * a.T_ * a.ldx + p.column, *dy = a.dy + p.b * a.T_ * a.lddy + p.column;
-        typename E::T *dx = a.dx + p.b * a.T_ * a.lddx + p.column;
+        const int64_t row0 = p.b * a.T_ + p.begin;
+        const typename E::T *x = a.x + row0 * a.ldx + p.column, *dy = a.dy + row0 * a.lddy + p.column;
+        typename E::T *dx = a.dx + (row0 - (K - 1)) * a.lddx + p.column;            // of the step that nothing later reaches
         // K - 1 steps more than the span's: what later steps add to its inputs
-        const int64_t stop = p.end + K - 1;
-        for (int64_t t0 = p.begin; t0 < stop; t0 += kAhead) {
-            Eight<E> xs[kAhead], gs[kAhead];
+        const int own = static_cast<int>(p.end - p.begin), stop = own + K - 1;
+        const int there = a.T_ - p.begin < stop ? static_cast<int>(a.T_ - p.begin) : stop;
+        const auto some = [&](auto whole, int t0) {     // whole: kGradAhead steps of the span whose results are all its own, all columns
+            constexpr bool WHOLE = decltype(whole)::value;
+            const int columns = WHOLE ? C : left;
+            Columns<E, C> xs[kGradAhead], gs[kGradAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int there = t0 + i < a.T_ && t0 + i < stop ? left : 0;
-                xs[i] = load_eight<E>(x + (t0 + i) * a.ldx, there);
-                gs[i] = load_eight<E>(dy + (t0 + i) * a.lddy, there);
+            for (int i = 0; i < kGradAhead; ++i) {
+                xs[i] = load_columns<E, C>(x + i * a.ldx, WHOLE || t0 + i < there ? columns : 0);
+                gs[i] = load_columns<E, C>(dy + i * a.lddy, WHOLE || t0 + i < there ? columns : 0);
             }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int64_t t = t0 + i;
-                if (t >= stop) break;
-                const bool there = t < a.T_, own = t < p.end;
-                if (RESETS && there && a.reset[p.b * a.T_ + t] != 0) {
-                    clear<K>(seen);
+            for (int i = 0; i < kGradAhead; ++i) {
+                const int t = t0 + i;
+                if (!WHOLE && t >= stop) break;
+                if (RESETS && (WHOLE || t < there) && a.reset[row0 + t] != 0) {
+                    clear<C, K>(seen);
                     visible = 0;
                 }
-                widen<E>(xs[i], seen[K - 1]);
-                float d[8], z[8];
-                widen<E>(gs[i], d);
+                widen<E, C>(xs[i], seen[K - 1]);
+                float d[C], z[C];
+                widen<E, C>(gs[i], d);
                 if (a.silu) {
-                    convolve<E, K>(seen, tap, bias, z);
+                    convolve<C, K>(seen, tap, bias, z);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
+                    for (int j = 0; j < C; ++j) {
                         z[j] = finite_below(z[j]);
                         d[j] *= silu_slope(z[j], sigmoid(z[j]));
                     }
                 }
-                if (there) {
+                if (WHOLE || t < there) {
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
                         const bool reaches = !RESETS || K - 1 - k <= visible;
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
+                        for (int j = 0; j < C; ++j)
                             if (reaches) open[k][j] = __builtin_fmaf(tap[k][j], d[j], open[k][j]);
                     }
-                    if (own)
+                    if (WHOLE || t < own)
 #pragma unroll
                         for (int k = 0; k <= K; ++k)
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) dw[k][j] = k < K ? __builtin_fmaf(d[j], seen[k < K ? k : 0][j], dw[k][j]) : dw[k][j] + d[j];
+                            for (int j = 0; j < C; ++j) dw[k][j] = k < K ? __builtin_fmaf(d[j], seen[k < K ? k : 0][j], dw[k][j]) : dw[k][j] + d[j];
                 }
-                const int64_t done = t - (K - 1);       // nothing later reaches that step's input
-                if (done >= p.begin) store_eight<E>(dx + done * a.lddx, left, open[0]);
-                shift_out<K>(open);
+                if (WHOLE || t >= K - 1) store_columns<E, C>(dx + i * a.lddx, columns, open[0]);
+                shift_out<C, K>(open);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) open[K - 1][j] = 0.0f;
-                shift_out<K>(seen);
+                for (int j = 0; j < C; ++j) open[K - 1][j] = 0.0f;
+                shift_out<C, K>(seen);
                 visible = visible < K - 1 ? visible + 1 : K - 1;
             }
+            x += kGradAhead * a.ldx;
+            dy += kGradAhead * a.lddy;
+            dx += kGradAhead * a.lddx;
+        };
+        for (int t0 = 0; t0 < stop; t0 += kGradAhead) {
+            if (t0 >= K - 1 && t0 + kGradAhead <= own && left >= C) some(std::true_type{}, t0);
+            else some(std::false_type{}, t0);
         }
     }
     // the sums of the workgroup's spans, of columns [D][K] and then [D]
@@ -231,14 +269,14 @@ __global__ __launch_bounds__(kThreads) void conv_grad_kernel(const ConvArgs<E> a
     for (int k = 0; k <= K; ++k) {
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sums[threadIdx.x][j] = dw[k][j];
+        for (int j = 0; j < C; ++j) sums[threadIdx.x][j] = dw[k][j];
         __syncthreads();
         if (group > 0 || p.b >= a.B) continue;
         for (int g = 1; g < together; ++g)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) dw[k][j] += sums[(g << a.shift) + lane][j];
+            for (int j = 0; j < C; ++j) dw[k][j] += sums[(g << a.shift) + lane][j];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < C; ++j)
             if (p.column + j < a.D) part[k < K ? (p.column + j) * static_cast<int64_t>(K) + k : static_cast<int64_t>(a.D) * K + p.column + j] = dw[k][j];
     }
 }
@@ -258,21 +296,24 @@ struct Walk {
 
 constexpr int64_t kWalks = 1 << 18;                     // lanes that fill the card
 
-Walk walk_of(int64_t B, int64_t T, int32_t D, int64_t least)
+Walk walk_of(int64_t B, int64_t T, int32_t D, int columns, int64_t least)
 {
     Walk w{};
-    const int64_t eights = ceil_div(D, 8);
-    while ((1 << w.shift) < eights && (1 << w.shift) < kWave) ++w.shift;
-    w.slabs = static_cast<int>(ceil_div(eights, 1 << w.shift));
-    w.together = kThreads >> w.shift;
-    const int64_t wanted = ceil_div(kWalks, B * eights);
+    const int64_t lanes = ceil_div(D, columns);
+    while ((1 << w.shift) < lanes && (1 << w.shift) < kWave) ++w.shift;
+    w.slabs = static_cast<int>(ceil_div(lanes, 1 << w.shift));
+    const int64_t wanted = ceil_div(kWalks, B * lanes);
     const int64_t span = ceil_div(T, wanted);
-    w.span = span < least ? (T < least ? T : least) : span;
-    w.groups = ceil_div(ceil_div(T, w.span), w.together);
+    w.span = round_up(span < least ? (T < least ? T : least) : span, kAhead);
+    const int64_t spans = ceil_div(T, w.span);
+    w.together = kThreads >> w.shift;
+    while (w.together > 1 && w.together / 2 >= spans && (w.together / 2) << w.shift >= kWave) w.together /= 2;
+    w.groups = ceil_div(spans, w.together);
     w.spans = w.groups * w.together;
     return w;
 }
 constexpr int64_t kLeastSteps = 8, kLeastGradSteps = 32;
+constexpr int kGradColumns = 4;                         // columns of a lane
 
 int check_conv(int32_t W, int64_t B, int64_t T, int32_t D, int32_t K)
 {
@@ -285,7 +326,7 @@ int check_conv(int32_t W, int64_t B, int64_t T, int32_t D, int32_t K)
 int64_t parts_bytes(int64_t B, int64_t T, int32_t D, int32_t K)
 {
     if (B == 0 || T == 0) return 0;
-    return B * walk_of(B, T, D, kLeastGradSteps).groups * D * (K + 1) * 4;
+    return B * walk_of(B, T, D, kGradColumns, kLeastGradSteps).groups * D * (K + 1) * 4;
 }
 
 template <class E>
@@ -313,7 +354,7 @@ dim3 grid_of(const Walk &w, int64_t B)
 }
 
 template <class E>
-int conv(const typename E::T *x, int64_t ldx, const typename E::T *weights, int64_t ld, int32_t W, int64_t offset, typename E::T *y, int64_t ldy, int64_t B,
+int conv(const typename E::T *x, int64_t ldx, const typename E::T *wlanes, int64_t ld, int32_t W, int64_t offset, typename E::T *y, int64_t ldy, int64_t B,
          int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const typename E::T *before, typename E::T *after, void *stream)
 {
     const int rc = check_conv(W, B, T, D, K);
@@ -329,25 +370,35 @@ int conv(const typename E::T *x, int64_t ldx, const typename E::T *weights, int6
         hipLaunchKernelGGL(keep_kernel<E>, dim3(static_cast<unsigned>(ceil_div(ends, 256))), dim3(256), 0, st, before, after, ends);
         return launched();
     }
-    if (!x || !y || !weights) return CX_ERR_NULL;
+    if (!x || !y || !wlanes) return CX_ERR_NULL;
     if (bad_matrix(B * T, ldx, D) || bad_matrix(B * T, ldy, D)) return CX_ERR_SHAPE;
-    if (misaligned_to(x, kElem) || misaligned_to(weights, kElem) || misaligned_to(y, kElem)) return CX_ERR_ALIGN;
-    const Extent in[4] = {matrix_of(x, B * T, ldx, D, kElem), matrix_of(weights, W, ld, offset + static_cast<int64_t>(D) * (K + 1), kElem), dense_of(reset, B * T),
+    if (misaligned_to(x, kElem) || misaligned_to(wlanes, kElem) || misaligned_to(y, kElem)) return CX_ERR_ALIGN;
+    const Extent in[4] = {matrix_of(x, B * T, ldx, D, kElem), matrix_of(wlanes, W, ld, offset + static_cast<int64_t>(D) * (K + 1), kElem), dense_of(reset, B * T),
                           dense_of(before, ends * kElem)};
     const Extent out[2] = {matrix_of(y, B * T, ldy, D, kElem), dense_of(after, ends * kElem)};
     const Same same[1] = {{1, 3}};
     if (outputs_share_but(in, out, same)) return CX_ERR_ALIAS;
-    const Walk w = walk_of(B, T, D, kLeastSteps);
+    constexpr int kForward = sizeof(typename E::T) == 4 ? 4 : 8;         // 16 bytes
+    const Walk w = walk_of(B, T, D, kForward, kLeastSteps);
     if (w.groups * w.slabs > 0x7fffffff) return CX_ERR_SHAPE;
     ConvArgs<E> a{};
-    a.x = x; a.ldx = ldx; a.weights = weights + offset; a.ldw = ld; a.y = y; a.ldy = ldy; a.before = before; a.after = after; a.reset = reset;
+    a.x = x; a.ldx = ldx; a.wlanes = wlanes + offset; a.ldw = ld; a.y = y; a.ldy = ldy; a.before = before; a.after = after; a.reset = reset;
     a.B = B; a.T_ = T; a.per_worker = B / W; a.D = D; a.silu = silu != 0;
     set_walk(a, w);
-    return by_taps(K, [&](auto k) { hipLaunchKernelGGL((conv_kernel<E, decltype(k)::value>), grid_of(w, B), dim3(kThreads), 0, st, a); });
+    if (T == 1) {
+        a.slabs = static_cast<int32_t>(ceil_div(ceil_div(D, kForward), kWave));
+        return by_taps(K, [&](auto k) {
+            hipLaunchKernelGGL((conv_step_kernel<E, kForward, decltype(k)::value>), dim3(static_cast<unsigned>(B * a.slabs)), dim3(kWave), 0, st, a);
+        });
+    }
+    return by_taps(K, [&](auto k) {
+        if (reset) hipLaunchKernelGGL((conv_kernel<E, kForward, decltype(k)::value, true>), grid_of(w, B), dim3(w.together << w.shift), 0, st, a);
+        else hipLaunchKernelGGL((conv_kernel<E, kForward, decltype(k)::value, false>), grid_of(w, B), dim3(w.together << w.shift), 0, st, a);
+    });
 }
 
 template <class E>
-int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int64_t lddy, const typename E::T *weights, int64_t ldw, int32_t W,
+int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int64_t lddy, const typename E::T *wlanes, int64_t ldw, int32_t W,
               int64_t offset, typename E::T *dx, int64_t lddx, const typename E::T *g_in, typename E::T *g_out, int64_t ld, int64_t B, int64_t T,
               int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const typename E::T *before, void *workspace, int64_t workspace_bytes, void *stream)
 {
@@ -359,12 +410,12 @@ int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int6
     const bool none = B == 0 || T == 0;
     const int64_t ends = B * (K - 1) * D, bytes = parts_bytes(B, T, D, K);
     if (!none) {
-        if (!x || !dy || !weights || !dx || !workspace) return CX_ERR_NULL;
+        if (!x || !dy || !wlanes || !dx || !workspace) return CX_ERR_NULL;
         if (bad_matrix(B * T, ldx, D) || bad_matrix(B * T, lddy, D) || bad_matrix(B * T, lddx, D) || workspace_bytes < bytes) return CX_ERR_SHAPE;
     }
-    if (misaligned_to(x, kElem) || misaligned_to(dy, kElem) || misaligned_to(weights, kElem) || misaligned_to(dx, kElem) || misaligned_to(g_in, kElem) ||
+    if (misaligned_to(x, kElem) || misaligned_to(dy, kElem) || misaligned_to(wlanes, kElem) || misaligned_to(dx, kElem) || misaligned_to(g_in, kElem) ||
         misaligned_to(g_out, kElem) || misaligned_to(before, kElem) || misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const Extent in[6] = {matrix_of(x, B * T, ldx, D, kElem), matrix_of(dy, B * T, lddy, D, kElem), matrix_of(weights, W, ldw, offset + columns, kElem),
+    const Extent in[6] = {matrix_of(x, B * T, ldx, D, kElem), matrix_of(dy, B * T, lddy, D, kElem), matrix_of(wlanes, W, ldw, offset + columns, kElem),
                           dense_of(reset, B * T), dense_of(before, ends * kElem), matrix_of(g_in, W, ld, offset + columns, kElem)};
     const Extent out[3] = {matrix_of(dx, B * T, lddx, D, kElem), matrix_of(g_out, W, ld, offset + columns, kElem), dense_of(workspace, bytes)};
     const Same same[1] = {{1, 5}};
@@ -373,15 +424,15 @@ int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int6
     float *parts = static_cast<float *>(workspace);
     int64_t count = 0;
     if (!none) {
-        const Walk w = walk_of(B, T, D, kLeastGradSteps);
+        const Walk w = walk_of(B, T, D, kGradColumns, kLeastGradSteps);
         if (w.groups * w.slabs > 0x7fffffff) return CX_ERR_SHAPE;
         ConvArgs<E> a{};
-        a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.weights = weights + offset; a.ldw = ldw; a.dx = dx; a.lddx = lddx; a.before = before;
+        a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.wlanes = wlanes + offset; a.ldw = ldw; a.dx = dx; a.lddx = lddx; a.before = before;
         a.reset = reset; a.parts = parts; a.B = B; a.T_ = T; a.per_worker = B / W; a.D = D; a.silu = silu != 0;
         set_walk(a, w);
         const int rc2 = by_taps(K, [&](auto k) {
-            if (reset) hipLaunchKernelGGL((conv_grad_kernel<E, decltype(k)::value, true>), grid_of(w, B), dim3(kThreads), 0, st, a);
-            else hipLaunchKernelGGL((conv_grad_kernel<E, decltype(k)::value, false>), grid_of(w, B), dim3(kThreads), 0, st, a);
+            if (reset) hipLaunchKernelGGL((conv_grad_kernel<E, kGradColumns, decltype(k)::value, true>), grid_of(w, B), dim3(w.together << w.shift), 0, st, a);
+            else hipLaunchKernelGGL((conv_grad_kernel<E, kGradColumns, decltype(k)::value, false>), grid_of(w, B), dim3(w.together << w.shift), 0, st, a);
         });
         if (rc2 != CX_OK) return rc2;
         count = B / W * w.groups;
@@ -395,18 +446,18 @@ int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int6
 extern "C" {
 
 #define CX_LM_CONV(SUFFIX, E)                                                                                                         \
-    int cx_short_conv##SUFFIX(const E::T *x, int64_t ldx, const E::T *weights, int64_t ldw, int32_t W, int64_t offset, E::T *y,       \
+    int cx_short_conv##SUFFIX(const E::T *x, int64_t ldx, const E::T *wlanes, int64_t ldw, int32_t W, int64_t offset, E::T *y,       \
                               int64_t ldy, int64_t B, int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset,            \
                               const E::T *before, E::T *after, void *stream)                                                          \
     {                                                                                                                                 \
-        return conv<E>(x, ldx, weights, ldw, W, offset, y, ldy, B, T, D, K, silu, reset, before, after, stream);                      \
+        return conv<E>(x, ldx, wlanes, ldw, W, offset, y, ldy, B, T, D, K, silu, reset, before, after, stream);                      \
     }                                                                                                                                 \
-    int cx_short_conv_grad##SUFFIX(const E::T *x, int64_t ldx, const E::T *dy, int64_t lddy, const E::T *weights, int64_t ldw,        \
+    int cx_short_conv_grad##SUFFIX(const E::T *x, int64_t ldx, const E::T *dy, int64_t lddy, const E::T *wlanes, int64_t ldw,        \
                                    int32_t W, int64_t offset, E::T *dx, int64_t lddx, const E::T *g_in, E::T *g_out, int64_t ldg,     \
                                    int64_t B, int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset,                    \
                                    const E::T *before, void *workspace, int64_t workspace_bytes, void *stream)                        \
     {                                                                                                                                 \
-        return conv_grad<E>(x, ldx, dy, lddy, weights, ldw, W, offset, dx, lddx, g_in, g_out, ldg, B, T, D, K, silu, reset, before,   \
+        return conv_grad<E>(x, ldx, dy, lddy, wlanes, ldw, W, offset, dx, lddx, g_in, g_out, ldg, B, T, D, K, silu, reset, before,   \
                             workspace, workspace_bytes, stream);                                                                      \
     }
 CX_LM_CONV(, F32)

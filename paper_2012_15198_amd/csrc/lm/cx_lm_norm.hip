@@ -36,7 +36,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const DropArgs<E> a)
     const int64_t row0 = first / a.eights;
     const uint32_t at0 = static_cast<uint32_t>(first - row0 * a.eights) + threadIdx.x;
     const uint64_t key = a.d.rng[0], draw = a.d.rng[1];
-    Eight<E> x[kDropEach], r[kDropEach];
+    Columns<E, 8> x[kDropEach], r[kDropEach];
     int64_t row[kDropEach];
     int column[kDropEach];
 #pragma unroll
@@ -48,23 +48,23 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const DropArgs<E> a)
         row[k] = row0 + q;
         column[k] = static_cast<int>(at - q * a.eights) * 8;
         if (row[k] < a.rows) {
-            x[k] = load_eight<E, true>(a.x + row[k] * a.ldx + column[k], a.D - column[k]);
-            if (a.residual) r[k] = load_eight<E, true>(a.residual + row[k] * a.ldr + column[k], a.D - column[k]);
+            x[k] = load_columns<E, 8, true>(a.x + row[k] * a.ldx + column[k], a.D - column[k]);
+            if (a.residual) r[k] = load_columns<E, 8, true>(a.residual + row[k] * a.ldr + column[k], a.D - column[k]);
         }
     }
 #pragma unroll
     for (int k = 0; k < kDropEach; ++k) {
         if (row[k] >= a.rows) continue;
         float v[8];
-        widen<E>(x[k], v);
+        widen<E, 8>(x[k], v);
         if (a.d.border) drop(random_block(key, draw, static_cast<uint64_t>(row[k]) * a.eights + column[k] / 8), a.d.border, a.d.scale, v);
         if (a.residual) {
             float f[8];
-            widen<E>(r[k], f);
+            widen<E, 8>(r[k], f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = f[j] + v[j];
         }
-        store_eight<E>(a.out + row[k] * a.ldo + column[k], a.D - column[k], v);
+        store_columns<E, 8>(a.out + row[k] * a.ldo + column[k], a.D - column[k], v);
     }
 }
 
@@ -150,19 +150,19 @@ __global__ __launch_bounds__(kMaxLanes) void norm_kernel(const NormArgs<E> a)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int column = (v * lanes + lane) * 8, left = here ? a.D - column : 0;
-        const Eight<E> xs = load_eight<E, true>(a.x + row * a.ldx + column, left);
-        Eight<E> rs;
-        if (a.residual) rs = load_eight<E, true>(a.residual + row * a.ldr + column, left);
-        widen<E>(xs, s[v]);
+        const Columns<E, 8> xs = load_columns<E, 8, true>(a.x + row * a.ldx + column, left);
+        Columns<E, 8> rs;
+        if (a.residual) rs = load_columns<E, 8, true>(a.residual + row * a.ldr + column, left);
+        widen<E, 8>(xs, s[v]);
         if constexpr (DROP)
             if (left > 0) drop(random_block(a.d.rng[0], a.d.rng[1], static_cast<uint64_t>(row) * a.eights + column / 8), a.d.border, a.d.scale, s[v]);
         if (a.residual) {
             float f[8];
-            widen<E>(rs, f);
+            widen<E, 8>(rs, f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[v][j] = f[j] + s[v][j];
         }
-        if (a.s && left > 0) store_eight<E>(a.s + row * a.lds + column, left, s[v]);
+        if (a.s && left > 0) store_columns<E, 8>(a.s + row * a.lds + column, left, s[v]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) squares = __builtin_fmaf(s[v][j], s[v][j], squares);
     }
@@ -174,14 +174,14 @@ __global__ __launch_bounds__(kMaxLanes) void norm_kernel(const NormArgs<E> a)
     for (int v = 0; v < V; ++v) {
         const int column = (v * lanes + lane) * 8, left = here ? a.D - column : 0;
         float f[8];
-        widen<E>(load_eight<E>(a.weights + w * a.ldw + column, left), f);
+        widen<E, 8>(load_columns<E, 8>(a.weights + w * a.ldw + column, left), f);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             s[v][j] = s[v][j] * inv * f[j];
             const unsigned u = __float_as_uint(s[v][j]) & 0x7fffffffu;        // ordered like the magnitudes, NaN above infinity
             if (j < left) high = u > high ? u : high;
         }
-        if (a.y && left > 0) store_eight<E>(a.y + row * a.ldy + column, left, s[v]);
+        if (a.y && left > 0) store_columns<E, 8>(a.y + row * a.ldy + column, left, s[v]);
     }
     if (!a.q) return;
     const float most = __uint_as_float(row_max(high, a.shift, lds, 1)), whole = most / kLargest8;
@@ -225,17 +225,17 @@ __global__ __launch_bounds__(kMaxLanes) void norm_grad_kernel(const NormArgs<E> 
         const int64_t row = w * a.N + (here ? r0 + group : begin);
         const float inv = a.inv_in[row];
         float unit[V][8], g[V][8];
-        Eight<E> more[V];
+        Columns<E, 8> more[V];
         float dot = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int column = (v * lanes + lane) * 8, left = here ? a.D - column : 0;
-            const Eight<E> ss = load_eight<E, true>(a.s_in + row * a.lds + column, left), ds = load_eight<E, true>(a.dy + row * a.lddy + column, left);
-            if (a.ds_in) more[v] = load_eight<E, true>(a.ds_in + row * a.ldi + column, left);
+            const Columns<E, 8> ss = load_columns<E, 8, true>(a.s_in + row * a.lds + column, left), ds = load_columns<E, 8, true>(a.dy + row * a.lddy + column, left);
+            if (a.ds_in) more[v] = load_columns<E, 8, true>(a.ds_in + row * a.ldi + column, left);
             float f[8];
-            widen<E>(ss, unit[v]);
-            widen<E>(ds, g[v]);
-            widen<E>(load_eight<E>(a.weights + w * a.ldw + column, left), f);
+            widen<E, 8>(ss, unit[v]);
+            widen<E, 8>(ds, g[v]);
+            widen<E, 8>(load_columns<E, 8>(a.weights + w * a.ldw + column, left), f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 unit[v][j] *= inv;
@@ -252,16 +252,16 @@ __global__ __launch_bounds__(kMaxLanes) void norm_grad_kernel(const NormArgs<E> 
             const int column = (v * lanes + lane) * 8, left = here ? a.D - column : 0;
             if (left <= 0) continue;
             float f[8];
-            if (a.ds_in) widen<E>(more[v], f);
+            if (a.ds_in) widen<E, 8>(more[v], f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float own = __builtin_fmaf(-unit[v][j], mean, g[v][j]);
                 g[v][j] = a.ds_in ? __builtin_fmaf(inv, own, f[j]) : inv * own;
             }
-            if (a.ds) store_eight<E>(a.ds + row * a.ldds + column, left, g[v]);
+            if (a.ds) store_columns<E, 8>(a.ds + row * a.ldds + column, left, g[v]);
             if (a.dx) {
                 if constexpr (DROP) drop(random_block(a.d.rng[0], a.d.rng[1], static_cast<uint64_t>(row) * a.eights + column / 8), a.d.border, a.d.scale, g[v]);
-                store_eight<E>(a.dx + row * a.lddx + column, left, g[v]);
+                store_columns<E, 8>(a.dx + row * a.lddx + column, left, g[v]);
             }
         }
     }

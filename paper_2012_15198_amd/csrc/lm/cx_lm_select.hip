@@ -53,17 +53,17 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
     const int bs = threadIdx.x / kMaxStates, bn = threadIdx.x % kMaxStates;          // a thread's element of B and of C
     const uint32_t b_at = place_in<T>(a.ldb, bs, bn), c_at = place_in<T>(a.ldc, bs, bn), state_at = (c * a.N) * 4;
     const auto steps_from = [&](int64_t t0) { return end - t0 >= kTile ? kTile : end > t0 ? static_cast<int>(end - t0) : 0; };
-    Four<E> u, dt, z{};
+    Columns<E, 4> u, dt, z{};
     T b_next, c_next;
     const auto load = [&](int64_t t0) {
         const int64_t row = row0 + t0;
         const int steps = steps_from(t0), there = es < steps ? left : 0;
         const bool has = bn < a.N && bs < steps;
-        u = load_four<E>(at_byte(a.u + row * a.ldu + column0, u_at), there);
-        dt = load_four<E>(at_byte(a.dt + row * a.lddt + column0, dt_at), there);
+        u = load_columns<E, 4>(at_byte(a.u + row * a.ldu + column0, u_at), there);
+        dt = load_columns<E, 4>(at_byte(a.dt + row * a.lddt + column0, dt_at), there);
         b_next = has ? *at_byte(a.bm + row * a.ldb, b_at) : 0;
         if constexpr (!MAPS) {
-            if (a.z) z = load_four<E>(at_byte(a.z + row * a.ldz + column0, z_at), there);
+            if (a.z) z = load_columns<E, 4>(at_byte(a.z + row * a.ldz + column0, z_at), there);
             c_next = has ? *at_byte(a.cm + row * a.ldc, c_at) : 0;
         }
     };
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
         const bool there = es < steps_from(t0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float uj = value_of<E>(u, j), zj = finite_below(value_of<E>(z, j)), soft = softplus(value_of<E>(dt, j) + bias[j]);
+            const float uj = value_of<E, 4>(u, j), zj = finite_below(value_of<E, 4>(z, j)), soft = softplus(value_of<E, 4>(dt, j) + bias[j]);
             const float delta = there ? soft : 0.0f;                    // behind the end: a step that changes nothing
             step[turn][es][ec + j] = float2{delta, delta * uj};
             if constexpr (!MAPS) {
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
                 gate[j] = next_gate[j];
                 direct[j] = next_direct[j];
             }
-            if (es < steps) store_four<E>(at_byte(a.y + (row0 + t0) * a.ldy + column0, y_at), left, v);
+            if (es < steps) store_columns<E, 4>(at_byte(a.y + (row0 + t0) * a.ldy + column0, y_at), left, v);
         }
     };
     if (begin < end) {

@@ -125,19 +125,19 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
     const uint32_t u_at = place_in<T>(a.ldu, es, ec), dt_at = place_in<T>(a.lddt, es, ec), z_at = place_in<T>(a.ldz, es, ec), dy_at = place_in<T>(a.lddy, es, ec);
     const int bs = threadIdx.x / kMaxStates, bn = threadIdx.x % kMaxStates;          // a thread's element of B and of C
     const uint32_t b_at = place_in<T>(a.ldb, bs, bn), c_at = place_in<T>(a.ldc, bs, bn), state_at = (c * a.N) * 4;
-    Four<E> u, dt, z{}, dy;
+    Columns<E, 4> u, dt, z{}, dy;
     T b_next, c_next;
     float entering[NQ];
     const auto load = [&](int64_t t0) {
         const int64_t row = row0 + t0;
         const int steps = end - t0 < kTile ? static_cast<int>(end - t0) : kTile, there = es < steps ? left : 0;
         const bool has = bn < a.N && bs < steps;
-        dt = load_four<E>(at_byte(a.dt + row * a.lddt + column0, dt_at), there);
-        dy = load_four<E>(at_byte(a.dy + row * a.lddy + column0, dy_at), there);
-        if (a.z) z = load_four<E>(at_byte(a.z + row * a.ldz + column0, z_at), there);
+        dt = load_columns<E, 4>(at_byte(a.dt + row * a.lddt + column0, dt_at), there);
+        dy = load_columns<E, 4>(at_byte(a.dy + row * a.lddy + column0, dy_at), there);
+        if (a.z) z = load_columns<E, 4>(at_byte(a.z + row * a.ldz + column0, z_at), there);
         c_next = has ? *at_byte(a.cm + row * a.ldc, c_at) : 0;
         if constexpr (!MAPS) {
-            u = load_four<E>(at_byte(a.u + row * a.ldu + column0, u_at), there);
+            u = load_columns<E, 4>(at_byte(a.u + row * a.ldu + column0, u_at), there);
             b_next = has ? *at_byte(a.bm + row * a.ldb, b_at) : 0;
             load_states<NQ>(at_byte(a.states_in + (b * chunks + t0 / kTile) * of + static_cast<int64_t>(column0) * a.N, state_at), n0, a.N, any, entering);
         }
@@ -150,13 +150,13 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         const bool there = es < steps;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float v = value_of<E>(dt, j) + bias[j], zj = finite_below(value_of<E>(z, j)), e = sigmoid(zj), dyj = value_of<E>(dy, j);
+            const float v = value_of<E, 4>(dt, j) + bias[j], zj = finite_below(value_of<E, 4>(z, j)), e = sigmoid(zj), dyj = value_of<E, 4>(dy, j);
             const float delta = there ? softplus(v) : 0.0f;             // behind the end: a step that changes nothing
             pull[es][ec + j] = a.z ? dyj * (zj * e) : dyj;
             if constexpr (MAPS) {
                 step[es][ec + j] = float2{delta, 0.0f};
             } else {
-                const float uj = value_of<E>(u, j);
+                const float uj = value_of<E, 4>(u, j);
                 step[es][ec + j] = float2{delta, delta * uj};
                 parked[0][es][ec + j] = uj;
                 parked[1][es][ec + j] = sigmoid(v);
@@ -249,9 +249,9 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
             }
             const int64_t row = row0 + t0;
             if (there) {
-                store_four<E>(at_byte(a.du + row * a.lddu + column0, place_in<T>(a.lddu, es, ec)), left, du);
-                store_four<E>(at_byte(a.ddt + row * a.ldddt + column0, place_in<T>(a.ldddt, es, ec)), left, ddt);
-                if (a.dz) store_four<E>(at_byte(a.dz + row * a.lddz + column0, place_in<T>(a.lddz, es, ec)), left, dz);
+                store_columns<E, 4>(at_byte(a.du + row * a.lddu + column0, place_in<T>(a.lddu, es, ec)), left, du);
+                store_columns<E, 4>(at_byte(a.ddt + row * a.ldddt + column0, place_in<T>(a.ldddt, es, ec)), left, ddt);
+                if (a.dz) store_columns<E, 4>(at_byte(a.dz + row * a.lddz + column0, place_in<T>(a.lddz, es, ec)), left, dz);
             }
             if (bn < a.N && bs < steps) {
                 float *share = at_byte(a.shared_parts + (slab * a.B * a.T_ + row) * 2 * a.N, (bs * 2 * a.N + bn) * 4);

@@ -1,4 +1,4 @@
-// What the operators of a residual block share (internal header): eight columns of a row at a time, random bits of a counter,
+// What the operators of a residual block share (internal header): a few columns of a row at a time, random bits of a counter,
 // and sums of a worker's parameter gradients over the parts that workgroups leave.
 #ifndef CX_LM_BLOCK_HPP
 #define CX_LM_BLOCK_HPP
@@ -9,59 +9,76 @@
 namespace {
 
 // ---------------------------------------------------------------------------------
-// Eight columns of a row: 16 bytes of a 16-bit type, two times 16 bytes of float32.
+// C = 4 or 8 columns of a row as they lie in memory, widened where they are used: what is loaded ahead is then not waited for.
 // ---------------------------------------------------------------------------------
-template <class E>
-struct Eight {
-    static constexpr int kWords = sizeof(typename E::T) / 2;
-    u4 w[kWords];
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+typedef u2 u2_at2 __attribute__((aligned(2)));
+
+template <class E, int C>
+struct Columns {
+    static constexpr int kWords = C * sizeof(typename E::T) / 4;
+    unsigned w[kWords];
 };
 
-// `left`: columns from p to the row's end; those behind it are zeros.
-template <class E, bool LAST = false>
-__device__ __forceinline__ Eight<E> load_eight(const typename E::T *p, int left)
+// `left`: columns from p to the row's end; those behind it are zeros.  LAST: nothing of the call reads it again.
+template <class E, int C, bool LAST = false>
+__device__ __forceinline__ Columns<E, C> load_columns(const typename E::T *p, int left)
 {
-    Eight<E> r;
-    if (left >= 8) {
+    constexpr int kWords = Columns<E, C>::kWords;
+    Columns<E, C> r;
+    if (left >= C) {
+        if constexpr (kWords == 2) {
+            const u2 v = LAST ? __builtin_nontemporal_load(reinterpret_cast<const u2_at2 *>(p)) : *reinterpret_cast<const u2_at2 *>(p);
+            r.w[0] = v[0];
+            r.w[1] = v[1];
+        } else {
 #pragma unroll
-        for (int k = 0; k < Eight<E>::kWords; ++k) r.w[k] = LAST ? load16_last<E>(p + k * E::kPer16) : load16<E>(p + k * E::kPer16);
+            for (int k = 0; k < kWords / 4; ++k) {
+                const u4 v = LAST ? load16_last<E>(p + k * E::kPer16) : load16<E>(p + k * E::kPer16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r.w[4 * k + j] = v[j];
+            }
+        }
     } else {
 #pragma unroll
-        for (int k = 0; k < Eight<E>::kWords; ++k) r.w[k] = u4{};
+        for (int j = 0; j < kWords; ++j) r.w[j] = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < C; ++j)
             if (j < left) {
-                if constexpr (sizeof(typename E::T) == 4) r.w[j / 4][j % 4] = __float_as_uint(p[j]);
-                else r.w[0][j / 2] |= static_cast<unsigned>(p[j]) << (16 * (j & 1));
+                if constexpr (sizeof(typename E::T) == 4) r.w[j] = __float_as_uint(p[j]);
+                else r.w[j / 2] |= static_cast<unsigned>(p[j]) << (16 * (j & 1));
             }
     }
     return r;
 }
-
-template <class E>
-__device__ __forceinline__ void widen(const Eight<E> &r, float (&v)[8])
+template <class E, int C>
+__device__ __forceinline__ float value_of(const Columns<E, C> &r, int j)
 {
-    if constexpr (sizeof(typename E::T) == 4) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r.w[j / 4][j % 4]);
-    } else {
-        E::unpack(r.w[0], v);
-    }
+    if constexpr (sizeof(typename E::T) == 4) return __uint_as_float(r.w[j]);
+    else return (j & 1) ? E::high(r.w[j / 2]) : E::low(r.w[j / 2]);
 }
-
-template <class E>
-__device__ __forceinline__ void store_eight(typename E::T *p, int left, const float (&v)[8])
+template <class E, int C>
+__device__ __forceinline__ void widen(const Columns<E, C> &r, float (&v)[C])
 {
-    if (left >= 8) {
+#pragma unroll
+    for (int j = 0; j < C; ++j) v[j] = value_of<E, C>(r, j);
+}
+template <class E, int C>
+__device__ __forceinline__ void store_columns(typename E::T *p, int left, const float (&v)[C])
+{
+    if (left >= C) {
         if constexpr (sizeof(typename E::T) == 4) {
-            store16<E>(p, u4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-            store16<E>(p + 4, u4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+#pragma unroll
+            for (int k = 0; k < C / 4; ++k)
+                store16<E>(p + 4 * k, u4{__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3])});
+        } else if constexpr (C == 4) {
+            *reinterpret_cast<u2_at2 *>(p) = u2{E::two(v[0], v[1]), E::two(v[2], v[3])};
         } else {
             store16<E>(p, E::pack(v));
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < C; ++j)
             if (j < left) p[j] = E::narrow(v[j]);
     }
 }

@@ -54,47 +54,6 @@ struct SelectArgs {
     int64_t span_steps, piece_steps;                    // multiples of kTile
 };
 
-// Four columns of a row as they lie in memory, widened where they are used: what is loaded ahead is then not waited for.
-template <class E>
-struct Four {
-    unsigned w[sizeof(typename E::T)];
-};
-// `left`: columns from p to the row's end, zeros behind them.
-template <class E>
-__device__ __forceinline__ Four<E> load_four(const typename E::T *p, int left)
-{
-    Four<E> r;
-    constexpr int kWords = sizeof(typename E::T);
-    if (left >= 4) {
-        if constexpr (kWords == 4) {
-            const u4 w = load16<E>(p);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) r.w[j] = w[j];
-        } else {
-            typedef unsigned u2 __attribute__((ext_vector_type(2)));
-            typedef u2 u2_at2 __attribute__((aligned(2)));
-            const u2 w = *reinterpret_cast<const u2_at2 *>(p);
-            r.w[0] = w[0];
-            r.w[1] = w[1];
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < kWords; ++j) r.w[j] = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < left) {
-                if constexpr (kWords == 4) r.w[j] = __float_as_uint(p[j]);
-                else r.w[j / 2] |= static_cast<unsigned>(p[j]) << (16 * (j & 1));
-            }
-    }
-    return r;
-}
-template <class E>
-__device__ __forceinline__ float value_of(const Four<E> &r, int j)
-{
-    if constexpr (sizeof(typename E::T) == 4) return __uint_as_float(r.w[j]);
-    else return (j & 1) ? E::high(r.w[j / 2]) : E::low(r.w[j / 2]);
-}
 // Rows of a tile have uniform addresses, threads a place in them: 32 bits of bytes, which rows of at most kMaxPitch elements leave room for.
 constexpr int64_t kMaxPitch = int64_t(1) << 24;
 template <class T>
@@ -108,29 +67,7 @@ __device__ __forceinline__ uint32_t place_in(int64_t ld, int step, int column) {
 [[maybe_unused]] bool bad_strip(int64_t rows, int64_t ld, int64_t columns) { return bad_matrix(rows, ld, columns) || ld > kMaxPitch; }
 
 template <class E>
-__device__ __forceinline__ void load_four(const typename E::T *p, int left, float (&v)[4])
-{
-    const Four<E> r = load_four<E>(p, left);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = value_of<E>(r, j);
-}
-template <class E>
-__device__ __forceinline__ void store_four(typename E::T *p, int left, const float (&v)[4])
-{
-    if (left >= 4) {
-        if constexpr (sizeof(typename E::T) == 4) {
-            store16<E>(p, u4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-        } else {
-            typedef unsigned u2 __attribute__((ext_vector_type(2)));
-            typedef u2 u2_at2 __attribute__((aligned(2)));
-            *reinterpret_cast<u2_at2 *>(p) = u2{E::two(v[0], v[1]), E::two(v[2], v[3])};
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (j < left) p[j] = E::narrow(v[j]);
-}
+__device__ __forceinline__ void load_four(const typename E::T *p, int left, float (&v)[4]) { widen<E, 4>(load_columns<E, 4>(p, left), v); }
 
 // Lane 16 q + c of a wavefront has quarter q of the states of its column c.  Sums over quarters cross its four rows of 16 lanes.
 __device__ __forceinline__ float add32(float x, float y)               // rows 0 and 1: x of both halves of the wavefront; rows 2 and 3: y
