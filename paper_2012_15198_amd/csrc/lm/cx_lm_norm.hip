@@ -6,6 +6,10 @@
 //
 // A row stays in the registers of a group of lanes between its statistics and its results, so that each matrix is read and
 // written once.  A lane holds up to four times eight columns; groups are a power of two of lanes.
+//
+// Bound by memory: 65,536 rows of 768 in bfloat16 take 81 us with dropout (4.9 TB/s), their gradient 107 and 5 for the sums of its parts (4.7 TB/s), dropout
+// alone 48 (6.3 TB/s); 8,192 rows of 2,048 to 8 bits 25 (4.7 TB/s).  Tried for the gradient and not kept: the next row's loads ahead (103 to 133), rows
+// widened twice to that end (spills), results past the caches (110).
 #include "lm_block.hpp"
 
 namespace {
@@ -114,8 +118,8 @@ struct NormArgs {
 // A row's sum over its lanes, in every lane.  `turn`: two buffers, so that one barrier does.
 __device__ __forceinline__ float row_sum(float v, int shift, float (&lds)[2][kMaxLanes / kWave], int turn)
 {
-    if (shift <= 6) return sum_lanes(v, 1 << shift);
-    v = sum_lanes(v, kWave);
+    v = sum_lanes(v, shift < 6 ? shift : 6);
+    if (shift <= 6) return v;
     const int wave = threadIdx.x / kWave, waves = 1 << (shift - 6), first = wave & ~(waves - 1);
     if ((threadIdx.x & (kWave - 1)) == 0) lds[turn][wave] = v;
     __syncthreads();
@@ -125,8 +129,8 @@ __device__ __forceinline__ float row_sum(float v, int shift, float (&lds)[2][kMa
 }
 __device__ __forceinline__ unsigned row_max(unsigned v, int shift, float (&lds)[2][kMaxLanes / kWave], int turn)
 {
-    if (shift <= 6) return max_lanes(v, 1 << shift);
-    v = max_lanes(v, kWave);
+    v = max_lanes(v, shift < 6 ? shift : 6);
+    if (shift <= 6) return v;
     const int wave = threadIdx.x / kWave, waves = 1 << (shift - 6), first = wave & ~(waves - 1);
     if ((threadIdx.x & (kWave - 1)) == 0) lds[turn][wave] = __uint_as_float(v);
     __syncthreads();
@@ -289,15 +293,17 @@ struct Layout {
     int shift, eights, threads;                         // lanes of a row as a power of two, eights of a lane
 };
 
-// The fewest idle places: lanes are a power of two, eights 1 to 4.
-Layout layout_of(int32_t D)
+// The forward pass gives a lane one eight of columns where a row has no more than 4,096: 32 rows of 1,024 take 3.4 us in bfloat16 against 4.9 with four
+// of 32 lanes, 4,000 float32 rows of 515 10.0 against 11.7, 65,536 rows of 768 83 against 81.  The gradient keeps sums of its columns over rows and takes
+// the fewest idle places: the last takes 107 us with three eights of 32 lanes, 120 with one of 128, the second 15.5 and 14.3.
+Layout layout_of(int32_t D, bool gradient)
 {
     const int n = static_cast<int>(ceil_div(D, 8));
     Layout best{};
     int least = 1 << 30;
     for (int shift = 1; (1 << shift) <= kMaxLanes; ++shift) {
         const int each = static_cast<int>(ceil_div(n, 1 << shift));
-        if (each > kMaxEights) continue;
+        if (each > (!gradient && n <= kMaxLanes ? 1 : kMaxEights)) continue;
         if ((each << shift) < least) {
             least = each << shift;
             best = {shift, each, (1 << shift) > kThreads ? 1 << shift : kThreads};
@@ -310,7 +316,7 @@ constexpr int64_t kParts = 1024;                        // workgroups of a gradi
 
 int64_t parts_of(int32_t W, int64_t N, int32_t D)
 {
-    const Layout l = layout_of(D);
+    const Layout l = layout_of(D, true);
     const int64_t groups = l.threads >> l.shift, most = ceil_div(N, groups), wanted = ceil_div(kParts, W);
     const int64_t rows = ceil_div(ceil_div(N, wanted < most ? wanted : most), groups) * groups;
     return ceil_div(N, rows);
@@ -359,7 +365,7 @@ int add_norm(const typename E::T *x, int64_t ldx, const typename E::T *residual,
                            dense_of(q ? scale : nullptr, rows * 4)};
     const Same same[3] = {{0, 0}, {0, 1}, {1, 0}};
     if (outputs_share_but(in, out, same)) return CX_ERR_ALIAS;
-    const Layout l = layout_of(D);
+    const Layout l = layout_of(D, false);
     a.x = x; a.ldx = ldx; a.residual = residual; a.ldr = ldr; a.weights = weights + offset; a.ldw = ld; a.s = s; a.lds = lds; a.y = y; a.ldy = ldy;
     a.inv = inv; a.q = q; a.ldq = ldq; a.scale = scale; a.N = N; a.D = D; a.eights = static_cast<int32_t>(ceil_div(D, 8)); a.shift = l.shift; a.eps = eps;
     const dim3 grid(static_cast<unsigned>(ceil_div(N, l.threads >> l.shift)), W);
@@ -398,7 +404,7 @@ int add_norm_grad(const typename E::T *dy, int64_t lddy, const typename E::T *s,
     const hipStream_t st = static_cast<hipStream_t>(stream);
     float *sums = static_cast<float *>(workspace);
     if (N > 0) {
-        const Layout l = layout_of(D);
+        const Layout l = layout_of(D, true);
         a.dy = dy; a.lddy = lddy; a.s_in = s; a.lds = lds; a.inv_in = inv; a.weights = weights + offset; a.ldw = ldw; a.ds_in = ds_in; a.ldi = ldi;
         a.ds = ds; a.ldds = ldds; a.dx = dx; a.lddx = lddx; a.parts = sums; a.N = N; a.part_rows = 0;
         a.D = D; a.eights = static_cast<int32_t>(ceil_div(D, 8)); a.shift = l.shift;

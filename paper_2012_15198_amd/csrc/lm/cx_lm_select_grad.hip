@@ -27,12 +27,6 @@ struct Reduced {
     int which, j;
     bool holds;
 };
-constexpr int kMirror = 0x140, kHalfMirror = 0x141, kOppositePair = 0x4e, kBeside = 0xb1;
-template <int PATTERN>
-__device__ __forceinline__ float add_partner(float v)
-{
-    return v + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), PATTERN, 0xf, 0xf, true));
-}
 // Every lane adds both, then keeps one.
 template <int PATTERN>
 __device__ __forceinline__ float half_of(int second, float x, float y)

@@ -99,11 +99,12 @@ __device__ __forceinline__ u4 random_block(uint64_t key, uint64_t draw, uint64_t
     uint32_t k0 = static_cast<uint32_t>(key), k1 = static_cast<uint32_t>(key >> 32);
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
-        const uint32_t h0 = __umulhi(0xD2511F53u, c0), l0 = 0xD2511F53u * c0, h1 = __umulhi(0xCD9E8D57u, c2), l1 = 0xCD9E8D57u * c2;
-        c0 = h1 ^ c1 ^ k0;
-        c1 = l1;
-        c2 = h0 ^ c3 ^ k1;
-        c3 = l0;
+        // one multiplication each: both halves of the products
+        const uint64_t m0 = static_cast<uint64_t>(c0) * 0xD2511F53u, m1 = static_cast<uint64_t>(c2) * 0xCD9E8D57u;
+        c0 = static_cast<uint32_t>(m1 >> 32) ^ c1 ^ k0;
+        c1 = static_cast<uint32_t>(m1);
+        c2 = static_cast<uint32_t>(m0 >> 32) ^ c3 ^ k1;
+        c3 = static_cast<uint32_t>(m0);
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
@@ -139,18 +140,50 @@ __device__ __forceinline__ float finite_below(float v) { return v < -3.0e38f ? -
 __device__ __forceinline__ float silu_slope(float v, float e) { return e * __builtin_fmaf(v, 1.0f - e, 1.0f); }
 
 // ---------------------------------------------------------------------------------
-// Sums over lanes
+// Sums over lanes.  A value is read from the partner's lane by the addition itself within a row of 16 lanes, rows are exchanged whole; all lanes
+// that are to take part have to be active.
 // ---------------------------------------------------------------------------------
-__device__ __forceinline__ float sum_lanes(float v, int lanes)
+constexpr int kBeside = 0xb1, kOppositePair = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;      // lanes 1 0 3 2; 2 3 0 1; 7 .. 0 of eight; 15 .. 0 of a row
+template <int PATTERN>
+__device__ __forceinline__ unsigned partner(unsigned v) { return __builtin_amdgcn_mov_dpp(v, PATTERN, 0xf, 0xf, true); }
+template <int PATTERN>
+__device__ __forceinline__ float add_partner(float v) { return v + __uint_as_float(partner<PATTERN>(__float_as_uint(v))); }
+__device__ __forceinline__ float add32(float x, float y)               // rows 0 and 1: x of both halves of the wavefront; rows 2 and 3: y
 {
-    for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor(v, o);
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float add16(float x, float y)               // even rows: x of the row and the next; odd rows: y of the row and the one before
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Over groups of 1 << shift <= 64 lanes, in every lane.  Each stage doubles the lanes that hold the same sum.
+__device__ __forceinline__ float sum_lanes(float v, int shift)
+{
+    if (shift > 0) v = add_partner<kBeside>(v);
+    if (shift > 1) v = add_partner<kOppositePair>(v);
+    if (shift > 2) v = add_partner<kHalfMirror>(v);
+    if (shift > 3) v = add_partner<kMirror>(v);
+    if (shift > 4) v = add16(v, v);
+    if (shift > 5) v = add32(v, v);
     return v;
 }
-__device__ __forceinline__ unsigned max_lanes(unsigned v, int lanes)
+__device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
+__device__ __forceinline__ unsigned max_lanes(unsigned v, int shift)
 {
-    for (int o = 1; o < lanes; o <<= 1) {
-        const unsigned u = __shfl_xor(v, o);
-        v = u > v ? u : v;
+    if (shift > 0) v = larger(v, partner<kBeside>(v));
+    if (shift > 1) v = larger(v, partner<kOppositePair>(v));
+    if (shift > 2) v = larger(v, partner<kHalfMirror>(v));
+    if (shift > 3) v = larger(v, partner<kMirror>(v));
+    if (shift > 4) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = larger(r[0], r[1]);
+    }
+    if (shift > 5) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        v = larger(r[0], r[1]);
     }
     return v;
 }

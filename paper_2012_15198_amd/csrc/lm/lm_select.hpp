@@ -70,16 +70,6 @@ template <class E>
 __device__ __forceinline__ void load_four(const typename E::T *p, int left, float (&v)[4]) { widen<E, 4>(load_columns<E, 4>(p, left), v); }
 
 // Lane 16 q + c of a wavefront has quarter q of the states of its column c.  Sums over quarters cross its four rows of 16 lanes.
-__device__ __forceinline__ float add32(float x, float y)               // rows 0 and 1: x of both halves of the wavefront; rows 2 and 3: y
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-__device__ __forceinline__ float add16(float x, float y)               // even rows: x of the row and the next; odd rows: y of the row and the one before
-{
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 // Four steps' sums over the quarters: the one of step quarter_step(q) in quarter q's lanes.
 __device__ __forceinline__ float quarters_sum(const float (&v)[4]) { return add16(add32(v[0], v[1]), add32(v[2], v[3])); }
 __device__ __forceinline__ int quarter_step(int q) { return (q & 1) * 2 + q / 2; }
