@@ -21,7 +21,8 @@ struct ConvArgs {
     int64_t ldx, ldy, lddy, lddx, ldw;
     const uint8_t *reset;
     float *parts;
-    int64_t B, T_, per_worker;                          // sequences of a worker
+    int64_t B, T_;
+    uint32_t per_worker;                                // sequences of a worker
     int64_t span, spans;                                // steps of a lane's walk; spans of a sequence, rounded up to whole workgroups
     int32_t D, shift, slabs;                            // 1 << shift lanes beside each other
     bool silu;
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(const ConvArgs<E> a)
     if (!p.any) return;
     const int left = a.D - p.column;
     float tap[K][C], bias[C], seen[K][C];
-    load_taps<E, C, K>(a, p.b / a.per_worker, p.column, left, tap, bias);
+    load_taps<E, C, K>(a, static_cast<uint32_t>(p.b) / a.per_worker, p.column, left, tap, bias);
     enter<E, C, K>(a, p.b, p.begin, p.column, left, seen);
     if (K > 1 && p.begin == 0 && a.after) {             // by the lanes that have read `before`, which may be the same
         float last[K][C];
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(kWave) void conv_step_kernel(const ConvArgs<E> a)
     for (int k = 0; k < K - 1; ++k) inputs[k] = load_columns<E, C>(a.before + (b * (K - 1) + k) * a.D + column, a.before && !fresh ? left : 0);
     inputs[K - 1] = load_columns<E, C>(a.x + b * a.ldx + column, left);
     float tap[K][C], bias[C], seen[K][C], z[C];
-    load_taps<E, C, K>(a, b / a.per_worker, column, left, tap, bias);
+    load_taps<E, C, K>(a, static_cast<uint32_t>(b) / a.per_worker, column, left, tap, bias);
 #pragma unroll
     for (int k = 0; k < K; ++k) widen<E, C>(inputs[k], seen[k]);
     convolve<C, K>(seen, tap, bias, z);
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(kThreads) void conv_grad_kernel(const ConvArgs<E> a
     float dw[K + 1][C] = {};                            // the bias's behind the taps'
     if (p.any) {
         float tap[K][C], bias[C], seen[K][C];
-        load_taps<E, C, K>(a, p.b / a.per_worker, p.column, left, tap, bias);
+        load_taps<E, C, K>(a, static_cast<uint32_t>(p.b) / a.per_worker, p.column, left, tap, bias);
         enter<E, C, K>(a, p.b, p.begin, p.column, left, seen);
         float open[K][C] = {};                          // gradients of the inputs of steps t - K + 1 .. t, oldest first
         int visible = 0;                                // steps behind that step t's taps see and that belong to this span
@@ -383,7 +384,7 @@ int conv(const typename E::T *x, int64_t ldx, const typename E::T *wlanes, int64
     if (w.groups * w.slabs > 0x7fffffff) return CX_ERR_SHAPE;
     ConvArgs<E> a{};
     a.x = x; a.ldx = ldx; a.wlanes = wlanes + offset; a.ldw = ld; a.y = y; a.ldy = ldy; a.before = before; a.after = after; a.reset = reset;
-    a.B = B; a.T_ = T; a.per_worker = B / W; a.D = D; a.silu = silu != 0;
+    a.B = B; a.T_ = T; a.per_worker = static_cast<uint32_t>(B / W); a.D = D; a.silu = silu != 0;
     set_walk(a, w);
     if (T == 1) {
         a.slabs = static_cast<int32_t>(ceil_div(ceil_div(D, kForward), kWave));
@@ -428,7 +429,7 @@ int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int6
         if (w.groups * w.slabs > 0x7fffffff) return CX_ERR_SHAPE;
         ConvArgs<E> a{};
         a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.wlanes = wlanes + offset; a.ldw = ldw; a.dx = dx; a.lddx = lddx; a.before = before;
-        a.reset = reset; a.parts = parts; a.B = B; a.T_ = T; a.per_worker = B / W; a.D = D; a.silu = silu != 0;
+        a.reset = reset; a.parts = parts; a.B = B; a.T_ = T; a.per_worker = static_cast<uint32_t>(B / W); a.D = D; a.silu = silu != 0;
         set_walk(a, w);
         const int rc2 = by_taps(K, [&](auto k) {
             if (reset) hipLaunchKernelGGL((conv_grad_kernel<E, kGradColumns, decltype(k)::value, true>), grid_of(w, B), dim3(w.together << w.shift), 0, st, a);

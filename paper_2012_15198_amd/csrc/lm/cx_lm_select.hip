@@ -20,7 +20,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
     __shared__ alignas(16) float2 step[2][kTile][kColumns];            // delta, delta u
     __shared__ alignas(16) float both[2][kTile][2][kMaxStates];        // B, C
     __shared__ alignas(16) float out[MAPS ? 1 : 2][MAPS ? 1 : kTile][kOutPitch];
-    const int64_t b = blockIdx.x / a.slabs, w = b / a.per_worker, row0 = b * a.T_;
+    const int64_t b = blockIdx.x / a.slabs, w = static_cast<uint32_t>(b) / a.per_worker, row0 = b * a.T_;
     const int column0 = static_cast<int>(blockIdx.x % a.slabs) * kColumns;
     // maps: piece i of each span; spans may have fewer steps than their pieces' together
     const int parts = a.pieces / a.spans, span = MAPS ? blockIdx.y / parts : blockIdx.y;
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
 template <class E, int NQ>
 __global__ __launch_bounds__(kThreads) void select_step_kernel(const SelectArgs<E> a)
 {
-    const int64_t b = blockIdx.x / a.slabs, w = b / a.per_worker;
+    const int64_t b = blockIdx.x / a.slabs, w = static_cast<uint32_t>(b) / a.per_worker;
     const int q = threadIdx.x / 16 % kQuarters, n0 = q * NQ;
     const int d = static_cast<int>(blockIdx.x % a.slabs) * kColumns + threadIdx.x / kWave * 16 + threadIdx.x % 16;
     const bool any = d < a.D;
@@ -159,14 +159,15 @@ __global__ __launch_bounds__(kThreads) void select_step_kernel(const SelectArgs<
     const float skip = E::widen(params[of + a.D + at]), z = a.z ? E::widen(a.z[b * a.ldz + at]) : 0.0f;
     const bool cut = a.reset && a.reset[b] != 0;
     if (a.states) store_states<NQ>(a.states + b * of + state, n0, a.N, any, h);
+    const int here = any ? a.N - n0 : 0;
+    const Columns<E, 4> logs = load_columns<E, 4>(params + state + n0, here), bs = load_columns<E, 4>(a.bm + b * a.ldb + n0, here),
+                        cs = load_columns<E, 4>(a.cm + b * a.ldc + n0, here);
     float y = 0.0f;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        const bool has = n0 + i < a.N;
-        const float rate = has ? -kLog2e * exp2_fast(kLog2e * E::widen(params[state + n0 + i])) : 0.0f;
-        const float in = has ? delta * u * E::widen(a.bm[b * a.ldb + n0 + i]) : 0.0f, read = has ? E::widen(a.cm[b * a.ldc + n0 + i]) : 0.0f;
+        const float rate = i < here ? -kLog2e * exp2_fast(kLog2e * value_of<E, 4>(logs, i)) : 0.0f, in = i < here ? delta * u * value_of<E, 4>(bs, i) : 0.0f;
         h[i] = cut ? in : __builtin_fmaf(exp2_fast(rate * delta), h[i], in);
-        y = __builtin_fmaf(read, h[i], y);
+        y = __builtin_fmaf(i < here ? value_of<E, 4>(cs, i) : 0.0f, h[i], y);
     }
     if (a.h_last) store_states<NQ>(a.h_last + b * of + state, n0, a.N, any, h);
     y = add32(y, y);
@@ -219,7 +220,7 @@ int select_scan(const typename E::T *u, int64_t ldu, const typename E::T *dt, in
     if (outputs_share_but(in, out, same)) return CX_ERR_ALIAS;
     SelectArgs<E> a{};
     a.u = u; a.ldu = ldu; a.dt = dt; a.lddt = lddt; a.bm = bm; a.ldb = ldb; a.cm = cm; a.ldc = ldc; a.z = z; a.ldz = ldz; a.params = params + offset;
-    a.ldp = ldp; a.y = y; a.ldy = ldy; a.reset = reset; a.h0 = h0; a.h_last = h_last; a.states = states; a.B = B; a.T_ = T; a.per_worker = B / W;
+    a.ldp = ldp; a.y = y; a.ldy = ldy; a.reset = reset; a.h0 = h0; a.h_last = h_last; a.states = states; a.B = B; a.T_ = T; a.per_worker = static_cast<uint32_t>(B / W);
     a.D = D; a.N = N; a.slabs = s.slabs; a.spans = s.spans; a.span_steps = s.steps; a.pieces = s.pieces; a.piece_steps = s.piece_steps;
     a.maps = static_cast<float *>(workspace);
     a.sums = a.maps + B * s.pieces * D * N;

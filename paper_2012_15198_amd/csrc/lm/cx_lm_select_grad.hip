@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
     __shared__ alignas(16) float both[kTile][2][kMaxStates];           // B, C
     __shared__ alignas(16) float out[MAPS ? 1 : 3][MAPS ? 1 : kTile][kOutPitch];       // y', into, across
     __shared__ alignas(16) float shares[MAPS ? 1 : kWaves][kTile][2][kMaxStates];      // dB, dC of a wavefront's columns
-    const int64_t b = blockIdx.x / a.slabs, w = b / a.per_worker, row0 = b * a.T_;
+    const int64_t b = blockIdx.x / a.slabs, w = static_cast<uint32_t>(b) / a.per_worker, row0 = b * a.T_;
     const int slab = static_cast<int>(blockIdx.x % a.slabs), column0 = slab * kColumns;
     const int parts = a.pieces / a.spans, piece = blockIdx.y + parts, span = MAPS ? piece / parts : blockIdx.y;       // maps: all but the first span's
     const int64_t span_begin = span * a.span_steps, span_end = span_begin + a.span_steps < a.T_ ? span_begin + a.span_steps : a.T_;
@@ -364,7 +364,7 @@ int select_scan_grad(const typename E::T *u, int64_t ldu, const typename E::T *d
     if (!none) {
         a.u = u; a.ldu = ldu; a.dt = dt; a.lddt = lddt; a.bm = bm; a.ldb = ldb; a.cm = cm; a.ldc = ldc; a.z = z; a.ldz = ldz; a.params = params + offset;
         a.ldp = ldp; a.dy = dy; a.lddy = lddy; a.du = du; a.lddu = lddu; a.ddt = ddt; a.ldddt = ldddt; a.dbm = dbm; a.lddb = lddb; a.dcm = dcm; a.lddc = lddc;
-        a.dz = dz; a.lddz = lddz; a.reset = reset; a.states_in = states; a.per_worker = B / W; a.slabs = space.s.slabs; a.spans = space.s.spans;
+        a.dz = dz; a.lddz = lddz; a.reset = reset; a.states_in = states; a.per_worker = static_cast<uint32_t>(B / W); a.slabs = space.s.slabs; a.spans = space.s.spans;
         a.span_steps = space.s.steps; a.pieces = space.s.pieces; a.piece_steps = space.s.piece_steps;
         a.maps = reinterpret_cast<float *>(base);
         a.sums = reinterpret_cast<float *>(base + space.sums);

@@ -49,7 +49,8 @@ struct SelectArgs {
     float *maps;                                        // split: [B][pieces][D][N] what a piece of a span makes of zeros, then what enters it
     float *sums;                                        // [B][pieces][D] sum of delta; below zero: the piece forgets what enters
     float *shared_parts, *parts;                        // gradient: [slabs][B][T][2][N] of B and C; [W][parts][D (N + 2)] of the parameters
-    int64_t B, T_, per_worker;
+    int64_t B, T_;
+    uint32_t per_worker;                                // sequences of a worker
     int32_t D, N, slabs, spans, pieces;                 // pieces of all spans, as many of each
     int64_t span_steps, piece_steps;                    // multiples of kTile
 };
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(kWave *kStretches) void enter_kernel(const SelectAr
     const int64_t i = at0 < all ? at0 : all - 1;
     const int64_t b = i / of, at = i - b * of;
     const int d = static_cast<int>(at / a.N), n = static_cast<int>(at - static_cast<int64_t>(d) * a.N);
-    const float rate = -kLog2e * exp2_fast(kLog2e * E::widen(a.params[(b / a.per_worker) * a.ldp + static_cast<int64_t>(d) * a.N + n]));
+    const float rate = -kLog2e * exp2_fast(kLog2e * E::widen(a.params[(static_cast<uint32_t>(b) / a.per_worker) * a.ldp + static_cast<int64_t>(d) * a.N + n]));
     float *maps = a.maps + b * a.pieces * of + at;
     const float *sums = a.sums + b * a.pieces * a.D + d;
     const int each = (needed + stretches) / stretches, begin = stretch * each;         // of needed + 1 places, the last of which only receives
