@@ -209,7 +209,7 @@ int cx_distill_step_f16(const uint16_t *z, int64_t ld, int64_t N, int32_t V, int
  *     out = round(residual + keep x s)     s = 2^16 / (2^16 - k),  k = round(p 2^16) <= 65535, 0 <= p < 1
  * keep of row n and column d: at least k is the 16-bit half (d mod 8) of block (n ceil(D / 8) + floor(d / 8), rng[1]) of Philox4x32 with ten
  * rounds (Salmon et al. 2011) and key rng[0]: halves of the four words in turn, the lower one first; of each 64-bit number the lower word first.
- *   x, out   [N][D], N <= 2^31; residual: the same or NULL.  out may be x or residual
+ *   x, out   [N][D], N <= 2^31, N ceil(D / 8) < 2^33; residual: the same or NULL.  out may be x or residual
  *   rng      int64 [2] DEVICE: key and draw; another draw is another mask.  Read when the kernel runs, so that a captured call whose
  *            caller adds to rng[1] between replays draws anew
  * The gradient is the same call on the result's gradient, with the same rng.  A dropped element counts for nothing, NaN and infinities included.
@@ -309,7 +309,8 @@ int cx_short_conv_grad_f16(const uint16_t *x, int64_t ldx, const uint16_t *dy, i
  *     delta_t = softplus(dt_t + bias) ;  a_t[n] = exp(-delta_t exp(A_log[n]))
  *     h_t[n] = a_t[n] (reset_t ? 0 : h_{t-1}[n]) + delta_t B_t[n] u_t
  *     y_t = round((sum_n C_t[n] h_t[n] + skip u_t) (z ? z_t sigmoid(z_t) : 1))
- * u, dt, z, y are matrices of B * T rows and D columns, bm (B) and cm (C) of N columns, each with its own ld; 1 <= N <= CX_MAX_STATES.
+ * u, dt, z, y are matrices of B * T rows and D columns, bm (B) and cm (C) of N columns, each with its own ld <= 2^24; 1 <= N <= CX_MAX_STATES,
+ * B D <= 2^29.
  * W workers have B / W sequences each (B a multiple of W); A_log [D][N], bias [D] and skip [D] lie one behind the other in columns
  * [offset, offset + D (N + 2)) of the worker's flat row.
  *   z        NULL: no gate

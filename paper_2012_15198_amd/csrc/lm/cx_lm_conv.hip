@@ -16,7 +16,7 @@ constexpr int64_t kMaxSeq = CX_MAX_TOKENS;
 template <class E>
 struct ConvArgs {
     using T = typename E::T;
-    const T *x, *dy, *wlanes, *before;
+    const T *x, *dy, *weights, *before;
     T *y, *dx, *after;
     int64_t ldx, ldy, lddy, lddx, ldw;
     const uint8_t *reset;
@@ -31,7 +31,7 @@ struct ConvArgs {
 template <class E, int C, int K>
 __device__ __forceinline__ void load_taps(const ConvArgs<E> &a, int64_t w, int column, int left, float (&tap)[K][C], float (&bias)[C])
 {
-    const typename E::T *p = a.wlanes + w * a.ldw;
+    const typename E::T *p = a.weights + w * a.ldw;
     widen<E, C>(load_columns<E, C>(p + static_cast<int64_t>(a.D) * K + column, left), bias);
     float flat[K][C];                                   // C K elements in a row: column j, tap k at j K + k
 #pragma unroll
@@ -282,14 +282,6 @@ __global__ __launch_bounds__(kThreads) void conv_grad_kernel(const ConvArgs<E> a
     }
 }
 
-// No steps: what the next one sees passes through.
-template <class E>
-__global__ __launch_bounds__(256) void keep_kernel(const typename E::T *from, typename E::T *to, int64_t n)
-{
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i < n) to[i] = from ? from[i] : static_cast<typename E::T>(0);
-}
-
 struct Walk {
     int shift, slabs, together;
     int64_t span, spans, groups;                        // groups of spans that share a workgroup
@@ -355,7 +347,7 @@ dim3 grid_of(const Walk &w, int64_t B)
 }
 
 template <class E>
-int conv(const typename E::T *x, int64_t ldx, const typename E::T *wlanes, int64_t ld, int32_t W, int64_t offset, typename E::T *y, int64_t ldy, int64_t B,
+int conv(const typename E::T *x, int64_t ldx, const typename E::T *weights, int64_t ld, int32_t W, int64_t offset, typename E::T *y, int64_t ldy, int64_t B,
          int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const typename E::T *before, typename E::T *after, void *stream)
 {
     const int rc = check_conv(W, B, T, D, K);
@@ -366,15 +358,11 @@ int conv(const typename E::T *x, int64_t ldx, const typename E::T *wlanes, int64
     const int64_t ends = B * (K - 1) * D;
     if (misaligned_to(before, kElem) || misaligned_to(after, kElem)) return CX_ERR_ALIGN;
     if (before != after && overlap(before, ends * kElem, after, ends * kElem)) return CX_ERR_ALIAS;
-    if (T == 0) {
-        if (!after || after == before || ends == 0) return CX_OK;
-        hipLaunchKernelGGL(keep_kernel<E>, dim3(static_cast<unsigned>(ceil_div(ends, 256))), dim3(256), 0, st, before, after, ends);
-        return launched();
-    }
-    if (!x || !y || !wlanes) return CX_ERR_NULL;
+    if (T == 0) return pass_through(before, after, ends, st);
+    if (!x || !y || !weights) return CX_ERR_NULL;
     if (bad_matrix(B * T, ldx, D) || bad_matrix(B * T, ldy, D)) return CX_ERR_SHAPE;
-    if (misaligned_to(x, kElem) || misaligned_to(wlanes, kElem) || misaligned_to(y, kElem)) return CX_ERR_ALIGN;
-    const Extent in[4] = {matrix_of(x, B * T, ldx, D, kElem), matrix_of(wlanes, W, ld, offset + static_cast<int64_t>(D) * (K + 1), kElem), dense_of(reset, B * T),
+    if (misaligned_to(x, kElem) || misaligned_to(weights, kElem) || misaligned_to(y, kElem)) return CX_ERR_ALIGN;
+    const Extent in[4] = {matrix_of(x, B * T, ldx, D, kElem), matrix_of(weights, W, ld, offset + static_cast<int64_t>(D) * (K + 1), kElem), dense_of(reset, B * T),
                           dense_of(before, ends * kElem)};
     const Extent out[2] = {matrix_of(y, B * T, ldy, D, kElem), dense_of(after, ends * kElem)};
     const Same same[1] = {{1, 3}};
@@ -383,7 +371,7 @@ int conv(const typename E::T *x, int64_t ldx, const typename E::T *wlanes, int64
     const Walk w = walk_of(B, T, D, kForward, kLeastSteps);
     if (w.groups * w.slabs > 0x7fffffff) return CX_ERR_SHAPE;
     ConvArgs<E> a{};
-    a.x = x; a.ldx = ldx; a.wlanes = wlanes + offset; a.ldw = ld; a.y = y; a.ldy = ldy; a.before = before; a.after = after; a.reset = reset;
+    a.x = x; a.ldx = ldx; a.weights = weights + offset; a.ldw = ld; a.y = y; a.ldy = ldy; a.before = before; a.after = after; a.reset = reset;
     a.B = B; a.T_ = T; a.per_worker = static_cast<uint32_t>(B / W); a.D = D; a.silu = silu != 0;
     set_walk(a, w);
     if (T == 1) {
@@ -399,7 +387,7 @@ int conv(const typename E::T *x, int64_t ldx, const typename E::T *wlanes, int64
 }
 
 template <class E>
-int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int64_t lddy, const typename E::T *wlanes, int64_t ldw, int32_t W,
+int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int64_t lddy, const typename E::T *weights, int64_t ldw, int32_t W,
               int64_t offset, typename E::T *dx, int64_t lddx, const typename E::T *g_in, typename E::T *g_out, int64_t ld, int64_t B, int64_t T,
               int32_t D, int32_t K, int32_t silu, const uint8_t *reset, const typename E::T *before, void *workspace, int64_t workspace_bytes, void *stream)
 {
@@ -411,12 +399,12 @@ int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int6
     const bool none = B == 0 || T == 0;
     const int64_t ends = B * (K - 1) * D, bytes = parts_bytes(B, T, D, K);
     if (!none) {
-        if (!x || !dy || !wlanes || !dx || !workspace) return CX_ERR_NULL;
+        if (!x || !dy || !weights || !dx || !workspace) return CX_ERR_NULL;
         if (bad_matrix(B * T, ldx, D) || bad_matrix(B * T, lddy, D) || bad_matrix(B * T, lddx, D) || workspace_bytes < bytes) return CX_ERR_SHAPE;
     }
-    if (misaligned_to(x, kElem) || misaligned_to(dy, kElem) || misaligned_to(wlanes, kElem) || misaligned_to(dx, kElem) || misaligned_to(g_in, kElem) ||
+    if (misaligned_to(x, kElem) || misaligned_to(dy, kElem) || misaligned_to(weights, kElem) || misaligned_to(dx, kElem) || misaligned_to(g_in, kElem) ||
         misaligned_to(g_out, kElem) || misaligned_to(before, kElem) || misaligned_to(workspace, 16)) return CX_ERR_ALIGN;
-    const Extent in[6] = {matrix_of(x, B * T, ldx, D, kElem), matrix_of(dy, B * T, lddy, D, kElem), matrix_of(wlanes, W, ldw, offset + columns, kElem),
+    const Extent in[6] = {matrix_of(x, B * T, ldx, D, kElem), matrix_of(dy, B * T, lddy, D, kElem), matrix_of(weights, W, ldw, offset + columns, kElem),
                           dense_of(reset, B * T), dense_of(before, ends * kElem), matrix_of(g_in, W, ld, offset + columns, kElem)};
     const Extent out[3] = {matrix_of(dx, B * T, lddx, D, kElem), matrix_of(g_out, W, ld, offset + columns, kElem), dense_of(workspace, bytes)};
     const Same same[1] = {{1, 5}};
@@ -428,7 +416,7 @@ int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int6
         const Walk w = walk_of(B, T, D, kGradColumns, kLeastGradSteps);
         if (w.groups * w.slabs > 0x7fffffff) return CX_ERR_SHAPE;
         ConvArgs<E> a{};
-        a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.wlanes = wlanes + offset; a.ldw = ldw; a.dx = dx; a.lddx = lddx; a.before = before;
+        a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.weights = weights + offset; a.ldw = ldw; a.dx = dx; a.lddx = lddx; a.before = before;
         a.reset = reset; a.parts = parts; a.B = B; a.T_ = T; a.per_worker = static_cast<uint32_t>(B / W); a.D = D; a.silu = silu != 0;
         set_walk(a, w);
         const int rc2 = by_taps(K, [&](auto k) {
@@ -447,18 +435,18 @@ int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int6
 extern "C" {
 
 #define CX_LM_CONV(SUFFIX, E)                                                                                                         \
-    int cx_short_conv##SUFFIX(const E::T *x, int64_t ldx, const E::T *wlanes, int64_t ldw, int32_t W, int64_t offset, E::T *y,       \
+    int cx_short_conv##SUFFIX(const E::T *x, int64_t ldx, const E::T *weights, int64_t ldw, int32_t W, int64_t offset, E::T *y,       \
                               int64_t ldy, int64_t B, int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset,            \
                               const E::T *before, E::T *after, void *stream)                                                          \
     {                                                                                                                                 \
-        return conv<E>(x, ldx, wlanes, ldw, W, offset, y, ldy, B, T, D, K, silu, reset, before, after, stream);                      \
+        return conv<E>(x, ldx, weights, ldw, W, offset, y, ldy, B, T, D, K, silu, reset, before, after, stream);                      \
     }                                                                                                                                 \
-    int cx_short_conv_grad##SUFFIX(const E::T *x, int64_t ldx, const E::T *dy, int64_t lddy, const E::T *wlanes, int64_t ldw,        \
+    int cx_short_conv_grad##SUFFIX(const E::T *x, int64_t ldx, const E::T *dy, int64_t lddy, const E::T *weights, int64_t ldw,        \
                                    int32_t W, int64_t offset, E::T *dx, int64_t lddx, const E::T *g_in, E::T *g_out, int64_t ldg,     \
                                    int64_t B, int64_t T, int32_t D, int32_t K, int32_t silu, const uint8_t *reset,                    \
                                    const E::T *before, void *workspace, int64_t workspace_bytes, void *stream)                        \
     {                                                                                                                                 \
-        return conv_grad<E>(x, ldx, dy, lddy, wlanes, ldw, W, offset, dx, lddx, g_in, g_out, ldg, B, T, D, K, silu, reset, before,   \
+        return conv_grad<E>(x, ldx, dy, lddy, weights, ldw, W, offset, dx, lddx, g_in, g_out, ldg, B, T, D, K, silu, reset, before,   \
                             workspace, workspace_bytes, stream);                                                                      \
     }
 CX_LM_CONV(, F32)

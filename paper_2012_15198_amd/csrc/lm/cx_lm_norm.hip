@@ -15,7 +15,7 @@
 namespace {
 
 constexpr int kThreads = 256, kMaxLanes = 512, kMaxEights = 4;
-constexpr int64_t kMaxRows = int64_t(1) << 31;
+constexpr int64_t kMaxRows = int64_t(1) << 31, kMaxGroups = int64_t(1) << 24;       // a launch has fewer than 2^32 threads
 constexpr float kLargest8 = 448.0f, kLeastScale = 0x1p-126f;
 
 // ---------------------------------------------------------------------------------
@@ -80,7 +80,9 @@ int dropout(const typename E::T *x, int64_t ldx, const typename E::T *residual, 
     if (N < 0 || N > kMaxRows || D < 1 || D > CX_MAX_WIDTH || !drop_of(p, rng, a.d)) return CX_ERR_SHAPE;
     if (N == 0) return CX_OK;
     if (!x || !out || !rng) return CX_ERR_NULL;
-    if (bad_matrix(N, ldx, D) || (residual && bad_matrix(N, ldr, D)) || bad_matrix(N, ldo, D)) return CX_ERR_SHAPE;
+    a.eights = static_cast<int32_t>(ceil_div(D, 8));
+    const int64_t groups = ceil_div(N * a.eights, kThreads * kDropEach);
+    if (bad_matrix(N, ldx, D) || (residual && bad_matrix(N, ldr, D)) || bad_matrix(N, ldo, D) || groups >= kMaxGroups) return CX_ERR_SHAPE;
     constexpr int kElem = sizeof(typename E::T);
     if (misaligned_to(x, kElem) || misaligned_to(residual, kElem) || misaligned_to(out, kElem) || misaligned_to(rng, 8)) return CX_ERR_ALIGN;
     const Extent in[3] = {matrix_of(x, N, ldx, D, kElem), matrix_of(residual, N, ldr, D, kElem), dense_of(rng, 16)};
@@ -88,10 +90,7 @@ int dropout(const typename E::T *x, int64_t ldx, const typename E::T *residual, 
     const Same same[2] = {{0, 0}, {0, 1}};
     if (outputs_share_but(in, outs, same)) return CX_ERR_ALIAS;
     a.x = x; a.ldx = ldx; a.residual = residual; a.ldr = ldr; a.out = out; a.ldo = ldo; a.rows = N; a.D = D;
-    a.eights = static_cast<int32_t>(ceil_div(D, 8));
     a.per = static_cast<uint32_t>(ceil_div(int64_t(1) << 32, a.eights));
-    const int64_t groups = ceil_div(N * a.eights, kThreads * kDropEach);
-    if (groups > 0x7fffffff) return CX_ERR_SHAPE;
     hipLaunchKernelGGL(dropout_kernel<E>, dim3(static_cast<unsigned>(groups)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
     return launched();
 }
@@ -147,7 +146,8 @@ __global__ __launch_bounds__(kMaxLanes) void norm_kernel(const NormArgs<E> a)
 {
     __shared__ float lds[2][kMaxLanes / kWave];
     const int lanes = 1 << a.shift, lane = threadIdx.x & (lanes - 1);
-    const int64_t w = blockIdx.y, r = static_cast<int64_t>(blockIdx.x) * (blockDim.x >> a.shift) + (threadIdx.x >> a.shift), row = w * a.N + r;
+    const int64_t w = blockIdx.y, block = static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x;
+    const int64_t r = block * (blockDim.x >> a.shift) + (threadIdx.x >> a.shift), row = w * a.N + r;
     const bool here = r < a.N;
     float s[V][8];
     float squares = 0.0f;
@@ -368,7 +368,8 @@ int add_norm(const typename E::T *x, int64_t ldx, const typename E::T *residual,
     const Layout l = layout_of(D, false);
     a.x = x; a.ldx = ldx; a.residual = residual; a.ldr = ldr; a.weights = weights + offset; a.ldw = ld; a.s = s; a.lds = lds; a.y = y; a.ldy = ldy;
     a.inv = inv; a.q = q; a.ldq = ldq; a.scale = scale; a.N = N; a.D = D; a.eights = static_cast<int32_t>(ceil_div(D, 8)); a.shift = l.shift; a.eps = eps;
-    const dim3 grid(static_cast<unsigned>(ceil_div(N, l.threads >> l.shift)), W);
+    const int64_t blocks = ceil_div(N, l.threads >> l.shift), wide = blocks < (1 << 22) ? blocks : 1 << 22;
+    const dim3 grid(static_cast<unsigned>(wide), W, static_cast<unsigned>(ceil_div(blocks, wide)));
     return by_layout<E>(l, a.d.border != 0, [&](auto v, auto drops) {
         hipLaunchKernelGGL((norm_kernel<E, decltype(v)::value, decltype(drops)::value>), grid, dim3(l.threads), 0, static_cast<hipStream_t>(stream), a);
     });

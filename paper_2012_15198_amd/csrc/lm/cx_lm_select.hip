@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
         else if (a.h0) load_states<NQ>(a.h0 + b * of + state, n0, a.N, any, h);
     }
     const uint32_t u_at = place_in<T>(a.ldu, es, ec), dt_at = place_in<T>(a.lddt, es, ec), z_at = place_in<T>(a.ldz, es, ec), y_at = place_in<T>(a.ldy, es, ec);
-    const int bs = threadIdx.x / kMaxStates, bn = threadIdx.x % kMaxStates;          // a thread's element of B and of C
+    const int bs = threadIdx.x / kMaxStates, bp = threadIdx.x % kMaxStates, bn = state_of<NQ>(bp);           // a thread's element of B and of C
     const uint32_t b_at = place_in<T>(a.ldb, bs, bn), c_at = place_in<T>(a.ldc, bs, bn), state_at = (c * a.N) * 4;
     const auto steps_from = [&](int64_t t0) { return end - t0 >= kTile ? kTile : end > t0 ? static_cast<int>(end - t0) : 0; };
     Columns<E, 4> u, dt, z{};
@@ -81,8 +81,8 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
                 gates[j] = a.z ? open : 1.0f;
             }
         }
-        both[turn][bs][0][bn] = E::widen(b_next);
-        if constexpr (!MAPS) both[turn][bs][1][bn] = E::widen(c_next);
+        both[turn][bs][0][bp] = E::widen(b_next);
+        if constexpr (!MAPS) both[turn][bs][1][bp] = E::widen(c_next);
     };
     const auto tile = [&](int64_t t0, auto turn_of) {
         constexpr int turn = decltype(turn_of)::value;
@@ -100,9 +100,9 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
             float y = 0.0f;
 #pragma unroll
             for (int j = 0; j < NQ; ++j) {
-                const float in = s.y * both[turn][i][0][n0 + j], keep = exp2_fast(rate[j] * s.x);
+                const float in = s.y * both[turn][i][0][q * 4 + j], keep = exp2_fast(rate[j] * s.x);
                 h[j] = cut ? in : __builtin_fmaf(keep, h[j], in);
-                if constexpr (!MAPS) y = __builtin_fmaf(both[turn][i][1][n0 + j], h[j], y);
+                if constexpr (!MAPS) y = __builtin_fmaf(both[turn][i][1][q * 4 + j], h[j], y);
             }
             if constexpr (MAPS) {
                 sum += s.x;
@@ -196,11 +196,7 @@ int select_scan(const typename E::T *u, int64_t ldu, const typename E::T *dt, in
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (misaligned_to(h0, 4) || misaligned_to(h_last, 4)) return CX_ERR_ALIGN;
     if (h0 != h_last && overlap(h0, state_bytes, h_last, state_bytes)) return CX_ERR_ALIAS;
-    if (T == 0) {
-        if (!h_last || h_last == h0) return CX_OK;
-        hipLaunchKernelGGL(pass_states_kernel, dim3(static_cast<unsigned>(ceil_div(state_bytes / 4, 256))), dim3(256), 0, st, h0, h_last, state_bytes / 4);
-        return launched();
-    }
+    if (T == 0) return pass_through(h0, h_last, state_bytes / 4, st);
     if (!u || !dt || !bm || !cm || !params || !y) return CX_ERR_NULL;
     const int64_t rows = B * T;
     if (bad_strip(rows, ldu, D) || bad_strip(rows, lddt, D) || bad_strip(rows, ldb, N) || bad_strip(rows, ldc, N) || (z && bad_strip(rows, ldz, D)) ||

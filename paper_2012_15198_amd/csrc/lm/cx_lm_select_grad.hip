@@ -40,10 +40,11 @@ __device__ __forceinline__ Reduced reduce_columns(const float (&pb)[NQ], const f
     const int lane = threadIdx.x & 15;
     Reduced r;
     r.which = lane >> 3;
-    if constexpr (NQ == 4) {
+    if constexpr (NQ >= 3) {
         // Two additions a pair: the second value's in all lanes, then the first one's over it in the half of the lanes (banks of four) that keep it.
         // A value is read across lanes two instructions after it was written at the earliest.
-        float b0 = pb[0], b1 = pb[1], b2 = pb[2], b3 = pb[3], c0 = pc[0], c1 = pc[1], c2 = pc[2], c3 = pc[3];
+        const float b0 = pb[0], b1 = pb[1], b2 = pb[2], b3 = NQ > 3 ? pb[NQ - 1] : 0.0f;
+        float c0 = pc[0], c1 = pc[1], c2 = pc[2], c3 = NQ > 3 ? pc[NQ - 1] : 0.0f;
         asm("s_nop 1\n\t"
             "v_add_f32_dpp %0, %0, %0 row_mirror row_mask:0xf bank_mask:0xf\n\t"
             "v_add_f32_dpp %1, %1, %1 row_mirror row_mask:0xf bank_mask:0xf\n\t"
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         else if (a.dh_last) load_states<NQ>(a.dh_last + b * of + state, n0, a.N, any, carry);
     }
     const uint32_t u_at = place_in<T>(a.ldu, es, ec), dt_at = place_in<T>(a.lddt, es, ec), z_at = place_in<T>(a.ldz, es, ec), dy_at = place_in<T>(a.lddy, es, ec);
-    const int bs = threadIdx.x / kMaxStates, bn = threadIdx.x % kMaxStates;          // a thread's element of B and of C
+    const int bs = threadIdx.x / kMaxStates, bp = threadIdx.x % kMaxStates, bn = state_of<NQ>(bp);           // a thread's element of B and of C
     const uint32_t b_at = place_in<T>(a.ldb, bs, bn), c_at = place_in<T>(a.ldc, bs, bn), state_at = (c * a.N) * 4;
     Columns<E, 4> u, dt, z{}, dy;
     T b_next, c_next;
@@ -157,8 +158,8 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
                 parked[2][es][ec + j] = dyj * silu_slope(zj, e);
             }
         }
-        if constexpr (!MAPS) both[bs][0][bn] = E::widen(b_next);
-        both[bs][1][bn] = E::widen(c_next);
+        if constexpr (!MAPS) both[bs][0][bp] = E::widen(b_next);
+        both[bs][1][bp] = E::widen(c_next);
         float h[MAPS ? 1 : kTile + 1][NQ], keep[MAPS ? 1 : kTile][NQ];
         if constexpr (!MAPS)
 #pragma unroll
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
                 const bool cut = RESETS && ((resets >> i) & 1u);
 #pragma unroll
                 for (int j = 0; j < NQ; ++j) {
-                    const float r = __builtin_fmaf(both[i][1][n0 + j], g_i, carry[j]);
+                    const float r = __builtin_fmaf(both[i][1][q * 4 + j], g_i, carry[j]);
                     carry[j] = cut ? 0.0f : exp2_fast(rate[j] * delta_i) * r;
                 }
                 sum += delta_i;
@@ -188,10 +189,10 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
                 float y = 0.0f;
 #pragma unroll
                 for (int j = 0; j < NQ; ++j) {
-                    const float in = s.y * both[i][0][n0 + j];
+                    const float in = s.y * both[i][0][q * 4 + j];
                     keep[i][j] = exp2_fast(rate[j] * s.x);
                     h[i + 1][j] = cut ? in : __builtin_fmaf(keep[i][j], h[i][j], in);
-                    y = __builtin_fmaf(both[i][1][n0 + j], h[i + 1][j], y);
+                    y = __builtin_fmaf(both[i][1][q * 4 + j], h[i + 1][j], y);
                 }
                 four[i % 4] = y;
                 if (i % 4 == 3) out[0][i - 3 + quarter_step(q)][c] = quarters_sum(four);
@@ -205,8 +206,8 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
                 float into = 0.0f, across = 0.0f, pb[NQ], pc[NQ];
 #pragma unroll
                 for (int j = 0; j < NQ; ++j) {
-                    const float r = __builtin_fmaf(both[i][1][n0 + j], g_i, carry[j]);
-                    into = __builtin_fmaf(r, both[i][0][n0 + j], into);
+                    const float r = __builtin_fmaf(both[i][1][q * 4 + j], g_i, carry[j]);
+                    into = __builtin_fmaf(r, both[i][0][q * 4 + j], into);
                     const float moved = cut ? 0.0f : r * (keep[i][j] * h[i][j]);
                     across = __builtin_fmaf(rate[j], moved, across);
                     drate[j] = __builtin_fmaf(s.x, moved, drate[j]);
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
 #pragma unroll
                 for (int j = 0; j < NQ; ++j) asm volatile("" : "+v"(drate[j]));       // summed here: 64 products waiting for it would cost as many registers
                 const Reduced sums = reduce_columns<NQ>(pb, pc);
-                if (sums.holds) shares[wave][i][sums.which][n0 + sums.j] = sums.v;
+                if (sums.holds) shares[wave][i][sums.which][q * 4 + sums.j] = sums.v;
             }
         }
         __syncthreads();
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
                 for (int which = 0; which < 2; ++which) {
                     float v = 0.0f;
 #pragma unroll
-                    for (int k = 0; k < kWaves; ++k) v += shares[k][bs][which][bn];
+                    for (int k = 0; k < kWaves; ++k) v += shares[k][bs][which][bp];
                     share[which * a.N] = v;
                 }
             }
@@ -290,15 +291,16 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
 template <class E>
 __global__ __launch_bounds__(256) void share_kernel(const SelectArgs<E> a)
 {
-    const int64_t of = 2 * static_cast<int64_t>(a.N), all = a.B * a.T_ * of, i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= all) return;
-    float v = 0.0f;
+    const int64_t of = 2 * static_cast<int64_t>(a.N), all = a.B * a.T_ * of;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * 256) {
+        float v = 0.0f;
 #pragma unroll 4
-    for (int k = 0; k < a.slabs; ++k) v += a.shared_parts[k * all + i];
-    const int64_t row = i / of;
-    const int at = static_cast<int>(i - row * of);
-    if (at < a.N) a.dbm[row * a.lddb + at] = E::narrow(v);
-    else a.dcm[row * a.lddc + at - a.N] = E::narrow(v);
+        for (int k = 0; k < a.slabs; ++k) v += a.shared_parts[k * all + i];
+        const int64_t row = i / of;
+        const int at = static_cast<int>(i - row * of);
+        if (at < a.N) a.dbm[row * a.lddb + at] = E::narrow(v);
+        else a.dcm[row * a.lddc + at - a.N] = E::narrow(v);
+    }
 }
 
 constexpr int64_t kAtOnce = 512;                        // workgroups that run at a time: two to a CU, by their registers
@@ -384,11 +386,11 @@ int select_scan_grad(const typename E::T *u, int64_t ldu, const typename E::T *d
             hipLaunchKernelGGL((select_grad_kernel<E, decltype(nq)::value, decltype(resets)::value, kWalk>), dim3(groups, a.spans), dim3(kThreads), 0, st, a);
         });
         if (rc2 != CX_OK) return rc2;
-        hipLaunchKernelGGL(share_kernel<E>, dim3(static_cast<unsigned>(ceil_div(rows * 2 * N, 256))), dim3(256), 0, st, a);
+        const int64_t blocks = ceil_div(rows * 2 * N, 256);
+        hipLaunchKernelGGL(share_kernel<E>, dim3(static_cast<unsigned>(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(256), 0, st, a);
         if (launched() != CX_OK) return CX_ERR_HIP;
-    } else if (dh0 && dh0 != dh_last && B > 0) {
-        hipLaunchKernelGGL(pass_states_kernel, dim3(static_cast<unsigned>(ceil_div(state_bytes / 4, 256))), dim3(256), 0, st, dh_last, dh0, state_bytes / 4);
-        if (launched() != CX_OK) return CX_ERR_HIP;
+    } else if (pass_through(dh_last, dh0, state_bytes / 4, st) != CX_OK) {
+        return CX_ERR_HIP;
     }
     if (none && g_in == g_out) return CX_OK;
     return sum_parts<E>(a.parts, none ? 0 : B / W * a.spans, count, g_in ? g_in + offset : nullptr, g_out + offset, ld, W, st);

@@ -224,6 +224,22 @@ template <class E>
     return launched();
 }
 
+// No steps: the state passes through.
+constexpr int64_t kPassBlocks = 1 << 16;
+template <class T>
+__global__ __launch_bounds__(256) void pass_through_kernel(const T *from, T *to, int64_t n)
+{
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) to[i] = from ? from[i] : static_cast<T>(0);
+}
+template <class T>
+[[maybe_unused]] int pass_through(const T *from, T *to, int64_t n, hipStream_t st)
+{
+    if (!to || to == from || n == 0) return CX_OK;
+    const int64_t blocks = ceil_div(n, 256);
+    hipLaunchKernelGGL(pass_through_kernel<T>, dim3(static_cast<unsigned>(blocks < kPassBlocks ? blocks : kPassBlocks)), dim3(256), 0, st, from, to, n);
+    return launched();
+}
+
 // Pairs of an output and an input that may be the same array, element for element.
 struct Same {
     int out, in;

@@ -70,6 +70,10 @@ __device__ __forceinline__ uint32_t place_in(int64_t ld, int step, int column) {
 template <class E>
 __device__ __forceinline__ void load_four(const typename E::T *p, int left, float (&v)[4]) { widen<E, 4>(load_columns<E, 4>(p, left), v); }
 
+// In LDS the states of a quarter take four places, NQ of them used: whatever NQ is, a lane reads its own in one piece.
+template <int NQ>
+__device__ __forceinline__ int state_of(int place) { return place % 4 < NQ ? place / 4 * NQ + place % 4 : kMaxStates; }
+
 // Lane 16 q + c of a wavefront has quarter q of the states of its column c.  Sums over quarters cross its four rows of 16 lanes.
 // Four steps' sums over the quarters: the one of step quarter_step(q) in quarter q's lanes.
 __device__ __forceinline__ float quarters_sum(const float (&v)[4]) { return add16(add32(v[0], v[1]), add32(v[2], v[3])); }
@@ -171,17 +175,10 @@ template <class E>
     return launched();
 }
 
-// No steps: the state passes through.
-__global__ __launch_bounds__(256) void pass_states_kernel(const float *from, float *to, int64_t n)
-{
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i < n) to[i] = from ? from[i] : 0.0f;
-}
-
 [[maybe_unused]] int check_select(int32_t W, int64_t B, int64_t T, int32_t D, int32_t N)
 {
     return W < 1 || W > CX_MAX_ROWS || B < 0 || B > CX_MAX_SEQUENCES || B % W != 0 || T < 0 || T > kMaxSeq || D < 1 || D > CX_MAX_WIDTH || N < 1 ||
-                   N > kMaxStates || B * D > (int64_t(1) << 31)
+                   N > kMaxStates || B * D > (int64_t(1) << 29)        // a launch has fewer than 2^32 threads, four to a column
                ? CX_ERR_SHAPE
                : CX_OK;
 }
@@ -224,6 +221,7 @@ template <class F>
     };
     if (N <= 4) with(std::integral_constant<int, 1>{});
     else if (N <= 8) with(std::integral_constant<int, 2>{});
+    else if (N <= 12) with(std::integral_constant<int, 3>{});
     else with(std::integral_constant<int, 4>{});
     return launched();
 }

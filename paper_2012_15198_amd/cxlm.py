@@ -36,11 +36,12 @@ _lib = None
 _torch = None
 _dtypes = {}                     # "", "_bf16", "_f16" -> the torch type of the matrices
 _calls = {}                      # name -> the library's function
+_device_now = None               # the current device's number, without torch's check that it is in use
 
 
 def lib() -> ctypes.CDLL:
     """The loaded library; raises if it was not built."""
-    global _lib, _torch
+    global _lib, _torch, _device_now
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -87,6 +88,7 @@ def lib() -> ctypes.CDLL:
         getattr(L, name).restype = ctypes.c_int
         _calls[name] = getattr(L, name)
     _dtypes.update({"": torch.float32, "_bf16": torch.bfloat16, "_f16": torch.float16})
+    _device_now = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _lib, _torch = L, torch
     return L
 
@@ -522,11 +524,9 @@ def cx_distill_step_f16(z, ids, t, labels, gout, loss, dz, tau: float, w_kl: flo
 
 
 # ------------------------------------------------------------------------------------------------- dropout, residual and norm
-def _spread(name, arg, t, dtype, rows, columns, device):
+def _place(name, arg, t, dtype, rows, columns, device):
     """(address, row stride) of a matrix that may be absent."""
-    if t is None:
-        return None, 0
-    return t.data_ptr(), _matrix(name, arg, t, dtype, rows, columns, device)
+    return (None, 0) if t is None else (t.data_ptr(), _matrix(name, arg, t, dtype, rows, columns, device))
 
 
 def _rng(name, rng, p, device):
@@ -542,6 +542,12 @@ def _flat(name, arg, rows, dtype, W, offset, count, device):
     return ld
 
 
+def _workers(rows):
+    """Workers whose flat rows these are; 0 for what is no matrix, which the checks after it name."""
+    shape = rows.shape
+    return shape[0] if len(shape) == 2 else 0
+
+
 def _gradients(name, g_in, g_out, dtype, W, offset, count, device):
     """(address of g_in, address and row stride of g_out) of flat gradient rows."""
     ld = _flat(name, "g_out", g_out, dtype, W, offset, count, device)
@@ -554,8 +560,9 @@ def _gradients(name, g_in, g_out, dtype, W, offset, count, device):
 
 def _current(name, device):
     """Last check before the call: kernels run on the current device."""
-    _on_device(name, device)
-    if device != _torch.cuda.current_device():
+    if device < 0:
+        _on_device(name, device)
+    if device != _device_now():
         raise ValueError(f"{name}: tensors on cuda:{device}, which is not the current device")
 
 
@@ -570,12 +577,13 @@ def _dropout(name, suffix, x, rng, out, p, residual, stream):
     dtype, device = _dtypes[suffix], x.get_device()
     ldx = _matrix(name, "x", x, dtype, None, None, device)
     N, D = x.shape
-    _narrow(name, D)
-    residual_at = _spread(name, "residual", residual, dtype, N, D, device)
+    if D > _INT32:
+        _too_wide(name)
+    rp, ldr = _place(name, "residual", residual, dtype, N, D, device)
     ldo = _matrix(name, "out", out, dtype, N, D, device)
-    rp = _dense(name, "rng", rng, _torch.int64, (2,), device)
+    gp = _dense(name, "rng", rng, _torch.int64, (2,), device)
     _current(name, device)
-    _call(name, x.data_ptr(), ldx, *residual_at, out.data_ptr(), ldo, N, D, rp, p, cxmix._stream(stream))
+    _call(name, x.data_ptr(), ldx, rp, ldr, out.data_ptr(), ldo, N, D, gp, p, cxmix._stream(stream))
 
 
 def cx_dropout(x, rng, out, p: float, residual=None, stream=None):
@@ -591,29 +599,37 @@ def cx_dropout_f16(x, rng, out, p: float, residual=None, stream=None):
     _dropout("cx_dropout_f16", "_f16", x, rng, out, p, residual, stream)
 
 
+def _rows_of_workers(name, rows, W, D):
+    """Rows of each of W workers."""
+    if D > _INT32 or W > _INT32:
+        _too_wide(name)
+    if W == 0 or rows % W:
+        raise ValueError(f"{name}: {rows} rows are not the same number of each of {W} workers")
+    return rows // W
+
+
 def _add_norm(name, suffix, x, residual, weights, offset, s, y, eps, inv, q, scale, p, rng, stream):
     if _lib is None:
         lib()
     dtype, device = _dtypes[suffix], x.get_device()
     ldx = _matrix(name, "x", x, dtype, None, None, device)
     rows, D = x.shape
-    W = weights.shape[0] if len(weights.shape) == 2 else 0
+    W = _workers(weights)
     ldw = _flat(name, "weights", weights, dtype, None, offset, D, device)
-    _narrow(name, D, W)
-    if W == 0 or rows % W:
-        raise ValueError(f"{name}: {rows} rows are not the same number of each of {W} workers")
-    residual_at, s_at, y_at = (_spread(name, arg, t, dtype, rows, D, device) for arg, t in (("residual", residual), ("s", s), ("y", y)))
-    ip = _optional(name, "inv", inv, _torch.float32, (rows,), device)
-    q_at, sp = (None, 0), None
+    N = _rows_of_workers(name, rows, W, D)
+    rp, ldr = _place(name, "residual", residual, dtype, rows, D, device)
+    sp, lds = _place(name, "s", s, dtype, rows, D, device)
+    yp, ldy = _place(name, "y", y, dtype, rows, D, device)
+    ip = None if inv is None else _dense(name, "inv", inv, _torch.float32, (rows,), device)
+    qp, ldq, cp = None, 0, None
     if q is not None or scale is not None:
         if q is None or q.dtype not in (_torch.uint8, _torch.float8_e4m3fn):
             raise ValueError(f"{name}: q: expected uint8 or float8_e4m3fn [{rows}][{D}] beside scale")
-        q_at = _spread(name, "q", q, q.dtype, rows, D, device)
-        sp = _dense(name, "scale", scale, _torch.float32, (rows,), device)
-    rp = _rng(name, rng, p, device)
+        qp, ldq = _place(name, "q", q, q.dtype, rows, D, device)
+        cp = _dense(name, "scale", scale, _torch.float32, (rows,), device)
+    gp = _rng(name, rng, p, device)
     _current(name, device)
-    _call(name, x.data_ptr(), ldx, *residual_at, weights.data_ptr(), ldw, W, offset, rows // W, D, eps, rp, p, *s_at, *y_at, ip, *q_at, sp,
-          cxmix._stream(stream))
+    _call(name, x.data_ptr(), ldx, rp, ldr, weights.data_ptr(), ldw, W, offset, N, D, eps, gp, p, sp, lds, yp, ldy, ip, qp, ldq, cp, cxmix._stream(stream))
 
 
 def cx_add_norm(x, residual, weights, offset: int, s, y, eps: float, inv=None, q=None, scale=None, p: float = 0.0, rng=None, stream=None):
@@ -636,20 +652,21 @@ def _add_norm_grad(name, suffix, dy, s, inv, weights, offset, ds_in, ds, g_in, g
     dtype, device = _dtypes[suffix], dy.get_device()
     lddy = _matrix(name, "dy", dy, dtype, None, None, device)
     rows, D = dy.shape
-    W = weights.shape[0] if len(weights.shape) == 2 else 0
+    W = _workers(weights)
     ldw = _flat(name, "weights", weights, dtype, None, offset, D, device)
-    _narrow(name, D, W)
-    if W == 0 or rows % W:
-        raise ValueError(f"{name}: {rows} rows are not the same number of each of {W} workers")
+    N = _rows_of_workers(name, rows, W, D)
     lds = _matrix(name, "s", s, dtype, rows, D, device)
     ip = _dense(name, "inv", inv, _torch.float32, (rows,), device)
-    in_at, ds_at, dx_at = (_spread(name, arg, t, dtype, rows, D, device) for arg, t in (("ds_in", ds_in), ("ds", ds), ("dx", dx)))
-    grads = _gradients(name, g_in, g_out, dtype, W, offset, D, device)
-    rp = _rng(name, rng, p, device)
+    mp, ldm = _place(name, "ds_in", ds_in, dtype, rows, D, device)
+    sp, ldds = _place(name, "ds", ds, dtype, rows, D, device)
+    xp, lddx = _place(name, "dx", dx, dtype, rows, D, device)
+    gip, gop, ldg = _gradients(name, g_in, g_out, dtype, W, offset, D, device)
+    gp = _rng(name, rng, p, device)
     _current(name, device)
-    work = _scratch(name, workspace, "cx_norm_workspace", (W, rows // W, D), device, stream)
-    _call(name, dy.data_ptr(), lddy, s.data_ptr(), lds, ip, weights.data_ptr(), ldw, W, offset, rows // W, D, *in_at, rp, p, *ds_at, *dx_at, *grads,
-          *_span(work), cxmix._stream(stream))
+    work = _scratch(name, workspace, "cx_norm_workspace", (W, N, D), device, stream)
+    wp, size = _span(work)
+    _call(name, dy.data_ptr(), lddy, s.data_ptr(), lds, ip, weights.data_ptr(), ldw, W, offset, N, D, mp, ldm, gp, p, sp, ldds, xp, lddx, gip, gop, ldg, wp,
+          size, cxmix._stream(stream))
 
 
 def cx_add_norm_grad(dy, s, inv, weights, offset: int, ds_in, ds, g_in, g_out, dx=None, p: float = 0.0, rng=None, workspace=None, stream=None):
@@ -683,7 +700,7 @@ def _short_conv(name, suffix, x, weights, offset, y, T, K, silu, before, after, 
     dtype, device = _dtypes[suffix], x.get_device()
     ldx = _matrix(name, "x", x, dtype, None, None, device)
     rows, D = x.shape
-    W = weights.shape[0] if len(weights.shape) == 2 else 0
+    W = _workers(weights)
     _narrow(name, D, W, K)
     B = _by_worker(name, rows, T, W, before, after)
     ldw = _flat(name, "weights", weights, dtype, None, offset, D * (K + 1), device)
@@ -715,19 +732,19 @@ def _short_conv_grad(name, suffix, x, dy, weights, offset, dx, g_in, g_out, T, K
     dtype, device = _dtypes[suffix], x.get_device()
     ldx = _matrix(name, "x", x, dtype, None, None, device)
     rows, D = x.shape
-    W = weights.shape[0] if len(weights.shape) == 2 else 0
+    W = _workers(weights)
     _narrow(name, D, W, K)
     B = _by_worker(name, rows, T, W, before)
     ldw = _flat(name, "weights", weights, dtype, None, offset, D * (K + 1), device)
     lddy = _matrix(name, "dy", dy, dtype, rows, D, device)
     lddx = _matrix(name, "dx", dx, dtype, rows, D, device)
-    grads = _gradients(name, g_in, g_out, dtype, W, offset, D * (K + 1), device)
+    gip, gop, ldg = _gradients(name, g_in, g_out, dtype, W, offset, D * (K + 1), device)
     bp = _optional(name, "before", before, dtype, (B, K - 1, D), device)
     rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
     _current(name, device)
     work = _scratch(name, workspace, "cx_conv_workspace", (W, B, T, D, K), device, stream)
-    _call(name, x.data_ptr(), ldx, dy.data_ptr(), lddy, weights.data_ptr(), ldw, W, offset, dx.data_ptr(), lddx, *grads, B, T, D, K, int(bool(silu)), rp, bp,
-          *_span(work), cxmix._stream(stream))
+    _call(name, x.data_ptr(), ldx, dy.data_ptr(), lddy, weights.data_ptr(), ldw, W, offset, dx.data_ptr(), lddx, gip, gop, ldg, B, T, D, K, int(bool(silu)),
+          rp, bp, *_span(work), cxmix._stream(stream))
 
 
 def cx_short_conv_grad(x, dy, weights, offset: int, dx, g_in, g_out, T: int, K: int, silu: bool = True, before=None, reset=None,
@@ -762,13 +779,13 @@ def _select_inputs(name, dtype, u, dt, bm, cm, z, params, offset, T, device, *en
     ldb = _matrix(name, "bm", bm, dtype, rows, None, device)
     N = bm.shape[1]
     ldc = _matrix(name, "cm", cm, dtype, rows, N, device)
-    z_at = _spread(name, "z", z, dtype, rows, D, device)
-    W = params.shape[0] if len(params.shape) == 2 else 0
-    _narrow(name, D, W, N)
+    zp, ldz = _place(name, "z", z, dtype, rows, D, device)
+    W = _workers(params)
+    if D > _INT32 or W > _INT32 or N > _INT32:
+        _too_wide(name)
     B = _by_worker(name, rows, T, W, *ends)
     ldp = _flat(name, "params", params, dtype, None, offset, D * (N + 2), device)
-    head = (u.data_ptr(), ldu, dt.data_ptr(), lddt, bm.data_ptr(), ldb, cm.data_ptr(), ldc, *z_at, params.data_ptr(), ldp, W, offset)
-    return head, B, D, N, W
+    return (u.data_ptr(), ldu, dt.data_ptr(), lddt, bm.data_ptr(), ldb, cm.data_ptr(), ldc, zp, ldz, params.data_ptr(), ldp, W, offset), B, D, N, W
 
 
 def _select_scan(name, suffix, u, dt, bm, cm, params, offset, y, T, z, h0, h_last, reset, states, workspace, stream):
@@ -777,13 +794,14 @@ def _select_scan(name, suffix, u, dt, bm, cm, params, offset, y, T, z, h0, h_las
     dtype, device, f32 = _dtypes[suffix], u.get_device(), _torch.float32
     head, B, D, N, _ = _select_inputs(name, dtype, u, dt, bm, cm, z, params, offset, T, device, h0, h_last)
     ldy = _matrix(name, "y", y, dtype, u.shape[0], D, device)
-    hp = _optional(name, "h0", h0, f32, (B, D, N), device)
-    lp = _optional(name, "h_last", h_last, f32, (B, D, N), device)
-    sp = _optional(name, "states", states, f32, (B, -(-T // CX_SCAN_CHUNK), D, N), device)
-    rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
+    hp = None if h0 is None else _dense(name, "h0", h0, f32, (B, D, N), device)
+    lp = None if h_last is None else _dense(name, "h_last", h_last, f32, (B, D, N), device)
+    sp = None if states is None else _dense(name, "states", states, f32, (B, -(-T // CX_SCAN_CHUNK), D, N), device)
+    rp = None if reset is None else _dense(name, "reset", reset, _torch.uint8, (B, T), device)
     _current(name, device)
     work = _scratch(name, workspace, None if T <= 1 else "cx_select_workspace", (B, T, D, N), device, stream)
-    _call(name, *head, y.data_ptr(), ldy, B, T, D, N, rp, hp, lp, sp, *_span(work), cxmix._stream(stream))
+    wp, size = _span(work)
+    _call(name, *head, y.data_ptr(), ldy, B, T, D, N, rp, hp, lp, sp, wp, size, cxmix._stream(stream))
 
 
 def cx_select_scan(u, dt, bm, cm, params, offset: int, y, T: int, z=None, h0=None, h_last=None, reset=None, states=None, workspace=None,
@@ -812,17 +830,21 @@ def _select_scan_grad(name, suffix, u, dt, bm, cm, params, offset, dy, du, ddt, 
     rows = u.shape[0]
     if (z is None) != (dz is None):
         raise ValueError(f"{name}: z and dz go together")
-    outs = [(t.data_ptr(), _matrix(name, arg, t, dtype, rows, columns, device))
-            for arg, t, columns in (("dy", dy, D), ("du", du, D), ("ddt", ddt, D), ("dbm", dbm, N), ("dcm", dcm, N))]
-    dz_at = _spread(name, "dz", dz, dtype, rows, D, device)
-    grads = _gradients(name, g_in, g_out, dtype, W, offset, D * (N + 2), device)
+    lddy = _matrix(name, "dy", dy, dtype, rows, D, device)
+    lddu = _matrix(name, "du", du, dtype, rows, D, device)
+    ldddt = _matrix(name, "ddt", ddt, dtype, rows, D, device)
+    lddb = _matrix(name, "dbm", dbm, dtype, rows, N, device)
+    lddc = _matrix(name, "dcm", dcm, dtype, rows, N, device)
+    zp, lddz = _place(name, "dz", dz, dtype, rows, D, device)
+    gip, gop, ldg = _gradients(name, g_in, g_out, dtype, W, offset, D * (N + 2), device)
     sp = (_dense if T > 0 else _optional)(name, "states", states, f32, (B, -(-T // CX_SCAN_CHUNK), D, N), device)
     lp = _optional(name, "dh_last", dh_last, f32, (B, D, N), device)
     hp = _optional(name, "dh0", dh0, f32, (B, D, N), device)
     rp = _optional(name, "reset", reset, _torch.uint8, (B, T), device)
     _current(name, device)
     work = _scratch(name, workspace, "cx_select_grad_workspace", (B, T, D, N), device, stream)
-    _call(name, *head, *(v for at in outs for v in at), *dz_at, *grads, B, T, D, N, rp, sp, lp, hp, *_span(work), cxmix._stream(stream))
+    _call(name, *head, dy.data_ptr(), lddy, du.data_ptr(), lddu, ddt.data_ptr(), ldddt, dbm.data_ptr(), lddb, dcm.data_ptr(), lddc, zp, lddz, gip, gop, ldg,
+          B, T, D, N, rp, sp, lp, hp, *_span(work), cxmix._stream(stream))
 
 
 def cx_select_scan_grad(u, dt, bm, cm, params, offset: int, dy, du, ddt, dbm, dcm, g_in, g_out, T: int, states, z=None, dz=None,

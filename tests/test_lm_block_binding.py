@@ -82,7 +82,7 @@ def test_dropout_refusals(suffix):
     for p in ("x", "out", "rng"):
         assert call(**{p: None}) == -1, p
     for bad in (dict(N=-1), dict(N=(1 << 31) + 1), dict(D=0), dict(D=lm.CX_MAX_WIDTH + 1), dict(ldx=7), dict(ldr=7), dict(ldo=7), dict(p=-0.1), dict(p=1.0),
-                dict(p=float("nan")), dict(p=0.999999)):
+                dict(p=float("nan")), dict(p=0.999999), dict(N=1 << 30, D=64, ldx=64, ldr=64, ldo=64)):
         assert call(**bad) == -2, bad
     assert call(x=PLACES[0] + 1) == -5 and call(rng=PLACES[3] + 4) == -5
     refuses_overlaps(call, places(call), ["rng"], ["out"], [])
@@ -148,7 +148,8 @@ def test_select_refusals(suffix):
     for p in ("u", "dt", "bm", "cm", "w", "y", "ws"):
         assert call(**{p: None}) == -1, p
     common = (dict(W=0), dict(W=3), dict(B=-2), dict(T=-1), dict(T=lm.CX_MAX_TOKENS + 1), dict(D=0), dict(N=0), dict(N=lm.CX_MAX_STATES + 1, ldb=99, ldc=99), dict(off=-1),
-              dict(off=5), dict(ldu=7), dict(lddt=7), dict(ldb=4), dict(ldc=4), dict(ldz=7), dict(ldu=(1 << 24) + 1), dict(B=2 * lm.CX_MAX_SEQUENCES))
+              dict(off=5), dict(ldu=7), dict(lddt=7), dict(ldb=4), dict(ldc=4), dict(ldz=7), dict(ldu=(1 << 24) + 1), dict(B=2 * lm.CX_MAX_SEQUENCES),
+              dict(B=(1 << 20) + 2, D=512))
     for bad in (*common, dict(ldy=7), dict(wn=lm.cx_select_workspace(4, 400, 8, 5) - 1)):
         assert call(**bad) == -2, bad
     for p in ("u", "dt", "bm", "cm", "z", "w", "y", "h0", "hl", "states", "ws"):
