@@ -70,17 +70,19 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
     float gate[4], direct[4];
     const auto elements = [&](int64_t t0, int turn, float (&gates)[4], float (&directs)[4]) {
         const bool there = es < steps_from(t0);
+        float delta[4], enters[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float uj = value_of<E, 4>(u, j), zj = finite_below(value_of<E, 4>(z, j)), soft = softplus(value_of<E, 4>(dt, j) + bias[j]);
-            const float delta = there ? soft : 0.0f;                    // behind the end: a step that changes nothing
-            step[turn][es][ec + j] = float2{delta, delta * uj};
+            delta[j] = there ? soft : 0.0f;                             // behind the end: a step that changes nothing
+            enters[j] = delta[j] * uj;
             if constexpr (!MAPS) {
                 const float open = zj * sigmoid(zj);
                 directs[j] = skip[j] * uj;
                 gates[j] = a.z ? open : 1.0f;
             }
         }
+        put_pairs(&step[turn][es][ec], delta, enters);
         both[turn][bs][0][bp] = E::widen(b_next);
         if constexpr (!MAPS) both[turn][bs][1][bp] = E::widen(c_next);
     };
@@ -115,9 +117,10 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
         __syncthreads();
         if constexpr (!MAPS) {
             float v[4];
+            get_four(&out[turn][es][ec], v);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[j] = (out[turn][es][ec + j] + direct[j]) * gate[j];
+                v[j] = (v[j] + direct[j]) * gate[j];
                 gate[j] = next_gate[j];
                 direct[j] = next_direct[j];
             }

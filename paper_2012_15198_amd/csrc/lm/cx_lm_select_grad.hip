@@ -143,21 +143,25 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         const int steps = end - t0 < kTile ? static_cast<int>(end - t0) : kTile;
         const unsigned resets = resets_of<RESETS>(a.reset, row0 + t0, steps);
         const bool there = es < steps;
+        float delta[4], enters[4], g[4], own[3][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float v = value_of<E, 4>(dt, j) + bias[j], zj = finite_below(value_of<E, 4>(z, j)), e = sigmoid(zj), dyj = value_of<E, 4>(dy, j);
-            const float delta = there ? softplus(v) : 0.0f;             // behind the end: a step that changes nothing
-            pull[es][ec + j] = a.z ? dyj * (zj * e) : dyj;
-            if constexpr (MAPS) {
-                step[es][ec + j] = float2{delta, 0.0f};
-            } else {
-                const float uj = value_of<E, 4>(u, j);
-                step[es][ec + j] = float2{delta, delta * uj};
-                parked[0][es][ec + j] = uj;
-                parked[1][es][ec + j] = sigmoid(v);
-                parked[2][es][ec + j] = dyj * silu_slope(zj, e);
+            const float v = value_of<E, 4>(dt, j) + bias[j], zj = finite_below(value_of<E, 4>(z, j)), e = sigmoid(zj), dyj = value_of<E, 4>(dy, j), soft = softplus(v);
+            delta[j] = there ? soft : 0.0f;                             // behind the end: a step that changes nothing
+            g[j] = a.z ? dyj * (zj * e) : dyj;
+            enters[j] = 0.0f;
+            if constexpr (!MAPS) {
+                own[0][j] = value_of<E, 4>(u, j);
+                own[1][j] = sigmoid(v);
+                own[2][j] = dyj * silu_slope(zj, e);
+                enters[j] = delta[j] * own[0][j];
             }
         }
+        put_pairs(&step[es][ec], delta, enters);
+        put_four(&pull[es][ec], g);
+        if constexpr (!MAPS)
+#pragma unroll
+            for (int k = 0; k < 3; ++k) put_four(&parked[k][es][ec], own[k]);
         if constexpr (!MAPS) both[bs][0][bp] = E::widen(b_next);
         both[bs][1][bp] = E::widen(c_next);
         float h[MAPS ? 1 : kTile + 1][NQ], keep[MAPS ? 1 : kTile][NQ];
@@ -229,17 +233,22 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         }
         __syncthreads();
         if constexpr (!MAPS) {
-            float du[4], ddt[4], dz[4];
+            float du[4], ddt[4], dz[4], own_u[4], opens[4], slopes[4], g_[4], y[4], into[4], across[4];
+            get_four(&parked[0][es][ec], own_u);
+            get_four(&parked[1][es][ec], opens);
+            get_four(&parked[2][es][ec], slopes);
+            get_four(&pull[es][ec], g_);
+            get_four(&out[0][es][ec], y);
+            get_four(&out[1][es][ec], into);
+            get_four(&out[2][es][ec], across);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float uj = parked[0][es][ec + j], g = pull[es][ec + j], delta = step[es][ec + j].x;
-                const float y = out[0][es][ec + j] + skip[j] * uj, into = out[1][es][ec + j], across = kLn2 * out[2][es][ec + j];
-                du[j] = __builtin_fmaf(delta, into, skip[j] * g);
-                ddt[j] = __builtin_fmaf(uj, into, across) * parked[1][es][ec + j];
-                dz[j] = parked[2][es][ec + j] * y;
+                du[j] = __builtin_fmaf(step[es][ec + j].x, into[j], skip[j] * g_[j]);
+                ddt[j] = __builtin_fmaf(own_u[j], into[j], kLn2 * across[j]) * opens[j];
+                dz[j] = slopes[j] * __builtin_fmaf(skip[j], own_u[j], y[j]);
                 if (there) {
                     dbias[j] += ddt[j];
-                    dskip[j] = __builtin_fmaf(g, uj, dskip[j]);
+                    dskip[j] = __builtin_fmaf(g_[j], own_u[j], dskip[j]);
                 }
             }
             const int64_t row = row0 + t0;

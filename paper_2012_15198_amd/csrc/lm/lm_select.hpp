@@ -70,6 +70,22 @@ __device__ __forceinline__ uint32_t place_in(int64_t ld, int step, int column) {
 template <class E>
 __device__ __forceinline__ void load_four(const typename E::T *p, int left, float (&v)[4]) { widen<E, 4>(load_columns<E, 4>(p, left), v); }
 
+// Four neighbours in LDS in one piece: four writes of one would meet in the same banks.
+typedef float f4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void put_four(float *p, const float (&v)[4]) { *reinterpret_cast<f4 *>(p) = f4{v[0], v[1], v[2], v[3]}; }
+__device__ __forceinline__ void get_four(const float *p, float (&v)[4])
+{
+    const f4 w = *reinterpret_cast<const f4 *>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = w[j];
+}
+__device__ __forceinline__ void put_pairs(float2 *p, const float (&x)[4], const float (&y)[4])
+{
+    f4 *to = reinterpret_cast<f4 *>(p);
+    to[0] = f4{x[0], y[0], x[1], y[1]};
+    to[1] = f4{x[2], y[2], x[3], y[3]};
+}
+
 // In LDS the states of a quarter take four places, NQ of them used: whatever NQ is, a lane reads its own in one piece.
 template <int NQ>
 __device__ __forceinline__ int state_of(int place) { return place % 4 < NQ ? place / 4 * NQ + place % 4 : kMaxStates; }
