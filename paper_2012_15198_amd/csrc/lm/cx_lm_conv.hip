@@ -26,6 +26,7 @@ struct ConvArgs {
     int64_t span, spans;                                // steps of a lane's walk; spans of a sequence, rounded up to whole workgroups
     int32_t D, shift, slabs;                            // 1 << shift lanes beside each other
     bool silu;
+    bool shared_ends;                                   // the last lane begins C columns before the end of the row: what it has in common with the one before both compute
 };
 
 template <class E, int C, int K>
@@ -109,6 +110,7 @@ __device__ __forceinline__ Place place_of(const ConvArgs<E> &a)
     p.end = p.begin + a.span < a.T_ ? p.begin + a.span : a.T_;
     p.column = ((slab << a.shift) + lane) * C;
     p.any = p.begin < a.T_ && p.column < a.D && p.b < a.B;
+    if (a.shared_ends && p.column < a.D && p.column > a.D - C) p.column = a.D - C;
     return p;
 }
 
@@ -289,6 +291,8 @@ struct Walk {
 
 constexpr int64_t kWalks = 1 << 18;                     // lanes that fill the card
 
+constexpr int64_t kLeastSteps = 8, kLeastGradSteps = 32, kFewWalks = 1 << 15;
+
 Walk walk_of(int64_t B, int64_t T, int32_t D, int columns, int64_t least)
 {
     Walk w{};
@@ -297,6 +301,7 @@ Walk walk_of(int64_t B, int64_t T, int32_t D, int columns, int64_t least)
     w.slabs = static_cast<int>(ceil_div(lanes, 1 << w.shift));
     const int64_t wanted = ceil_div(kWalks, B * lanes);
     const int64_t span = ceil_div(T, wanted);
+    if (B * lanes * ceil_div(T, least) < kFewWalks) least = kLeastSteps;       // too few to hide a step's loads
     w.span = round_up(span < least ? (T < least ? T : least) : span, kAhead);
     const int64_t spans = ceil_div(T, w.span);
     w.together = kThreads >> w.shift;
@@ -305,7 +310,6 @@ Walk walk_of(int64_t B, int64_t T, int32_t D, int columns, int64_t least)
     w.spans = w.groups * w.together;
     return w;
 }
-constexpr int64_t kLeastSteps = 8, kLeastGradSteps = 32;
 constexpr int kGradColumns = 4;                         // columns of a lane
 
 int check_conv(int32_t W, int64_t B, int64_t T, int32_t D, int32_t K)
@@ -374,6 +378,7 @@ int conv(const typename E::T *x, int64_t ldx, const typename E::T *weights, int6
     a.x = x; a.ldx = ldx; a.weights = weights + offset; a.ldw = ld; a.y = y; a.ldy = ldy; a.before = before; a.after = after; a.reset = reset;
     a.B = B; a.T_ = T; a.per_worker = static_cast<uint32_t>(B / W); a.D = D; a.silu = silu != 0;
     set_walk(a, w);
+    a.shared_ends = D >= kForward && !(before && before == after);      // a state in place has one reader and writer
     if (T == 1) {
         a.slabs = static_cast<int32_t>(ceil_div(ceil_div(D, kForward), kWave));
         return by_taps(K, [&](auto k) {
@@ -419,6 +424,7 @@ int conv_grad(const typename E::T *x, int64_t ldx, const typename E::T *dy, int6
         a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.weights = weights + offset; a.ldw = ldw; a.dx = dx; a.lddx = lddx; a.before = before;
         a.reset = reset; a.parts = parts; a.B = B; a.T_ = T; a.per_worker = static_cast<uint32_t>(B / W); a.D = D; a.silu = silu != 0;
         set_walk(a, w);
+        a.shared_ends = D >= kGradColumns;
         const int rc2 = by_taps(K, [&](auto k) {
             if (reset) hipLaunchKernelGGL((conv_grad_kernel<E, kGradColumns, decltype(k)::value, true>), grid_of(w, B), dim3(w.together << w.shift), 0, st, a);
             else hipLaunchKernelGGL((conv_grad_kernel<E, kGradColumns, decltype(k)::value, false>), grid_of(w, B), dim3(w.together << w.shift), 0, st, a);

@@ -49,7 +49,8 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
         if (a.spans > 1) load_states<NQ>(a.maps + (b * a.pieces + span * parts) * of + state, n0, a.N, any, h);
         else if (a.h0) load_states<NQ>(a.h0 + b * of + state, n0, a.N, any, h);
     }
-    const uint32_t u_at = place_in<T>(a.ldu, es, ec), dt_at = place_in<T>(a.lddt, es, ec), z_at = place_in<T>(a.ldz, es, ec), y_at = place_in<T>(a.ldy, es, ec);
+    const int back = back_of<E>(left, a.D), first = ec - back + kEach;      // of loads, from kEach columns before the slab's on
+    const uint32_t u_at = place_in<T>(a.ldu, es, first), dt_at = place_in<T>(a.lddt, es, first), z_at = place_in<T>(a.ldz, es, first), y_at = place_in<T>(a.ldy, es, ec);
     const int bs = threadIdx.x / kMaxStates, bp = threadIdx.x % kMaxStates, bn = state_of<NQ>(bp);           // a thread's element of B and of C
     const uint32_t b_at = place_in<T>(a.ldb, bs, bn), c_at = place_in<T>(a.ldc, bs, bn), state_at = (c * a.N) * 4;
     const auto steps_from = [&](int64_t t0) { return end - t0 >= kTile ? kTile : end > t0 ? static_cast<int>(end - t0) : 0; };
@@ -59,17 +60,20 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
         const int64_t row = row0 + t0;
         const int steps = steps_from(t0), there = es < steps ? left : 0;
         const bool has = bn < a.N && bs < steps;
-        u = load_columns<E, 4>(at_byte(a.u + row * a.ldu + column0, u_at), there);
-        dt = load_columns<E, 4>(at_byte(a.dt + row * a.lddt + column0, dt_at), there);
+        u = load_back<E>(at_byte(a.u + row * a.ldu + column0 - kEach, u_at), there, back);
+        dt = load_back<E>(at_byte(a.dt + row * a.lddt + column0 - kEach, dt_at), there, back);
         b_next = has ? *at_byte(a.bm + row * a.ldb, b_at) : 0;
         if constexpr (!MAPS) {
-            if (a.z) z = load_columns<E, 4>(at_byte(a.z + row * a.ldz + column0, z_at), there);
+            if (a.z) z = load_back<E>(at_byte(a.z + row * a.ldz + column0 - kEach, z_at), there, back);
             c_next = has ? *at_byte(a.cm + row * a.ldc, c_at) : 0;
         }
     };
     float gate[4], direct[4];
     const auto elements = [&](int64_t t0, int turn, float (&gates)[4], float (&directs)[4]) {
         const bool there = es < steps_from(t0);
+        settle<E>(u, back);
+        settle<E>(dt, back);
+        if constexpr (!MAPS) settle<E>(z, back);
         float delta[4], enters[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

@@ -117,7 +117,8 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         if (a.spans > 1) load_states<NQ>(a.maps + (b * a.pieces + span * parts + parts - 1) * of + state, n0, a.N, any, carry);
         else if (a.dh_last) load_states<NQ>(a.dh_last + b * of + state, n0, a.N, any, carry);
     }
-    const uint32_t u_at = place_in<T>(a.ldu, es, ec), dt_at = place_in<T>(a.lddt, es, ec), z_at = place_in<T>(a.ldz, es, ec), dy_at = place_in<T>(a.lddy, es, ec);
+    const int back = back_of<E>(left, a.D), first = ec - back + kEach;      // of loads, from kEach columns before the slab's on
+    const uint32_t u_at = place_in<T>(a.ldu, es, first), dt_at = place_in<T>(a.lddt, es, first), z_at = place_in<T>(a.ldz, es, first), dy_at = place_in<T>(a.lddy, es, first);
     const int bs = threadIdx.x / kMaxStates, bp = threadIdx.x % kMaxStates, bn = state_of<NQ>(bp);           // a thread's element of B and of C
     const uint32_t b_at = place_in<T>(a.ldb, bs, bn), c_at = place_in<T>(a.ldc, bs, bn), state_at = (c * a.N) * 4;
     Columns<E, 4> u, dt, z{}, dy;
@@ -127,12 +128,12 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         const int64_t row = row0 + t0;
         const int steps = end - t0 < kTile ? static_cast<int>(end - t0) : kTile, there = es < steps ? left : 0;
         const bool has = bn < a.N && bs < steps;
-        dt = load_columns<E, 4>(at_byte(a.dt + row * a.lddt + column0, dt_at), there);
-        dy = load_columns<E, 4>(at_byte(a.dy + row * a.lddy + column0, dy_at), there);
-        if (a.z) z = load_columns<E, 4>(at_byte(a.z + row * a.ldz + column0, z_at), there);
+        dt = load_back<E>(at_byte(a.dt + row * a.lddt + column0 - kEach, dt_at), there, back);
+        dy = load_back<E>(at_byte(a.dy + row * a.lddy + column0 - kEach, dy_at), there, back);
+        if (a.z) z = load_back<E>(at_byte(a.z + row * a.ldz + column0 - kEach, z_at), there, back);
         c_next = has ? *at_byte(a.cm + row * a.ldc, c_at) : 0;
         if constexpr (!MAPS) {
-            u = load_columns<E, 4>(at_byte(a.u + row * a.ldu + column0, u_at), there);
+            u = load_back<E>(at_byte(a.u + row * a.ldu + column0 - kEach, u_at), there, back);
             b_next = has ? *at_byte(a.bm + row * a.ldb, b_at) : 0;
             load_states<NQ>(at_byte(a.states_in + (b * chunks + t0 / kTile) * of + static_cast<int64_t>(column0) * a.N, state_at), n0, a.N, any, entering);
         }
@@ -143,6 +144,10 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         const int steps = end - t0 < kTile ? static_cast<int>(end - t0) : kTile;
         const unsigned resets = resets_of<RESETS>(a.reset, row0 + t0, steps);
         const bool there = es < steps;
+        settle<E>(dt, back);
+        settle<E>(dy, back);
+        settle<E>(z, back);
+        if constexpr (!MAPS) settle<E>(u, back);
         float delta[4], enters[4], g[4], own[3][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

@@ -67,6 +67,25 @@ template <class T>
 __device__ __forceinline__ uint32_t place_in(int64_t ld, int step, int column) { return (static_cast<uint32_t>(step) * static_cast<uint32_t>(ld) + column) * sizeof(T); }
 [[maybe_unused]] bool bad_strip(int64_t rows, int64_t ld, int64_t columns) { return bad_matrix(rows, ld, columns) || ld > kMaxPitch; }
 
+// Where a row of 16-bit elements ends inside a thread's four, they are read as the row's last four and moved into place where they are used: element by
+// element the halves would be waited for to be put together.
+template <class E>
+__device__ __forceinline__ int back_of(int left, int D) { return sizeof(typename E::T) == 2 && left > 0 && left < kEach && D >= kEach ? kEach - left : 0; }
+template <class E>
+__device__ __forceinline__ Columns<E, 4> load_back(const typename E::T *p, int left, int back)
+{
+    return load_columns<E, 4>(p, left > 0 ? left + back : 0);
+}
+template <class E>
+__device__ __forceinline__ void settle(Columns<E, 4> &r, int back)
+{
+    if constexpr (sizeof(typename E::T) == 2) {
+        const uint64_t v = (static_cast<uint64_t>(r.w[1]) << 32 | r.w[0]) >> (16 * back);
+        r.w[0] = static_cast<unsigned>(v);
+        r.w[1] = static_cast<unsigned>(v >> 32);
+    }
+}
+
 template <class E>
 __device__ __forceinline__ void load_four(const typename E::T *p, int left, float (&v)[4]) { widen<E, 4>(load_columns<E, 4>(p, left), v); }
 
@@ -206,13 +225,13 @@ struct Spans {
 
 // Into how many spans the steps are split: as many as make the rounds of `at_once` workgroups take least, in tiles, with a quarter for the maps' launch
 // where there is one.  Spans have at least kLeastTiles tiles.
-constexpr int64_t kLeastTiles = 4, kMostSpans = 256, kMapsAtOnce = 1536;
+constexpr int64_t kLeastTiles = 2, kMostSpans = 256, kMapsAtOnce = 1536;
 [[maybe_unused]] Spans spans_of(int64_t B, int64_t T, int32_t D, int64_t at_once)
 {
     const int64_t slabs = ceil_div(D, kColumns), groups = B * slabs, tiles = ceil_div(T, kTile);
     int64_t best = 1, least = 4 * ceil_div(groups, at_once) * tiles;
     for (int64_t spans = 2; spans <= kMostSpans && spans * kLeastTiles <= tiles && groups < 8 * at_once; ++spans) {
-        const int64_t each = ceil_div(tiles, spans), cost = 4 * ceil_div(groups * spans, at_once) * each + ceil_div(groups * (spans - 1), at_once) * each + spans;
+        const int64_t each = ceil_div(tiles, spans), cost = 4 * ceil_div(groups * spans, at_once) * each + ceil_div(groups * (spans - 1), at_once) * each + spans / 4;
         if (cost < least) {
             least = cost;
             best = spans;

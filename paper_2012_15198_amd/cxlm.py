@@ -11,6 +11,7 @@ allocator, for the current stream.  A call on another stream by handle brings it
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 from . import cxmix
@@ -180,6 +181,7 @@ def _span(work):
     return (None, 0) if work is None else (work.data_ptr(), work.numel())
 
 
+@functools.lru_cache(maxsize=1024)                       # a training step asks for the same few sizes again: 1 us of a call's 8
 def _size(fn, *args) -> int:
     L = _lib or lib()
     if max(args) > _INT32 or min(args) < -_INT32:        # the 64-bit ones have limits below 2^31 too
