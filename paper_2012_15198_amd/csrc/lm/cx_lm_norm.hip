@@ -7,8 +7,8 @@
 // A row stays in the registers of a group of lanes between its statistics and its results, so that each matrix is read and
 // written once.  A lane holds up to four times eight columns; groups are a power of two of lanes.
 //
-// Bound by memory: 65,536 rows of 768 in bfloat16 take 81 us with dropout (4.9 TB/s), their gradient 107 and 5 for the sums of its parts (4.7 TB/s), dropout
-// alone 48 (6.3 TB/s); 8,192 rows of 2,048 to 8 bits 25 (4.7 TB/s).  Tried for the gradient and not kept: the next row's loads ahead (103 to 133), rows
+// Bound by memory: 65,536 rows of 768 in bfloat16 take 73 us with dropout (5.5 TB/s), their gradient 107 and 5 for the sums of its parts (4.7 TB/s), dropout
+// alone 48 (6.3 TB/s); 8,192 rows of 2,048 to 8 bits 22 (5.4 TB/s).  Tried for the gradient and not kept: the next row's loads ahead (103 to 133), rows
 // widened twice to that end (spills), results past the caches (110).
 #include "lm_block.hpp"
 
@@ -17,6 +17,10 @@ namespace {
 constexpr int kThreads = 256, kMaxLanes = 512, kMaxEights = 4;
 constexpr int64_t kMaxRows = int64_t(1) << 31, kMaxGroups = int64_t(1) << 24;       // a launch has fewer than 2^32 threads
 constexpr float kLargest8 = 448.0f, kLeastScale = 0x1p-126f;
+
+// What is read once goes past the caches, of 16-bit rows: a lane's eight float32 columns are two reads of half of each line.
+template <class E>
+constexpr bool kPast = sizeof(typename E::T) == 2;
 
 // ---------------------------------------------------------------------------------
 // Dropout alone
@@ -52,8 +56,8 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const DropArgs<E> a)
         row[k] = row0 + q;
         column[k] = static_cast<int>(at - q * a.eights) * 8;
         if (row[k] < a.rows) {
-            x[k] = load_columns<E, 8, true>(a.x + row[k] * a.ldx + column[k], a.D - column[k]);
-            if (a.residual) r[k] = load_columns<E, 8, true>(a.residual + row[k] * a.ldr + column[k], a.D - column[k]);
+            x[k] = load_columns<E, 8, kPast<E>>(a.x + row[k] * a.ldx + column[k], a.D - column[k]);
+            if (a.residual) r[k] = load_columns<E, 8, kPast<E>>(a.residual + row[k] * a.ldr + column[k], a.D - column[k]);
         }
     }
 #pragma unroll
@@ -141,7 +145,8 @@ __device__ __forceinline__ unsigned row_max(unsigned v, int shift, float (&lds)[
     return v;
 }
 
-template <class E, int V, bool DROP>
+// LARGE: the matrices are beyond the caches, which are passed by.
+template <class E, int V, bool DROP, bool LARGE>
 __global__ __launch_bounds__(kMaxLanes) void norm_kernel(const NormArgs<E> a)
 {
     __shared__ float lds[2][kMaxLanes / kWave];
@@ -154,9 +159,9 @@ __global__ __launch_bounds__(kMaxLanes) void norm_kernel(const NormArgs<E> a)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int column = (v * lanes + lane) * 8, left = here ? a.D - column : 0;
-        const Columns<E, 8> xs = load_columns<E, 8, true>(a.x + row * a.ldx + column, left);
+        const Columns<E, 8> xs = load_columns<E, 8, LARGE>(a.x + row * a.ldx + column, left);
         Columns<E, 8> rs;
-        if (a.residual) rs = load_columns<E, 8, true>(a.residual + row * a.ldr + column, left);
+        if (a.residual) rs = load_columns<E, 8, LARGE>(a.residual + row * a.ldr + column, left);
         widen<E, 8>(xs, s[v]);
         if constexpr (DROP)
             if (left > 0) drop(random_block(a.d.rng[0], a.d.rng[1], static_cast<uint64_t>(row) * a.eights + column / 8), a.d.border, a.d.scale, s[v]);
@@ -166,7 +171,7 @@ __global__ __launch_bounds__(kMaxLanes) void norm_kernel(const NormArgs<E> a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[v][j] = f[j] + s[v][j];
         }
-        if (a.s && left > 0) store_columns<E, 8>(a.s + row * a.lds + column, left, s[v]);
+        if (a.s && left > 0) store_columns<E, 8, LARGE>(a.s + row * a.lds + column, left, s[v]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) squares = __builtin_fmaf(s[v][j], s[v][j], squares);
     }
@@ -185,7 +190,7 @@ __global__ __launch_bounds__(kMaxLanes) void norm_kernel(const NormArgs<E> a)
             const unsigned u = __float_as_uint(s[v][j]) & 0x7fffffffu;        // ordered like the magnitudes, NaN above infinity
             if (j < left) high = u > high ? u : high;
         }
-        if (a.y && left > 0) store_columns<E, 8>(a.y + row * a.ldy + column, left, s[v]);
+        if (a.y && left > 0) store_columns<E, 8, LARGE>(a.y + row * a.ldy + column, left, s[v]);
     }
     if (!a.q) return;
     const float most = __uint_as_float(row_max(high, a.shift, lds, 1)), whole = most / kLargest8;
@@ -234,8 +239,8 @@ __global__ __launch_bounds__(kMaxLanes) void norm_grad_kernel(const NormArgs<E> 
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int column = (v * lanes + lane) * 8, left = here ? a.D - column : 0;
-            const Columns<E, 8> ss = load_columns<E, 8, true>(a.s_in + row * a.lds + column, left), ds = load_columns<E, 8, true>(a.dy + row * a.lddy + column, left);
-            if (a.ds_in) more[v] = load_columns<E, 8, true>(a.ds_in + row * a.ldi + column, left);
+            const Columns<E, 8> ss = load_columns<E, 8, kPast<E>>(a.s_in + row * a.lds + column, left), ds = load_columns<E, 8, kPast<E>>(a.dy + row * a.lddy + column, left);
+            if (a.ds_in) more[v] = load_columns<E, 8, kPast<E>>(a.ds_in + row * a.ldi + column, left);
             float f[8];
             widen<E, 8>(ss, unit[v]);
             widen<E, 8>(ds, g[v]);
@@ -293,17 +298,18 @@ struct Layout {
     int shift, eights, threads;                         // lanes of a row as a power of two, eights of a lane
 };
 
-// The forward pass gives a lane one eight of columns where a row has no more than 4,096: 32 rows of 1,024 take 3.4 us in bfloat16 against 4.9 with four
-// of 32 lanes, 4,000 float32 rows of 515 10.0 against 11.7, 65,536 rows of 768 83 against 81.  The gradient keeps sums of its columns over rows and takes
-// the fewest idle places: the last takes 107 us with three eights of 32 lanes, 120 with one of 128, the second 15.5 and 14.3.
-Layout layout_of(int32_t D, bool gradient)
+// Two layouts: one eight of columns to a lane where a row has no more than 4,096, and the fewest idle places.  The first is the forward pass's: 32 rows
+// of 1,024 take 3.4 us in bfloat16 against 4.9, 4,000 float32 rows of 515 9.4 against 10.6.  The gradient keeps sums of its columns over rows and takes the
+// second: 65,536 rows of 768 in bfloat16 107 us with three eights of 32 lanes, 120 with one of 128.  So does a forward pass of matrices beyond the caches, with
+// its reads and results past them: the same rows 73 us against 81, 34,080 rows of 1,266 70 against 87, but 8,192 rows of 2,048 to 8 bits, 117 MB, 26.6 against 21.8.
+Layout layout_of(int32_t D, bool fewest)
 {
     const int n = static_cast<int>(ceil_div(D, 8));
     Layout best{};
     int least = 1 << 30;
     for (int shift = 1; (1 << shift) <= kMaxLanes; ++shift) {
         const int each = static_cast<int>(ceil_div(n, 1 << shift));
-        if (each > (!gradient && n <= kMaxLanes ? 1 : kMaxEights)) continue;
+        if (each > (!fewest && n <= kMaxLanes ? 1 : kMaxEights)) continue;
         if ((each << shift) < least) {
             least = each << shift;
             best = {shift, each, (1 << shift) > kThreads ? 1 << shift : kThreads};
@@ -312,6 +318,7 @@ Layout layout_of(int32_t D, bool gradient)
     return best;
 }
 
+constexpr int64_t kCaches = 256 << 20;                  // bytes
 constexpr int64_t kParts = 1024;                        // workgroups of a gradient
 
 int64_t parts_of(int32_t W, int64_t N, int32_t D)
@@ -365,13 +372,19 @@ int add_norm(const typename E::T *x, int64_t ldx, const typename E::T *residual,
                            dense_of(q ? scale : nullptr, rows * 4)};
     const Same same[3] = {{0, 0}, {0, 1}, {1, 0}};
     if (outputs_share_but(in, out, same)) return CX_ERR_ALIAS;
-    const Layout l = layout_of(D, false);
+    const int64_t bytes = rows * D * (kElem * (1 + (residual != nullptr) + (s != nullptr) + (y != nullptr)) + (q != nullptr));
+    const bool large = kElem == 2 && bytes >= kCaches;
+    const Layout l = layout_of(D, large);
     a.x = x; a.ldx = ldx; a.residual = residual; a.ldr = ldr; a.weights = weights + offset; a.ldw = ld; a.s = s; a.lds = lds; a.y = y; a.ldy = ldy;
     a.inv = inv; a.q = q; a.ldq = ldq; a.scale = scale; a.N = N; a.D = D; a.eights = static_cast<int32_t>(ceil_div(D, 8)); a.shift = l.shift; a.eps = eps;
     const int64_t blocks = ceil_div(N, l.threads >> l.shift), wide = blocks < (1 << 22) ? blocks : 1 << 22;
     const dim3 grid(static_cast<unsigned>(wide), W, static_cast<unsigned>(ceil_div(blocks, wide)));
     return by_layout<E>(l, a.d.border != 0, [&](auto v, auto drops) {
-        hipLaunchKernelGGL((norm_kernel<E, decltype(v)::value, decltype(drops)::value>), grid, dim3(l.threads), 0, static_cast<hipStream_t>(stream), a);
+        constexpr bool kMayBe = kElem == 2;
+        if (kMayBe && large)
+            hipLaunchKernelGGL((norm_kernel<E, decltype(v)::value, decltype(drops)::value, kMayBe>), grid, dim3(l.threads), 0, static_cast<hipStream_t>(stream), a);
+        else
+            hipLaunchKernelGGL((norm_kernel<E, decltype(v)::value, decltype(drops)::value, false>), grid, dim3(l.threads), 0, static_cast<hipStream_t>(stream), a);
     });
 }
 

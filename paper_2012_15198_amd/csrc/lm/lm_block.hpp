@@ -63,18 +63,25 @@ __device__ __forceinline__ void widen(const Columns<E, C> &r, float (&v)[C])
 #pragma unroll
     for (int j = 0; j < C; ++j) v[j] = value_of<E, C>(r, j);
 }
-template <class E, int C>
+// THROUGH: past the caches, for results so large that none keeps them for their reader.
+template <class E, int C, bool THROUGH = false>
 __device__ __forceinline__ void store_columns(typename E::T *p, int left, const float (&v)[C])
 {
+    const auto put = [](typename E::T *to, const u4 &w) {
+        if constexpr (THROUGH) store16_through<E>(to, w);
+        else store16<E>(to, w);
+    };
     if (left >= C) {
         if constexpr (sizeof(typename E::T) == 4) {
 #pragma unroll
             for (int k = 0; k < C / 4; ++k)
-                store16<E>(p + 4 * k, u4{__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3])});
+                put(p + 4 * k, u4{__float_as_uint(v[4 * k]), __float_as_uint(v[4 * k + 1]), __float_as_uint(v[4 * k + 2]), __float_as_uint(v[4 * k + 3])});
         } else if constexpr (C == 4) {
-            *reinterpret_cast<u2_at2 *>(p) = u2{E::two(v[0], v[1]), E::two(v[2], v[3])};
+            const u2 w{E::two(v[0], v[1]), E::two(v[2], v[3])};
+            if constexpr (THROUGH) __builtin_nontemporal_store(w, reinterpret_cast<u2_at2 *>(p));
+            else *reinterpret_cast<u2_at2 *>(p) = w;
         } else {
-            store16<E>(p, E::pack(v));
+            put(p, E::pack(v));
         }
     } else {
 #pragma unroll
