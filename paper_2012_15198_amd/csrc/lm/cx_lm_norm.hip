@@ -7,7 +7,7 @@
 // A row stays in the registers of a group of lanes between its statistics and its results, so that each matrix is read and
 // written once.  A lane holds up to four times eight columns; groups are a power of two of lanes.
 //
-// Bound by memory: 65,536 rows of 768 in bfloat16 take 73 us with dropout (5.5 TB/s), their gradient 107 and 5 for the sums of its parts (4.7 TB/s), dropout
+// Bound by memory: 65,536 rows of 768 in bfloat16 take 73 us with dropout (5.5 TB/s), their gradient 103 to 119, by how warm the card is, and 5 for the sums of its parts (4.9 to 4.2 TB/s), dropout
 // alone 48 (6.3 TB/s); 8,192 rows of 2,048 to 8 bits 22 (5.4 TB/s).  Tried for the gradient and not kept: the next row's loads ahead (103 to 133), rows
 // widened twice to that end (spills), results past the caches (110).
 #include "lm_block.hpp"
@@ -319,12 +319,13 @@ Layout layout_of(int32_t D, bool fewest)
 }
 
 constexpr int64_t kCaches = 256 << 20;                  // bytes
-constexpr int64_t kParts = 1024;                        // workgroups of a gradient
+// Workgroups of a gradient: what the card takes at once, by the registers of three or four eights (34,080 rows of 1,266 101 us with 512, 115 with 1,024).
+constexpr int64_t kParts = 512, kPartsOfFew = 1024;
 
 int64_t parts_of(int32_t W, int64_t N, int32_t D)
 {
     const Layout l = layout_of(D, true);
-    const int64_t groups = l.threads >> l.shift, most = ceil_div(N, groups), wanted = ceil_div(kParts, W);
+    const int64_t groups = l.threads >> l.shift, most = ceil_div(N, groups), wanted = ceil_div(l.eights > 2 ? kParts : kPartsOfFew, W);
     const int64_t rows = ceil_div(ceil_div(N, wanted < most ? wanted : most), groups) * groups;
     return ceil_div(N, rows);
 }
