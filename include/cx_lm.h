@@ -231,7 +231,8 @@ int cx_dropout_f16(const uint16_t *x, int64_t ldx, const uint16_t *residual, int
  *   s, y     the same or NULL; s may be x or residual, y may be x;  inv: float [W * N] or NULL, which the gradient needs
  *   q, scale bytes [W * N][ldq], D columns, with float [W * N]; or both NULL.  One of s, y and q at least is wanted
  * 0 <= eps < infinity.  Squares whose sum leaves float32's range make inv and the row's y 0; an infinity's own y is NaN.  A NaN in a row makes
- * all of its y NaN, and so does eps = 0 in a row of zeros.  A NaN among a row's y makes its scale and its q NaN.
+ * all of its y NaN, and so does eps = 0 in a row of zeros.  A NaN among a row's y makes its scale and its q NaN; an infinite y
+ * without one an infinite scale, q NaN in its place and 0 elsewhere.
  */
 int cx_add_norm(const float *x, int64_t ldx, const float *residual, int64_t ldr, const float *weights, int64_t ldw, int32_t W,
                 int64_t offset, int64_t N, int32_t D, float eps, const int64_t *rng, float p, float *s, int64_t lds, float *y, int64_t ldy,
