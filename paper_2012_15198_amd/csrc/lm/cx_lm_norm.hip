@@ -7,9 +7,10 @@
 // A row stays in the registers of a group of lanes between its statistics and its results, so that each matrix is read and
 // written once.  A lane holds up to four times eight columns; groups are a power of two of lanes.
 //
-// Bound by memory: 65,536 rows of 768 in bfloat16 take 73 us with dropout (5.5 TB/s), their gradient 103 to 119, by how warm the card is, and 5 for the sums of its parts (4.9 to 4.2 TB/s), dropout
-// alone 48 (6.3 TB/s); 8,192 rows of 2,048 to 8 bits 22 (5.4 TB/s).  Tried for the gradient and not kept: the next row's loads ahead (103 to 133), rows
-// widened twice to that end (spills), results past the caches (110).
+// Bound by memory: 65,536 rows of 768 in bfloat16 take 73 us with dropout (5.5 TB/s), their gradient 103 to 119, by how warm the card is, and 5 for the
+// sums of its parts (4.9 to 4.2 TB/s), dropout alone 48 (6.3 TB/s); 8,192 rows of 2,048 to 8 bits 22 (two sets of operands by turns, 234 MB, of which the
+// last level of the caches keeps a part).  Tried for the gradient and not kept: the next row's loads ahead (103 to 133), rows widened twice to that end
+// (spills), results past the caches (110).
 #include "lm_block.hpp"
 
 namespace {
