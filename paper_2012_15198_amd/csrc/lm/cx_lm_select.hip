@@ -42,7 +42,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
     bool gone = false;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        rate[i] = any && n0 + i < a.N ? -kLog2e * exp2_fast(kLog2e * E::widen(params[state + n0 + i])) : 0.0f;
+        rate[i] = any && n0 + i < a.N ? rate_of(E::widen(params[state + n0 + i])) : 0.0f;
         h[i] = 0.0f;
     }
     if constexpr (!MAPS) {
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void select_step_kernel(const SelectArgs<
     float y = 0.0f;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        const float rate = i < here ? -kLog2e * exp2_fast(kLog2e * value_of<E, 4>(logs, i)) : 0.0f, in = i < here ? delta * u * value_of<E, 4>(bs, i) : 0.0f;
+        const float rate = i < here ? rate_of(value_of<E, 4>(logs, i)) : 0.0f, in = i < here ? delta * u * value_of<E, 4>(bs, i) : 0.0f;
         h[i] = cut ? in : __builtin_fmaf(exp2_fast(rate * delta), h[i], in);
         y = __builtin_fmaf(i < here ? value_of<E, 4>(cs, i) : 0.0f, h[i], y);
     }

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
     bool gone = false;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        rate[i] = any && n0 + i < a.N ? -kLog2e * exp2_fast(kLog2e * E::widen(params[state + n0 + i])) : 0.0f;
+        rate[i] = any && n0 + i < a.N ? rate_of(E::widen(params[state + n0 + i])) : 0.0f;
         carry[i] = 0.0f;
     }
     if constexpr (!MAPS) {
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 du[j] = __builtin_fmaf(step[es][ec + j].x, into[j], skip[j] * g_[j]);
-                ddt[j] = __builtin_fmaf(own_u[j], into[j], kLn2 * across[j]) * opens[j];
+                ddt[j] = opens[j] == 0.0f ? 0.0f : __builtin_fmaf(own_u[j], into[j], kLn2 * across[j]) * opens[j];       // closed: rates may be as large as numbers are
                 dz[j] = slopes[j] * __builtin_fmaf(skip[j], own_u[j], y[j]);
                 if (there) {
                     dbias[j] += ddt[j];

@@ -37,6 +37,9 @@ __device__ __forceinline__ float softplus(float v)
     return __builtin_fmaf(p, s, __builtin_fmaxf(v, 0.0f));  // a NaN is in s
 }
 
+// log2 of what a step of delta = 1 leaves of a state.  Finite where exp(A_log) leaves float32's range, so that its product with a delta of 0 is 0.
+__device__ __forceinline__ float rate_of(float a_log) { return finite_below(-kLog2e * exp2_fast(kLog2e * a_log)); }
+
 template <class E>
 struct SelectArgs {
     using T = typename E::T;
@@ -163,7 +166,7 @@ __global__ __launch_bounds__(kWave *kStretches) void enter_kernel(const SelectAr
     const int64_t i = at0 < all ? at0 : all - 1;
     const int64_t b = i / of, at = i - b * of;
     const int d = static_cast<int>(at / a.N), n = static_cast<int>(at - static_cast<int64_t>(d) * a.N);
-    const float rate = -kLog2e * exp2_fast(kLog2e * E::widen(a.params[(static_cast<uint32_t>(b) / a.per_worker) * a.ldp + static_cast<int64_t>(d) * a.N + n]));
+    const float rate = rate_of(E::widen(a.params[(static_cast<uint32_t>(b) / a.per_worker) * a.ldp + static_cast<int64_t>(d) * a.N + n]));
     float *maps = a.maps + b * a.pieces * of + at;
     const float *sums = a.sums + b * a.pieces * a.D + d;
     const int each = (needed + stretches) / stretches, begin = stretch * each;         // of needed + 1 places, the last of which only receives

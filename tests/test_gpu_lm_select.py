@@ -161,6 +161,30 @@ def test_padding_steps_leave_the_state(suffix, T):
     assert (grads["dt"] == 0).all() and (grads["bm"] == 0).all() and all(v.isfinite().all() for v in grads.values())
 
 
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("T", [1, 15, 50, 900])
+@pytest.mark.parametrize("a_log", [88.5, 200.0])
+def test_rates_beyond_float32_forget_at_every_step_but_padding(suffix, T, a_log):
+    """exp(A_log) log2(e) is beyond float32: a step leaves nothing of the state, one with a dt of -inf all of it; both as resets and a rate of 1 do, to the bit."""
+    D, N, outs = 20, 5, []
+    for log in (a_log, 0.0):
+        c = Case(suffix, 1, 1, T, D, N)
+        pad = torch.arange(T) % 7 >= 4
+        pad[T - 1] = True
+        c.dt[pad] = -torch.inf
+        c.rows[:, OFFSET:OFFSET + D * N] = log
+        c.reset = None if log else (~pad).to(torch.uint8).view(1, T)
+        reset, d = None if log else c.reset.to(DEV), c.on()
+        y, h_last, dh0, g = torch.empty_like(d["u"]), torch.empty((1, D, N), device=DEV), torch.empty((1, D, N), device=DEV), torch.zeros_like(c.rows.to(DEV))
+        states = lm.select_states(y, T, N)
+        c.forward(d, y, states, c.h0.to(DEV), h_last, reset)
+        grads = c.backward(d, states, None, g, c.dh.to(DEV), dh0, reset)
+        assert (g[:, OFFSET:OFFSET + D * N] == 0).all() and (grads["dt"][pad.to(DEV)] == 0).all()
+        outs.append([y, h_last, dh0, g[:, OFFSET + D * N:OFFSET + D * (N + 2)], *grads.values()])
+    for k, (large, resets) in enumerate(zip(*outs)):
+        assert large.isfinite().all() and torch.equal(large, resets), k
+
+
 def test_closed_gates():
     """z of -inf: a result of 0, and gradients of 0 through it."""
     c = Case("", 1, 1, 20, 10, 3)
