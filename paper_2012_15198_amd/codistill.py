@@ -315,6 +315,8 @@ def main(argv=None):
     ap.add_argument("--blocks", type=int, default=0, help="residual blocks in the gated recurrence's place")
     ap.add_argument("--dropout", type=float, default=0.0, help="share of what blocks add that is dropped")
     a = ap.parse_args(argv)
+    if a.blocks < 0:
+        ap.error("--blocks: a number of blocks")
     if a.dropout and not a.blocks:
         ap.error("--dropout: of --blocks")
     model = Blocks(a.workers, a.vocab, a.width, a.blocks, a.dropout, seed=a.seed) if a.blocks else Replicas(a.workers, a.vocab, a.width, seed=a.seed)

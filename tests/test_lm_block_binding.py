@@ -292,3 +292,10 @@ def test_sizes_beyond_32_bits_are_refused(suffix):
                        ("cx_select_scan", (m(2, 9), m(2, 9), m(2, wide), m(2, wide), m(1, 10 * wide), 0, m(2, 9), 2))):
         with pytest.raises(lm.CxError, match="CX_ERR_SHAPE"):
             getattr(lm, name + suffix)(*args)
+
+
+@pytest.mark.parametrize("argv", [["--blocks", "-1"], ["--dropout", "0.1"]])
+def test_training_command_refuses(argv):
+    from paper_2012_15198_amd import codistill
+    with pytest.raises(SystemExit):
+        codistill.main(argv)
