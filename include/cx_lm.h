@@ -224,7 +224,7 @@ int cx_dropout_f16(const uint16_t *x, int64_t ldx, const uint16_t *residual, int
 /* ------------------------------------------------------------------------------------
  * cx_add_norm -- residual addition and root-mean-square norm of N rows of each of W workers:
  *     t = residual + drop(x) ;  s = round(t) ;  inv = 1 / sqrt(mean(t^2) + eps) ;  y = round(t inv w)
- *     scale = max(max |t inv w| / 448, 2^-126) ;  q = (t inv w / scale) rounded to e4m3 (4 exponent, 3 mantissa bits, largest 448)
+ *     scale = max(max |t inv w| / 448, 2^-126) ;  q = t inv w / scale in float32, rounded to e4m3 (4 exponent, 3 mantissa bits, largest 448)
  * drop as cx_dropout with p, rng and the row's number in 0 .. W N - 1 (p = 0: nothing is dropped, rng may be NULL); t is not rounded between.
  * w is [D] in columns [offset, offset + D) of the worker's flat row weights[w].
  *   x        [W * N][D], D <= CX_MAX_NORM_WIDTH; residual: the same or NULL (zeros)

@@ -195,8 +195,26 @@ __global__ __launch_bounds__(kMaxLanes) void norm_kernel(const NormArgs<E> a)
     }
     if (!a.q) return;
     const float most = __uint_as_float(row_max(high, a.shift, lds, 1)), whole = most / kLargest8;
-    const float scale = whole < kLeastScale ? kLeastScale : whole, factor = 1.0f / scale;
+    const float scale = whole < kLeastScale ? kLeastScale : whole;
     if (here && lane == 0) a.scale[row] = scale;
+    // The float32 quotients by the scale, correctly rounded: with the rounded reciprocal, the product and what it leaves of the dividend give them wherever
+    // that remainder is normal (Markstein 1990).  A division each takes 23 us instead of 22 for 8,192 rows of 2,048, the product alone 21, but it is off
+    // by one and moves results next to a midpoint of e4m3 by a step.
+    if (scale > 0x1p-80f && scale < 0x1p+120f) {
+        const float factor = 1.0f / scale;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float near = s[v][j] * factor;
+                s[v][j] = __builtin_fmaf(__builtin_fmaf(-near, scale, s[v][j]), factor, near);
+            }
+    } else {                                            // an infinite scale and a NaN too
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[v][j] /= scale;
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int column = (v * lanes + lane) * 8, left = here ? a.D - column : 0;
@@ -204,8 +222,8 @@ __global__ __launch_bounds__(kMaxLanes) void norm_kernel(const NormArgs<E> a)
         unsigned q[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            q[k] = __builtin_amdgcn_cvt_pk_fp8_f32(s[v][4 * k] * factor, s[v][4 * k + 1] * factor, 0, false);
-            q[k] = __builtin_amdgcn_cvt_pk_fp8_f32(s[v][4 * k + 2] * factor, s[v][4 * k + 3] * factor, q[k], true);
+            q[k] = __builtin_amdgcn_cvt_pk_fp8_f32(s[v][4 * k], s[v][4 * k + 1], 0, false);
+            q[k] = __builtin_amdgcn_cvt_pk_fp8_f32(s[v][4 * k + 2], s[v][4 * k + 3], q[k], true);
         }
         uint8_t *p = a.q + row * a.ldq + column;
         if (left >= 8) {

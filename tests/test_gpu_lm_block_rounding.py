@@ -1,0 +1,49 @@
+"""What the residual block's operators round, and where."""
+import pytest
+import torch
+
+import lm_reference as R
+from lm_block_util import DEV
+from paper_2012_15198_amd import cxlm as lm
+
+pytestmark = pytest.mark.gpu
+
+
+def rows_at_midpoints(dtype, gen):
+    """[W][D] weights whose quotients by their scale lie at or next to the midpoints of e4m3; a row's largest first."""
+    W = 128
+    most = 1 + torch.arange(W) / 128 if dtype == torch.bfloat16 else 1 + torch.rand(W, generator=gen)
+    most = most.to(dtype)
+    middle = torch.cat([torch.arange(17, 32, 2) * 2.0**k for k in range(-4, 4)])
+    at = (middle * most.float()[:, None] / 448).to(dtype)
+    whole = torch.int32 if dtype == torch.float32 else torch.int16
+    return torch.cat([most[:, None], *((at.view(whole) + k).view(dtype) for k in range(-2, 3))], 1)
+
+
+@pytest.mark.parametrize("suffix,power", [("", 0), ("", -100), ("", 122), ("_bf16", 0), ("_bf16", -100), ("_bf16", 122), ("_f16", 0)])
+def test_the_8_bit_output_is_the_quotient_by_the_scale(suffix, power):
+    """Rows of ones and eps = 0: inv is 1 and y the weights.  A product with the scale's reciprocal would be off by a step of e4m3 in some places."""
+    dtype = R.TYPES[suffix]
+    rows = rows_at_midpoints(dtype, torch.Generator().manual_seed(1))
+    rows = rows.clamp(max=rows[:, :1]) * 2.0**power
+    W, D = rows.shape
+    y = rows.float()
+    scale = y.amax(1) / 448
+    want, product = (y / scale[:, None]).to(torch.float8_e4m3fn).float(), (y * (1 / scale)[:, None]).to(torch.float8_e4m3fn).float()
+    assert (want != product).sum() >= 32
+    q, by = torch.empty((W, D), dtype=torch.float8_e4m3fn, device=DEV), torch.empty(W, device=DEV)
+    getattr(lm, "cx_add_norm" + suffix)(torch.ones((W, D), dtype=dtype, device=DEV), None, rows.to(DEV), 0, None, None, 0.0, q=q, scale=by)
+    assert torch.equal(by.cpu(), scale)
+    assert torch.equal(q.cpu().float(), want)
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("D", [9, 700])
+def test_an_infinite_result_has_an_infinite_scale(suffix, D):
+    rows = torch.ones((2, D), dtype=R.TYPES[suffix])
+    rows[0, 3], rows[0, 5] = torch.inf, -torch.inf
+    q, scale = torch.empty((2, D), dtype=torch.float8_e4m3fn, device=DEV), torch.empty(2, device=DEV)
+    getattr(lm, "cx_add_norm" + suffix)(torch.ones_like(rows).to(DEV), None, rows.to(DEV), 0, None, None, 0.0, q=q, scale=scale)
+    held = q.cpu().float()
+    assert scale[0] == torch.inf and held[0, 3].isnan() and held[0, 5].isnan() and held[0].isnan().sum() == 2 and (held[0].nan_to_num(0.0) == 0).all()
+    assert (held[1] == 448).all()
