@@ -248,6 +248,8 @@ int cx_add_norm_f16(const uint16_t *x, int64_t ldx, const uint16_t *residual, in
  * cx_add_norm_grad -- its gradient.  With g = dy w and the s and inv that the forward call left:
  *     ds = round(inv (g - s inv mean(g s inv)) + ds_in) ;  dx = round(drop of the same before its rounding)
  *     dw = round(g_in + sum over the worker's rows of dy s inv), into columns [offset, offset + D) of its flat gradient row g_out[w]
+ * s is t rounded to the rows' type, so that with 16 bits each term of dw carries that rounding beside the sum's own: half a step, 2^-8 of it at
+ * most in bfloat16 and 2^-11 in binary16.  No matrix of wider rows is kept for it.
  *   ds_in    gradient of s from elsewhere (the residual path behind the norm), or NULL
  *   ds       gradient of residual; dx: gradient of x; one of them may be NULL.  Each may be dy or ds_in
  *   g_in     NULL (nothing is added), g_out (added in place) or a second matrix with the same ld

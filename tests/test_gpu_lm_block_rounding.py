@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import lm_block_reference as B
 import lm_reference as R
 from lm_block_util import DEV
 from paper_2012_15198_amd import cxlm as lm
@@ -47,3 +48,20 @@ def test_an_infinite_result_has_an_infinite_scale(suffix, D):
     held = q.cpu().float()
     assert scale[0] == torch.inf and held[0, 3].isnan() and held[0, 5].isnan() and held[0].isnan().sum() == 2 and (held[0].nan_to_num(0.0) == 0).all()
     assert (held[1] == 448).all()
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+@pytest.mark.parametrize("W,N,D", [(2, 3_000, 40), (1, 500, 515)])
+def test_gradient_of_the_parameters_against_the_sum_that_was_not_rounded(suffix, W, N, D):
+    """s is the sum t rounded to the rows' type: each term of dw is off by no more than dy inv times that rounding, beside the error in 32 bits."""
+    gen, dtype = torch.Generator().manual_seed(N + D), R.TYPES[suffix]
+    x, r, dy = ((torch.randn((W * N, D), generator=gen) * a).to(dtype) for a in (1.0, 3.0, 1.0))
+    rows = (1 + 0.2 * torch.randn((W, D), generator=gen)).to(dtype)
+    s, ds, inv, g = torch.empty_like(x.to(DEV)), torch.empty_like(x.to(DEV)), torch.empty(W * N, device=DEV), torch.empty_like(rows.to(DEV))
+    getattr(lm, "cx_add_norm" + suffix)(x.to(DEV), r.to(DEV), rows.to(DEV), 0, s, None, 1e-6, inv=inv)
+    getattr(lm, "cx_add_norm_grad" + suffix)(dy.to(DEV), s, inv, rows.to(DEV), 0, None, ds, None, g)
+    ref = B.add_norm(x, r, rows.repeat_interleave(N, 0), torch.ones((W * N, D), dtype=torch.float64), float(torch.tensor(1e-6)))
+    t, by = ref["t"], ref["inv"][:, None]
+    terms = dy.double() * t * by
+    err = dy.double().abs() * (by * (R.half_ulp(t, dtype) + ref["t_err"]) + t.abs() * ref["inv_err"][:, None]) + 3 * R.U * terms.abs()
+    R.check(g, *B.summed(terms, err, terms.abs(), W, 1), "dw")
