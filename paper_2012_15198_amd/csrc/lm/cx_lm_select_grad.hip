@@ -61,7 +61,7 @@ __device__ __forceinline__ Reduced reduce_columns(const float (&pb)[NQ], const f
             "s_nop 0\n\t"
             "v_add_f32_dpp %2, %2, %2 quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
             "v_add_f32_dpp %3, %3, %3 quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf"
-            : "+v"(c0), "+v"(c1), "+v"(c2), "+v"(c3)
+            : "+&v"(c0), "+&v"(c1), "+&v"(c2), "+&v"(c3)        // written before b0 to b3 are read
             : "v"(b0), "v"(b1), "v"(b2), "v"(b3));
         r.v = add_partner<kBeside>((lane & 2) ? c3 : c2);
         r.j = ((lane >> 1) & 1) + ((lane >> 1) & 2);
