@@ -33,6 +33,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
     float bias[4], skip[4];
     load_four<E>(params + static_cast<int64_t>(a.D) * a.N + column0 + ec, left, bias);
     load_four<E>(params + static_cast<int64_t>(a.D) * (a.N + 1) + column0 + ec, left, skip);
+    close_behind(bias, left);
     // states
     const int q = threadIdx.x / 16 % kQuarters, c = threadIdx.x / kWave * 16 + threadIdx.x % 16, n0 = q * NQ;
     const bool any = column0 + c < a.D;
@@ -79,7 +80,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
         for (int j = 0; j < 4; ++j) {
             const float uj = value_of<E, 4>(u, j), zj = finite_below(value_of<E, 4>(z, j)), soft = softplus(value_of<E, 4>(dt, j) + bias[j]);
             delta[j] = there ? soft : 0.0f;                             // behind the end: a step that changes nothing
-            enters[j] = delta[j] * uj;
+            enters[j] = delta[j] == 0.0f ? 0.0f : delta[j] * uj;
             if constexpr (!MAPS) {
                 const float open = zj * sigmoid(zj);
                 directs[j] = skip[j] * uj;
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(const SelectArgs<E> a)
             }
         }
         put_pairs(&step[turn][es][ec], delta, enters);
-        both[turn][bs][0][bp] = E::widen(b_next);
+        both[turn][bs][0][bp] = E::widen(all_of_step(nothing_of(delta)) ? T(0) : b_next);
         if constexpr (!MAPS) both[turn][bs][1][bp] = E::widen(c_next);
     };
     const auto tile = [&](int64_t t0, auto turn_of) {
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void select_step_kernel(const SelectArgs<
     float y = 0.0f;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-        const float rate = i < here ? rate_of(value_of<E, 4>(logs, i)) : 0.0f, in = i < here ? delta * u * value_of<E, 4>(bs, i) : 0.0f;
+        const float rate = i < here ? rate_of(value_of<E, 4>(logs, i)) : 0.0f, in = i < here && delta != 0.0f ? delta * u * value_of<E, 4>(bs, i) : 0.0f;
         h[i] = cut ? in : __builtin_fmaf(exp2_fast(rate * delta), h[i], in);
         y = __builtin_fmaf(i < here ? value_of<E, 4>(cs, i) : 0.0f, h[i], y);
     }

@@ -103,6 +103,7 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
     __shared__ alignas(16) float parked[MAPS ? 1 : 3][MAPS ? 1 : kTile][kColumns];     // u, sigmoid(dt + bias), dy silu'(z): a thread's own, over the walks
     load_four<E>(params + static_cast<int64_t>(a.D) * a.N + column0 + ec, left, bias);
     load_four<E>(params + static_cast<int64_t>(a.D) * (a.N + 1) + column0 + ec, left, skip);
+    close_behind(bias, left);
     const int wave = threadIdx.x / kWave, q = threadIdx.x / 16 % kQuarters, c = wave * 16 + threadIdx.x % 16, n0 = q * NQ;
     const bool any = column0 + c < a.D;
     const int64_t state = (static_cast<int64_t>(column0) + c) * a.N, of = static_cast<int64_t>(a.D) * a.N, chunks = ceil_div(a.T_, kTile);
@@ -148,18 +149,19 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         settle<E>(dy, back);
         settle<E>(z, back);
         if constexpr (!MAPS) settle<E>(u, back);
-        float delta[4], enters[4], g[4], own[3][4];
+        float delta[4], enters[4], g[4], own[3][4], pulls = 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float v = value_of<E, 4>(dt, j) + bias[j], zj = finite_below(value_of<E, 4>(z, j)), e = sigmoid(zj), dyj = value_of<E, 4>(dy, j), soft = softplus(v);
             delta[j] = there ? soft : 0.0f;                             // behind the end: a step that changes nothing
-            g[j] = a.z ? dyj * (zj * e) : dyj;
+            g[j] = a.z && dyj != 0.0f ? dyj * (zj * e) : dyj;
+            pulls += __builtin_fabsf(dyj);
             enters[j] = 0.0f;
             if constexpr (!MAPS) {
                 own[0][j] = value_of<E, 4>(u, j);
                 own[1][j] = sigmoid(v);
-                own[2][j] = dyj * silu_slope(zj, e);
-                enters[j] = delta[j] * own[0][j];
+                own[2][j] = dyj == 0.0f ? 0.0f : dyj * silu_slope(zj, e);
+                enters[j] = delta[j] == 0.0f ? 0.0f : delta[j] * own[0][j];
             }
         }
         put_pairs(&step[es][ec], delta, enters);
@@ -167,8 +169,8 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
         if constexpr (!MAPS)
 #pragma unroll
             for (int k = 0; k < 3; ++k) put_four(&parked[k][es][ec], own[k]);
-        if constexpr (!MAPS) both[bs][0][bp] = E::widen(b_next);
-        both[bs][1][bp] = E::widen(c_next);
+        if constexpr (!MAPS) both[bs][0][bp] = E::widen(all_of_step(nothing_of(delta)) ? T(0) : b_next);
+        both[bs][1][bp] = E::widen(all_of_step(pulls == 0.0f) ? T(0) : c_next);
         float h[MAPS ? 1 : kTile + 1][NQ], keep[MAPS ? 1 : kTile][NQ];
         if constexpr (!MAPS)
 #pragma unroll
@@ -250,10 +252,10 @@ __global__ __launch_bounds__(kThreads, 2) void select_grad_kernel(const SelectAr
             for (int j = 0; j < 4; ++j) {
                 du[j] = __builtin_fmaf(step[es][ec + j].x, into[j], skip[j] * g_[j]);
                 ddt[j] = opens[j] == 0.0f ? 0.0f : __builtin_fmaf(own_u[j], into[j], kLn2 * across[j]) * opens[j];       // closed: rates may be as large as numbers are
-                dz[j] = slopes[j] * __builtin_fmaf(skip[j], own_u[j], y[j]);
+                dz[j] = slopes[j] == 0.0f ? 0.0f : slopes[j] * __builtin_fmaf(skip[j], own_u[j], y[j]);
                 if (there) {
                     dbias[j] += ddt[j];
-                    dskip[j] = __builtin_fmaf(g_[j], own_u[j], dskip[j]);
+                    if (g_[j] != 0.0f) dskip[j] = __builtin_fmaf(g_[j], own_u[j], dskip[j]);
                 }
             }
             const int64_t row = row0 + t0;

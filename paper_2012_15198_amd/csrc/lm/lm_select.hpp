@@ -117,6 +117,27 @@ __device__ __forceinline__ int state_of(int place) { return place % 4 < NQ ? pla
 __device__ __forceinline__ float quarters_sum(const float (&v)[4]) { return add16(add32(v[0], v[1]), add32(v[2], v[3])); }
 __device__ __forceinline__ int quarter_step(int q) { return (q & 1) * 2 + q / 2; }
 
+// A row of 16 lanes has the elements of one step, and that step's B and C: whether something holds in all of them.  Steps without a delta (padding: dt of
+// -inf) take their u and B as 0, the gradient steps without a dy their C, z and u, so that what padding holds does not get out of it.  The rows are
+// folded by the scalar unit: over lanes it would take a dozen of the vector unit's slots.
+static_assert(kColumns / kEach == 16 && kMaxStates == 16, "a step's threads in either shape");
+__device__ __forceinline__ bool all_of_step(bool v)
+{
+    uint64_t rows = __ballot(v);
+#pragma unroll
+    for (int k = 1; k < 16; k *= 2) rows &= rows >> k;      // a row's first bit: all of its bits
+    rows &= 0x0001000100010001u;
+    return __builtin_amdgcn_inverse_ballot_w64((rows << 16) - rows);
+}
+// Of a step's four deltas or sizes, none below zero: a NaN is not nothing.
+__device__ __forceinline__ bool nothing_of(const float (&v)[4]) { return (v[0] + v[1]) + (v[2] + v[3]) == 0.0f; }
+// Columns behind D make no steps.
+__device__ __forceinline__ void close_behind(float (&bias)[4], int left)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bias[j] = j < left ? bias[j] : -__builtin_inff();
+}
+
 // Bit i: step i of the tile that begins at `row` forgets.
 template <bool RESETS>
 __device__ __forceinline__ unsigned resets_of(const uint8_t *reset, int64_t row, int steps)
