@@ -143,8 +143,8 @@ __device__ __forceinline__ void drop(const u4 &bits, uint32_t border, float scal
 __device__ __forceinline__ float sigmoid(float v) { return rcp_fast(1.0f + exp2_fast(v * -kLog2e)); }
 // -inf as the lowest number: its product with a sigmoid of 0 is 0.  A NaN passes the comparison.
 __device__ __forceinline__ float finite_below(float v) { return v < -3.0e38f ? -3.0e38f : v; }
-// e = sigmoid(v), v from finite_below()
-__device__ __forceinline__ float silu_slope(float v, float e) { return e * __builtin_fmaf(v, 1.0f - e, 1.0f); }
+// e = sigmoid(v), v from finite_below(); +inf as the largest number, whose product with 1 - e is 0.  A NaN is in e.
+__device__ __forceinline__ float silu_slope(float v, float e) { return e * __builtin_fmaf(__builtin_fminf(v, 3.0e38f), 1.0f - e, 1.0f); }
 
 // ---------------------------------------------------------------------------------
 // Sums over lanes.  A value is read from the partner's lane by the addition itself within a row of 16 lanes, rows are exchanged whole; all lanes

@@ -65,3 +65,31 @@ def test_gradient_of_the_parameters_against_the_sum_that_was_not_rounded(suffix,
     terms = dy.double() * t * by
     err = dy.double().abs() * (by * (R.half_ulp(t, dtype) + ref["t_err"]) + t.abs() * ref["inv_err"][:, None]) + 3 * R.U * terms.abs()
     R.check(g, *B.summed(terms, err, terms.abs(), W, 1), "dw")
+
+
+@pytest.mark.parametrize("suffix", R.SUFFIXES)
+def test_slopes_of_the_gate_far_out(suffix):
+    """silu' is 1 at +inf and 0 at -inf: the gradients of the convolution's input and of the scan's gate stay finite there."""
+    dtype = R.TYPES[suffix]
+    D, T, w = 5, 6, 0.5
+    x = torch.ones((T, D), dtype=dtype)
+    x[1], x[3], x[4, 2] = torch.inf, -torch.inf, torch.nan
+    dy = torch.randn((T, D), generator=torch.Generator().manual_seed(1)).to(dtype)
+    rows, dx = torch.cat([torch.full((1, D), w), torch.zeros((1, D))], 1).to(dtype).to(DEV), torch.empty((T, D), dtype=dtype, device=DEV)
+    getattr(lm, "cx_short_conv_grad" + suffix)(x.to(DEV), dy.to(DEV), rows, 0, dx, None, torch.empty_like(rows), T, 1)
+    assert torch.equal(dx[1].cpu(), (dy[1].float() * w).to(dtype)) and (dx[3] == 0).all() and dx[4, 2].isnan()
+    assert dx.isnan().sum() == 1
+
+    u, steps, bm = (torch.full((T, n), 0.5, dtype=dtype, device=DEV) for n in (D, D, 2))
+    params = torch.full((1, D * 4), 0.25, dtype=dtype, device=DEV)
+    read, y = (torch.empty((T, D), dtype=dtype, device=DEV) for _ in range(2))
+    states = lm.select_states(u, T, 2)
+    getattr(lm, "cx_select_scan" + suffix)(u, steps, bm, bm, params, 0, read, T)
+    getattr(lm, "cx_select_scan" + suffix)(u, steps, bm, bm, params, 0, y, T, z=x.to(DEV), states=states)
+    assert (y[1] == torch.inf).all() and (y[3] == 0).all()
+    out = {k: torch.empty_like(u) for k in ("du", "ddt", "dz")}
+    getattr(lm, "cx_select_scan_grad" + suffix)(u, steps, bm, bm, params, 0, dy.to(DEV), out["du"], out["ddt"], torch.empty_like(bm), torch.empty_like(bm), None,
+                                                torch.empty_like(params), T, states, z=x.to(DEV), dz=out["dz"])
+    want = dy[1].double() * read[1].cpu().double()
+    assert ((out["dz"][1].cpu().double() - want).abs() <= 3 * torch.finfo(dtype).eps * want.abs()).all()          # read and dz are rounded once each
+    assert (out["dz"][3] == 0).all() and out["dz"].isnan().sum() == 1
