@@ -181,14 +181,24 @@ def _span(work):
     return (None, 0) if work is None else (work.data_ptr(), work.numel())
 
 
-@functools.lru_cache(maxsize=1024)                       # a training step asks for the same few sizes again: 1 us of a call's 8
+_INTS = {int}
+
+
 def _size(fn, *args) -> int:
+    # a training step asks for the same few sizes again: 1 us of a call's 8.  Kept of plain integers alone: a fraction equals one, a tensor may change
+    return (_known_size if set(map(type, args)) == _INTS else _asked_size)(fn, *args)
+
+
+def _asked_size(fn, *args) -> int:
     L = _lib or lib()
     if max(args) > _INT32 or min(args) < -_INT32:        # the 64-bit ones have limits below 2^31 too
         _too_wide(fn)
     n = ctypes.c_int64()
     _ok(fn, getattr(L, fn)(*args, ctypes.byref(n)))
     return n.value
+
+
+_known_size = functools.lru_cache(maxsize=1024)(_asked_size)
 
 
 def cx_lm_abi_version() -> int:
