@@ -7,7 +7,7 @@
 // row is read once, but for the K - 1 rows in front of a span (the gradient: also behind it).
 //
 // Bound by memory: 32 sequences of 2,048 x 1,024 in bfloat16 take 54 us (5.0 TB/s), the gradient 92 and 5 for the sums of its parts (4.4 TB/s): its
-// spans of 64 steps read 9 % more, and the formulas' vector instructions take half of the time.  Short spans hide what few lanes wait for: 6 sequences of
+// spans of 64 steps read 9 % more, and vector instructions issue in two thirds of the time, so that neither bounds it alone.  Short spans hide what few lanes wait for: 6 sequences of
 // 5,519 x 23 take 16 us in the gradient with 8 steps, 60 with 32.  A step of 64 x 2,048 takes 3.6.  Tried and not kept for the gradient: eight columns of a lane
 // (230 registers, 115 us), four rows ahead (99), results past the caches (96; 83 where the forward pass's go past them too, which takes 58 then).
 #include "lm_block.hpp"

@@ -7,8 +7,8 @@
 // A row stays in the registers of a group of lanes between its statistics and its results, so that each matrix is read and
 // written once.  A lane holds up to four times eight columns; groups are a power of two of lanes.
 //
-// Bound by memory: 65,536 rows of 768 in bfloat16 take 73 us with dropout (5.5 TB/s), their gradient 103 to 119, by how warm the card is, and 5 for the
-// sums of its parts (4.9 to 4.2 TB/s), dropout alone 48 (6.3 TB/s); 8,192 rows of 2,048 to 8 bits 22 (two sets of operands by turns, 234 MB, of which the
+// Bound by memory: 65,536 rows of 768 in bfloat16 take 72 us with dropout (5.6 TB/s), their gradient 103 to 119, by how warm the card is, and 5 for the
+// sums of its parts (4.9 to 4.2 TB/s), dropout alone 48 (6.3 TB/s); 8,192 rows of 2,048 to 8 bits 22 to 23 (two sets of operands by turns, 234 MB, of which the
 // last level of the caches keeps a part).  Tried for the gradient and not kept: the next row's loads ahead (103 to 133), rows widened twice to that end
 // (spills), results past the caches (110).
 #include "lm_block.hpp"
@@ -341,7 +341,9 @@ Layout layout_of(int32_t D, bool fewest)
 }
 
 constexpr int64_t kCaches = 256 << 20;                  // bytes
-// Workgroups of a gradient: what the card takes at once, by the registers of three or four eights (34,080 rows of 1,266 101 us with 512, 115 with 1,024).
+// Workgroups of a gradient, by the eights alone: two wavefronts to a SIMD of three or four (34,080 rows of 1,266 101 us with 512, 115 with 1,024), four of
+// fewer.  Not all variants fill them: three eights of 16 bits without dropout have 160 registers, which three wavefronts would have room for, two of
+// float32 with dropout 131, which leave room for three, and one has at most 89, for five.
 constexpr int64_t kParts = 512, kPartsOfFew = 1024;
 
 int64_t parts_of(int32_t W, int64_t N, int32_t D)

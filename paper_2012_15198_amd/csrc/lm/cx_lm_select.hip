@@ -1,8 +1,9 @@
 // C-ABI entry points cx_select_scan*, cx_select_workspace: the selective state space scan (see include/cx_lm.h, lm_select.hpp)
 //
-// Bound by the vector units: with 16 states a column's step takes 64 exponentials, products and sums six issue slots each, and a quarter as many again
-// for what the states share; 94 % of the cycles issue one (16 sequences of 2,048 x 1,024 in bfloat16: 82 us the maps of three spans in four, 7 what
-// enters, 155 the walk).  Without a split they would take 257 us, one wavefront to a SIMD.
+// Bound by the vector units: a state's step takes an exponential, which counts as two, and four products and sums, 96 issue slots with 16 states (80 without
+// results), and a quarter as many again go to what the states share; 94 % of the busy cycles issue one (16 sequences of 2,048 x 1,024 in bfloat16: 87 us
+// the maps of three spans in four, 7 what enters, 160 the walk).  Without a split they took 257 us, one wavefront to a SIMD, and 245 with it, before
+// padding was kept out of the states (2 %).
 #include "lm_select.hpp"
 
 namespace {

@@ -8,8 +8,9 @@
 //   dA_log = A sum_t r_t delta_t keep_t h_{t-1}    dbias = sum_t ddt    dskip = sum_t g u
 //
 // A tile's states are computed again from the one kept where it begins and stay in registers with their gates; the walk back meets them there.
-// That takes 250 registers, so two wavefronts to a SIMD, which issue vector instructions in 80 % of the cycles (16 sequences of 2,048 x 1,024 with 16
-// states in bfloat16: 60 us the maps, 7 what enters, 480 the walks, 13 and 6 the sums over columns and parts).
+// That takes 246 to 256 registers with 16 states, so two wavefronts to a SIMD, which issue vector instructions in 80 % of the busy cycles (16 sequences of
+// 2,048 x 1,024 in bfloat16: 63 us the maps, 7 what enters, 480 to 499 the walks, 13 and 6 the sums over columns and parts).  The workspace has a float of
+// dB and of dC for each step, state and 64 columns: 268 MB for 16 sequences of 2,048 x 4,096 with 16 states.
 #include "lm_select.hpp"
 
 namespace {

@@ -23,9 +23,9 @@ constexpr int kMaxStates = CX_MAX_STATES;
 constexpr int64_t kMaxSeq = CX_MAX_TOKENS;
 static_assert(kTile * kColumns == kThreads * kEach && kColumns * kQuarters == kThreads && kMaxStates == 16, "the two shapes");
 
-// log(1 + e^v) to a few units in the last place at either end: with e = exp(-|v|) <= 1 it is max(v, 0) + log1p(e), and log1p(e) = s P(s^2) with
+// log(1 + e^v) within (3 |v| + 24) 2^-24 of itself: with e = exp(-|v|) <= 1 it is max(v, 0) + log1p(e), and log1p(e) = s P(s^2) with
 // s = e / (2 + e) <= 1/3 and P(q) = 2 artanh(sqrt q) / sqrt q.  The coefficients are the polynomial of the least largest relative error on
-// [0, 1/9] (Remez exchange), 8e-9 after their rounding.  -inf gives 0.
+// [0, 1/9] (Remez exchange), 8e-9 after their rounding.  What grows with |v| is the rounding of the exponent.  -inf gives 0.
 __device__ __forceinline__ float softplus(float v)
 {
     const float e = exp2_fast(-kLog2e * __builtin_fabsf(v)), s = e * rcp_fast(2.0f + e), q = s * s;
