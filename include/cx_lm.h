@@ -320,8 +320,8 @@ int cx_short_conv_grad_f16(const uint16_t *x, int64_t ldx, const uint16_t *dy, i
  *   reset    uint8 [B][T] or NULL: nonzero where a document begins; nothing of the state before it is used, NaN and infinities included
  *   h0       float [B][D][N] or NULL (zeros);  h_last: the same or NULL, may be h0 (generation: T = 1, state in place)
  *   states   float [B][ceil(T / CX_SCAN_CHUNK)][D][N] or NULL: the state that enters every CX_SCAN_CHUNK-th step, which the gradient needs
- * A dt of -inf (padding) leaves the state as it is, whatever u holds; in a row of nothing else whatever B and C hold too.  Long sequences are computed as compositions of maps, so an infinite state may turn into a
- * NaN.  A single step needs no workspace.
+ * A dt of -inf (padding) leaves the state as it is, whatever u holds; in a row of nothing else whatever B and C hold too.  Long sequences are
+ * computed as compositions of maps, so an infinite state may turn into a NaN.  A single step needs no workspace.
  */
 int cx_select_workspace(int64_t B, int64_t T, int32_t D, int32_t N, int64_t *bytes);
 int cx_select_scan(const float *u, int64_t ldu, const float *dt, int64_t lddt, const float *bm, int64_t ldb, const float *cm, int64_t ldc,
